@@ -53,7 +53,10 @@ enum {
     CIRC_ERR_UNSUPPORTED = -6     /* valid request that this build cannot serve */
 };
 
-enum { CIRC_F32 = 0, CIRC_BF16 = 1 };
+/* Element types; CIRC_E4M3 (8 bits) only as the output of circ_norm_forward.  Class-index types of the calls at the end of
+ * this file. */
+enum { CIRC_F32 = 0, CIRC_BF16 = 1, CIRC_E4M3 = 2 };
+enum { CIRC_I32 = 0, CIRC_I64 = 1 };
 
 /* Kernel variants (circ_set_variant). */
 enum {
@@ -330,6 +333,118 @@ enum { CIRC_POOL_MAX = 0, CIRC_POOL_AVG = 1, CIRC_POOL_L2 = 2 };
  */
 CIRC_API int circ_pool_forward(const void* x, void* y, int N, int H, int W, int C, int window, int stride, int mode, int dtype,
                                void* stream);
+
+/*
+ * Operators around the circulant layers of a network that reads and predicts tokens: the table lookup in front of the
+ * layers, the norm between them, the loss behind them and the clipping of their gradients before the update.
+ *
+ * They share these rules, next to the general ones above:
+ *   - Matrices are row-major and contiguous (circ_loss_* take row strides); every pointer is a DEVICE pointer owned by the
+ *     caller, aligned to its element size.  16-byte aligned rows are the fast case, any other works.
+ *   - A handle holds the sizes, the types and a workspace, no tensor.  Each handle is used by one stream at a time.
+ *   - Calls only enqueue on `stream`.  A workspace that a call needs is allocated by its first call, or before by the
+ *     handle's reserve call (needed before stream capture; CIRC_ERR_UNSUPPORTED otherwise).
+ *   - Zero rows are served (nothing is read; sums over no row are written as 0).
+ *   - Sums are taken in float32 or float64 in an order that depends on the sizes only: results repeat bit for bit.
+ *   - Destroy calls take NULL.  Errors: CIRC_ERR_ARG (NULL or misaligned pointer, unknown type code), CIRC_ERR_SHAPE (a size
+ *     out of range), CIRC_ERR_ALLOC, CIRC_ERR_CUDA, CIRC_ERR_UNSUPPORTED.
+ */
+
+/*
+ * circ_embed_* -- embedding table.
+ *   circ_embed_create       : vocab rows of dim elements.  Defaults: float32 table and y, 64-bit ids, scale 1, no padding id.
+ *   circ_embed_set_dtypes   : element types of the table (and of its gradient), of y (and of its gradient): CIRC_F32 or
+ *                             CIRC_BF16; ids_type: CIRC_I32 or CIRC_I64.
+ *   circ_embed_set_scale    : y[t] = scale * table[ids[t]].
+ *   circ_embed_set_padding  : an id that stands for no token; -1: none.
+ *   circ_embed_forward      : table [vocab][dim], ids [tokens], y [tokens][dim].  An id that is the padding id or lies outside
+ *                             [0, vocab) gives a zero row.
+ *   circ_embed_backward     : grad_table[v] = scale * sum of grad_y[t] over the tokens t with ids[t] = v, zero for rows without
+ *                             one; overwritten, not accumulated.  ids [tokens], grad_y [tokens][dim], grad_table [vocab][dim].
+ *                             Float32 sums whatever the types, rounded once.
+ *   circ_embed_reserve      : workspace for backward calls of up to max_tokens tokens.
+ */
+typedef struct circ_embed* circ_embed_handle;
+CIRC_API circ_embed_handle circ_embed_create(int vocab, int dim);
+CIRC_API int circ_embed_set_dtypes(circ_embed_handle h, int table_dtype, int y_dtype, int ids_type);
+CIRC_API int circ_embed_set_scale(circ_embed_handle h, float scale);
+CIRC_API int circ_embed_set_padding(circ_embed_handle h, long padding);
+CIRC_API int circ_embed_reserve(circ_embed_handle h, long max_tokens);
+CIRC_API int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, void* y, long tokens, void* stream);
+CIRC_API int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y, void* grad_table, long tokens, void* stream);
+CIRC_API void circ_embed_destroy(circ_embed_handle h);
+
+/*
+ * circ_norm_* -- root-mean-square norm of rows of dim elements, with the residual's addition in front of it.
+ *   circ_norm_create     : eps >= 0.  Defaults: float32 x and y, one scale per row for 8-bit outputs.
+ *   circ_norm_set_dtypes : x_dtype: x, residual, sum, grad_sum and grad_x (CIRC_F32 or CIRC_BF16); y_dtype: y and grad_y
+ *                          (CIRC_F32, CIRC_BF16, or CIRC_E4M3: then grad_y has x_dtype).
+ *   circ_norm_set_group  : elements that share a scale of an 8-bit y: 32, 64 or 128 (must divide dim), or 0: the whole row.
+ *   circ_norm_forward    : s = x + residual, rstd = 1 / sqrt(mean(s^2) + eps), y = s rstd gain.
+ *       x, residual [rows][dim]; residual NULL: s = x.  gain: float32 [dim], NULL: ones.
+ *       sum  : receives s, may be x or residual; NULL to skip.     rstd : float32 [rows], for the backward pass; NULL to skip.
+ *       y    : [rows][dim]; the norm is taken of s before it is rounded to x_dtype.
+ *       y_scale : float32 [rows][dim / group], 8-bit y only: scale = max|y| / 448 over the group (1 where all are 0, NaN where one
+ *              is not finite), y / scale rounded to the nearest e4m3 value; the value stored stands for y_scale * y.
+ *   circ_norm_backward   : gradients from grad_y = dL/dy and, where s is used elsewhere too, grad_sum = dL/ds (NULL: 0).
+ *       grad_x    : dL/dx = dL/dresidual, may be grad_sum; NULL to skip.    grad_gain : float32 [dim], overwritten; NULL to skip.
+ *       sum, rstd : of the forward pass (sum is x where there was no residual).
+ *   circ_norm_unpack     : out = y_scale * y of an 8-bit y, float32 or bfloat16 (out_dtype).
+ *   circ_norm_reserve    : workspace of the backward calls.
+ */
+typedef struct circ_norm* circ_norm_handle;
+CIRC_API circ_norm_handle circ_norm_create(int dim, float eps);
+CIRC_API int circ_norm_set_dtypes(circ_norm_handle h, int x_dtype, int y_dtype);
+CIRC_API int circ_norm_set_group(circ_norm_handle h, int group);
+CIRC_API int circ_norm_reserve(circ_norm_handle h);
+CIRC_API int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, const float* gain, void* sum, void* y, float* y_scale,
+                               float* rstd, long rows, void* stream);
+CIRC_API int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, const float* rstd, const void* grad_y,
+                                const void* grad_sum, void* grad_x, float* grad_gain, long rows, void* stream);
+CIRC_API int circ_norm_unpack(circ_norm_handle h, const void* y, const float* y_scale, void* out, int out_dtype, long rows, void* stream);
+CIRC_API void circ_norm_destroy(circ_norm_handle h);
+
+/*
+ * circ_loss_* -- softmax cross entropy over `classes` scores a row, and its gradient.
+ *   circ_loss_create     : defaults: float32 logits, 64-bit targets, target -100 ignored.
+ *   circ_loss_set_dtypes : logits_dtype: logits and their gradient (CIRC_F32 or CIRC_BF16); ids_type of the targets.
+ *   circ_loss_set_ignore : a target that stands for "no target".  Targets outside [0, classes) always do.
+ *   circ_loss_forward    : logits [rows] of `stride` elements (>= classes), targets [rows].  Any of the three results may be NULL:
+ *       row_loss : float32 [rows], log sum exp(logits) - logits[target], 0 for a row without a target
+ *       lse      : float32 [rows], log sum exp(logits)
+ *       mean     : float32 [1], sum of row_loss / rows that have a target (0 if none has)
+ *   circ_loss_backward   : the same, and grad_logits [rows] of `grad_stride` elements =
+ *       grad_mean / (rows that have a target) * (softmax(logits) - onehot(target)), 0 for a row without a target; what lies
+ *       between classes and grad_stride is left alone.  grad_logits may be logits (with the same stride).
+ *   circ_loss_reserve    : workspace for calls of up to max_rows rows.
+ * Classes masked with -inf have probability 0.  A row with nothing left has lse -inf, loss +inf and a zero gradient.
+ */
+typedef struct circ_loss* circ_loss_handle;
+CIRC_API circ_loss_handle circ_loss_create(int classes);
+CIRC_API int circ_loss_set_dtypes(circ_loss_handle h, int logits_dtype, int ids_type);
+CIRC_API int circ_loss_set_ignore(circ_loss_handle h, long ignore);
+CIRC_API int circ_loss_reserve(circ_loss_handle h, long max_rows);
+CIRC_API int circ_loss_forward(circ_loss_handle h, const void* logits, long stride, const void* targets, float* row_loss, float* lse,
+                               float* mean, long rows, void* stream);
+CIRC_API int circ_loss_backward(circ_loss_handle h, const void* logits, long stride, const void* targets, float* row_loss, float* lse,
+                                float* mean, void* grad_logits, long grad_stride, float grad_mean, long rows, void* stream);
+CIRC_API void circ_loss_destroy(circ_loss_handle h);
+
+/*
+ * circ_clip_* -- clipping of gradients by their global norm: norm = sqrt(sum of g^2 over all tensors),
+ * out = g * min(1, max_norm / (norm + 1e-6)).
+ *   circ_clip_create      : `count` tensors of sizes[i] elements (0 is allowed); grad_dtypes[i], out_dtypes[i]: CIRC_F32 or
+ *                           CIRC_BF16.  The arrays are HOST memory, read during the call.
+ *   circ_clip_set_tensors : HOST arrays of `count` device addresses; outs NULL, or outs[i] = grads[i]: in place.  Must be called once
+ *                           before circ_clip_forward and again when an address changes; ordered on `stream`.
+ *   circ_clip_forward     : norm: DEVICE float32 [1], NULL to skip.  max_norm >= 0.
+ * A norm that is not finite follows the formula: NaN makes every output NaN, infinity makes them 0 (NaN where g is infinite).
+ */
+typedef struct circ_clip* circ_clip_handle;
+CIRC_API circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_dtypes, const int* out_dtypes);
+CIRC_API int circ_clip_set_tensors(circ_clip_handle h, const void* const* grads, void* const* outs, void* stream);
+CIRC_API int circ_clip_forward(circ_clip_handle h, float max_norm, float* norm, void* stream);
+CIRC_API void circ_clip_destroy(circ_clip_handle h);
 
 #ifdef __cplusplus
 }

@@ -17,7 +17,8 @@ LIB_PATH = _HERE / "libcirc.so"
 
 CIRC_OK = 0
 CIRC_ERR_ARG, CIRC_ERR_SHAPE, CIRC_ERR_ALLOC, CIRC_ERR_CUDA, CIRC_ERR_DEVICE_TIMEOUT, CIRC_ERR_UNSUPPORTED = -1, -2, -3, -4, -5, -6
-CIRC_F32, CIRC_BF16 = 0, 1
+CIRC_F32, CIRC_BF16, CIRC_E4M3 = 0, 1, 2
+CIRC_I32, CIRC_I64 = 0, 1
 CIRC_POOL_MAX, CIRC_POOL_AVG, CIRC_POOL_L2 = 0, 1, 2
 CIRC_VARIANT_AUTO, CIRC_VARIANT_FUSED, CIRC_VARIANT_STAGED, CIRC_VARIANT_TENSOR = 0, 1, 2, 3
 # include/circ_debug.h
@@ -29,7 +30,7 @@ CIRC_KERNEL_S3_TMA = 22
 CIRC_INJECT_NONE, CIRC_INJECT_TENSOR_NO_COPY, CIRC_INJECT_BULK_NO_COPY = 0, 1, 2
 
 # name -> (restype, argtypes); mirrors include/circ.h one to one
-_vp, _ci, _cl = ctypes.c_void_p, ctypes.c_int, ctypes.c_long
+_vp, _ci, _cl, _cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_long, ctypes.c_float
 SIGNATURES = {
     "circ_fc_create": (_vp, [_ci, _ci, _ci, _vp]),
     "circ_fc_forward": (_ci, [_vp, _vp, _vp, _ci, _vp]),
@@ -72,6 +73,33 @@ SIGNATURES = {
     "circ_debug_set_transforms": (_ci, [_vp, _ci, _ci]),
     "circ_conv_set_stride": (_ci, [_vp, _ci]),
     "circ_pool_forward": (_ci, [_vp, _vp, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _ci, _vp]),
+    "circ_embed_create": (_vp, [_ci, _ci]),
+    "circ_embed_set_dtypes": (_ci, [_vp, _ci, _ci, _ci]),
+    "circ_embed_set_scale": (_ci, [_vp, _cf]),
+    "circ_embed_set_padding": (_ci, [_vp, _cl]),
+    "circ_embed_reserve": (_ci, [_vp, _cl]),
+    "circ_embed_forward": (_ci, [_vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_embed_backward": (_ci, [_vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_embed_destroy": (None, [_vp]),
+    "circ_norm_create": (_vp, [_ci, _cf]),
+    "circ_norm_set_dtypes": (_ci, [_vp, _ci, _ci]),
+    "circ_norm_set_group": (_ci, [_vp, _ci]),
+    "circ_norm_reserve": (_ci, [_vp]),
+    "circ_norm_forward": (_ci, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_norm_backward": (_ci, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_norm_unpack": (_ci, [_vp, _vp, _vp, _vp, _ci, _cl, _vp]),
+    "circ_norm_destroy": (None, [_vp]),
+    "circ_loss_create": (_vp, [_ci]),
+    "circ_loss_set_dtypes": (_ci, [_vp, _ci, _ci]),
+    "circ_loss_set_ignore": (_ci, [_vp, _cl]),
+    "circ_loss_reserve": (_ci, [_vp, _cl]),
+    "circ_loss_forward": (_ci, [_vp, _vp, _cl, _vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_loss_backward": (_ci, [_vp, _vp, _cl, _vp, _vp, _vp, _vp, _vp, _cl, _cf, _cl, _vp]),
+    "circ_loss_destroy": (None, [_vp]),
+    "circ_clip_create": (_vp, [_ci, _vp, _vp, _vp]),
+    "circ_clip_set_tensors": (_ci, [_vp, _vp, _vp, _vp]),
+    "circ_clip_forward": (_ci, [_vp, _cf, _vp, _vp]),
+    "circ_clip_destroy": (None, [_vp]),
     "circ_last_error": (ctypes.c_char_p, []),
     "circ_last_code": (_ci, []),
 }
@@ -114,6 +142,21 @@ def _ptr(a) -> int | None:
         return a.ctypes.data
     assert a.is_contiguous()
     return a.data_ptr()
+
+
+def _rows_ptr(a) -> int | None:
+    """Address of a matrix whose rows may lie further apart than they are long (the call is told the stride)."""
+    if a is None or isinstance(a, (int, np.ndarray)):
+        return _ptr(a)
+    assert a.numel() == 0 or a.stride(-1) == 1
+    return a.data_ptr()
+
+
+def _made(h):
+    """The handle of a create call; raises if it is NULL."""
+    if not h:
+        raise CircError(circ_last_code(), circ_last_error())
+    return h
 
 
 def _stream(stream) -> int | None:
@@ -293,6 +336,138 @@ def circ_last_variant(h: int) -> int:
 def circ_weight_bytes(h: int) -> int:
     """Bytes of device memory the handle holds for the layer's weights in all stored forms."""
     return load().circ_weight_bytes(h)
+
+
+# ---- operators around the circulant layers of a token model ------------------------------------------
+
+def circ_embed_create(vocab: int, dim: int) -> int:
+    return _made(load().circ_embed_create(vocab, dim))
+
+
+def circ_embed_set_dtypes(h: int, table_dtype: int, y_dtype: int, ids_type: int) -> None:
+    _check(load().circ_embed_set_dtypes(h, table_dtype, y_dtype, ids_type))
+
+
+def circ_embed_set_scale(h: int, scale: float) -> None:
+    _check(load().circ_embed_set_scale(h, scale))
+
+
+def circ_embed_set_padding(h: int, padding: int) -> None:
+    """``padding``: the id that stands for no token (-1: none)."""
+    _check(load().circ_embed_set_padding(h, padding))
+
+
+def circ_embed_reserve(h: int, max_tokens: int) -> None:
+    _check(load().circ_embed_reserve(h, max_tokens))
+
+
+def circ_embed_forward(h: int, table, ids, y, tokens: int, stream=None) -> None:
+    """Enqueue ``y[t] = scale * table[ids[t]]`` (a zero row for the padding id and for ids outside the table)."""
+    _check(load().circ_embed_forward(h, _ptr(table), _ptr(ids), _ptr(y), tokens, _stream(stream)))
+
+
+def circ_embed_backward(h: int, ids, grad_y, grad_table, tokens: int, stream=None) -> None:
+    """Enqueue ``grad_table[v] = scale * sum of grad_y[t] over tokens with ids[t] == v`` (every row is written)."""
+    _check(load().circ_embed_backward(h, _ptr(ids), _ptr(grad_y), _ptr(grad_table), tokens, _stream(stream)))
+
+
+def circ_embed_destroy(h: int | None) -> None:
+    load().circ_embed_destroy(h)
+
+
+def circ_norm_create(dim: int, eps: float) -> int:
+    return _made(load().circ_norm_create(dim, eps))
+
+
+def circ_norm_set_dtypes(h: int, x_dtype: int, y_dtype: int) -> None:
+    _check(load().circ_norm_set_dtypes(h, x_dtype, y_dtype))
+
+
+def circ_norm_set_group(h: int, group: int) -> None:
+    """Elements that share a scale of an 8-bit output: 32, 64, 128, or 0 for a whole row."""
+    _check(load().circ_norm_set_group(h, group))
+
+
+def circ_norm_reserve(h: int) -> None:
+    _check(load().circ_norm_reserve(h))
+
+
+def circ_norm_forward(h: int, x, residual, gain, sum, y, y_scale, rstd, rows: int, stream=None) -> None:
+    """Enqueue ``sum = x + residual; y = sum * rstd * gain``; ``residual``, ``gain``, ``sum``, ``rstd`` may be None."""
+    _check(load().circ_norm_forward(h, _ptr(x), _ptr(residual), _ptr(gain), _ptr(sum), _ptr(y), _ptr(y_scale), _ptr(rstd), rows, _stream(stream)))
+
+
+def circ_norm_backward(h: int, sum, gain, rstd, grad_y, grad_sum, grad_x, grad_gain, rows: int, stream=None) -> None:
+    """Enqueue the gradients of the norm; ``grad_sum`` (what flows past the norm), ``grad_x`` or ``grad_gain`` may be None."""
+    _check(load().circ_norm_backward(h, _ptr(sum), _ptr(gain), _ptr(rstd), _ptr(grad_y), _ptr(grad_sum), _ptr(grad_x), _ptr(grad_gain), rows,
+                                     _stream(stream)))
+
+
+def circ_norm_unpack(h: int, y, y_scale, out, out_dtype: int, rows: int, stream=None) -> None:
+    """Enqueue ``out = y_scale * y`` for an 8-bit output of ``circ_norm_forward``."""
+    _check(load().circ_norm_unpack(h, _ptr(y), _ptr(y_scale), _ptr(out), out_dtype, rows, _stream(stream)))
+
+
+def circ_norm_destroy(h: int | None) -> None:
+    load().circ_norm_destroy(h)
+
+
+def circ_loss_create(classes: int) -> int:
+    return _made(load().circ_loss_create(classes))
+
+
+def circ_loss_set_dtypes(h: int, logits_dtype: int, ids_type: int) -> None:
+    _check(load().circ_loss_set_dtypes(h, logits_dtype, ids_type))
+
+
+def circ_loss_set_ignore(h: int, ignore: int) -> None:
+    _check(load().circ_loss_set_ignore(h, ignore))
+
+
+def circ_loss_reserve(h: int, max_rows: int) -> None:
+    _check(load().circ_loss_reserve(h, max_rows))
+
+
+def circ_loss_forward(h: int, logits, stride: int, targets, row_loss, lse, mean, rows: int, stream=None) -> None:
+    """Enqueue the softmax cross entropy; ``stride``: elements between rows of ``logits``; results that are None are skipped."""
+    _check(load().circ_loss_forward(h, _rows_ptr(logits), stride, _ptr(targets), _ptr(row_loss), _ptr(lse), _ptr(mean), rows, _stream(stream)))
+
+
+def circ_loss_backward(h: int, logits, stride: int, targets, row_loss, lse, mean, grad_logits, grad_stride: int, grad_mean: float, rows: int,
+                       stream=None) -> None:
+    """``circ_loss_forward`` and the gradient of ``grad_mean * mean`` with respect to the logits (may replace them)."""
+    _check(load().circ_loss_backward(h, _rows_ptr(logits), stride, _ptr(targets), _ptr(row_loss), _ptr(lse), _ptr(mean), _rows_ptr(grad_logits),
+                                     grad_stride, grad_mean, rows, _stream(stream)))
+
+
+def circ_loss_destroy(h: int | None) -> None:
+    load().circ_loss_destroy(h)
+
+
+def circ_clip_create(sizes, grad_dtypes, out_dtypes) -> int:
+    """``sizes``: elements of each tensor; the types: one code for all tensors, or one for each."""
+    n = len(sizes)
+    grads, outs = ([t] * n if isinstance(t, int) else list(t) for t in (grad_dtypes, out_dtypes))
+    assert len(grads) == n and len(outs) == n
+    return _made(load().circ_clip_create(n, (ctypes.c_long * n)(*sizes), (ctypes.c_int * n)(*grads), (ctypes.c_int * n)(*outs)))
+
+
+def circ_clip_set_tensors(h: int, grads, outs=None, stream=None) -> None:
+    """The tensors of the following ``circ_clip_forward`` calls, in the order of their sizes; ``outs`` None: in place."""
+    n = len(grads)
+    assert outs is None or len(outs) == n
+    g = (ctypes.c_void_p * n)(*map(_ptr, grads))
+    o = None if outs is None else (ctypes.c_void_p * n)(*map(_ptr, outs))
+    _check(load().circ_clip_set_tensors(h, g, o, _stream(stream)))
+
+
+def circ_clip_forward(h: int, max_norm: float, norm, stream=None) -> None:
+    """Enqueue the norm over all tensors (``norm``: a device float, or None) and their scaling."""
+    _check(load().circ_clip_forward(h, max_norm, _ptr(norm), _stream(stream)))
+
+
+def circ_clip_destroy(h: int | None) -> None:
+    load().circ_clip_destroy(h)
 
 
 # ---- include/circ_debug.h: test and measurement aids ------------------------------------------------

@@ -1,0 +1,167 @@
+"""Clipping by the global norm against the formula in 64 bits: one tensor to many, empty ones, mixed types, unaligned
+addresses, in place and into copies, norms below the limit and not finite; refusals.
+
+Bounds (u: unit roundoff of float32).  Squares are added in float32 over at most 256 values a lane and block tree (chains of at
+most 300 additions), then in float64: the norm's relative error is at most 152 u, the factor's 3 u more, and every output is
+rounded once more."""
+import math
+
+import pytest
+import torch
+
+import paper_1708_08917_b200 as circ
+from row_helpers import CODE, U, device, guarded, rng, rounding, small
+
+F32, BF16 = torch.float32, torch.bfloat16
+NORM = 152 * U
+
+
+def plain(tensors, max_norm):
+    norm = math.sqrt(sum(float((t.double() ** 2).sum()) for t in tensors))
+    return norm, min(1.0, max_norm / (norm + 1e-6))
+
+
+def check(outs, tensors, dtypes, norm, want, factor):
+    assert abs(norm - want) <= NORM * want
+    for o, t, d in zip(outs, tensors, dtypes):
+        ref = t.double() * factor
+        assert o.dtype == d and bool(((o.double().cpu() - ref).abs() <= (NORM + 5 * U + rounding(d)) * ref.abs() + small(d)).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[1], [0, 1, 0], [7, 33, 1000], [16384], [16385, 3, 70000], [4096] * 300, [5] * 1000, [1 << 20, 1, 255, 250001]])
+@pytest.mark.parametrize("grads,outs,offset", [(F32, F32, 0), (BF16, F32, 0), (F32, BF16, 1), (BF16, BF16, 3), ("mixed", "mixed", 0)])
+@pytest.mark.parametrize("over", [4.0, 0.5])
+def test_clipped_copies(sizes, grads, outs, offset, over):
+    g = rng(sum(sizes))
+    gd = [F32 if i % 3 else BF16 for i in range(len(sizes))] if grads == "mixed" else [grads] * len(sizes)
+    od = [BF16 if i % 4 else F32 for i in range(len(sizes))] if outs == "mixed" else [outs] * len(sizes)
+    tensors = [(0.01 * torch.randn(n, generator=g)).to(d) for n, d in zip(sizes, gd)]
+    max_norm = float(torch.tensor(plain(tensors, 1.0)[0] / over, dtype=F32))
+    h = circ.circ_clip_create(sizes, [CODE[d] for d in gd], [CODE[d] for d in od])
+    held = [device(t, offset) for t in tensors]
+    results = [guarded((n,), d, offset) for n, d in zip(sizes, od)]
+    circ.circ_clip_set_tensors(h, held, [r[0] for r in results], torch.cuda.current_stream())
+    norm, norm_ok = guarded((1,), F32)
+    circ.circ_clip_forward(h, max_norm, norm, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    first = [r[0].clone() for r in results]
+    circ.circ_clip_forward(h, max_norm, None, torch.cuda.current_stream())        # again, without the norm: the same bits
+    torch.cuda.synchronize()
+    circ.circ_clip_destroy(h)
+    norm_ok()
+    for (o, ok), f in zip(results, first):
+        ok()
+        assert torch.equal(o, f)
+    check([r[0] for r in results], tensors, od, float(norm), *plain(tensors, max_norm))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("over", [10.0, 0.1])
+def test_in_place_and_changed_addresses(dtype, over):
+    sizes = [1000, 17, 40000]
+    h = circ.circ_clip_create(sizes, CODE[dtype], CODE[dtype])
+    norm = torch.empty(1, device="cuda")
+    for seed in (1, 2):                                                          # the second time with other tensors
+        g = rng(seed)
+        tensors = [torch.randn(n, generator=g).to(dtype) for n in sizes]
+        max_norm = float(torch.tensor(plain(tensors, 1.0)[0] / over, dtype=F32))
+        held = [device(t) for t in tensors]
+        circ.circ_clip_set_tensors(h, held, held if seed == 1 else None, torch.cuda.current_stream())
+        circ.circ_clip_forward(h, max_norm, norm, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        check(held, tensors, [dtype] * 3, float(norm), *plain(tensors, max_norm))
+        if over < 1:
+            assert all(torch.equal(a.cpu(), b) for a, b in zip(held, tensors))   # nothing to clip: not a bit changes
+    circ.circ_clip_destroy(h)
+
+
+@pytest.mark.gpu
+def test_zeros_a_limit_of_zero_large_values_and_values_that_are_not_finite():
+    n = 5000
+    norm = torch.empty(1, device="cuda")
+    h = circ.circ_clip_create([n], circ.CIRC_F32, circ.CIRC_F32)
+
+    def clipped(t, limit):
+        held, out = device(t), torch.full((n,), float("nan"), device="cuda")
+        circ.circ_clip_set_tensors(h, [held], [out], torch.cuda.current_stream())
+        circ.circ_clip_forward(h, limit, norm, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        return float(norm), out.cpu()
+
+    x = torch.randn(n, generator=rng(6))
+    got, out = clipped(torch.zeros(n), 1.0)
+    assert got == 0 and bool((out == 0).all())
+    got, out = clipped(x, 0.0)
+    assert bool((out == 0).all())
+    got, out = clipped(x * 1e17, 1.0)                      # squares of 1e34, their sum still a float32
+    assert abs(got - float((x * 1e17).double().norm())) <= NORM * got and abs(float(out.norm()) - 1) < 1e-3
+    y = x.clone()
+    y[123] = float("nan")
+    got, out = clipped(y, 1.0)
+    assert math.isnan(got) and bool(out.isnan().all())
+    y[123] = float("inf")
+    got, out = clipped(y, 1.0)
+    assert got == math.inf and bool(out[123].isnan()) and bool((out[:123] == 0).all())
+    circ.circ_clip_destroy(h)
+
+
+@pytest.mark.gpu
+def test_nothing_but_empty_tensors_and_a_captured_graph():
+    norm = torch.full((1,), float("nan"), device="cuda")
+    h = circ.circ_clip_create([0, 0], circ.CIRC_F32, circ.CIRC_BF16)
+    circ.circ_clip_set_tensors(h, [None, None], [None, None])
+    circ.circ_clip_forward(h, 1.0, norm, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_clip_destroy(h)
+    assert float(norm) == 0
+    x = torch.randn(100000, device="cuda")
+    out, want = torch.zeros_like(x), x * min(1.0, 2.0 / (float(x.double().norm()) + 1e-6))
+    h = circ.circ_clip_create([100000], circ.CIRC_F32, circ.CIRC_F32)
+    circ.circ_clip_set_tensors(h, [x], [out], torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        circ.circ_clip_forward(h, 2.0, norm, torch.cuda.current_stream())
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.allclose(out, want, rtol=1e-5)
+    del graph
+    circ.circ_clip_destroy(h)
+
+
+def refused(code, call, *args):
+    with pytest.raises(circ.CircError) as e:
+        call(*args)
+    assert e.value.code == code
+
+
+def test_refusals_before_any_device_call():
+    refused(circ.CIRC_ERR_ARG, circ.circ_clip_create, [], 0, 0)
+    refused(circ.CIRC_ERR_SHAPE, circ.circ_clip_create, [-1], 0, 0)
+    refused(circ.CIRC_ERR_SHAPE, circ.circ_clip_create, [1 << 41], 0, 0)
+    refused(circ.CIRC_ERR_ARG, circ.circ_clip_create, [4], circ.CIRC_E4M3, 0)
+    refused(circ.CIRC_ERR_ARG, circ.circ_clip_create, [4], 0, 5)
+    refused(circ.CIRC_ERR_ARG, circ.circ_clip_set_tensors, None, [64], None)
+    refused(circ.CIRC_ERR_ARG, circ.circ_clip_forward, None, 1.0, None)
+    circ.circ_clip_destroy(None)
+
+
+@pytest.mark.gpu
+def test_refusals_of_bad_arguments():
+    h = circ.circ_clip_create([8], circ.CIRC_F32, circ.CIRC_BF16)
+    a, b = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda", dtype=BF16)
+    try:
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_forward, h, 1.0, None)                            # no tensors yet
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_set_tensors, h, [a], [a])                         # in place with two types
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_set_tensors, h, [a], None)
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_set_tensors, h, [None], [b])
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_set_tensors, h, [a.data_ptr() + 2], [b])
+        circ.circ_clip_set_tensors(h, [a], [b], torch.cuda.current_stream())
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_forward, h, -1.0, None)
+        refused(circ.CIRC_ERR_ARG, circ.circ_clip_forward, h, float("nan"), None)
+        with pytest.raises(AssertionError):
+            circ.circ_clip_set_tensors(h, [a[::2]], [b])
+    finally:
+        torch.cuda.synchronize()
+        circ.circ_clip_destroy(h)
