@@ -17,28 +17,399 @@ struct Embed {
     Scratch ws;
 };
 
-template <typename TT, typename TY, typename ID>
+// ---- forward -------------------------------------------------------------------------------------------------
+// Pure data movement.  The output is walked as one run of vectors (VEC elements, 16 bytes or more per access when the rows
+// allow it): a thread takes UNROLL of them, a thread block apart, so that several rows' loads are in flight behind their ids.
+template <typename TT, typename TY, typename ID, int VEC, int UNROLL>
 __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict__ table, const ID* __restrict__ ids, TY* __restrict__ y,
-                                                            int vocab, int dim, float scale, long padding) {
-    const long t = blockIdx.x;
-    const long id = (long)ids[t];
-    const bool row = id >= 0 && id < vocab && id != padding;
-    for (int c = threadIdx.x; c < dim; c += blockDim.x)
-        store_one(y + t * dim + c, row ? scale * to_float(table[id * dim + c]) : 0.f);
+                                                            long vectors, int vec_per_row, int vocab, int dim, float scale, long padding) {
+    const long first = (long)blockIdx.x * (256 * UNROLL);
+    // one 64-bit division a thread block; the rest is small-integer arithmetic
+    const long row0 = first / vec_per_row;
+    const unsigned in_row = (unsigned)(first - row0 * vec_per_row) + threadIdx.x;
+    float v[UNROLL][VEC];
+    long at[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const unsigned k = in_row + u * 256u, dr = k / (unsigned)vec_per_row;
+        const long t = row0 + dr;
+        const int c = (int)(k - dr * vec_per_row) * VEC;
+        at[u] = first + u * 256 + threadIdx.x < vectors ? t * dim + c : -1;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[u][e] = 0.f;
+        if (at[u] < 0) continue;
+        const long id = (long)__ldg(ids + t);
+        if (id >= 0 && id < vocab && id != padding) load_vec<VEC>(table + id * dim + c, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        if (at[u] < 0) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[u][e] *= scale;
+        store_vec<VEC>(y + at[u], v[u]);
+    }
 }
 
-// One thread block per table row: every thread walks all ids in order and adds up its columns of the matching rows.
-template <typename TT, typename TY, typename ID>
-__global__ void __launch_bounds__(256) embed_backward_kernel(const ID* __restrict__ ids, const TY* __restrict__ dy, TT* __restrict__ dt,
-                                                             long tokens, int dim, float scale, long padding) {
-    const long v = blockIdx.x;
-    for (int c = threadIdx.x; c < dim; c += blockDim.x) {
-        float sum = 0.f;
-        if (v != padding)
-            for (long t = 0; t < tokens; ++t)
-                if ((long)ids[t] == v) sum += to_float(dy[t * dim + c]);
-        store_one(dt + v * dim + c, scale * sum);
+// ---- backward ------------------------------------------------------------------------------------------------
+// The tokens are sorted by id (1), then every table row is the sum of its run of sorted tokens (2), and runs that were
+// cut for balance are put together (3).  Nothing is added through atomics: the order of every sum follows from the ids.
+//
+// (1) A thread block owns a class of table rows, the ids equal to it modulo the number of classes, and reads all ids: with its
+// counts per (warp, row) it knows the place of each of its tokens in the whole order without hearing from another block, since the
+// tokens in front of its class are those of lower classes.  (Classes and not ranges: ids are commonly handed out by frequency, and
+// a block with the first 1/128 of the ids had half of the tokens.)  Warps take consecutive parts of the tokens, so that equal ids
+// stay in the order of their positions.  The rows' order behind is (class, id); `slot` numbers the rows in that order.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortUnroll = 16;
+constexpr int kSortRows = 1536;      // table rows of a block: 32 warps x 1536 counts are 192 KB of shared memory
+
+// The row's number within class `cls` of 2^bits classes; kNotOurs for an id of another class or for no token.  `less`: a lower class.
+// Negative ids are above every row as unsigned numbers.
+constexpr unsigned kNotOurs = 0xffffffffu;
+template <typename ID>
+__device__ __forceinline__ unsigned class_row(ID id, unsigned cls, int bits, unsigned vocab, unsigned padding, bool& less) {
+    const unsigned lo = (unsigned)id, own = lo & ((1u << bits) - 1);
+    bool token = lo < vocab && lo != padding;
+    if constexpr (sizeof(ID) == 8) token = token && (unsigned)((uint64_t)id >> 32) == 0;
+    less = token && own < cls;
+    return token && own == cls ? lo >> bits : kNotOurs;
+}
+
+template <typename ID>
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, int vocab, unsigned padding, int bits, int rows_per_block,
+                                                                  int* __restrict__ start, int* __restrict__ order, int* __restrict__ cuts) {
+    extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places
+    __shared__ int part[kSortWarps], below[kSortWarps];
+    pdl_trigger();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int per_warp = ((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
+    const int begin = warp * per_warp < tokens ? warp * per_warp : tokens, end = begin + per_warp < tokens ? begin + per_warp : tokens;
+    int* mine = count + warp * rows_per_block;
+    // rows of the first 16 x 32 tokens of the warp stay in registers for the second pass
+    unsigned kept[kSortUnroll];
+    auto fetch = [&](int t0, unsigned (&row)[kSortUnroll], int& less) {
+        ID id[kSortUnroll];
+#pragma unroll
+        for (int u = 0; u < kSortUnroll; ++u) id[u] = t0 + u * 32 + lane < end ? __ldg(ids + t0 + u * 32 + lane) : (ID)-1;
+#pragma unroll
+        for (int u = 0; u < kSortUnroll; ++u) {
+            bool l;
+            row[u] = class_row(id[u], blockIdx.x, bits, (unsigned)vocab, padding, l);
+            less += l;
+        }
+    };
+    int less = 0;
+    fetch(begin, kept, less);
+    for (int i = threadIdx.x; i < kSortWarps / 4 * rows_per_block; i += kSortThreads) reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *cuts = 0;
+    __syncthreads();
+    auto tally = [&](const unsigned (&row)[kSortUnroll]) {
+#pragma unroll
+        for (int u = 0; u < kSortUnroll; ++u)
+            if (row[u] != kNotOurs) atomicAdd(mine + row[u], 1);
+    };
+    tally(kept);
+    for (int t0 = begin + 32 * kSortUnroll; t0 < end; t0 += 32 * kSortUnroll) {
+        unsigned row[kSortUnroll];
+        fetch(t0, row, less);
+        tally(row);
     }
+    less = __reduce_add_sync(0xffffffffu, less);
+    if (lane == 0) below[warp] = less;
+    __syncthreads();
+    // exclusive sums over the block's rows; a thread takes consecutive ones
+    const int rpt = (rows_per_block + kSortThreads - 1) / kSortThreads;
+    int sum = 0;
+    for (int i = 0; i < rpt; ++i) {
+        const int r = threadIdx.x * rpt + i;
+        if (r < rows_per_block)
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) sum += count[w * rows_per_block + r];
+    }
+    int scan = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+    }
+    if (lane == 31) part[warp] = scan;
+    __syncthreads();
+    int place = scan - sum + __reduce_add_sync(0xffffffffu, below[lane] + (lane < warp ? part[lane] : 0));
+    for (int i = 0; i < rpt; ++i) {
+        const int r = threadIdx.x * rpt + i;
+        if (r >= rows_per_block) break;
+        start[(size_t)blockIdx.x * rows_per_block + r] = place;
+        int n[kSortWarps];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) n[w] = count[w * rows_per_block + r];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            count[w * rows_per_block + r] = place;
+            place += n[w];
+        }
+        if (blockIdx.x == gridDim.x - 1 && r == rows_per_block - 1) start[(size_t)gridDim.x * rows_per_block] = place;
+    }
+    __syncthreads();
+    auto deal = [&](int t0, const unsigned (&row)[kSortUnroll]) {
+#pragma unroll
+        for (int u = 0; u < kSortUnroll; ++u) {
+            const bool ours = row[u] != kNotOurs;
+            const unsigned some = __ballot_sync(0xffffffffu, ours);
+            if (!some) continue;
+            if (ours) {
+                const unsigned same = __match_any_sync(some, row[u]);
+                const int rank = __popc(same & ((1u << lane) - 1)), base = mine[row[u]];
+                __syncwarp(some);
+                if (rank == 0) mine[row[u]] = base + __popc(same);
+                order[base + rank] = t0 + u * 32 + lane;
+            }
+            __syncwarp();
+        }
+    };
+    deal(begin, kept);
+    for (int t0 = begin + 32 * kSortUnroll; t0 < end; t0 += 32 * kSortUnroll) {
+        unsigned row[kSortUnroll];
+        fetch(t0, row, less);
+        deal(t0, row);
+    }
+}
+
+// (2) The work is the list of all rows, each with its reads and then its write, laid out on a line whose unit is a byte of
+// traffic per column; `workers` groups of GROUP threads take equal stretches of it, whatever the ids are.  A stretch that ends in
+// a run of more than kWholeRun tokens cuts it (the part before goes to `carry`, the part in which the row ends to `tail`); shorter
+// runs go whole to the worker they end with.
+constexpr int kWholeRun = 64;
+
+struct EmbedSum {
+    const int* start;      // [slots + 1]
+    const int* order;      // [tokens]
+    float* carry;          // [workers][dim]
+    float* tail;           // [workers][dim]
+    int* cuts;             // rows that are put together from parts
+    int4* cut;             // [cuts] (row, first worker that holds a part of it, the one in which it ends, 0), in any order
+    int vocab, dim, workers;
+    int bits, per_class, slots;     // slot = (id mod 2^bits) * per_class + id / 2^bits; those of ids >= vocab are empty
+    int read_cost, row_cost;
+    float scale;
+};
+struct Bound {
+    int row, read;         // reads before `read` and slots before `row` lie before the bound
+};
+__device__ __forceinline__ int slot_id(const EmbedSum& a, int slot) { return ((slot % a.per_class) << a.bits) + slot / a.per_class; }
+// The bounds at x0 <= x1, one search in each half of the warp; all lanes call this with the same arguments and get the same answer.
+__device__ __forceinline__ void embed_bounds(const EmbedSum& a, long x0, long x1, Bound& b0, Bound& b1) {
+    const int lane = threadIdx.x % 32, half = lane / 16, probe = lane % 16;
+    const long x = half ? x1 : x0;
+    auto line = [&](int v, int s) { return (long)s * a.read_cost + (long)v * a.row_cost; };
+    // the last slot v in [0, slots] with line(v) <= x: 16 probes a step, of which the first always holds
+    int lo = 0;
+    for (int n = a.slots + 1; n > 1;) {
+        const int step = (n + 15) / 16, v = lo + probe * step;
+        const bool before = v <= a.slots && line(v, __ldg(a.start + v)) <= x;
+        const unsigned hits = __ballot_sync(0xffffffffu, before) >> (half * 16) & 0xffffu;
+        lo += (31 - __clz(hits)) * step;
+        n = step;
+    }
+    const int s = __ldg(a.start + lo), cnt = lo < a.slots ? __ldg(a.start + lo + 1) - s : 0;
+    int read = s;
+    if (cnt > kWholeRun) {
+        const long into = (x - line(lo, s) + a.read_cost - 1) / a.read_cost;
+        read += (int)(into < cnt ? into : cnt);
+    }
+    b0 = Bound{__shfl_sync(0xffffffffu, lo, 0), __shfl_sync(0xffffffffu, read, 0)};
+    b1 = Bound{__shfl_sync(0xffffffffu, lo, 16), __shfl_sync(0xffffffffu, read, 16)};
+}
+
+// A thread has PARTS vectors of a row, GROUP vectors apart: enough bytes a row that the walk over rows costs little next to them.
+constexpr int kSumBlocks = 4;        // resident blocks of 256 threads on an SM, 48 KB of ring each
+constexpr int ring_depth(int bytes) { return bytes <= 16 ? 12 : 6; }
+// Copies BYTES from global to shared memory without waiting where that is possible (4, 8 or 16 bytes).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+    else if constexpr (BYTES >= 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+    else
+        *static_cast<uint16_t*>(dst) = *static_cast<const uint16_t*>(src);
+}
+template <typename TT, typename TY, int VEC, int PARTS, int GROUP>
+__global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, const TY* __restrict__ dy, TT* __restrict__ dt) {
+    // Loads run ahead of the sums over the sorted tokens, whatever the rows they belong to: DEPTH tokens are in flight in a ring of
+    // shared memory in which every thread copies and reads its own vectors (no barrier between threads is needed).
+    constexpr int BYTES = VEC * (int)sizeof(TY), DEPTH = ring_depth(PARTS * BYTES);
+    extern __shared__ __align__(16) unsigned char ring[];
+    auto place = [&](int slot, int c) { return ring + ((size_t)(slot * PARTS + c) * 256 + threadIdx.x) * BYTES; };
+    pdl_trigger();
+    pdl_wait();
+    const int p = blockIdx.x * (256 / GROUP) + threadIdx.x / GROUP, lane = threadIdx.x % 32;
+    if (p >= a.workers) return;      // whole warps: GROUP is a multiple of 32
+    const int col = (int)(blockIdx.y * (PARTS * GROUP) + threadIdx.x % GROUP) * VEC;
+    const long total = (long)__ldg(a.start + a.slots) * a.read_cost + (long)a.slots * a.row_cost;
+    Bound from, to;
+    embed_bounds(a, (long)((double)total * p / a.workers), p + 1 == a.workers ? total : (long)((double)total * (p + 1) / a.workers), from, to);
+    int j = from.read, ahead = j, tokens = 0, slot = 0, slot_in = 0;      // `tokens`: 32 sorted tokens, one a lane, of which `ahead` is next
+    auto fetch = [&]() {
+        if (ahead < to.read) {
+            const int k = (ahead - from.read) % 32;
+            if (k == 0) tokens = ahead + lane < to.read ? __ldg(a.order + ahead + lane) : 0;
+            const TY* src = dy + (long)__shfl_sync(0xffffffffu, tokens, k) * a.dim + col;
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c)
+                if (col + c * GROUP * VEC < a.dim) copy_async<BYTES>(place(slot_in, c), src + c * GROUP * VEC);
+            ++ahead;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        slot_in = slot_in + 1 == DEPTH ? 0 : slot_in + 1;
+    };
+#pragma unroll 1
+    for (int u = 0; u < DEPTH; ++u) fetch();
+    int in_class = from.row % a.per_class, id = slot_id(a, from.row), ends = 0;
+    bool begun = from.read > __ldg(a.start + from.row);     // the first row began in an earlier stretch
+    for (int v = from.row;; ++v) {
+        const int k = (v - from.row) % 32;
+        if (k == 0) ends = __ldg(a.start + (v + lane < a.slots ? v + lane + 1 : a.slots));
+        const bool open = v == to.row;                      // the part of a row that ends in a later stretch
+        const int end = open ? to.read : __shfl_sync(0xffffffffu, ends, k);
+        if (open && end == j && !(begun && v == from.row)) break;
+        float sum[PARTS][VEC];
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[c][e] = 0.f;
+#pragma unroll 1
+        for (; j < end; ++j) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c)
+                if (col + c * GROUP * VEC < a.dim) {
+                    RawVec<TY, VEC> raw;
+                    raw.load(reinterpret_cast<const TY*>(place(slot, c)));
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[c][e] += raw.get(e);
+                }
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
+            fetch();
+        }
+        if (open || begun) {
+            float* part = (open ? a.carry : a.tail) + (size_t)p * a.dim + col;
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c)
+                if (col + c * GROUP * VEC < a.dim) store_vec<VEC>(part + c * GROUP * VEC, sum[c]);
+            if (open) break;
+            begun = false;
+            if (blockIdx.y == 0 && threadIdx.x % GROUP == 0) {
+                const double at = (double)__ldg(a.start + v) * a.read_cost + (double)v * a.row_cost;
+                int q = (int)(at / (double)total * a.workers);                 // the stretch that holds the row's first read, up to rounding
+                while (q > 0 && (long)((double)total * q / a.workers) > (long)at) --q;
+                while ((long)((double)total * (q + 1) / a.workers) <= (long)at) ++q;
+                a.cut[atomicAdd(a.cuts, 1)] = make_int4(id, q, p, 0);
+            }
+        } else if (id < a.vocab) {
+            TT* row = dt + (size_t)id * a.dim + col;
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c)
+                if (col + c * GROUP * VEC < a.dim) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[c][e] *= a.scale;
+                    store_vec_once<VEC>(row + c * GROUP * VEC, sum[c]);
+                }
+        }
+        id += 1 << a.bits;
+        if (++in_class == a.per_class) {
+            in_class = 0;
+            id = (v + 1) / a.per_class;
+        }
+    }
+}
+
+// (3) Rows that were cut: carry of the stretches before, in their order, and the tail.  A warp takes 128 columns of a row; where
+// the row has many parts, a block takes 32 columns and its 8 warps share the parts, so that a row with most of the tokens is no
+// chain of loads.
+constexpr int kLongChain = 6;
+
+template <typename TT>
+__global__ void __launch_bounds__(256) embed_join_kernel(EmbedSum a, TT* __restrict__ dt) {
+    pdl_wait();
+    __shared__ float parts[8][33];
+    const int cuts = *a.cuts, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int slices = (a.dim + 127) / 128, thin = (a.dim + 31) / 32;
+    for (int item = blockIdx.x * 8 + warp; item < cuts * slices; item += gridDim.x * 8) {
+        const int4 cut = a.cut[item / slices];
+        if (cut.z - cut.y > kLongChain) continue;
+        const int col = item % slices * 128 + lane;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int q = cut.y; q <= cut.z; ++q) {
+            const float* src = (q < cut.z ? a.carry : a.tail) + (size_t)q * a.dim;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + 32 * e < a.dim) sum[e] += src[col + 32 * e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + 32 * e < a.dim) store_one(dt + (size_t)cut.x * a.dim + col + 32 * e, a.scale * sum[e]);
+    }
+    for (int k = 0; k < cuts; ++k) {
+        const int4 cut = a.cut[k];
+        const int n = cut.z - cut.y;
+        if (n <= kLongChain) continue;
+        const int per = (n + 7) / 8;
+        for (int s = blockIdx.x; s < thin; s += gridDim.x) {
+            const int col = s * 32 + lane, from = cut.y + warp * per, to = from + per < cut.z ? from + per : cut.z;
+            float sum = 0.f;
+            if (col < a.dim)
+#pragma unroll 8
+                for (int q = from; q < to; ++q) sum += a.carry[(size_t)q * a.dim + col];
+            parts[warp][lane] = sum;
+            __syncthreads();
+            if (warp == 0 && col < a.dim) {
+#pragma unroll
+                for (int w = 1; w < 8; ++w) sum += parts[w][lane];
+                store_one(dt + (size_t)cut.x * a.dim + col, a.scale * (sum + a.tail[(size_t)cut.z * a.dim + col]));
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Launch shape of a backward call and its pieces of the workspace.
+struct EmbedPlan {
+    int bits, rows_per_block, blocks, vec, parts, group, slices, workers;
+    size_t order_at, carry_at, tail_at, cut_at, bytes;
+};
+static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
+    EmbedPlan pl;
+    pl.bits = 7;     // 128 classes: a block on most of the SMs, and no division
+    while (((e->vocab - 1) >> pl.bits) + 1 > kSortRows) ++pl.bits;
+    pl.blocks = 1 << pl.bits;
+    pl.rows_per_block = ((e->vocab - 1) >> pl.bits) + 1;
+    // 16-byte accesses of the wider type: whole lines for a warp on both sides
+    const int wide = e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
+    pl.vec = aligned && e->dim % 8 == 0 ? wide : 1;
+    const int vectors = (e->dim + pl.vec - 1) / pl.vec;
+    pl.parts = vectors > 32 ? 2 : 1;
+    const int threads = (vectors + pl.parts - 1) / pl.parts;
+    pl.group = threads <= 32 ? 32 : threads <= 64 ? 64 : threads <= 128 ? 128 : 256;
+    pl.slices = (threads + pl.group - 1) / pl.group;
+    // stretches of equal traffic, two for each place on the machine: reads take longer than writes of the same size, and the second
+    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); a few rows each at least
+    long workers = 2 * 148L * kSumBlocks * 256 / pl.group / pl.slices;
+    const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 3) / 4;
+    if (workers > most) workers = most;
+    pl.workers = (int)(workers < 1 ? 1 : workers);
+    auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    pl.order_at = up(sizeof(int) * ((size_t)pl.blocks * pl.rows_per_block + 1));
+    pl.carry_at = pl.order_at + up(sizeof(int) * (size_t)(tokens ? tokens : 1));
+    pl.tail_at = pl.carry_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
+    pl.cut_at = pl.tail_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
+    pl.bytes = pl.cut_at + 256 + up(sizeof(int4) * (size_t)pl.workers);
+    return pl;
+}
+// What a call of this many tokens needs, whatever the alignment of its pointers.
+static size_t embed_bytes(const Embed* e, long tokens) {
+    const size_t a = plan_embed(e, tokens, true).bytes, b = plan_embed(e, tokens, false).bytes;
+    return a > b ? a : b;
 }
 
 static int check_embed(const Embed* e, long tokens) {
@@ -112,7 +483,8 @@ int circ_embed_set_padding(circ_embed_handle h, long padding) {
 
 int circ_embed_reserve(circ_embed_handle h, long max_tokens) {
     Embed* e = reinterpret_cast<Embed*>(h);
-    return check_embed(e, max_tokens);
+    const int rc = check_embed(e, max_tokens);
+    return rc != CIRC_OK ? rc : ensure_scratch(e->ws, embed_bytes(e, max_tokens), 0, "circ_embed_reserve");
 }
 
 int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, void* y, long tokens, void* stream) {
@@ -127,15 +499,29 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
         set_error(CIRC_ERR_ARG, "table, ids and y must be aligned to their element sizes");
         return CIRC_ERR_ARG;
     }
+    if (tokens > (1L << 48) / e->dim) {
+        set_error(CIRC_ERR_SHAPE, "tokens=%ld of %d elements are too many", tokens, e->dim);
+        return CIRC_ERR_SHAPE;
+    }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool vec = e->dim % 8 == 0 && !misaligned(table, 16) && !misaligned(y, 16);
     with_dtype(e->table_dtype, [&](auto* t) {
         with_dtype(e->y_dtype, [&](auto* o) {
             with_index_type(e->ids_type, [&](auto* i) {
                 using TT = tag_type<decltype(t)>;
                 using TY = tag_type<decltype(o)>;
                 using ID = tag_type<decltype(i)>;
-                embed_forward_kernel<TT, TY, ID><<<(unsigned)tokens, 256, 0, s>>>(
-                    static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), e->vocab, e->dim, e->scale, e->padding);
+                auto go = [&](auto kernel, int vec, int unroll) {
+                    const int per_row = e->dim / vec;
+                    const long vectors = tokens * per_row, blocks = (vectors + 256L * unroll - 1) / (256L * unroll);
+                    kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), vectors,
+                                                            per_row, e->vocab, e->dim, e->scale, e->padding);
+                };
+                if (vec)
+                    tokens * (e->dim / 8) <= 148L * 256 ? go(embed_forward_kernel<TT, TY, ID, 8, 1>, 8, 1)    // one vector a thread fills the machine
+                                                        : go(embed_forward_kernel<TT, TY, ID, 8, 4>, 8, 4);
+                else
+                    go(embed_forward_kernel<TT, TY, ID, 1, 8>, 1, 8);
             });
         });
     });
@@ -158,19 +544,54 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    with_dtype(e->table_dtype, [&](auto* t) {
-        with_dtype(e->y_dtype, [&](auto* o) {
-            with_index_type(e->ids_type, [&](auto* i) {
-                using TT = tag_type<decltype(t)>;
-                using TY = tag_type<decltype(o)>;
-                using ID = tag_type<decltype(i)>;
-                embed_backward_kernel<TT, TY, ID><<<(unsigned)e->vocab, 256, 0, s>>>(
-                    static_cast<const ID*>(ids), static_cast<const TY*>(grad_y), static_cast<TT*>(grad_table), tokens, e->dim, e->scale,
-                    e->padding);
-            });
-        });
+    if ((rc = ensure_scratch(e->ws, embed_bytes(e, tokens), s, "circ_embed_reserve")) != CIRC_OK) return rc;
+    const EmbedPlan pl = plan_embed(e, tokens, !misaligned(grad_y, 16) && !misaligned(grad_table, 16));
+    char* ws = static_cast<char*>(e->ws.ptr);
+    int* start = reinterpret_cast<int*>(ws);
+    int* order = reinterpret_cast<int*>(ws + pl.order_at);
+    const EmbedSum a{start, order, reinterpret_cast<float*>(ws + pl.carry_at), reinterpret_cast<float*>(ws + pl.tail_at),
+                     reinterpret_cast<int*>(ws + pl.cut_at), reinterpret_cast<int4*>(ws + pl.cut_at + 256), e->vocab, e->dim, pl.workers, pl.bits, pl.rows_per_block,
+                     pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype),
+                     (int)dtype_bytes(e->table_dtype), e->scale};
+    const size_t smem = sizeof(int) * kSortWarps * (size_t)pl.rows_per_block;
+    cudaError_t err = cudaSuccess;
+    with_index_type(e->ids_type, [&](auto* i) {
+        using ID = tag_type<decltype(i)>;
+        err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(int) * kSortWarps * kSortRows));
+        if (err != cudaSuccess) return;
+        embed_sort_kernel<ID><<<pl.blocks, kSortThreads, smem, s>>>(static_cast<const ID*>(ids), (int)tokens, e->vocab, (unsigned)e->padding,
+                                                                    pl.bits, pl.rows_per_block, start, order, a.cuts);
     });
-    count_launches(1);
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
+    with_dtype(e->table_dtype, [&](auto* t) {
+        using TT = tag_type<decltype(t)>;
+        with_dtype(e->y_dtype, [&](auto* o) {
+            using TY = tag_type<decltype(o)>;
+            constexpr int WIDE = std::is_same<TY, __nv_bfloat16>::value && std::is_same<TT, __nv_bfloat16>::value ? 8 : 4;
+            auto go = [&](auto kernel) {
+                const int per_block = 256 / pl.group, bytes = pl.parts * pl.vec * (int)sizeof(TY);
+                const size_t ring = (size_t)ring_depth(bytes) * bytes * 256;
+                err = launch_kernel(PDL_EARLY, kernel, dim3((pl.workers + per_block - 1) / per_block, pl.slices), 256, ring, s, a,
+                                    static_cast<const TY*>(grad_y), static_cast<TT*>(grad_table));
+            };
+            auto by_group = [&](auto vec, auto parts) {
+                constexpr int V = decltype(vec)::value, P = decltype(parts)::value;
+                pl.group == 32 ? go(embed_sum_kernel<TT, TY, V, P, 32>) : pl.group == 64 ? go(embed_sum_kernel<TT, TY, V, P, 64>)
+                    : pl.group == 128 ? go(embed_sum_kernel<TT, TY, V, P, 128>) : go(embed_sum_kernel<TT, TY, V, P, 256>);
+            };
+            using One = std::integral_constant<int, 1>;
+            using Two = std::integral_constant<int, 2>;
+            using Wide = std::integral_constant<int, WIDE>;
+            if (pl.parts == 1)     // at most 32 vectors a row
+                pl.vec == 1 ? go(embed_sum_kernel<TT, TY, 1, 1, 32>) : go(embed_sum_kernel<TT, TY, WIDE, 1, 32>);
+            else
+                pl.vec == 1 ? by_group(One{}, Two{}) : by_group(Wide{}, Two{});
+        });
+        if (err == cudaSuccess && tokens > kWholeRun)
+            err = launch_kernel(PDL_EARLY, embed_join_kernel<TT>, dim3(148), 256, 0, s, a, static_cast<TT*>(grad_table));
+    });
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
+    count_launches(2 + (tokens > kWholeRun));
     CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
     return CIRC_OK;
 }

@@ -3,6 +3,8 @@
 #pragma once
 #include <math.h>
 
+#include <type_traits>
+
 #include "circ_common.cuh"
 #include "circ_io.cuh"
 
@@ -29,6 +31,101 @@ inline void with_index_type(int type, F&& f) {
 }
 template <typename T>
 using tag_type = std::remove_pointer_t<T>;
+
+// VEC consecutive elements <-> float32 registers: 16-byte accesses (the address must be 16-byte aligned), or VEC = 1.
+template <int VEC>
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        v[0] = *p;
+    } else {
+#pragma unroll
+        for (int r = 0; r < VEC; r += 4) {
+            const float4 t = *reinterpret_cast<const float4*>(p + r);
+            v[r] = t.x; v[r + 1] = t.y; v[r + 2] = t.z; v[r + 3] = t.w;
+        }
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        v[0] = __bfloat162float(*p);
+    } else if constexpr (VEC == 4) {      // 8 bytes
+        const uint2 t = *reinterpret_cast<const uint2*>(p);
+        v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xffff0000u);
+        v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int r = 0; r < VEC; r += 8) {
+            const uint4 t = *reinterpret_cast<const uint4*>(p + r);
+            const uint32_t u[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {     // a bfloat16 is the upper half of a float32
+                v[r + 2 * h] = __uint_as_float(u[h] << 16);
+                v[r + 2 * h + 1] = __uint_as_float(u[h] & 0xffff0000u);
+            }
+        }
+    }
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void store_vec(T* p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1)
+        store_one(p, v[0]);
+    else
+        store_run<VEC>(p, v);
+}
+
+// The same for outputs that this kernel does not read again (first to leave the L2 cache).
+template <int VEC>
+__device__ __forceinline__ void store_vec_once(float* p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1)
+        __stcs(p, v[0]);
+    else
+#pragma unroll
+        for (int r = 0; r < VEC; r += 4) __stcs(reinterpret_cast<float4*>(p + r), make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]));
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec_once(__nv_bfloat16* p, const float (&v)[VEC]) {
+    if constexpr (VEC == 1)
+        store_one(p, v[0]);
+    else if constexpr (VEC == 4)
+        __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])));
+    else
+#pragma unroll
+        for (int r = 0; r < VEC; r += 8)
+            __stcs(reinterpret_cast<uint4*>(p + r), make_uint4(pack_bf16(v[r], v[r + 1]), pack_bf16(v[r + 2], v[r + 3]),
+                                                              pack_bf16(v[r + 4], v[r + 5]), pack_bf16(v[r + 6], v[r + 7])));
+}
+
+// The same, kept as loaded until an element is asked for (half the registers of bfloat16 data in flight).
+template <typename T, int VEC>
+struct RawVec {
+    static constexpr int WORDS = (int)(VEC * sizeof(T) + 3) / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (VEC == 1) {
+            w[0] = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)*reinterpret_cast<const uint16_t*>(p);
+        } else if constexpr (WORDS == 2) {
+            const uint2 t = *reinterpret_cast<const uint2*>(p);
+            w[0] = t.x; w[1] = t.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; i += 4) {
+                const uint4 t = *reinterpret_cast<const uint4*>(p + i * 4 / (int)sizeof(T));
+                w[i] = t.x; w[i + 1] = t.y; w[i + 2] = t.z; w[i + 3] = t.w;
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(w[e]);
+        else      // a bfloat16 is the upper half of a float32
+            return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    }
+};
 
 // Sum over the lanes of a warp, the same bits in every lane.
 __device__ __forceinline__ float warp_sum(float v) {
