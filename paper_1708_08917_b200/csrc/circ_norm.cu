@@ -31,28 +31,167 @@ __device__ __forceinline__ float from_e4m3(uint8_t v) {
 // group's values have no meaning then, and the NaN says so).
 __device__ __forceinline__ float group_scale(float top) { return top == 0.f ? 1.f : top <= 3.402823466e38f ? top / kE4m3Max : NAN; }
 
+// The e4m3 codes of VEC values, packed (`mine`: the values' lanes that exist).
+template <int VEC>
+__device__ __forceinline__ void pack_e4m3(const float (&v)[VEC], uint32_t (&w)[VEC / 4]) {
+#pragma unroll
+    for (int e = 0; e < VEC; e += 4) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[e], v[e + 1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[e + 2], v[e + 3]), __NV_SATFINITE, __NV_E4M3);
+        w[e / 4] = lo | hi << 16;
+    }
+}
+
+struct NormForward {
+    const float* gain;
+    float* y_scale;
+    float* rstd;
+    long rows;
+    int dim, group;
+    float eps;
+};
+
+// One row per `threads` threads (a warp: several rows a block), every value read once and kept in registers until the row's sum
+// is known: the memory traffic is the floor's.  The sum of the residual stream leaves before the reduction.  A whole-row scale comes
+// with the same reduction as the mean, from max|s gain| (y = rstd s gain, and rstd > 0).
+template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED>
+__global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX* residual, TX* sum, TY* y, NormForward a) {
+    constexpr bool E4M3 = std::is_same<TY, uint8_t>::value;
+    __shared__ float red[2][16];
+    const int threads = blockDim.x, tid = threadIdx.x;
+    const long row = (long)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= a.rows) return;       // whole warps; blocks of several rows have one warp a row and no barrier
+    const RowSpan<VEC, ALIGNED> span(row, a.dim);
+    float s[ITEMS][VEC];
+    {
+        RawVec<TX, VEC> xr[ITEMS], rr[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.load(xr[i], x, tid + i * threads);
+        if (residual) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) span.load(rr[i], residual, tid + i * threads);
+        } else {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) rr[i].clear();
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s[i][e] = xr[i].get(e) + rr[i].get(e);
+    }
+    if (sum)
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.store(sum, tid + i * threads, s[i]);
+    const bool row_scale = E4M3 && a.group == a.dim;
+    float sq = 0.f, top = 0.f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sq = fmaf(s[i][e], s[i][e], sq);
+        if (row_scale) {
+            float g[VEC];
+            span.load_columns(g, a.gain, tid + i * threads);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) top = max_nan(top, fabsf(s[i][e] * g[e]));
+        }
+    }
+    sq = warp_sum(sq);
+    if (row_scale) top = warp_max_nan(top);
+    if (threads > 32) {
+        const int warps = threads / 32, lane = tid % 32;
+        if (lane == 0) {
+            red[0][tid / 32] = sq;
+            red[1][tid / 32] = top;
+        }
+        __syncthreads();
+        sq = warp_sum(lane < warps ? red[0][lane] : 0.f);
+        if (row_scale) top = warp_max_nan(lane < warps ? red[1][lane] : 0.f);
+    }
+    const float rstd = rsqrtf(sq / (float)a.dim + a.eps);
+    if (a.rstd && tid == 0) a.rstd[row] = rstd;
+    float inv = 0.f;
+    if (row_scale) {
+        const float scale = group_scale(top * rstd);
+        inv = 1.f / scale;
+        if (tid == 0) a.y_scale[row] = scale;
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int v = tid + i * threads;
+        float out[VEC];
+        span.load_columns(out, a.gain, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) out[e] *= s[i][e] * rstd;
+        if constexpr (E4M3) {
+            if (!row_scale) {      // the lanes of a group (32, 64 or 128 elements) are neighbours in the warp, and groups do not cross rows
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) t = max_nan(t, fabsf(out[e]));
+                for (int o = a.group / VEC / 2; o > 0; o >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, o));
+                const float scale = group_scale(t);
+                inv = 1.f / scale;
+                if (span.any(v) && v % (a.group / VEC) == 0) a.y_scale[(row * a.dim + span.col(v)) / a.group] = scale;
+            }
+            // times 1 / scale instead of a division by scale: at most the rounding of a value that lies in the middle between two
+            // codes changes
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) out[e] *= inv;
+            uint32_t w[VEC / 4];
+            pack_e4m3<VEC>(out, w);
+            if (!span.any(v)) continue;
+            uint8_t* dst = y + span.at(v);
+            if (span.whole(v)) {
+                if constexpr (VEC == 8)
+                    *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+                else
+                    *reinterpret_cast<uint32_t*>(dst) = w[0];
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (e >= span.lo(v) && e < span.hi(v)) dst[e] = (uint8_t)(w[e / 4] >> (e % 4 * 8));
+            }
+        } else {
+            span.store(y, v, out);
+        }
+    }
+}
+
+// Rows that do not fit the registers of a block, or tensors that do not start on 16-byte boundaries: element by element, rows
+// read again (from L1 / L2) for each step.
 template <typename TX, typename TY>
-__global__ void __launch_bounds__(256) norm_forward_kernel(const TX* x, const TX* residual, const float* __restrict__ gain, TX* sum, TY* y,
-                                                           float* y_scale, float* rstd_out, int dim, int group, float eps) {
+__global__ void __launch_bounds__(512) norm_forward_any_kernel(const TX* x, const TX* residual, TX* sum, TY* y, NormForward a) {
     __shared__ float red[33];
+    const int dim = a.dim, group = a.group;
     const size_t row = blockIdx.x, base = row * dim;
     auto value = [&](int c) { return to_float(x[base + c]) + (residual ? to_float(residual[base + c]) : 0.f); };
+    auto gained = [&](int c, float rstd) { return value(c) * rstd * (a.gain ? a.gain[c] : 1.f); };
     float sq = 0.f;
     for (int c = threadIdx.x; c < dim; c += blockDim.x) {
         const float v = value(c);
         sq = fmaf(v, v, sq);
     }
-    const float rstd = rsqrtf(block_sum(sq, red) / (float)dim + eps);
-    if (rstd_out && threadIdx.x == 0) rstd_out[row] = rstd;
+    const float rstd = rsqrtf(block_sum(sq, red) / (float)dim + a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
     if constexpr (std::is_same<TY, uint8_t>::value) {
-        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-        for (int g = warp; g < dim / group; g += blockDim.x / 32) {
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
+        if (group == dim) {
             float top = 0.f;
-            for (int c = lane; c < group; c += 32) top = max_nan(top, fabsf(value(g * group + c) * rstd * (gain ? gain[g * group + c] : 1.f)));
-            const float scale = group_scale(warp_max_nan(top));
-            if (lane == 0) y_scale[row * (dim / group) + g] = scale;
-            for (int c = g * group + lane; c < (g + 1) * group; c += 32)
-                y[base + c] = to_e4m3(value(c) * rstd * (gain ? gain[c] : 1.f) / scale);
+            for (int c = threadIdx.x; c < dim; c += blockDim.x) top = max_nan(top, fabsf(gained(c, rstd)));
+            top = warp_max_nan(top);
+            __syncthreads();
+            if (lane == 0) red[warp] = top;
+            __syncthreads();
+            const float scale = group_scale(warp_max_nan(lane < warps ? red[lane] : 0.f));
+            if (threadIdx.x == 0) a.y_scale[row] = scale;
+            for (int c = threadIdx.x; c < dim; c += blockDim.x) y[base + c] = to_e4m3(gained(c, rstd) * (1.f / scale));
+        } else {
+            for (int g = warp; g < dim / group; g += warps) {
+                float top = 0.f;
+                for (int c = lane; c < group; c += 32) top = max_nan(top, fabsf(gained(g * group + c, rstd)));
+                const float scale = group_scale(warp_max_nan(top));
+                if (lane == 0) a.y_scale[row * (dim / group) + g] = scale;
+                for (int c = g * group + lane; c < (g + 1) * group; c += 32) y[base + c] = to_e4m3(gained(c, rstd) * (1.f / scale));
+            }
         }
         __syncthreads();    // sum may be x or residual
         if (sum)
@@ -60,36 +199,165 @@ __global__ void __launch_bounds__(256) norm_forward_kernel(const TX* x, const TX
     } else {
         for (int c = threadIdx.x; c < dim; c += blockDim.x) {
             const float v = value(c);
-            store_one(y + base + c, v * rstd * (gain ? gain[c] : 1.f));
+            store_one(y + base + c, v * rstd * (a.gain ? a.gain[c] : 1.f));
             if (sum) store_one(sum + base + c, v);
         }
     }
 }
 
-template <typename TX, typename TY>
-__global__ void __launch_bounds__(256) norm_backward_kernel(const TX* __restrict__ sum, const float* __restrict__ gain,
-                                                            const float* __restrict__ rstd_in, const TY* __restrict__ dy, const TX* ds, TX* dx, int dim) {
-    __shared__ float red[33];
-    const size_t row = blockIdx.x, base = row * dim;
-    const float rstd = rstd_in[row];
-    float dot = 0.f;
-    for (int c = threadIdx.x; c < dim; c += blockDim.x)
-        dot = fmaf(to_float(dy[base + c]) * (gain ? gain[c] : 1.f), to_float(sum[base + c]) * rstd, dot);
-    dot = block_sum(dot, red) / (float)dim;
-    for (int c = threadIdx.x; c < dim; c += blockDim.x) {
-        const float u = to_float(dy[base + c]) * (gain ? gain[c] : 1.f), hh = to_float(sum[base + c]) * rstd;
-        store_one(dx + base + c, rstd * (u - hh * dot) + (ds ? to_float(ds[base + c]) : 0.f));
+// ---- backward ------------------------------------------------------------------------------------------------
+// One pass over the tensors gives both gradients: a block walks rows blockIdx.x, + gridDim.x, ..., holds a row in registers while its
+// mean(u h) is summed up, and adds grad_y h to its own columns' share of grad_gain, in registers.  The shares of the blocks go to
+// `part` [blocks][dim], and a second kernel adds them up in the blocks' order.
+struct NormBackward {
+    const float* gain;
+    const float* rstd;
+    float* part;        // NULL: grad_gain is not wanted
+    long rows;
+    int dim;
+};
+
+template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED>
+__global__ void __launch_bounds__(512) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
+    __shared__ float red[2][16];
+    pdl_trigger();
+    const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
+    // rows do not start at the same column of a vector when they are not aligned: a share is kept by column then, in shared memory
+    extern __shared__ __align__(16) float share[];
+    float acc[ITEMS][VEC];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[i][e] = 0.f;
+    if (!ALIGNED && a.part) {
+        for (int c = tid; c < a.dim; c += threads) share[c] = 0.f;
+        __syncthreads();
+    }
+    int flip = 0;
+    for (long row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+        const RowSpan<VEC, ALIGNED> span(row, a.dim);
+        RawVec<TX, VEC> sr[ITEMS], cr[ITEMS];
+        RawVec<TY, VEC> yr[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.load(sr[i], sum, tid + i * threads);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.load(yr[i], dy, tid + i * threads);
+        if (ds && dx) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) span.load(cr[i], ds, tid + i * threads);
+        } else {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) cr[i].clear();
+        }
+        const float rstd = __ldg(a.rstd + row);
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float g[VEC];
+            span.load_columns(g, a.gain, tid + i * threads);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float h = sr[i].get(e) * rstd, d = yr[i].get(e);
+                dot = fmaf(d * g[e], h, dot);
+                if constexpr (ALIGNED) acc[i][e] = fmaf(d, h, acc[i][e]);
+            }
+            if (!ALIGNED && a.part) {
+                const int v = tid + i * threads;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)     // a column is one thread's in each row, and rows are separated by the barrier below
+                    if (span.any(v) && e >= span.lo(v) && e < span.hi(v))
+                        share[span.col(v) + e] = fmaf(yr[i].get(e), sr[i].get(e) * rstd, share[span.col(v) + e]);
+            }
+        }
+        dot = warp_sum(dot);
+        if (lane == 0) red[flip][tid / 32] = dot;
+        __syncthreads();                          // the other half of `red` serves the next row
+        dot = warp_sum(lane < threads / 32 ? red[flip][lane] : 0.f) / (float)a.dim;
+        if (!dx) continue;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float g[VEC];
+            span.load_columns(g, a.gain, tid + i * threads);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) g[e] = rstd * (yr[i].get(e) * g[e] - sr[i].get(e) * rstd * dot) + cr[i].get(e);
+            span.store(dx, tid + i * threads, g);
+        }
+    }
+    if (!a.part) return;
+    float* part = a.part + (size_t)blockIdx.x * a.dim;
+    if constexpr (ALIGNED) {
+        const RowSpan<VEC, true> span(0, a.dim);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.store(part, tid + i * threads, acc[i]);
+    } else {
+        __syncthreads();
+        for (int c = tid; c < a.dim; c += threads) part[c] = share[c];
     }
 }
 
 template <typename TX, typename TY>
-__global__ void __launch_bounds__(256) norm_gain_kernel(const TX* __restrict__ sum, const float* __restrict__ rstd, const TY* __restrict__ dy,
-                                                        float* __restrict__ dgain, long rows, int dim) {
-    const int c = blockIdx.x * blockDim.x + threadIdx.x;
-    if (c >= dim) return;
+__global__ void __launch_bounds__(512) norm_backward_any_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
+    __shared__ float red[33];
+    const int dim = a.dim;
+    const size_t row = blockIdx.x, base = row * dim;
+    const float rstd = a.rstd[row];
+    auto gain = [&](int c) { return a.gain ? a.gain[c] : 1.f; };
+    float dot = 0.f;
+    for (int c = threadIdx.x; c < dim; c += blockDim.x) dot = fmaf(to_float(dy[base + c]) * gain(c), to_float(sum[base + c]) * rstd, dot);
+    dot = block_sum(dot, red) / (float)dim;
+    for (int c = threadIdx.x; c < dim; c += blockDim.x)
+        store_one(dx + base + c, rstd * (to_float(dy[base + c]) * gain(c) - to_float(sum[base + c]) * rstd * dot) + (ds ? to_float(ds[base + c]) : 0.f));
+}
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(256) norm_gain_any_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, NormBackward a) {
+    pdl_trigger();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.dim) return;
     float acc = 0.f;
-    for (long r = 0; r < rows; ++r) acc = fmaf(to_float(dy[r * dim + c]), to_float(sum[r * dim + c]) * rstd[r], acc);
-    dgain[c] = acc;
+#pragma unroll 4
+    for (long r = blockIdx.y; r < a.rows; r += gridDim.y) acc = fmaf(to_float(dy[r * a.dim + c]), to_float(sum[r * a.dim + c]) * __ldg(a.rstd + r), acc);
+    a.part[(size_t)blockIdx.y * a.dim + c] = acc;
+}
+
+// grad_gain[c] = part[0][c] + part[1][c] + ...: a block has 32 columns, its warps take consecutive parts.
+__global__ void __launch_bounds__(512) norm_gain_kernel(const float* __restrict__ part, float* __restrict__ dgain, int parts, int dim) {
+    __shared__ float sums[16][33];
+    pdl_wait();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = blockIdx.x * 32 + lane;
+    const int per = (parts + 15) / 16, from = warp * per, to = from + per < parts ? from + per : parts;
+    float s = 0.f;
+    if (c < dim)
+#pragma unroll 8
+        for (int i = from; i < to; ++i) s += part[(size_t)i * dim + c];
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < dim) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += sums[w][lane];
+        dgain[c] = s;
+    }
+}
+
+constexpr int kNormParts = 148 * 4;   // blocks of a backward call at most
+
+// Launch shape of a row kernel: `items` vectors a thread (1, 2, 4 or 8), `threads` a multiple of 32 (at most 512); items 0: the row
+// does not fit.  Rows of one warp are put several in a block.
+struct RowShape {
+    int items, threads;
+};
+static RowShape row_shape(int vectors, int want_items) {
+    for (int items = want_items; items <= 8; items *= 2) {
+        const int threads = ((vectors + items - 1) / items + 31) / 32 * 32;
+        if (threads <= 512) return RowShape{items, threads};
+    }
+    return RowShape{0, 0};
+}
+template <typename F>
+static void with_items(int items, F&& f) {
+    if (items == 1) f(std::integral_constant<int, 1>{});
+    else if (items == 2) f(std::integral_constant<int, 2>{});
+    else if (items == 4) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 8>{});
 }
 
 template <typename TO>
@@ -168,7 +436,8 @@ int circ_norm_set_group(circ_norm_handle h, int group) {
 
 int circ_norm_reserve(circ_norm_handle h) {
     Norm* n = reinterpret_cast<Norm*>(h);
-    return check_norm(n, 0);
+    const int rc = check_norm(n, 0);
+    return rc != CIRC_OK ? rc : ensure_scratch(n->ws, sizeof(float) * kNormParts * (size_t)n->dim, 0, "circ_norm_reserve");
 }
 
 int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, const float* gain, void* sum, void* y, float* y_scale,
@@ -188,13 +457,32 @@ int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, c
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const NormForward a{gain, y_scale, rstd, rows, n->dim, norm_group(n), n->eps};
     with_dtype(n->x_dtype, [&](auto* t) {
         using TX = tag_type<decltype(t)>;
         auto go = [&](auto* o) {
             using TY = tag_type<decltype(o)>;
-            norm_forward_kernel<TX, TY><<<(unsigned)rows, 256, 0, s>>>(static_cast<const TX*>(x), static_cast<const TX*>(residual), gain,
-                                                                       static_cast<TX*>(sum), static_cast<TY*>(y), y_scale, rstd, n->dim,
-                                                                       norm_group(n), n->eps);
+            // 16 bytes a vector; 8 elements only where no tensor is wider than 16 bits
+            constexpr int VEC = std::is_same<TX, float>::value || std::is_same<TY, float>::value ? 4 : 8;
+            const TX *xs = static_cast<const TX*>(x), *rs = static_cast<const TX*>(residual);
+            TX* ss = static_cast<TX*>(sum);
+            TY* ys = static_cast<TY*>(y);
+            auto launch = [&](auto aligned) {
+                constexpr bool ALIGNED = decltype(aligned)::value;
+                const int vectors = RowSpan<VEC, ALIGNED>::most(n->dim);
+                // few rows: as many threads as possible, each waits for one vector; many: four vectors in flight a thread
+                const RowShape shape = row_shape(vectors, rows <= 148 ? 1 : vectors >= 128 ? 4 : vectors > 32 ? 2 : 1);
+                if (!shape.items) return false;
+                const int per_block = shape.threads == 32 ? (rows < 148 * 4 ? 1 : 4) : 1;
+                with_items(shape.items, [&](auto items) {
+                    norm_forward_kernel<TX, TY, VEC, decltype(items)::value, ALIGNED>
+                        <<<(unsigned)((rows + per_block - 1) / per_block), dim3(shape.threads, per_block), 0, s>>>(xs, rs, ss, ys, a);
+                });
+                return true;
+            };
+            const bool bases = !misaligned(x, 16) && !misaligned(residual, 16) && !misaligned(sum, 16) && !misaligned(y, 16);
+            const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : launch(std::false_type{}));
+            if (!done) norm_forward_any_kernel<TX, TY><<<(unsigned)rows, 512, 0, s>>>(xs, rs, ss, ys, a);
         };
         if (e4m3)
             go(static_cast<uint8_t*>(nullptr));
@@ -227,19 +515,57 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
+    if (grad_gain && (rc = ensure_scratch(n->ws, sizeof(float) * kNormParts * (size_t)n->dim, s, "circ_norm_reserve")) != CIRC_OK) return rc;
+    const NormBackward a{gain, rstd, grad_gain ? static_cast<float*>(n->ws.ptr) : nullptr, rows, n->dim};
+    int parts = 0, launches = 0;
+    cudaError_t err = cudaSuccess;
     with_dtype(n->x_dtype, [&](auto* t) {
         with_dtype(gy, [&](auto* o) {
             using TX = tag_type<decltype(t)>;
             using TY = tag_type<decltype(o)>;
-            if (grad_x)
-                norm_backward_kernel<TX, TY><<<(unsigned)rows, 256, 0, s>>>(static_cast<const TX*>(sum), gain, rstd, static_cast<const TY*>(grad_y),
-                                                                            static_cast<const TX*>(grad_sum), static_cast<TX*>(grad_x), n->dim);
-            if (grad_gain)
-                norm_gain_kernel<TX, TY><<<(unsigned)((n->dim + 255) / 256), 256, 0, s>>>(static_cast<const TX*>(sum), rstd,
-                                                                                          static_cast<const TY*>(grad_y), grad_gain, rows, n->dim);
+            constexpr int VEC = std::is_same<TX, float>::value || std::is_same<TY, float>::value ? 4 : 8;
+            const TX *ss = static_cast<const TX*>(sum), *cs = static_cast<const TX*>(grad_sum);
+            const TY* ys = static_cast<const TY*>(grad_y);
+            TX* xs = static_cast<TX*>(grad_x);
+            auto launch = [&](auto aligned) {
+                constexpr bool ALIGNED = decltype(aligned)::value;
+                const int vectors = RowSpan<VEC, ALIGNED>::most(n->dim);
+                const RowShape shape = row_shape(vectors, rows <= 148 ? 1 : vectors >= 64 ? 2 : 1);
+                if (!shape.items) return false;
+                const size_t share = ALIGNED || !grad_gain ? 0 : sizeof(float) * (size_t)n->dim;
+                with_items(shape.items, [&](auto items) {
+                    auto kernel = norm_backward_kernel<TX, TY, VEC, decltype(items)::value, ALIGNED>;
+                    // a wave of blocks that walk the rows: as many as are resident, and no more shares than kNormParts
+                    int per_sm = 1;
+                    if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess) return;
+                    if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, shape.threads, share)) != cudaSuccess) return;
+                    const long wave = 148L * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm);
+                    parts = (int)(rows < wave ? rows : wave);
+                    kernel<<<parts, shape.threads, share, s>>>(ss, ys, cs, xs, a);
+                    ++launches;
+                });
+                return true;
+            };
+            const bool bases = !misaligned(sum, 16) && !misaligned(grad_y, 16) && !misaligned(grad_sum, 16) && !misaligned(grad_x, 16);
+            const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : n->dim <= 16384 && launch(std::false_type{}));
+            if (done || err != cudaSuccess) return;
+            if (grad_x) {
+                norm_backward_any_kernel<TX, TY><<<(unsigned)rows, 512, 0, s>>>(ss, ys, cs, xs, a);
+                ++launches;
+            }
+            if (grad_gain) {
+                parts = rows < 64 ? (int)rows : 64;
+                norm_gain_any_kernel<TX, TY><<<dim3((n->dim + 255) / 256, parts), 256, 0, s>>>(ss, ys, a);
+                ++launches;
+            }
         });
     });
-    count_launches((grad_x != nullptr) + (grad_gain != nullptr));
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
+    if (grad_gain) {
+        CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, norm_gain_kernel, dim3((n->dim + 31) / 32), 512, 0, s, a.part, grad_gain, parts, n->dim), CIRC_ERR_CUDA);
+        ++launches;
+    }
+    count_launches(launches);
     CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
     return CIRC_OK;
 }

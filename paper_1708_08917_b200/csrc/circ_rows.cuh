@@ -119,12 +119,82 @@ struct RawVec {
             }
         }
     }
+    // Elements lo <= e < hi only, zeros beside them.
+    __device__ __forceinline__ void load_part(const T* p, int lo, int hi) {
+        clear();
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e >= lo && e < hi) {
+                if constexpr (sizeof(T) == 4)
+                    w[e] = *reinterpret_cast<const uint32_t*>(p + e);
+                else
+                    w[e / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + e) << (e % 2 * 16);
+            }
+    }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (sizeof(T) == 4)
             return __uint_as_float(w[e]);
         else      // a bfloat16 is the upper half of a float32
             return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
     }
+};
+
+// A row of `dim` elements seen as vectors that are aligned in the whole tensor.  ALIGNED: every row starts and ends with a whole
+// vector.  Otherwise its first and last vectors are shared with the neighbouring rows; those are read and written by element.
+// All tensors of a call that have the row's shape and a 16-byte aligned start can be walked with the same spans (VEC elements are
+// at most 16 bytes in a 16-bit type, and two 16-byte pieces in float32).
+template <int VEC, bool ALIGNED>
+struct RowSpan {
+    size_t first;      // element index of vector 0 in the tensor
+    int shift, dim;    // column of its first element, <= 0
+    __device__ __forceinline__ RowSpan(long row, int d) {
+        const size_t base = (size_t)row * d;
+        first = ALIGNED ? base : base / VEC * VEC;
+        shift = ALIGNED ? 0 : -(int)(base - first);
+        dim = d;
+    }
+    __device__ __forceinline__ int col(int v) const { return v * VEC + shift; }
+    __device__ __forceinline__ size_t at(int v) const { return first + (size_t)v * VEC; }
+    __device__ __forceinline__ bool any(int v) const { return col(v) < dim; }
+    __device__ __forceinline__ bool whole(int v) const { return ALIGNED || (col(v) >= 0 && col(v) + VEC <= dim); }
+    __device__ __forceinline__ int lo(int v) const { return col(v) < 0 ? -col(v) : 0; }
+    __device__ __forceinline__ int hi(int v) const { return dim - col(v) < VEC ? dim - col(v) : VEC; }
+    template <typename T>
+    __device__ __forceinline__ void load(RawVec<T, VEC>& r, const T* p, int v) const {
+        if (!any(v)) r.clear();
+        else if (whole(v)) r.load(p + at(v));
+        else r.load_part(p + at(v), lo(v), hi(v));
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* p, int v, const float (&x)[VEC]) const {
+        if (!any(v)) return;
+        if (whole(v)) {
+            store_vec<VEC>(p + at(v), x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e >= lo(v) && e < hi(v)) store_one(p + at(v) + e, x[e]);
+        }
+    }
+    // A vector that all rows share (`p` indexed by column); NULL: ones.
+    __device__ __forceinline__ void load_columns(float (&g)[VEC], const float* __restrict__ p, int v) const {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) g[e] = 1.f;
+        if (!p || !any(v)) return;
+        if (ALIGNED) {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+                const float4 t = __ldg(reinterpret_cast<const float4*>(p + col(v) + e));
+                g[e] = t.x; g[e + 1] = t.y; g[e + 2] = t.z; g[e + 3] = t.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e >= lo(v) && e < hi(v)) g[e] = __ldg(p + col(v) + e);
+        }
+    }
+    // Vectors that a row of d elements may have.
+    static __host__ __device__ int most(int d) { return ALIGNED ? d / VEC : (d + 2 * VEC - 2) / VEC; }
 };
 
 // Sum over the lanes of a warp, the same bits in every lane.
