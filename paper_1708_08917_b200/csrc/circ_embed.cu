@@ -222,17 +222,6 @@ __device__ __forceinline__ void embed_bounds(const EmbedSum& a, long x0, long x1
 // A thread has PARTS vectors of a row, GROUP vectors apart: enough bytes a row that the walk over rows costs little next to them.
 constexpr int kSumBlocks = 4;        // resident blocks of 256 threads on an SM, 48 KB of ring each
 constexpr int ring_depth(int bytes) { return bytes <= 16 ? 12 : 6; }
-// Copies BYTES from global to shared memory without waiting where that is possible (4, 8 or 16 bytes).
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* dst, const void* src) {
-    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-    if constexpr (BYTES == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-    else if constexpr (BYTES >= 4)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
-    else
-        *static_cast<uint16_t*>(dst) = *static_cast<const uint16_t*>(src);
-}
 template <typename TT, typename TY, int VEC, int PARTS, int GROUP>
 __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, const TY* __restrict__ dy, TT* __restrict__ dt) {
     // Loads run ahead of the sums over the sorted tokens, whatever the rows they belong to: DEPTH tokens are in flight in a ring of

@@ -28,8 +28,16 @@ __device__ __forceinline__ float from_e4m3(uint8_t v) {
 }
 
 // The scale of a group whose largest magnitude is `top`: 1 for a group of zeros, NaN where a value is not finite (the
-// group's values have no meaning then, and the NaN says so).
-__device__ __forceinline__ float group_scale(float top) { return top == 0.f ? 1.f : top <= 3.402823466e38f ? top / kE4m3Max : NAN; }
+// group's values have no meaning then, and the NaN says so), at least the smallest normal number so that it has an inverse.
+__device__ __forceinline__ float group_scale(float top) {
+    const float scale = fmaxf(top * (1.f / kE4m3Max), 1.17549435e-38f);
+    return top == 0.f ? 1.f : top <= 3.402823466e38f ? scale : NAN;
+}
+__device__ __forceinline__ float inverse(float v) {     // of a normal number, within one unit of the last place
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 
 // The e4m3 codes of VEC values, packed (`mine`: the values' lanes that exist).
 template <int VEC>
@@ -47,7 +55,7 @@ struct NormForward {
     float* y_scale;
     float* rstd;
     long rows;
-    int dim, group;
+    int dim, group, group_bits;     // group = 2^group_bits unless it is the row
     float eps;
 };
 
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
     float inv = 0.f;
     if (row_scale) {
         const float scale = group_scale(top * rstd);
-        inv = 1.f / scale;
+        inv = inverse(scale);
         if (tid == 0) a.y_scale[row] = scale;
     }
 #pragma unroll
@@ -129,8 +137,9 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
                 for (int e = 0; e < VEC; ++e) t = max_nan(t, fabsf(out[e]));
                 for (int o = a.group / VEC / 2; o > 0; o >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, o));
                 const float scale = group_scale(t);
-                inv = 1.f / scale;
-                if (span.any(v) && v % (a.group / VEC) == 0) a.y_scale[(row * a.dim + span.col(v)) / a.group] = scale;
+                inv = inverse(scale);
+                const int c = span.col(v);
+                if (span.any(v) && (c & (a.group - 1)) == 0) a.y_scale[row * (a.dim >> a.group_bits) + (c >> a.group_bits)] = scale;
             }
             // times 1 / scale instead of a division by scale: at most the rounding of a value that lies in the middle between two
             // codes changes
@@ -183,14 +192,14 @@ __global__ void __launch_bounds__(512) norm_forward_any_kernel(const TX* x, cons
             __syncthreads();
             const float scale = group_scale(warp_max_nan(lane < warps ? red[lane] : 0.f));
             if (threadIdx.x == 0) a.y_scale[row] = scale;
-            for (int c = threadIdx.x; c < dim; c += blockDim.x) y[base + c] = to_e4m3(gained(c, rstd) * (1.f / scale));
+            for (int c = threadIdx.x; c < dim; c += blockDim.x) y[base + c] = to_e4m3(gained(c, rstd) * inverse(scale));
         } else {
             for (int g = warp; g < dim / group; g += warps) {
                 float top = 0.f;
                 for (int c = lane; c < group; c += 32) top = max_nan(top, fabsf(gained(g * group + c, rstd)));
                 const float scale = group_scale(warp_max_nan(top));
                 if (lane == 0) a.y_scale[row * (dim / group) + g] = scale;
-                for (int c = g * group + lane; c < (g + 1) * group; c += 32) y[base + c] = to_e4m3(gained(c, rstd) * (1.f / scale));
+                for (int c = g * group + lane; c < (g + 1) * group; c += 32) y[base + c] = to_e4m3(gained(c, rstd) * inverse(scale));
             }
         }
         __syncthreads();    // sum may be x or residual
@@ -217,13 +226,21 @@ struct NormBackward {
     int dim;
 };
 
-template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED>
+// A row's reduction waits for all of its loads, so the loads of the next rows must be in flight meanwhile.  RING (rows of at most 16 KB
+// a tensor, aligned): they go to a ring of kRowsAhead rows in shared memory, in which every thread copies and reads its own vectors.
+constexpr int kRowsAhead = 4;
+
+template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED, bool RING>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
+    static_assert(ALIGNED || !RING, "copies of whole vectors");
+    constexpr int XB = VEC * (int)sizeof(TX), YB = VEC * (int)sizeof(TY), BYTES = 2 * XB + YB;
     __shared__ float red[2][16];
     pdl_trigger();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
-    // rows do not start at the same column of a vector when they are not aligned: a share is kept by column then, in shared memory
-    extern __shared__ __align__(16) float share[];
+    // dynamic shared memory: the ring; or the share of grad_gain, where rows do not start at the same column of a vector
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* share = reinterpret_cast<float*>(smem);
+    auto place = [&](int slot, int i, int off) { return smem + (size_t)(slot * ITEMS + i) * BYTES * threads + (size_t)off * threads; };
     float acc[ITEMS][VEC];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
@@ -233,23 +250,57 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const TX* __restrict
         for (int c = tid; c < a.dim; c += threads) share[c] = 0.f;
         __syncthreads();
     }
+    long ahead = blockIdx.x;
+    int slot_in = 0, slot = 0;
+    auto fetch = [&]() {
+        if (ahead < a.rows) {
+            const RowSpan<VEC, ALIGNED> span(ahead, a.dim);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int v = tid + i * threads;
+                if (!span.any(v)) continue;
+                copy_async<XB>(place(slot_in, i, 0) + tid * XB, sum + span.at(v));
+                copy_async<YB>(place(slot_in, i, XB) + tid * YB, dy + span.at(v));
+                if (ds && dx) copy_async<XB>(place(slot_in, i, XB + YB) + tid * XB, ds + span.at(v));
+            }
+            ahead += gridDim.x;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        slot_in = slot_in + 1 == kRowsAhead ? 0 : slot_in + 1;
+    };
+    if constexpr (RING)
+#pragma unroll 1
+        for (int u = 0; u < kRowsAhead; ++u) fetch();
     int flip = 0;
     for (long row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
         const RowSpan<VEC, ALIGNED> span(row, a.dim);
+        const float rstd = __ldg(a.rstd + row);
         RawVec<TX, VEC> sr[ITEMS], cr[ITEMS];
         RawVec<TY, VEC> yr[ITEMS];
+        if constexpr (RING) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRowsAhead - 1) : "memory");
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) span.load(sr[i], sum, tid + i * threads);
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) span.load(yr[i], dy, tid + i * threads);
-        if (ds && dx) {
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) span.load(cr[i], ds, tid + i * threads);
+            for (int i = 0; i < ITEMS; ++i) {
+                sr[i].clear();
+                yr[i].clear();
+                cr[i].clear();
+                if (!span.any(tid + i * threads)) continue;
+                sr[i].load(reinterpret_cast<const TX*>(place(slot, i, 0)) + tid * VEC);
+                yr[i].load(reinterpret_cast<const TY*>(place(slot, i, XB)) + tid * VEC);
+                if (ds && dx) cr[i].load(reinterpret_cast<const TX*>(place(slot, i, XB + YB)) + tid * VEC);
+            }
+            slot = slot + 1 == kRowsAhead ? 0 : slot + 1;
         } else {
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) cr[i].clear();
+            for (int i = 0; i < ITEMS; ++i) span.load(sr[i], sum, tid + i * threads);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) span.load(yr[i], dy, tid + i * threads);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                if (ds && dx) span.load(cr[i], ds, tid + i * threads);
+                else cr[i].clear();
+            }
         }
-        const float rstd = __ldg(a.rstd + row);
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -269,6 +320,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const TX* __restrict
                         share[span.col(v) + e] = fmaf(yr[i].get(e), sr[i].get(e) * rstd, share[span.col(v) + e]);
             }
         }
+        if constexpr (RING) fetch();              // this row's vectors are in registers
         dot = warp_sum(dot);
         if (lane == 0) red[flip][tid / 32] = dot;
         __syncthreads();                          // the other half of `red` serves the next row
@@ -457,7 +509,7 @@ int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, c
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const NormForward a{gain, y_scale, rstd, rows, n->dim, norm_group(n), n->eps};
+    const NormForward a{gain, y_scale, rstd, rows, n->dim, norm_group(n), n->group == 32 ? 5 : n->group == 64 ? 6 : 7, n->eps};
     with_dtype(n->x_dtype, [&](auto* t) {
         using TX = tag_type<decltype(t)>;
         auto go = [&](auto* o) {
@@ -530,18 +582,21 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
             auto launch = [&](auto aligned) {
                 constexpr bool ALIGNED = decltype(aligned)::value;
                 const int vectors = RowSpan<VEC, ALIGNED>::most(n->dim);
-                const RowShape shape = row_shape(vectors, rows <= 148 ? 1 : vectors >= 64 ? 2 : 1);
+                const RowShape shape = row_shape(vectors, 1);
                 if (!shape.items) return false;
-                const size_t share = ALIGNED || !grad_gain ? 0 : sizeof(float) * (size_t)n->dim;
                 with_items(shape.items, [&](auto items) {
-                    auto kernel = norm_backward_kernel<TX, TY, VEC, decltype(items)::value, ALIGNED>;
-                    // a wave of blocks that walk the rows: as many as are resident, and no more shares than kNormParts
+                    constexpr int ITEMS = decltype(items)::value;
+                    constexpr bool RING = ALIGNED && ITEMS <= 2;
+                    constexpr int BYTES = VEC * (2 * (int)sizeof(TX) + (int)sizeof(TY));
+                    auto kernel = norm_backward_kernel<TX, TY, VEC, ITEMS, ALIGNED, RING>;
+                    const size_t smem = RING ? (size_t)kRowsAhead * ITEMS * BYTES * shape.threads : ALIGNED || !grad_gain ? 0 : sizeof(float) * (size_t)n->dim;
+                    // a wave of blocks that walk the rows, some rows each, and no more shares than kNormParts
                     int per_sm = 1;
-                    if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess) return;
-                    if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, shape.threads, share)) != cudaSuccess) return;
-                    const long wave = 148L * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm);
-                    parts = (int)(rows < wave ? rows : wave);
-                    kernel<<<parts, shape.threads, share, s>>>(ss, ys, cs, xs, a);
+                    if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024)) != cudaSuccess) return;
+                    if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, shape.threads, smem)) != cudaSuccess) return;
+                    const long wave = 148L * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm), some = (rows + 3) / 4 > 148 ? (rows + 3) / 4 : rows < 148 ? rows : 148;
+                    parts = (int)(some < wave ? some : wave);
+                    kernel<<<parts, shape.threads, smem, s>>>(ss, ys, cs, xs, a);
                     ++launches;
                 });
                 return true;

@@ -139,6 +139,18 @@ struct RawVec {
     }
 };
 
+// Copies BYTES from global to shared memory without waiting where that is possible (4, 8 or 16 bytes).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+    else if constexpr (BYTES >= 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+    else
+        *static_cast<uint16_t*>(dst) = *static_cast<const uint16_t*>(src);
+}
+
 // A row of `dim` elements seen as vectors that are aligned in the whole tensor.  ALIGNED: every row starts and ends with a whole
 // vector.  Otherwise its first and last vectors are shared with the neighbouring rows; those are read and written by element.
 // All tensors of a call that have the row's shape and a 16-byte aligned start can be walked with the same spans (VEC elements are
