@@ -345,7 +345,8 @@ CIRC_API int circ_pool_forward(const void* x, void* y, int N, int H, int W, int 
  *   - Calls only enqueue on `stream`.  A workspace that a call needs is allocated by its first call, or before by the
  *     handle's reserve call (needed before stream capture; CIRC_ERR_UNSUPPORTED otherwise).
  *   - Zero rows are served (nothing is read; sums over no row are written as 0).
- *   - Sums are taken in float32 or float64 in an order that depends on the sizes only: results repeat bit for bit.
+ *   - Sums are taken in float32 or float64 in an order that follows from the sizes, strides, alignment and ids alone: the same call
+ *     gives the same bits.
  *   - Destroy calls take NULL.  Errors: CIRC_ERR_ARG (NULL or misaligned pointer, unknown type code), CIRC_ERR_SHAPE (a size
  *     out of range), CIRC_ERR_ALLOC, CIRC_ERR_CUDA, CIRC_ERR_UNSUPPORTED.
  */

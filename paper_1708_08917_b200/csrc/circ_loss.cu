@@ -21,73 +21,439 @@ struct Loss {
 template <typename ID>
 __device__ __forceinline__ bool has_target(ID t, int classes, long ignore) { return t >= 0 && (long)t < classes && (long)t != ignore; }
 
-template <typename T, typename ID>
-__global__ void __launch_bounds__(256) loss_kernel(const T* z, long ld, const ID* __restrict__ targets, float* row_loss, float* lse_out, T* grad,
-                                                   long grad_ld, float grad_mean, int rows, int classes, long ignore) {
-    __shared__ float red[33];
-    const int row = blockIdx.x;
-    const T* zr = z + row * ld;
-    float top = -INFINITY;
-    for (int c = threadIdx.x; c < classes; c += blockDim.x) top = fmaxf(top, to_float(zr[c]));
+struct LossArgs {
+    long ld, grad_ld;
+    float *row_loss, *lse, *mean;
+    int* count;          // rows with a target, from loss_count_kernel; NULL: the block counts them itself
+    unsigned* done;      // blocks that have written their row losses (0 before and after a call)
+    float grad_mean;
+    int rows, classes;
+    long ignore;
+};
+
+// exp(z - top) summed up, with the sum's own `top`: the pair that a pass over a row carries along.
+struct Softmax {
+    float top, sum;
+};
+constexpr float kLog2e = 1.4426950408889634f;
+// exp(d); the difference to the row's top is taken before the factor, so that large scores lose nothing
+__device__ __forceinline__ float exp_of(float d) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d * kLog2e));
+    return r;
+}
+__device__ __forceinline__ Softmax join(Softmax a, Softmax b) {
+    const float top = fmaxf(a.top, b.top);
+    // a part whose top is -inf has the sum 0 or, from a NaN, NaN
+    return Softmax{top, a.sum * (a.top == -INFINITY ? 0.f : exp_of(a.top - top)) + b.sum * (b.top == -INFINITY ? 0.f : exp_of(b.top - top))};
+}
+__device__ __forceinline__ Softmax warp_join(Softmax v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = top;
-    __syncthreads();
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, red[w]);
-    const float base = top == -INFINITY ? 0.f : top;
+    for (int o = 16; o > 0; o >>= 1) v = join(v, Softmax{__shfl_xor_sync(0xffffffffu, v.top, o), __shfl_xor_sync(0xffffffffu, v.sum, o)});
+    return v;
+}
+// One vector of a row into the running pair: one exponential an element, one more where the top rises.
+template <int VEC>
+__device__ __forceinline__ void take(Softmax& v, const float (&z)[VEC]) {
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) top = fmaxf(top, z[e]);
+    if (top > v.top) {
+        v.sum *= v.top == -INFINITY ? 0.f : exp_of(v.top - top);
+        v.top = top;
+    }
+    const float base = v.top == -INFINITY ? 0.f : v.top;
     float sum = 0.f;
-    for (int c = threadIdx.x; c < classes; c += blockDim.x) sum += expf(to_float(zr[c]) - base);
-    sum = block_sum(sum, red);
-    const float lse = base + logf(sum);
-    const ID target = targets[row];
-    const bool valid = has_target(target, classes, ignore);
-    float loss = 0.f;
-    if (valid) {
-        const float zt = to_float(zr[target]);
-        loss = zt == -INFINITY && lse == lse ? INFINITY : lse - zt;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum += exp_of(z[e] - base);
+    v.sum += sum;
+}
+// Elements of a vector as scores; those beside the row's own are -inf.
+template <typename T, int VEC, typename SPAN>
+__device__ __forceinline__ void scores(const SPAN& span, int v, const RawVec<T, VEC>& raw, float (&z)[VEC]) {
+    const bool whole = span.any(v) && span.whole(v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) z[e] = whole || (span.any(v) && e >= span.lo(v) && e < span.hi(v)) ? raw.get(e) : -INFINITY;
+}
+
+// What is the same for a whole row once its sum is known.
+struct RowResult {
+    float base;        // the top, 0 where it is -inf
+    float factor;      // gradient = exp(z - base) * factor, less `hot` at the target
+    float hot;
+    bool zero;         // no gradient
+};
+template <typename ID>
+__device__ __forceinline__ RowResult finish_row(const LossArgs& a, int row, Softmax all, ID target, float target_score, int count, bool writes) {
+    RowResult r;
+    r.base = all.top == -INFINITY ? 0.f : all.top;
+    const bool valid = has_target(target, a.classes, a.ignore);
+    if (writes) {
+        const float lse = r.base + logf(all.sum);
+        if (a.lse) a.lse[row] = lse;
+        if (a.row_loss) a.row_loss[row] = !valid ? 0.f : target_score == -INFINITY && lse == lse ? INFINITY : lse - target_score;
     }
-    float count = 0.f;
-    if (grad) {
-        for (int r = threadIdx.x; r < rows; r += blockDim.x) count += has_target(targets[r], classes, ignore) ? 1.f : 0.f;
-        count = block_sum(count, red);
-    }
-    __syncthreads();    // every thread has read the target's score: grad may be z
-    if (threadIdx.x == 0) {
-        if (row_loss) row_loss[row] = loss;
-        if (lse_out) lse_out[row] = lse;
-    }
-    if (!grad) return;
-    T* gr = grad + row * grad_ld;
-    const float w = valid ? grad_mean / count : 0.f, inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int c = threadIdx.x; c < classes; c += blockDim.x) {
-        const float p = expf(to_float(zr[c]) - base) * inv;
-        store_one(gr + c, valid && sum != 0.f ? (p - (c == (long)target ? 1.f : 0.f)) * w : valid ? 0.f * sum : 0.f);
+    r.zero = !valid || all.sum == 0.f;
+    r.hot = a.grad_mean / (float)(count < 1 ? 1 : count);
+    r.factor = r.hot / all.sum;
+    return r;
+}
+template <typename T, int VEC, typename SPAN>
+__device__ __forceinline__ void write_gradient(const SPAN& span, T* grad, size_t first, int v, const float (&z)[VEC], const RowResult& r, int target) {
+    float g[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) g[e] = r.zero ? 0.f : exp_of(z[e] - r.base) * r.factor;
+    const int t = target - span.col(v);
+    if (!r.zero && t >= 0 && t < VEC)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e == t) g[e] -= r.hot;
+    T* dst = grad + first + (size_t)v * VEC;
+    if (span.whole(v)) {
+        store_vec_once<VEC>(dst, g);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e >= span.lo(v) && e < span.hi(v)) store_one(dst + e, g[e]);
     }
 }
 
 template <typename ID>
-__global__ void __launch_bounds__(1024) loss_mean_kernel(const float* __restrict__ row_loss, const ID* __restrict__ targets, float* mean, int rows,
-                                                         int classes, long ignore) {
-    __shared__ double sums[1024];
-    __shared__ int counts[1024];
+__device__ __forceinline__ int targets_of(const LossArgs& a, const ID* __restrict__ targets, int from, int step) {
+    int n = 0;
+#pragma unroll 4
+    for (int r = from; r < a.rows; r += step) n += has_target(targets[r], a.classes, a.ignore);
+    return n;
+}
+template <typename ID>
+__global__ void __launch_bounds__(1024) loss_count_kernel(LossArgs a, const ID* __restrict__ targets) {
+    __shared__ int part[32];
+    pdl_trigger();
+    const int n = __reduce_add_sync(0xffffffffu, targets_of(a, targets, threadIdx.x, 1024));
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = n;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int all = __reduce_add_sync(0xffffffffu, part[threadIdx.x]);
+        if (threadIdx.x == 0) *a.count = all;
+    }
+}
+
+// The block that is last to write its losses adds all of them up, in the order of the rows and in float64.  All threads call it.
+template <typename ID>
+__device__ __forceinline__ void finish_mean(const LossArgs& a, const ID* __restrict__ targets, unsigned blocks) {
+    __shared__ bool last;
+    __shared__ double sums[32];
+    __shared__ int counts[32];
+    if (!a.mean) return;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(a.done, 1u) == blocks - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
     double s = 0.0;
     int n = 0;
-    for (int r = threadIdx.x; r < rows; r += 1024)
-        if (has_target(targets[r], classes, ignore)) {
-            s += row_loss[r];
-            ++n;
-        }
-    sums[threadIdx.x] = s;
-    counts[threadIdx.x] = n;
-    __syncthreads();
-    for (int o = 512; o > 0; o >>= 1) {
-        if (threadIdx.x < o) {
-            sums[threadIdx.x] += sums[threadIdx.x + o];
-            counts[threadIdx.x] += counts[threadIdx.x + o];
-        }
-        __syncthreads();
+    for (int r = threadIdx.x; r < a.rows; r += blockDim.x) {
+        s += (double)__ldcg(a.row_loss + r);      // 0 for a row without a target
+        n += has_target(targets[r], a.classes, a.ignore);
     }
-    if (threadIdx.x == 0) *mean = counts[0] ? (float)(sums[0] / counts[0]) : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (threadIdx.x % 32 == 0) {
+        sums[threadIdx.x / 32] = s;
+        counts[threadIdx.x / 32] = n;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < (int)blockDim.x / 32; ++w) {
+            sums[0] += sums[w];
+            counts[0] += counts[w];
+        }
+        *a.mean = counts[0] ? (float)(sums[0] / counts[0]) : 0.f;
+        *a.done = 0;
+    }
+}
+
+// ---- short rows: a warp holds one in registers ----
+template <typename T, typename ID, int VEC, int ITEMS, bool ALIGNED, bool GRAD>
+__global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
+    __shared__ int part[8];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 8 + warp;
+    const bool live = row < a.rows;
+    const RowSpan<VEC, ALIGNED> span(live ? row : 0, live ? a.classes : 0, a.ld);
+    float s[ITEMS][VEC];
+    {
+        RawVec<T, VEC> raw[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) span.load(raw[i], z, lane + i * 32);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) scores(span, lane + i * 32, raw[i], s[i]);
+    }
+    const ID target = live ? targets[row] : (ID)-1;
+    const float target_score = live && has_target(target, a.classes, a.ignore) ? to_float(z[(size_t)row * a.ld + target]) : 0.f;
+    int count = 1;
+    if (GRAD && !a.count) {
+        const int n = __reduce_add_sync(0xffffffffu, targets_of(a, targets, threadIdx.x, 256));
+        if (lane == 0) part[warp] = n;
+        __syncthreads();
+        count = __reduce_add_sync(0xffffffffu, lane < 8 ? part[lane] : 0);
+    }
+    Softmax all{-INFINITY, 0.f};
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) take(all, s[i]);
+    all = warp_join(all);
+    if (GRAD && a.count) {
+        pdl_wait();
+        count = __ldcg(a.count);
+    }
+    if (live) {
+        const RowResult r = finish_row(a, row, all, target, target_score, count, lane == 0);
+        if constexpr (GRAD) {
+            const size_t first = (size_t)row * a.grad_ld + span.shift;
+            __syncwarp();      // every lane has its scores and the target's: grad may be z
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (span.any(lane + i * 32)) write_gradient<T, VEC>(span, grad, first, lane + i * 32, s[i], r, (int)target);
+        }
+    }
+    finish_mean(a, targets, gridDim.x);
+}
+
+// ---- long rows: a block, or the blocks of a cluster, hold one ----
+// GRAD: the row is copied to shared memory as it arrives, summed up from there, and read there a second time for the gradient, so that
+// it crosses the memory bus once.  Every thread copies and reads its own vectors.  Two blocks of up to 110 KB share an SM: one
+// fetches while the other computes.  Without a gradient nothing is kept.
+constexpr int kLossChunk = 4;     // vectors a thread in a group of copies
+
+__device__ __forceinline__ void wait_copies(int groups) {      // until at most `groups` groups of copies are in flight (exact up to 7)
+    switch (groups) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        case 6: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 7;" ::: "memory"); break;
+    }
+}
+
+template <typename T, typename ID, int VEC, bool ALIGNED, bool GRAD>
+__global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a, int cluster) {
+    extern __shared__ __align__(16) unsigned char held[];
+    __shared__ Softmax part[16];
+    __shared__ Softmax peers[8];
+    __shared__ int counts[16];
+    const int threads = blockDim.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = threads / 32;
+    const int rank = blockIdx.x % cluster, row = blockIdx.x / cluster;
+    const RowSpan<VEC, ALIGNED> span(row, a.classes, a.ld);
+    const int vectors = (a.classes - span.shift + VEC - 1) / VEC, per = (vectors + cluster - 1) / cluster;
+    const int v0 = rank * per, v1 = v0 + per < vectors ? v0 + per : vectors;
+    auto place = [&](int v) { return reinterpret_cast<T*>(held) + (size_t)(v - v0) * VEC; };
+    Softmax all{-INFINITY, 0.f};
+    const ID target = targets[row];
+    float target_score = 0.f;
+    if constexpr (GRAD) {
+        int groups = 0;
+        for (int v = v0 + tid; v < v1; v += kLossChunk * threads, ++groups) {
+#pragma unroll
+            for (int u = 0; u < kLossChunk; ++u) {
+                const int w = v + u * threads;
+                if (w < v1 && span.whole(w)) copy_async<16>(place(w), z + span.at(w));
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
+        int count = 0;
+        if (!a.count) count = __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, threads));
+        if (lane == 0) counts[warp] = count;
+        for (int v = v0 + tid; v < v1; v += kLossChunk * threads) {
+            wait_copies(--groups);
+#pragma unroll
+            for (int u = 0; u < kLossChunk; ++u) {
+                const int w = v + u * threads;
+                if (w >= v1) break;
+                RawVec<T, VEC> raw;
+                float s[VEC];
+                if (span.whole(w)) raw.load(place(w));
+                else span.load(raw, z, w);
+                scores(span, w, raw, s);
+                take(all, s);
+            }
+        }
+    } else {
+        if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
+        for (int v = v0 + tid; v < v1; v += kLossChunk * threads) {
+            RawVec<T, VEC> raw[kLossChunk];
+#pragma unroll
+            for (int u = 0; u < kLossChunk; ++u)
+                if (v + u * threads < v1) span.load(raw[u], z, v + u * threads);
+#pragma unroll
+            for (int u = 0; u < kLossChunk; ++u) {
+                if (v + u * threads >= v1) break;
+                float s[VEC];
+                scores(span, v + u * threads, raw[u], s);
+                take(all, s);
+            }
+        }
+    }
+    all = warp_join(all);
+    if (lane == 0) part[warp] = all;
+    __syncthreads();
+    all = warp_join(lane < warps ? part[lane] : Softmax{-INFINITY, 0.f});
+    if (cluster > 1) {
+        if (tid < cluster) {      // this block's pair to every block of the cluster
+            uint32_t dst;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"((uint32_t)__cvta_generic_to_shared(&peers[rank])), "r"(tid));
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst), "f"(all.top), "f"(all.sum) : "memory");
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        all = warp_join(lane < cluster ? peers[lane] : Softmax{-INFINITY, 0.f});
+    }
+    int count = 1;
+    if constexpr (GRAD) {
+        if (a.count) {
+            pdl_wait();
+            count = __ldcg(a.count);
+        } else {
+            count = __reduce_add_sync(0xffffffffu, lane < warps ? counts[lane] : 0);
+        }
+    }
+    const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
+    if constexpr (GRAD) {
+        // vectors that were not copied are read again: where grad is z, those are this thread's own
+        const size_t first = (size_t)row * a.grad_ld + span.shift;
+        for (int w = v0 + tid; w < v1; w += threads) {
+            RawVec<T, VEC> raw;
+            float s[VEC];
+            if (span.whole(w)) raw.load(place(w));
+            else span.load(raw, z, w);
+            scores(span, w, raw, s);
+            write_gradient<T, VEC>(span, grad, first, w, s, r, (int)target);
+        }
+    }
+    if (rank == 0) finish_mean(a, targets, gridDim.x / cluster);
+}
+
+// ---- anything else (unaligned tensors, strides of the two matrices that do not go together, rows longer than a cluster holds) ----
+template <typename T, typename ID>
+__global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
+    __shared__ Softmax part[16];
+    __shared__ int counts[16];
+    const int row = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const T* zr = z + (size_t)row * a.ld;
+    Softmax all{-INFINITY, 0.f};
+    for (int c0 = tid; c0 < a.classes; c0 += 512 * 8) {
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = c0 + e * 512 < a.classes ? to_float(zr[c0 + e * 512]) : -INFINITY;
+        take(all, s);
+    }
+    const ID target = targets[row];
+    const bool valid = has_target(target, a.classes, a.ignore);
+    const float target_score = valid ? to_float(zr[target]) : 0.f;
+    all = warp_join(all);
+    const int n = grad && !a.count ? __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, 512)) : 0;
+    if (lane == 0) {
+        part[warp] = all;
+        counts[warp] = n;
+    }
+    __syncthreads();         // every thread has read the target's score: grad may be z
+    all = warp_join(lane < 16 ? part[lane] : Softmax{-INFINITY, 0.f});
+    int count = __reduce_add_sync(0xffffffffu, lane < 16 ? counts[lane] : 0);
+    if (grad && a.count) {
+        pdl_wait();
+        count = __ldcg(a.count);
+    }
+    const RowResult r = finish_row(a, row, all, target, target_score, count, tid == 0);
+    if (grad) {
+        T* gr = grad + (size_t)row * a.grad_ld;
+        for (int c = tid; c < a.classes; c += 512)
+            store_one(gr + c, r.zero ? 0.f : exp_of(to_float(zr[c]) - r.base) * r.factor - (c == (int)target ? r.hot : 0.f));
+    }
+    finish_mean(a, targets, gridDim.x);
+}
+
+constexpr int kCountAlone = 1024;                  // rows from which on a kernel of its own counts the targets
+constexpr size_t kLossHeld = 110 * 1024;           // bytes of a row that a block holds: two blocks an SM
+constexpr size_t kLossMost = 216 * 1024;           // one block an SM
+
+template <typename... KArgs, typename... Args>
+static cudaError_t launch_loss(bool dependent, int cluster, void (*kernel)(KArgs...), unsigned blocks, int threads, size_t smem, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// The kernel for a call, by the rows' length, their number and the alignment.
+template <typename T, typename ID>
+static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const LossArgs& a, cudaStream_t s) {
+    constexpr int VEC = 16 / (int)sizeof(T);
+    const bool dependent = a.count != nullptr;
+    cudaError_t err = cudaErrorNotSupported;
+    auto with_rows = [&](auto aligned, auto gradient) {
+        constexpr bool ALIGNED = decltype(aligned)::value, GRAD = decltype(gradient)::value;
+        const int vectors = RowSpan<VEC, ALIGNED>::most(a.classes);
+        if (vectors <= 128) {
+            const unsigned blocks = (unsigned)((a.rows + 7L) / 8);
+            auto go = [&](auto items) {
+                err = launch_loss(dependent, 1, loss_warp_kernel<T, ID, VEC, decltype(items)::value, ALIGNED, GRAD>, blocks, 256, 0, s, z, targets, grad, a);
+            };
+            vectors <= 32 ? go(std::integral_constant<int, 1>{}) : vectors <= 64 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+            return;
+        }
+        // blocks a row: enough to hold it, and more while the rows do not fill the machine (4 vectors a thread left at least)
+        int cluster = 1;
+        auto bytes = [&]() { return (size_t)((vectors + cluster - 1) / cluster) * 16; };
+        while (cluster < 8 && ((GRAD && bytes() > kLossHeld) || ((long)a.rows * cluster < 148 && vectors / cluster > 2048))) cluster *= 2;
+        if (GRAD && bytes() > kLossMost) return;
+        const int each = (vectors + cluster - 1) / cluster, threads = each <= 512 ? 128 : each <= 2048 ? 256 : 512;
+        auto kernel = loss_block_kernel<T, ID, VEC, ALIGNED, GRAD>;
+        if (GRAD && (err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLossMost)) != cudaSuccess) return;
+        err = launch_loss(dependent, cluster, kernel, (unsigned)(a.rows * (long)cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
+    };
+    auto with_alignment = [&](auto gradient) {
+        if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) return;
+        if (a.classes % VEC == 0 && a.ld % VEC == 0) with_rows(std::true_type{}, gradient);
+        else with_rows(std::false_type{}, gradient);
+    };
+    grad ? with_alignment(std::true_type{}) : with_alignment(std::false_type{});
+    if (err == cudaErrorNotSupported) err = launch_loss(dependent, 1, loss_any_kernel<T, ID>, (unsigned)a.rows, 512, 0, s, z, targets, grad, a);
+    return err;
+}
+
+// Workspace: the counters (256 bytes), then a row of losses for calls that want their mean alone.
+static int ensure_loss(Loss* l, long rows, cudaStream_t s) {
+    const size_t need = 256 + sizeof(float) * (size_t)rows;
+    if (l->ws.bytes >= need) return CIRC_OK;
+    const int rc = ensure_scratch(l->ws, need, s, "circ_loss_reserve");
+    if (rc != CIRC_OK) return rc;
+    if (cudaMemsetAsync(l->ws.ptr, 0, 256, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+        free_on(l->device, l->ws);
+        set_error(CIRC_ERR_CUDA, "clearing the workspace failed: %s", cudaGetErrorString(cudaGetLastError()));
+        return CIRC_ERR_CUDA;
+    }
+    return CIRC_OK;
 }
 
 static int run_loss(Loss* l, const void* z, long ld, const void* targets, float* row_loss, float* lse, float* mean, void* grad, long grad_ld,
@@ -114,23 +480,28 @@ static int run_loss(Loss* l, const void* z, long ld, const void* targets, float*
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    if (mean && !row_loss) {
-        const int rc = ensure_scratch(l->ws, (size_t)rows * sizeof(float), s, "circ_loss_reserve");
-        if (rc != CIRC_OK) return rc;
-        row_loss = static_cast<float*>(l->ws.ptr);
-    }
+    const bool count_alone = grad && rows > kCountAlone;
+    const int rc = ensure_loss(l, mean && !row_loss ? rows : 0, s);
+    if (rc != CIRC_OK) return rc;
+    unsigned* words = static_cast<unsigned*>(l->ws.ptr);
+    if (mean && !row_loss) row_loss = reinterpret_cast<float*>(static_cast<char*>(l->ws.ptr) + 256);
+    const LossArgs a{ld, grad_ld, row_loss, lse, mean, count_alone ? reinterpret_cast<int*>(words + 1) : nullptr, words, grad_mean, (int)rows,
+                     l->classes, l->ignore};
+    cudaError_t err = cudaSuccess;
     with_dtype(l->dtype, [&](auto* t) {
         with_index_type(l->ids_type, [&](auto* i) {
             using T = tag_type<decltype(t)>;
             using ID = tag_type<decltype(i)>;
-            loss_kernel<T, ID><<<(unsigned)rows, 256, 0, s>>>(static_cast<const T*>(z), ld, static_cast<const ID*>(targets), row_loss, lse,
-                                                              static_cast<T*>(grad), grad_ld, grad_mean, (int)rows, l->classes, l->ignore);
-            if (mean)
-                loss_mean_kernel<ID><<<1, 1024, 0, s>>>(row_loss, static_cast<const ID*>(targets), mean, (int)rows, l->classes, l->ignore);
+            const ID* ids = static_cast<const ID*>(targets);
+            if (count_alone) {
+                loss_count_kernel<ID><<<1, 1024, 0, s>>>(a, ids);
+                if ((err = cudaGetLastError()) != cudaSuccess) return;
+            }
+            err = dispatch_loss<T, ID>(static_cast<const T*>(z), ids, static_cast<T*>(grad), a, s);
         });
     });
-    count_launches(1 + (mean != nullptr));
-    CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
+    count_launches(1 + count_alone);
     return CIRC_OK;
 }
 
@@ -186,7 +557,7 @@ int circ_loss_reserve(circ_loss_handle h, long max_rows) {
         set_error(CIRC_ERR_ARG, "bad handle or max_rows %ld", max_rows);
         return CIRC_ERR_ARG;
     }
-    return ensure_scratch(l->ws, (size_t)max_rows * sizeof(float), 0, "circ_loss_reserve");
+    return ensure_loss(l, max_rows, 0);
 }
 
 int circ_loss_forward(circ_loss_handle h, const void* logits, long stride, const void* targets, float* row_loss, float* lse, float* mean,

@@ -159,8 +159,9 @@ template <int VEC, bool ALIGNED>
 struct RowSpan {
     size_t first;      // element index of vector 0 in the tensor
     int shift, dim;    // column of its first element, <= 0
-    __device__ __forceinline__ RowSpan(long row, int d) {
-        const size_t base = (size_t)row * d;
+    __device__ __forceinline__ RowSpan(long row, int d) : RowSpan(row, d, d) {}
+    __device__ __forceinline__ RowSpan(long row, int d, long stride) {
+        const size_t base = (size_t)row * stride;
         first = ALIGNED ? base : base / VEC * VEC;
         shift = ALIGNED ? 0 : -(int)(base - first);
         dim = d;
