@@ -35,79 +35,120 @@ struct LossArgs {
 struct Softmax {
     float top, sum;
 };
-constexpr float kLog2e = 1.4426950408889634f;
-// exp(d); the difference to the row's top is taken before the factor, so that large scores lose nothing
-__device__ __forceinline__ float exp_of(float d) {
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float exp2_of(float d) {
     float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d * kLog2e));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
     return r;
 }
+// The exponentials of a row relative to `top`: exp(z - top) 2^shift = 2^(z log2(e) - base), one multiply-add and one exponential an
+// element.  base is top log2(e) rounded, shift what the rounding left: up to |top| 2^-23, so scores beyond 2^20 (a row that a mask's
+// lowest value fills) take the difference to the top first, and shift is 0.  A top of -inf counts as 0.
+struct Exponent {
+    float top, base, shift;
+    bool plain;
+    __device__ __forceinline__ explicit Exponent(float t) {
+        top = t == -INFINITY ? 0.f : t;
+        plain = !(fabsf(top) <= 1048576.f);
+        base = plain ? 0.f : top * kLog2e;
+        shift = plain ? 0.f : fmaf(top, kLog2e, -base);
+    }
+    template <int N>
+    __device__ __forceinline__ void of(const float (&z)[N], float (&e)[N]) const {
+        if (!plain) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = exp2_of(fmaf(z[i], kLog2e, -base));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = exp2_of((z[i] - top) * kLog2e);
+        }
+    }
+};
 __device__ __forceinline__ Softmax join(Softmax a, Softmax b) {
     const float top = fmaxf(a.top, b.top);
     // a part whose top is -inf has the sum 0 or, from a NaN, NaN
-    return Softmax{top, a.sum * (a.top == -INFINITY ? 0.f : exp_of(a.top - top)) + b.sum * (b.top == -INFINITY ? 0.f : exp_of(b.top - top))};
+    return Softmax{top, a.sum * (a.top == -INFINITY ? 0.f : exp2_of((a.top - top) * kLog2e)) +
+                            b.sum * (b.top == -INFINITY ? 0.f : exp2_of((b.top - top) * kLog2e))};
 }
 __device__ __forceinline__ Softmax warp_join(Softmax v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = join(v, Softmax{__shfl_xor_sync(0xffffffffu, v.top, o), __shfl_xor_sync(0xffffffffu, v.sum, o)});
     return v;
 }
-// One vector of a row into the running pair: one exponential an element, one more where the top rises.
-template <int VEC>
-__device__ __forceinline__ void take(Softmax& v, const float (&z)[VEC]) {
-    float top = z[0];
+// A thread's part of a row: vectors in any order, one exponential an element and one more where the top rises.
+struct Running {
+    float top = -INFINITY, sum = 0.f;      // sum of exp(z - top) 2^shift
+    Exponent ex{-INFINITY};
+    template <int VEC>
+    __device__ __forceinline__ void take(const float (&z)[VEC]) {
+        float most = z[0];
 #pragma unroll
-    for (int e = 1; e < VEC; ++e) top = fmaxf(top, z[e]);
-    if (top > v.top) {
-        v.sum *= v.top == -INFINITY ? 0.f : exp_of(v.top - top);
-        v.top = top;
+        for (int e = 1; e < VEC; ++e) most = fmaxf(most, z[e]);
+        if (most > top) {
+            const Exponent to(most);
+            sum *= top == -INFINITY ? 0.f : exp2_of((top - most) * kLog2e + (to.shift - ex.shift));
+            top = most;
+            ex = to;
+        }
+        float e[VEC], part = 0.f;
+        ex.of(z, e);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) part += e[i];
+        sum += part;
     }
-    const float base = v.top == -INFINITY ? 0.f : v.top;
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) sum += exp_of(z[e] - base);
-    v.sum += sum;
-}
+    __device__ __forceinline__ Softmax done() const { return Softmax{top, sum * exp2_of(-ex.shift)}; }
+};
 // Elements of a vector as scores; those beside the row's own are -inf.
 template <typename T, int VEC, typename SPAN>
 __device__ __forceinline__ void scores(const SPAN& span, int v, const RawVec<T, VEC>& raw, float (&z)[VEC]) {
-    const bool whole = span.any(v) && span.whole(v);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) z[e] = whole || (span.any(v) && e >= span.lo(v) && e < span.hi(v)) ? raw.get(e) : -INFINITY;
+    for (int e = 0; e < VEC; ++e) z[e] = raw.get(e);
+    if (span.any(v) && span.whole(v)) return;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        if (!span.any(v) || e < span.lo(v) || e >= span.hi(v)) z[e] = -INFINITY;
 }
 
 // What is the same for a whole row once its sum is known.
 struct RowResult {
-    float base;        // the top, 0 where it is -inf
-    float factor;      // gradient = exp(z - base) * factor, less `hot` at the target
+    Exponent ex;
+    float factor;      // gradient = exponential * factor, less `hot` at the target
     float hot;
     bool zero;         // no gradient
 };
 template <typename ID>
 __device__ __forceinline__ RowResult finish_row(const LossArgs& a, int row, Softmax all, ID target, float target_score, int count, bool writes) {
-    RowResult r;
-    r.base = all.top == -INFINITY ? 0.f : all.top;
+    RowResult r{Exponent(all.top), 0.f, 0.f, false};
     const bool valid = has_target(target, a.classes, a.ignore);
     if (writes) {
-        const float lse = r.base + logf(all.sum);
+        const float log_sum = logf(all.sum), lse = r.ex.top + log_sum;
         if (a.lse) a.lse[row] = lse;
-        if (a.row_loss) a.row_loss[row] = !valid ? 0.f : target_score == -INFINITY && lse == lse ? INFINITY : lse - target_score;
+        // the difference of the two scores first: it is small where both are large
+        if (a.row_loss) a.row_loss[row] = !valid ? 0.f : target_score == -INFINITY && lse == lse ? INFINITY : (r.ex.top - target_score) + log_sum;
     }
     r.zero = !valid || all.sum == 0.f;
     r.hot = a.grad_mean / (float)(count < 1 ? 1 : count);
-    r.factor = r.hot / all.sum;
+    r.factor = r.hot / (all.sum * exp2_of(r.ex.shift));
     return r;
+}
+// The gradient of a vector whose first element is `t` columns before the target (t outside [0, VEC): the target is not in it).
+template <int VEC>
+__device__ __forceinline__ void gradient(const float (&z)[VEC], const RowResult& r, int t, float (&g)[VEC]) {
+    r.ex.of(z, g);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) g[e] *= r.factor;
+    if ((unsigned)t < (unsigned)VEC)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e == t) g[e] -= r.hot;
+    if (r.zero)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) g[e] = 0.f;
 }
 template <typename T, int VEC, typename SPAN>
 __device__ __forceinline__ void write_gradient(const SPAN& span, T* grad, size_t first, int v, const float (&z)[VEC], const RowResult& r, int target) {
     float g[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) g[e] = r.zero ? 0.f : exp_of(z[e] - r.base) * r.factor;
-    const int t = target - span.col(v);
-    if (!r.zero && t >= 0 && t < VEC)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (e == t) g[e] -= r.hot;
+    gradient(z, r, target - span.col(v), g);
     T* dst = grad + first + (size_t)v * VEC;
     if (span.whole(v)) {
         store_vec_once<VEC>(dst, g);
@@ -201,10 +242,10 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
         __syncthreads();
         count = __reduce_add_sync(0xffffffffu, lane < 8 ? part[lane] : 0);
     }
-    Softmax all{-INFINITY, 0.f};
+    Running run;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) take(all, s[i]);
-    all = warp_join(all);
+    for (int i = 0; i < ITEMS; ++i) run.take(s[i]);
+    const Softmax all = warp_join(run.done());
     if (GRAD && a.count) {
         pdl_wait();
         count = __ldcg(a.count);
@@ -224,8 +265,9 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
 
 // ---- long rows: a block, or the blocks of a cluster, hold one ----
 // GRAD: the row is copied to shared memory as it arrives, summed up from there, and read there a second time for the gradient, so that
-// it crosses the memory bus once.  Every thread copies and reads its own vectors.  Two blocks of up to 110 KB share an SM: one
-// fetches while the other computes.  Without a gradient nothing is kept.
+// it crosses the memory bus once.  Every thread copies and reads its own vectors.  Several blocks share an SM: one fetches while the
+// others compute.  Without a gradient nothing is kept.  What bounds it next to the bus: two exponentials an element, at 16 a cycle on
+// an SM.  The loops run over whole vectors; a row's first and last elements beside them (odd strides) are one thread's each.
 constexpr int kLossChunk = 4;     // vectors a thread in a group of copies
 
 __device__ __forceinline__ void wait_copies(int groups) {      // until at most `groups` groups of copies are in flight (exact up to 7)
@@ -241,7 +283,7 @@ __device__ __forceinline__ void wait_copies(int groups) {      // until at most 
     }
 }
 
-template <typename T, typename ID, int VEC, bool ALIGNED, bool GRAD>
+template <typename T, typename ID, int VEC, bool GRAD>
 __global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a, int cluster) {
     extern __shared__ __align__(16) unsigned char held[];
     __shared__ Softmax part[16];
@@ -249,58 +291,73 @@ __global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* _
     __shared__ int counts[16];
     const int threads = blockDim.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = threads / 32;
     const int rank = blockIdx.x % cluster, row = blockIdx.x / cluster;
-    const RowSpan<VEC, ALIGNED> span(row, a.classes, a.ld);
-    const int vectors = (a.classes - span.shift + VEC - 1) / VEC, per = (vectors + cluster - 1) / cluster;
-    const int v0 = rank * per, v1 = v0 + per < vectors ? v0 + per : vectors;
-    auto place = [&](int v) { return reinterpret_cast<T*>(held) + (size_t)(v - v0) * VEC; };
-    Softmax all{-INFINITY, 0.f};
+    const RowSpan<VEC, false> span(row, a.classes, a.ld);
+    const int vectors = (a.classes - span.shift + VEC - 1) / VEC;
+    // whole vectors w0 <= w < w1 of the row; this block's: `mine` of them from `from` on, this thread's: every `threads`-th
+    const int w0 = span.whole(0) ? 0 : 1, w1 = span.whole(vectors - 1) ? vectors : vectors - 1;
+    const int per = (w1 - w0 + cluster - 1) / cluster, from = w0 + rank * per, mine = min(w1 - from, per);
+    // the vectors that are not whole: the block's thread 0 or 1 has one, or -1
+    const int rest = rank != 0 ? -1 : tid == 0 && w0 == 1 ? 0 : tid == 1 && w1 < vectors ? vectors - 1 : -1;
+    const T* src = z + span.at(from) + (size_t)tid * VEC;
+    T* kept = reinterpret_cast<T*>(held) + (size_t)tid * VEC;
+    const int step = threads * VEC;
+    Running run;
     const ID target = targets[row];
     float target_score = 0.f;
     if constexpr (GRAD) {
         int groups = 0;
-        for (int v = v0 + tid; v < v1; v += kLossChunk * threads, ++groups) {
+        for (int i = tid; i < mine; i += kLossChunk * threads, ++groups) {
+            const T* p = src + (size_t)(i - tid) * VEC;
+            T* k = kept + (i - tid) * VEC;
 #pragma unroll
-            for (int u = 0; u < kLossChunk; ++u) {
-                const int w = v + u * threads;
-                if (w < v1 && span.whole(w)) copy_async<16>(place(w), z + span.at(w));
-            }
+            for (int u = 0; u < kLossChunk; ++u)
+                if (i + u * threads < mine) copy_async<16>(k + u * step, p + u * step);
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
         if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
         int count = 0;
         if (!a.count) count = __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, threads));
         if (lane == 0) counts[warp] = count;
-        for (int v = v0 + tid; v < v1; v += kLossChunk * threads) {
+        for (int i = tid; i < mine; i += kLossChunk * threads) {
+            const T* k = kept + (i - tid) * VEC;
             wait_copies(--groups);
 #pragma unroll
             for (int u = 0; u < kLossChunk; ++u) {
-                const int w = v + u * threads;
-                if (w >= v1) break;
+                if (i + u * threads >= mine) break;
                 RawVec<T, VEC> raw;
                 float s[VEC];
-                if (span.whole(w)) raw.load(place(w));
-                else span.load(raw, z, w);
-                scores(span, w, raw, s);
-                take(all, s);
+                raw.load(k + u * step);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
+                run.take(s);
             }
         }
     } else {
         if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
-        for (int v = v0 + tid; v < v1; v += kLossChunk * threads) {
+        for (int i = tid; i < mine; i += kLossChunk * threads) {
+            const T* p = src + (size_t)(i - tid) * VEC;
             RawVec<T, VEC> raw[kLossChunk];
 #pragma unroll
             for (int u = 0; u < kLossChunk; ++u)
-                if (v + u * threads < v1) span.load(raw[u], z, v + u * threads);
+                if (i + u * threads < mine) raw[u].load(p + u * step);
 #pragma unroll
             for (int u = 0; u < kLossChunk; ++u) {
-                if (v + u * threads >= v1) break;
+                if (i + u * threads >= mine) break;
                 float s[VEC];
-                scores(span, v + u * threads, raw[u], s);
-                take(all, s);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[e] = raw[u].get(e);
+                run.take(s);
             }
         }
     }
-    all = warp_join(all);
+    if (rest >= 0) {
+        RawVec<T, VEC> raw;
+        float s[VEC];
+        span.load(raw, z, rest);
+        scores(span, rest, raw, s);
+        run.take(s);
+    }
+    Softmax all = warp_join(run.done());
     if (lane == 0) part[warp] = all;
     __syncthreads();
     all = warp_join(lane < warps ? part[lane] : Softmax{-INFINITY, 0.f});
@@ -324,15 +381,25 @@ __global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* _
     }
     const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
     if constexpr (GRAD) {
-        // vectors that were not copied are read again: where grad is z, those are this thread's own
         const size_t first = (size_t)row * a.grad_ld + span.shift;
-        for (int w = v0 + tid; w < v1; w += threads) {
+        T* dst = grad + first + (size_t)(from + tid) * VEC;
+        const int t0 = (int)target - span.col(from + tid);
+#pragma unroll 2
+        for (int i = 0; i < mine - tid; i += threads) {
+            RawVec<T, VEC> raw;
+            float s[VEC], g[VEC];
+            raw.load(kept + i * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
+            gradient(s, r, t0 - i * VEC, g);
+            store_vec_once<VEC>(dst + (size_t)i * VEC, g);
+        }
+        if (rest >= 0) {     // read again: where grad is z, these elements are this thread's own
             RawVec<T, VEC> raw;
             float s[VEC];
-            if (span.whole(w)) raw.load(place(w));
-            else span.load(raw, z, w);
-            scores(span, w, raw, s);
-            write_gradient<T, VEC>(span, grad, first, w, s, r, (int)target);
+            span.load(raw, z, rest);
+            scores(span, rest, raw, s);
+            write_gradient<T, VEC>(span, grad, first, rest, s, r, (int)target);
         }
     }
     if (rank == 0) finish_mean(a, targets, gridDim.x / cluster);
@@ -345,17 +412,17 @@ __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __r
     __shared__ int counts[16];
     const int row = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const T* zr = z + (size_t)row * a.ld;
-    Softmax all{-INFINITY, 0.f};
+    Running run;
     for (int c0 = tid; c0 < a.classes; c0 += 512 * 8) {
         float s[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = c0 + e * 512 < a.classes ? to_float(zr[c0 + e * 512]) : -INFINITY;
-        take(all, s);
+        run.take(s);
     }
     const ID target = targets[row];
     const bool valid = has_target(target, a.classes, a.ignore);
     const float target_score = valid ? to_float(zr[target]) : 0.f;
-    all = warp_join(all);
+    Softmax all = warp_join(run.done());
     const int n = grad && !a.count ? __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, 512)) : 0;
     if (lane == 0) {
         part[warp] = all;
@@ -371,8 +438,12 @@ __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __r
     const RowResult r = finish_row(a, row, all, target, target_score, count, tid == 0);
     if (grad) {
         T* gr = grad + (size_t)row * a.grad_ld;
-        for (int c = tid; c < a.classes; c += 512)
-            store_one(gr + c, r.zero ? 0.f : exp_of(to_float(zr[c]) - r.base) * r.factor - (c == (int)target ? r.hot : 0.f));
+        for (int c = tid; c < a.classes; c += 512) {
+            const float s[1] = {to_float(zr[c])};
+            float g[1];
+            gradient(s, r, (int)target - c, g);
+            store_one(gr + c, g[0]);
+        }
     }
     finish_mean(a, targets, gridDim.x);
 }
@@ -422,13 +493,14 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
             vectors <= 32 ? go(std::integral_constant<int, 1>{}) : vectors <= 64 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
             return;
         }
+        if (vectors > (1 << 26)) return;
         // blocks a row: enough to hold it, and more while the rows do not fill the machine (4 vectors a thread left at least)
         int cluster = 1;
         auto bytes = [&]() { return (size_t)((vectors + cluster - 1) / cluster) * 16; };
         while (cluster < 8 && ((GRAD && bytes() > kLossHeld) || ((long)a.rows * cluster < 148 && vectors / cluster > 2048))) cluster *= 2;
         if (GRAD && bytes() > kLossMost) return;
         const int each = (vectors + cluster - 1) / cluster, threads = each <= 512 ? 128 : each <= 2048 ? 256 : 512;
-        auto kernel = loss_block_kernel<T, ID, VEC, ALIGNED, GRAD>;
+        auto kernel = loss_block_kernel<T, ID, VEC, GRAD>;
         if (GRAD && (err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLossMost)) != cudaSuccess) return;
         err = launch_loss(dependent, cluster, kernel, (unsigned)(a.rows * (long)cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
     };
