@@ -64,37 +64,70 @@ struct Exponent {
         }
     }
 };
-__device__ __forceinline__ Softmax join(Softmax a, Softmax b) {
-    const float top = fmaxf(a.top, b.top);
-    // a part whose top is -inf has the sum 0 or, from a NaN, NaN
-    return Softmax{top, a.sum * (a.top == -INFINITY ? 0.f : exp2_of((a.top - top) * kLog2e)) +
-                            b.sum * (b.top == -INFINITY ? 0.f : exp2_of((b.top - top) * kLog2e))};
-}
+// The lanes' pairs as one: the top first, so that every lane takes one exponential.
 __device__ __forceinline__ Softmax warp_join(Softmax v) {
+    float top = v.top;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = join(v, Softmax{__shfl_xor_sync(0xffffffffu, v.top, o), __shfl_xor_sync(0xffffffffu, v.sum, o)});
-    return v;
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // a part whose top is -inf has the sum 0 or, from a NaN, NaN
+    return Softmax{top, warp_sum(v.sum * (v.top == -INFINITY ? 0.f : exp2_of((v.top - top) * kLog2e)))};
+}
+// The largest element of some vectors; bfloat16 ones are compared in pairs as they lie.
+template <int VEC, int N>
+__device__ __forceinline__ float most_of(const RawVec<float, VEC> (&raw)[N]) {
+    float most = raw[0].get(0);
+#pragma unroll
+    for (int i = 1; i < N * VEC; ++i) most = fmaxf(most, raw[i / VEC].get(i % VEC));
+    return most;
+}
+template <int VEC, int N>
+__device__ __forceinline__ float most_of(const RawVec<__nv_bfloat16, VEC> (&raw)[N]) {
+    constexpr int W = VEC / 2;
+    __nv_bfloat162 most = *reinterpret_cast<const __nv_bfloat162*>(&raw[0].w[0]);
+#pragma unroll
+    for (int i = 1; i < N * W; ++i) most = __hmax2(most, *reinterpret_cast<const __nv_bfloat162*>(&raw[i / W].w[i % W]));
+    return fmaxf(__low2float(most), __high2float(most));
 }
 // A thread's part of a row: vectors in any order, one exponential an element and one more where the top rises.
 struct Running {
     float top = -INFINITY, sum = 0.f;      // sum of exp(z - top) 2^shift
     Exponent ex{-INFINITY};
+    __device__ __forceinline__ void rise(float most) {
+        if (!(most > top)) return;
+        const Exponent to(most);
+        sum *= top == -INFINITY ? 0.f : exp2_of((top - most) * kLog2e + (to.shift - ex.shift));
+        top = most;
+        ex = to;
+    }
     template <int VEC>
     __device__ __forceinline__ void take(const float (&z)[VEC]) {
         float most = z[0];
 #pragma unroll
         for (int e = 1; e < VEC; ++e) most = fmaxf(most, z[e]);
-        if (most > top) {
-            const Exponent to(most);
-            sum *= top == -INFINITY ? 0.f : exp2_of((top - most) * kLog2e + (to.shift - ex.shift));
-            top = most;
-            ex = to;
-        }
+        rise(most);
         float e[VEC], part = 0.f;
         ex.of(z, e);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) part += e[i];
         sum += part;
+    }
+    // N vectors as loaded: one look at the top for all of them.
+    template <typename T, int VEC, int N>
+    __device__ __forceinline__ void take(const RawVec<T, VEC> (&raw)[N]) {
+        rise(most_of(raw));
+        float part[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float z[VEC], e[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) z[i] = raw[u].get(i);
+            ex.of(z, e);
+            part[u] = 0.f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) part[u] += e[i];
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) sum += part[u];
     }
     __device__ __forceinline__ Softmax done() const { return Softmax{top, sum * exp2_of(-ex.shift)}; }
 };
@@ -321,32 +354,34 @@ __global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* _
         for (int i = tid; i < mine; i += kLossChunk * threads) {
             const T* k = kept + (i - tid) * VEC;
             wait_copies(--groups);
+            if (i + (kLossChunk - 1) * threads < mine) {
+                RawVec<T, VEC> raw[kLossChunk];
 #pragma unroll
-            for (int u = 0; u < kLossChunk; ++u) {
-                if (i + u * threads >= mine) break;
-                RawVec<T, VEC> raw;
-                float s[VEC];
-                raw.load(k + u * step);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
-                run.take(s);
+                for (int u = 0; u < kLossChunk; ++u) raw[u].load(k + u * step);
+                run.take(raw);
+            } else {
+                for (int j = 0; i + j * threads < mine; ++j) {
+                    RawVec<T, VEC> raw[1];
+                    raw[0].load(k + j * step);
+                    run.take(raw);
+                }
             }
         }
     } else {
         if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
         for (int i = tid; i < mine; i += kLossChunk * threads) {
             const T* p = src + (size_t)(i - tid) * VEC;
-            RawVec<T, VEC> raw[kLossChunk];
+            if (i + (kLossChunk - 1) * threads < mine) {
+                RawVec<T, VEC> raw[kLossChunk];
 #pragma unroll
-            for (int u = 0; u < kLossChunk; ++u)
-                if (i + u * threads < mine) raw[u].load(p + u * step);
-#pragma unroll
-            for (int u = 0; u < kLossChunk; ++u) {
-                if (i + u * threads >= mine) break;
-                float s[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) s[e] = raw[u].get(e);
-                run.take(s);
+                for (int u = 0; u < kLossChunk; ++u) raw[u].load(p + u * step);
+                run.take(raw);
+            } else {
+                for (int j = 0; i + j * threads < mine; ++j) {
+                    RawVec<T, VEC> raw[1];
+                    raw[0].load(p + j * step);
+                    run.take(raw);
+                }
             }
         }
     }
@@ -383,16 +418,29 @@ __global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* _
     if constexpr (GRAD) {
         const size_t first = (size_t)row * a.grad_ld + span.shift;
         T* dst = grad + first + (size_t)(from + tid) * VEC;
-        const int t0 = (int)target - span.col(from + tid);
-#pragma unroll 2
-        for (int i = 0; i < mine - tid; i += threads) {
-            RawVec<T, VEC> raw;
-            float s[VEC], g[VEC];
-            raw.load(kept + i * VEC);
+        if (r.zero) {
+            const float g[VEC] = {};
+            for (int i = 0; i < mine - tid; i += threads) store_vec_once<VEC>(dst + (size_t)i * VEC, g);
+        } else {
+#pragma unroll 4
+            for (int i = 0; i < mine - tid; i += threads) {
+                RawVec<T, VEC> raw;
+                float s[VEC], g[VEC];
+                raw.load(kept + i * VEC);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
-            gradient(s, r, t0 - i * VEC, g);
-            store_vec_once<VEC>(dst + (size_t)i * VEC, g);
+                for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
+                r.ex.of(s, g);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) g[e] *= r.factor;
+                store_vec_once<VEC>(dst + (size_t)i * VEC, g);
+            }
+            const int t = (int)target - span.col(from);       // the target's element once more, by the thread that has written its vector
+            if (t >= 0 && t / VEC < mine && t / VEC % threads == tid) {
+                const float s[1] = {target_score};
+                float g[1];
+                gradient(s, r, 0, g);
+                store_one(grad + first + (size_t)from * VEC + t, g[0]);
+            }
         }
         if (rest >= 0) {     // read again: where grad is z, these elements are this thread's own
             RawVec<T, VEC> raw;
