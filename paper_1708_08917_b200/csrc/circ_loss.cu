@@ -53,15 +53,28 @@ struct Exponent {
         base = plain ? 0.f : top * kLog2e;
         shift = plain ? 0.f : fmaf(top, kLog2e, -base);
     }
-    template <int N>
-    __device__ __forceinline__ void of(const float (&z)[N], float (&e)[N]) const {
-        if (!plain) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) e[i] = exp2_of(fmaf(z[i], kLog2e, -base));
-        } else {
+    template <bool PLAIN, int N>
+    __device__ __forceinline__ void powers(const float (&z)[N], float (&e)[N]) const {
+        if constexpr (PLAIN) {
 #pragma unroll
             for (int i = 0; i < N; ++i) e[i] = exp2_of((z[i] - top) * kLog2e);
+        } else if constexpr (N % 2 == 0) {
+            const Pair k = pair_of(kLog2e, kLog2e), b = pair_of(-base, -base);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                split(pair_fma(pair_of(z[i], z[i + 1]), k, b), e[i], e[i + 1]);
+                e[i] = exp2_of(e[i]);
+                e[i + 1] = exp2_of(e[i + 1]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = exp2_of(fmaf(z[i], kLog2e, -base));
         }
+    }
+    template <int N>
+    __device__ __forceinline__ void of(const float (&z)[N], float (&e)[N]) const {
+        if (plain) powers<true>(z, e);
+        else powers<false>(z, e);
     }
 };
 // The lanes' pairs as one: the top first, so that every lane takes one exponential.
@@ -115,19 +128,27 @@ struct Running {
     template <typename T, int VEC, int N>
     __device__ __forceinline__ void take(const RawVec<T, VEC> (&raw)[N]) {
         rise(most_of(raw));
-        float part[N];
+        if (ex.plain) add<true>(raw);      // one branch for all of them
+        else add<false>(raw);
+    }
+    template <bool PLAIN, typename T, int VEC, int N>
+    __device__ __forceinline__ void add(const RawVec<T, VEC> (&raw)[N]) {
+        Pair part[N];
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             float z[VEC], e[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) z[i] = raw[u].get(i);
-            ex.of(z, e);
-            part[u] = 0.f;
+            ex.powers<PLAIN>(z, e);
+            part[u] = pair_of(e[0], e[1]);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) part[u] += e[i];
+            for (int i = 2; i < VEC; i += 2) part[u] = pair_add(part[u], pair_of(e[i], e[i + 1]));
         }
 #pragma unroll
-        for (int u = 0; u < N; ++u) sum += part[u];
+        for (int u = 1; u < N; ++u) part[0] = pair_add(part[0], part[u]);
+        float lo, hi;
+        split(part[0], lo, hi);
+        sum += lo + hi;
     }
     __device__ __forceinline__ Softmax done() const { return Softmax{top, sum * exp2_of(-ex.shift)}; }
 };
@@ -298,9 +319,10 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
 
 // ---- long rows: a block, or the blocks of a cluster, hold one ----
 // GRAD: the row is copied to shared memory as it arrives, summed up from there, and read there a second time for the gradient, so that
-// it crosses the memory bus once.  Every thread copies and reads its own vectors.  Several blocks share an SM: one fetches while the
-// others compute.  Without a gradient nothing is kept.  What bounds it next to the bus: two exponentials an element, at 16 a cycle on
-// an SM.  The loops run over whole vectors; a row's first and last elements beside them (odd strides) are one thread's each.
+// it crosses the memory bus once.  Every thread copies and reads its own vectors, so a vector's place is free for the next row's as
+// soon as its gradient is out: the blocks walk over the rows, and the next row streams in behind the gradient of this one.  Without a
+// gradient nothing is kept.  What bounds it next to the bus: two exponentials an element, at 16 a cycle on an SM.  The loops run over
+// whole vectors; a row's first and last elements beside them (odd strides) are one thread's each.
 constexpr int kLossChunk = 4;     // vectors a thread in a group of copies
 
 __device__ __forceinline__ void wait_copies(int groups) {      // until at most `groups` groups of copies are in flight (exact up to 7)
@@ -316,141 +338,176 @@ __device__ __forceinline__ void wait_copies(int groups) {      // until at most 
     }
 }
 
+// A block's part of a row.
+template <int VEC>
+struct LossPart {
+    RowSpan<VEC, false> span;
+    int vectors, w0, w1;      // vectors of the row, and the range of its whole ones
+    int from, mine;           // this block's: `mine` whole ones from `from` on; a thread's are every threads-th of them
+    __device__ __forceinline__ LossPart(const LossArgs& a, long row, int rank, int cluster) : span(row, a.classes, a.ld) {
+        vectors = (a.classes - span.shift + VEC - 1) / VEC;
+        w0 = span.whole(0) ? 0 : 1;
+        w1 = span.whole(vectors - 1) ? vectors : vectors - 1;
+        const int per = (w1 - w0 + cluster - 1) / cluster;
+        from = w0 + rank * per;
+        mine = min(w1 - from, per);
+    }
+};
+
 template <typename T, typename ID, int VEC, bool GRAD>
-__global__ void __launch_bounds__(512) loss_block_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a, int cluster) {
+__global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a, int cluster) {
     extern __shared__ __align__(16) unsigned char held[];
-    __shared__ Softmax part[16];
-    __shared__ Softmax peers[8];
+    __shared__ Softmax part[2][16];
+    __shared__ Softmax peers[2][8];
     __shared__ int counts[16];
     const int threads = blockDim.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = threads / 32;
-    const int rank = blockIdx.x % cluster, row = blockIdx.x / cluster;
-    const RowSpan<VEC, false> span(row, a.classes, a.ld);
-    const int vectors = (a.classes - span.shift + VEC - 1) / VEC;
-    // whole vectors w0 <= w < w1 of the row; this block's: `mine` of them from `from` on, this thread's: every `threads`-th
-    const int w0 = span.whole(0) ? 0 : 1, w1 = span.whole(vectors - 1) ? vectors : vectors - 1;
-    const int per = (w1 - w0 + cluster - 1) / cluster, from = w0 + rank * per, mine = min(w1 - from, per);
-    // the vectors that are not whole: the block's thread 0 or 1 has one, or -1
-    const int rest = rank != 0 ? -1 : tid == 0 && w0 == 1 ? 0 : tid == 1 && w1 < vectors ? vectors - 1 : -1;
-    const T* src = z + span.at(from) + (size_t)tid * VEC;
+    const int rank = blockIdx.x % cluster, rows_apart = gridDim.x / cluster;
     T* kept = reinterpret_cast<T*>(held) + (size_t)tid * VEC;
     const int step = threads * VEC;
-    Running run;
-    const ID target = targets[row];
-    float target_score = 0.f;
+    if (lane == 0) counts[warp] = 0;
     if constexpr (GRAD) {
-        int groups = 0;
-        for (int i = tid; i < mine; i += kLossChunk * threads, ++groups) {
-            const T* p = src + (size_t)(i - tid) * VEC;
-            T* k = kept + (i - tid) * VEC;
+        const LossPart<VEC> p(a, blockIdx.x / cluster, rank, cluster);
+        const T* src = z + p.span.at(p.from) + (size_t)tid * VEC;
+        for (int i = tid; i < p.mine; i += kLossChunk * threads) {
 #pragma unroll
             for (int u = 0; u < kLossChunk; ++u)
-                if (i + u * threads < mine) copy_async<16>(k + u * step, p + u * step);
+                if (i + u * threads < p.mine) copy_async<16>(kept + (i - tid) * VEC + u * step, src + (size_t)(i - tid) * VEC + u * step);
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
-        int count = 0;
-        if (!a.count) count = __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, threads));
-        if (lane == 0) counts[warp] = count;
-        for (int i = tid; i < mine; i += kLossChunk * threads) {
-            const T* k = kept + (i - tid) * VEC;
-            wait_copies(--groups);
-            if (i + (kLossChunk - 1) * threads < mine) {
-                RawVec<T, VEC> raw[kLossChunk];
+        const int n = a.count ? 0 : __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, threads));
+        if (lane == 0) counts[warp] = n;
+    }
+    int count = 0, flip = 0;
+    for (int row = blockIdx.x / cluster; row < a.rows; row += rows_apart, flip ^= 1) {
+        const LossPart<VEC> p(a, row, rank, cluster);
+        // the vectors that are not whole: the row's first block's thread 0 or 1 has one, or -1
+        const int rest = rank != 0 ? -1 : tid == 0 && p.w0 == 1 ? 0 : tid == 1 && p.w1 < p.vectors ? p.vectors - 1 : -1;
+        const ID target = targets[row];
+        const float target_score = has_target(target, a.classes, a.ignore) ? to_float(z[(size_t)row * a.ld + target]) : 0.f;
+        Running run;
+        if constexpr (GRAD) {
+            int groups = (p.mine - tid + kLossChunk * threads - 1) / (kLossChunk * threads);
+            for (int i = tid; i < p.mine; i += kLossChunk * threads) {
+                const T* k = kept + (i - tid) * VEC;
+                wait_copies(--groups);
+                if (i + (kLossChunk - 1) * threads < p.mine) {
+                    RawVec<T, VEC> raw[kLossChunk];
 #pragma unroll
-                for (int u = 0; u < kLossChunk; ++u) raw[u].load(k + u * step);
-                run.take(raw);
-            } else {
-                for (int j = 0; i + j * threads < mine; ++j) {
-                    RawVec<T, VEC> raw[1];
-                    raw[0].load(k + j * step);
+                    for (int u = 0; u < kLossChunk; ++u) raw[u].load(k + u * step);
                     run.take(raw);
+                } else {
+                    for (int j = 0; i + j * threads < p.mine; ++j) {
+                        RawVec<T, VEC> raw[1];
+                        raw[0].load(k + j * step);
+                        run.take(raw);
+                    }
                 }
             }
-        }
-    } else {
-        if (has_target(target, a.classes, a.ignore)) target_score = to_float(z[(size_t)row * a.ld + target]);
-        for (int i = tid; i < mine; i += kLossChunk * threads) {
-            const T* p = src + (size_t)(i - tid) * VEC;
-            if (i + (kLossChunk - 1) * threads < mine) {
+        } else {
+            const T* src = z + p.span.at(p.from) + (size_t)tid * VEC;
+            int i = tid;
+            for (; i + (kLossChunk - 1) * threads < p.mine; i += kLossChunk * threads) {
                 RawVec<T, VEC> raw[kLossChunk];
 #pragma unroll
-                for (int u = 0; u < kLossChunk; ++u) raw[u].load(p + u * step);
+                for (int u = 0; u < kLossChunk; ++u) raw[u].load(src + (size_t)(i - tid) * VEC + u * step);
                 run.take(raw);
-            } else {
-                for (int j = 0; i + j * threads < mine; ++j) {
-                    RawVec<T, VEC> raw[1];
-                    raw[0].load(p + j * step);
-                    run.take(raw);
-                }
+            }
+            for (; i < p.mine; i += threads) {
+                RawVec<T, VEC> raw[1];
+                raw[0].load(src + (size_t)(i - tid) * VEC);
+                run.take(raw);
             }
         }
-    }
-    if (rest >= 0) {
-        RawVec<T, VEC> raw;
-        float s[VEC];
-        span.load(raw, z, rest);
-        scores(span, rest, raw, s);
-        run.take(s);
-    }
-    Softmax all = warp_join(run.done());
-    if (lane == 0) part[warp] = all;
-    __syncthreads();
-    all = warp_join(lane < warps ? part[lane] : Softmax{-INFINITY, 0.f});
-    if (cluster > 1) {
-        if (tid < cluster) {      // this block's pair to every block of the cluster
-            uint32_t dst;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"((uint32_t)__cvta_generic_to_shared(&peers[rank])), "r"(tid));
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst), "f"(all.top), "f"(all.sum) : "memory");
+        if (rest >= 0) {
+            RawVec<T, VEC> raw;
+            float s[VEC];
+            p.span.load(raw, z, rest);
+            scores(p.span, rest, raw, s);
+            run.take(s);
         }
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        all = warp_join(lane < cluster ? peers[lane] : Softmax{-INFINITY, 0.f});
-    }
-    int count = 1;
-    if constexpr (GRAD) {
-        if (a.count) {
-            pdl_wait();
-            count = __ldcg(a.count);
-        } else {
-            count = __reduce_add_sync(0xffffffffu, lane < warps ? counts[lane] : 0);
+        Softmax all = warp_join(run.done());
+        if (lane == 0) part[flip][warp] = all;
+        __syncthreads();                    // the other halves of `part` and `peers` serve the next row
+        all = warp_join(lane < warps ? part[flip][lane] : Softmax{-INFINITY, 0.f});
+        if (cluster > 1) {
+            if (tid < cluster) {            // this block's pair to every block of the cluster
+                uint32_t dst;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"((uint32_t)__cvta_generic_to_shared(&peers[flip][rank])), "r"(tid));
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dst), "f"(all.top), "f"(all.sum) : "memory");
+            }
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            all = warp_join(lane < cluster ? peers[flip][lane] : Softmax{-INFINITY, 0.f});
         }
-    }
-    const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
-    if constexpr (GRAD) {
-        const size_t first = (size_t)row * a.grad_ld + span.shift;
-        T* dst = grad + first + (size_t)(from + tid) * VEC;
-        if (r.zero) {
-            const float g[VEC] = {};
-            for (int i = 0; i < mine - tid; i += threads) store_vec_once<VEC>(dst + (size_t)i * VEC, g);
-        } else {
-#pragma unroll 4
-            for (int i = 0; i < mine - tid; i += threads) {
+        if (GRAD && count == 0) {
+            if (a.count) {
+                pdl_wait();
+                count = __ldcg(a.count);
+            } else {
+                count = __reduce_add_sync(0xffffffffu, lane < warps ? counts[lane] : 0);
+            }
+            count = count < 1 ? 1 : count;
+        }
+        const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
+        if constexpr (GRAD) {
+            const size_t first = (size_t)row * a.grad_ld + p.span.shift;
+            T* dst = grad + first + (size_t)(p.from + tid) * VEC;
+            const bool more = row + rows_apart < a.rows;
+            const LossPart<VEC> q(a, more ? row + rows_apart : row, rank, cluster);
+            const T* src = z + q.span.at(q.from) + (size_t)tid * VEC;
+            const int next = more ? q.mine : 0, last = next > p.mine ? next : p.mine;
+            const Pair factor = pair_of(r.factor, r.factor);
+            auto put = [&](int o, auto plain) {           // the gradient of the vector that is kept at o
                 RawVec<T, VEC> raw;
                 float s[VEC], g[VEC];
-                raw.load(kept + i * VEC);
+                raw.load(kept + o);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
-                r.ex.of(s, g);
+                r.ex.template powers<decltype(plain)::value>(s, g);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) g[e] *= r.factor;
-                store_vec_once<VEC>(dst + (size_t)i * VEC, g);
+                for (int e = 0; e < VEC; e += 2) split(pair_mul(pair_of(g[e], g[e + 1]), factor), g[e], g[e + 1]);
+                store_vec_once<VEC>(dst + o, g);
+            };
+            for (int i = tid; i < last; i += kLossChunk * threads) {
+                const int o = (i - tid) * VEC, behind = i + (kLossChunk - 1) * threads;
+                if (behind < p.mine && !r.zero && !r.ex.plain) {
+#pragma unroll
+                    for (int u = 0; u < kLossChunk; ++u) put(o + u * step, std::false_type{});
+                } else {
+#pragma unroll 1
+                    for (int u = 0; u < kLossChunk && i + u * threads < p.mine; ++u) {
+                        const float g[VEC] = {};
+                        if (r.zero) store_vec_once<VEC>(dst + o + u * step, g);
+                        else if (r.ex.plain) put(o + u * step, std::true_type{});
+                        else put(o + u * step, std::false_type{});
+                    }
+                }
+                // behind the stores, which have taken what lay there
+                if (behind < next) {
+#pragma unroll
+                    for (int u = 0; u < kLossChunk; ++u) copy_async<16>(kept + o + u * step, src + o + u * step);
+                } else {
+#pragma unroll 1
+                    for (int u = 0; i + u * threads < next; ++u) copy_async<16>(kept + o + u * step, src + o + u * step);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            const int t = (int)target - span.col(from);       // the target's element once more, by the thread that has written its vector
-            if (t >= 0 && t / VEC < mine && t / VEC % threads == tid) {
+            const int t = (int)target - p.span.col(p.from);       // the target's element once more, by the thread that has written its vector
+            if (!r.zero && t >= 0 && t / VEC < p.mine && t / VEC % threads == tid) {
                 const float s[1] = {target_score};
                 float g[1];
                 gradient(s, r, 0, g);
-                store_one(grad + first + (size_t)from * VEC + t, g[0]);
+                store_one(grad + first + (size_t)p.from * VEC + t, g[0]);
+            }
+            if (rest >= 0) {     // read again: where grad is z, these elements are this thread's own
+                RawVec<T, VEC> raw;
+                float s[VEC];
+                p.span.load(raw, z, rest);
+                scores(p.span, rest, raw, s);
+                write_gradient<T, VEC>(p.span, grad, first, rest, s, r, (int)target);
             }
         }
-        if (rest >= 0) {     // read again: where grad is z, these elements are this thread's own
-            RawVec<T, VEC> raw;
-            float s[VEC];
-            span.load(raw, z, rest);
-            scores(span, rest, raw, s);
-            write_gradient<T, VEC>(span, grad, first, rest, s, r, (int)target);
-        }
     }
-    if (rank == 0) finish_mean(a, targets, gridDim.x / cluster);
+    if (rank == 0) finish_mean(a, targets, rows_apart);
 }
 
 // ---- anything else (unaligned tensors, strides of the two matrices that do not go together, rows longer than a cluster holds) ----
@@ -550,7 +607,10 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
         const int each = (vectors + cluster - 1) / cluster, threads = each <= 512 ? 128 : each <= 2048 ? 256 : 512;
         auto kernel = loss_block_kernel<T, ID, VEC, GRAD>;
         if (GRAD && (err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLossMost)) != cudaSuccess) return;
-        err = launch_loss(dependent, cluster, kernel, (unsigned)(a.rows * (long)cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
+        int per_sm = 1;
+        if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, GRAD ? bytes() : 0)) != cudaSuccess) return;
+        const long wave = 148L * (per_sm < 1 ? 1 : per_sm) / cluster, walkers = wave < 1 ? 1 : a.rows < wave ? a.rows : wave;
+        err = launch_loss(dependent, cluster, kernel, (unsigned)(walkers * cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
     };
     auto with_alignment = [&](auto gradient) {
         if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) return;
