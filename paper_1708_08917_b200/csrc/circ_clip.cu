@@ -27,47 +27,132 @@ struct Clip {
     std::vector<long> sizes;
     std::vector<int> types;
     std::vector<ClipPiece> pieces;
+    int count;     // pieces in use
     bool set;
     Scratch plan, partial;
 };
 
-constexpr int kPieceElems = 16384;
+// A piece is a block's unit of work: 256 threads take 32 elements each, in 16-byte vectors of the gradients that are all in flight
+// together.  Pieces start on 16-byte boundaries of their tensor's gradient, but for its first one, which has up to 7 elements more in
+// front.
+constexpr int kPieceElems = 8192;
 
+// Elements in front of the first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ int head_of(const T* p) {
+    constexpr unsigned VEC = 16 / sizeof(T);
+    return (int)((VEC - (unsigned)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) % VEC) % VEC);
+}
+
+// The sum of squares of a thread's elements of a piece; consecutive threads take consecutive vectors.
+template <typename TG>
+__device__ __forceinline__ float piece_squares(const TG* g, int count) {
+    constexpr int VEC = 16 / (int)sizeof(TG), DEPTH = kPieceElems / kClipThreads / VEC;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    const int tid = threadIdx.x, front = head_of(g), head = front < count ? front : count;
+    if (tid < head) part[0] = to_float(g[tid]) * to_float(g[tid]);
+    g += head;
+    count -= head;
+    RawVec<TG, VEC> raw[DEPTH];
+    if (count == kPieceElems) {
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) raw[u].load(g + (u * kClipThreads + tid) * VEC);
+    } else {
+        const int whole = count / VEC, c = whole * VEC + tid;
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) {
+            if (u * kClipThreads + tid < whole) raw[u].load(g + (u * kClipThreads + tid) * VEC);
+            else raw[u].clear();
+        }
+        if (c < count) part[1] = to_float(g[c]) * to_float(g[c]);
+    }
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) part[e % 4] = fmaf(raw[u].get(e), raw[u].get(e), part[e % 4]);
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// Pieces are walked in order here and in reverse order by the second kernel, which so finds the last ones in the L2 cache.
 __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const ClipPiece* __restrict__ pieces, int count, double* __restrict__ partial) {
-    __shared__ float red[33];
+    __shared__ double sums[kClipThreads / 32];
+    pdl_trigger();
     double total = 0.0;
     for (int i = blockIdx.x; i < count; i += gridDim.x) {
         const ClipPiece p = pieces[i];
-        float sum = 0.f;
-        for (int c = threadIdx.x; c < p.count; c += kClipThreads) {
-            const float g = p.types & 1 ? to_float(static_cast<const __nv_bfloat16*>(p.grad)[c]) : static_cast<const float*>(p.grad)[c];
-            sum = fmaf(g, g, sum);
-        }
-        total += block_sum(sum, red);
+        total += p.types & 1 ? piece_squares(static_cast<const __nv_bfloat16*>(p.grad), p.count) : piece_squares(static_cast<const float*>(p.grad), p.count);
     }
-    if (threadIdx.x == 0) partial[blockIdx.x] = total;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kClipThreads / 32; ++w) total += sums[w];
+        partial[blockIdx.x] = total;
+    }
+}
+
+// Vectors where gradient and output are aligned together (the same number of elements in front of their boundaries), else by element.
+template <typename TG, typename TO>
+__device__ __forceinline__ void piece_scale(const TG* g, TO* out, int count, float factor) {
+    constexpr int VEC = sizeof(TG) == 2 && sizeof(TO) == 2 ? 8 : 4, DEPTH = kPieceElems / kClipThreads / VEC;
+    const int tid = threadIdx.x, front = head_of(g), head = front < count ? front : count;
+    if (((reinterpret_cast<uintptr_t>(g + front) | reinterpret_cast<uintptr_t>(out + front)) & 15u) == 0) {
+        if (tid < head) store_one(out + tid, to_float(g[tid]) * factor);
+        g += head;
+        out += head;
+        count -= head;
+        const int whole = count / VEC, c = whole * VEC + tid;
+        RawVec<TG, VEC> raw[DEPTH];
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u)
+            if (u * kClipThreads + tid < whole) raw[u].load(g + (u * kClipThreads + tid) * VEC);
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) {
+            if (u * kClipThreads + tid >= whole) break;
+            float x[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[e] = raw[u].get(e) * factor;
+            store_vec_once<VEC>(out + (u * kClipThreads + tid) * VEC, x);
+        }
+        if (c < count) store_one(out + c, to_float(g[c]) * factor);
+    } else {
+#pragma unroll 8
+        for (int c = tid; c < count; c += kClipThreads) store_one(out + c, to_float(g[c]) * factor);
+    }
 }
 
 __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiece* __restrict__ pieces, int count, const double* __restrict__ partial,
                                                                   int partials, float max_norm, float* norm_out) {
+    __shared__ double sums[kClipThreads / 32];
+    pdl_wait();
     double total = 0.0;
-    for (int i = 0; i < partials; ++i) total += partial[i];
+    for (int i = threadIdx.x; i < partials; i += kClipThreads) total += __ldcg(partial + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = total;
+    __syncthreads();
+    total = 0.0;
+#pragma unroll
+    for (int w = 0; w < kClipThreads / 32; ++w) total += sums[w];
     const float norm = (float)sqrt(total);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
     const float ratio = max_norm / (norm + kClipEps), factor = ratio > 1.f ? 1.f : ratio;   // a NaN stays
-    for (int i = blockIdx.x; i < count; i += gridDim.x) {
+    for (int i = count - 1 - (int)blockIdx.x; i >= 0; i -= (int)gridDim.x) {
         const ClipPiece p = pieces[i];
-        for (int c = threadIdx.x; c < p.count; c += kClipThreads) {
-            const float g = p.types & 1 ? to_float(static_cast<const __nv_bfloat16*>(p.grad)[c]) : static_cast<const float*>(p.grad)[c];
-            if (p.types & 2)
-                store_one(static_cast<__nv_bfloat16*>(p.out) + c, g * factor);
-            else
-                static_cast<float*>(p.out)[c] = g * factor;
-        }
+        if (factor == 1.f && p.grad == p.out) continue;       // nothing to clip, in place
+        const float* gf = static_cast<const float*>(p.grad);
+        const __nv_bfloat16* gb = static_cast<const __nv_bfloat16*>(p.grad);
+        float* of = static_cast<float*>(p.out);
+        __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(p.out);
+        if (p.types == 0) piece_scale(gf, of, p.count, factor);
+        else if (p.types == 1) piece_scale(gb, of, p.count, factor);
+        else if (p.types == 2) piece_scale(gf, ob, p.count, factor);
+        else piece_scale(gb, ob, p.count, factor);
     }
 }
 
-constexpr int kClipBlocks = 148 * 4;
+constexpr int kClipBlocks = 148 * 8;   // a wave of eight blocks an SM
 
 }  // namespace circ
 
@@ -100,7 +185,7 @@ circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_
     if (!current_device(&device)) return nullptr;
     Clip* c = nullptr;
     try {
-        c = new Clip{device, {}, {}, {}, false, {nullptr, 0}, {nullptr, 0}};
+        c = new Clip{device, {}, {}, {}, 0, false, {nullptr, 0}, {nullptr, 0}};
         c->sizes.assign(sizes, sizes + count);
         for (int i = 0; i < count; ++i) c->types.push_back((grad_dtypes[i] == CIRC_BF16 ? 1 : 0) | (out_dtypes[i] == CIRC_BF16 ? 2 : 0));
         c->pieces.resize(pieces);
@@ -153,16 +238,19 @@ int circ_clip_set_tensors(circ_clip_handle h, const void* const* grads, void* co
             return CIRC_ERR_ARG;
         }
     }
-    size_t n = 0;
+    size_t n = 0;      // at most the pieces that circ_clip_create made room for: a first piece is longer than the others, never shorter
     for (int i = 0; i < count; ++i) {
         const size_t gb = c->types[i] & 1 ? 2 : 4, ob = c->types[i] & 2 ? 2 : 4;
         const char* g = static_cast<const char*>(grads[i]);
         char* o = outs ? static_cast<char*>(outs[i]) : const_cast<char*>(g);
-        for (long at = 0; at < c->sizes[i]; at += kPieceElems, ++n) {
-            const long left = c->sizes[i] - at;
-            c->pieces[n] = ClipPiece{g + at * gb, o + at * ob, (int)(left < kPieceElems ? left : kPieceElems), c->types[i]};
+        long most = kPieceElems + (long)((16 - reinterpret_cast<uintptr_t>(g) % 16) % 16 / gb);
+        for (long at = 0; at < c->sizes[i]; ++n, most = kPieceElems) {
+            const long left = c->sizes[i] - at, len = left < most ? left : most;
+            c->pieces[n] = ClipPiece{g + at * gb, o + at * ob, (int)len, c->types[i]};
+            at += len;
         }
     }
+    c->count = (int)n;
     c->set = false;
     if (n) CIRC_CUDA_TRY(cudaMemcpyAsync(c->plan.ptr, c->pieces.data(), sizeof(ClipPiece) * n, cudaMemcpyHostToDevice, s), CIRC_ERR_CUDA);
     c->set = true;
@@ -180,13 +268,13 @@ int circ_clip_forward(circ_clip_handle h, float max_norm, float* norm, void* str
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int pieces = (int)c->pieces.size(), blocks = pieces < kClipBlocks ? (pieces ? pieces : 1) : kClipBlocks;
+    const int pieces = c->count, blocks = pieces < kClipBlocks ? (pieces ? pieces : 1) : kClipBlocks;
     const ClipPiece* plan = static_cast<const ClipPiece*>(c->plan.ptr);
     double* partial = static_cast<double*>(c->partial.ptr);
     clip_norm_kernel<<<blocks, kClipThreads, 0, s>>>(plan, pieces, partial);
-    clip_scale_kernel<<<blocks, kClipThreads, 0, s>>>(plan, pieces, partial, blocks, max_norm, norm);
-    count_launches(2);
     CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
+    CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, clip_scale_kernel, dim3(blocks), kClipThreads, 0, s, plan, pieces, partial, blocks, max_norm, norm), CIRC_ERR_CUDA);
+    count_launches(2);
     return CIRC_OK;
 }
 
