@@ -28,6 +28,7 @@ struct Clip {
     std::vector<int> types;
     std::vector<ClipPiece> pieces;
     int count;     // pieces in use
+    int same_types;     // ClipPiece::types of every tensor, or -1
     bool set;
     Scratch plan, partial;
 };
@@ -92,10 +93,12 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const ClipPiece
     }
 }
 
+constexpr int kScaleBlocks = 4;       // of the second kernel on an SM, 64 KB in flight
+
 // Vectors where gradient and output are aligned together (the same number of elements in front of their boundaries), else by element.
 template <typename TG, typename TO>
 __device__ __forceinline__ void piece_scale(const TG* g, TO* out, int count, float factor) {
-    constexpr int VEC = sizeof(TG) == 2 && sizeof(TO) == 2 ? 8 : 4, DEPTH = kPieceElems / kClipThreads / VEC;
+    constexpr int VEC = sizeof(TG) == 2 && sizeof(TO) == 2 ? 8 : 4, DEPTH = 4;     // four vectors in flight a thread
     const int tid = threadIdx.x, front = head_of(g), head = front < count ? front : count;
     if (((reinterpret_cast<uintptr_t>(g + front) | reinterpret_cast<uintptr_t>(out + front)) & 15u) == 0) {
         if (tid < head) store_one(out + tid, to_float(g[tid]) * factor);
@@ -103,26 +106,31 @@ __device__ __forceinline__ void piece_scale(const TG* g, TO* out, int count, flo
         out += head;
         count -= head;
         const int whole = count / VEC, c = whole * VEC + tid;
-        RawVec<TG, VEC> raw[DEPTH];
+#pragma unroll 1
+        for (int v = tid; v < whole; v += DEPTH * kClipThreads) {
+            RawVec<TG, VEC> raw[DEPTH];
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u)
-            if (u * kClipThreads + tid < whole) raw[u].load(g + (u * kClipThreads + tid) * VEC);
+            for (int u = 0; u < DEPTH; ++u)
+                if (v + u * kClipThreads < whole) raw[u].load(g + (v + u * kClipThreads) * VEC);
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) {
-            if (u * kClipThreads + tid >= whole) break;
-            float x[VEC];
+            for (int u = 0; u < DEPTH; ++u) {
+                if (v + u * kClipThreads >= whole) break;
+                float x[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) x[e] = raw[u].get(e) * factor;
-            store_vec_once<VEC>(out + (u * kClipThreads + tid) * VEC, x);
+                for (int e = 0; e < VEC; ++e) x[e] = raw[u].get(e) * factor;
+                store_vec_once<VEC>(out + (v + u * kClipThreads) * VEC, x);
+            }
         }
         if (c < count) store_one(out + c, to_float(g[c]) * factor);
     } else {
-#pragma unroll 8
+#pragma unroll 4
         for (int c = tid; c < count; c += kClipThreads) store_one(out + c, to_float(g[c]) * factor);
     }
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiece* __restrict__ pieces, int count, const double* __restrict__ partial,
+// TYPES: those of all pieces (ClipPiece::types), or -1 where they differ.
+template <int TYPES>
+__global__ void __launch_bounds__(kClipThreads, kScaleBlocks) clip_scale_kernel(const ClipPiece* __restrict__ pieces, int count, const double* __restrict__ partial,
                                                                   int partials, float max_norm, float* norm_out) {
     __shared__ double sums[kClipThreads / 32];
     pdl_wait();
@@ -145,9 +153,10 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipPiec
         const __nv_bfloat16* gb = static_cast<const __nv_bfloat16*>(p.grad);
         float* of = static_cast<float*>(p.out);
         __nv_bfloat16* ob = static_cast<__nv_bfloat16*>(p.out);
-        if (p.types == 0) piece_scale(gf, of, p.count, factor);
-        else if (p.types == 1) piece_scale(gb, of, p.count, factor);
-        else if (p.types == 2) piece_scale(gf, ob, p.count, factor);
+        const int types = TYPES < 0 ? p.types : TYPES;
+        if (types == 0) piece_scale(gf, of, p.count, factor);
+        else if (types == 1) piece_scale(gb, of, p.count, factor);
+        else if (types == 2) piece_scale(gf, ob, p.count, factor);
         else piece_scale(gb, ob, p.count, factor);
     }
 }
@@ -185,10 +194,13 @@ circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_
     if (!current_device(&device)) return nullptr;
     Clip* c = nullptr;
     try {
-        c = new Clip{device, {}, {}, {}, 0, false, {nullptr, 0}, {nullptr, 0}};
+        c = new Clip{device, {}, {}, {}, 0, -1, false, {nullptr, 0}, {nullptr, 0}};
         c->sizes.assign(sizes, sizes + count);
         for (int i = 0; i < count; ++i) c->types.push_back((grad_dtypes[i] == CIRC_BF16 ? 1 : 0) | (out_dtypes[i] == CIRC_BF16 ? 2 : 0));
         c->pieces.resize(pieces);
+        c->same_types = c->types[0];
+        for (int t : c->types)
+            if (t != c->types[0]) c->same_types = -1;
     } catch (const std::bad_alloc&) {
         delete c;
         set_error(CIRC_ERR_ALLOC, "host allocation failed");
@@ -273,7 +285,10 @@ int circ_clip_forward(circ_clip_handle h, float max_norm, float* norm, void* str
     double* partial = static_cast<double*>(c->partial.ptr);
     clip_norm_kernel<<<blocks, kClipThreads, 0, s>>>(plan, pieces, partial);
     CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
-    CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, clip_scale_kernel, dim3(blocks), kClipThreads, 0, s, plan, pieces, partial, blocks, max_norm, norm), CIRC_ERR_CUDA);
+    auto* kernel = c->same_types < 0 ? clip_scale_kernel<-1> : c->same_types == 0 ? clip_scale_kernel<0> : c->same_types == 1 ? clip_scale_kernel<1>
+                   : c->same_types == 2 ? clip_scale_kernel<2> : clip_scale_kernel<3>;
+    const int scale_blocks = pieces < 148 * kScaleBlocks ? blocks : 148 * kScaleBlocks;
+    CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, kernel, dim3(scale_blocks), kClipThreads, 0, s, plan, pieces, partial, blocks, max_norm, norm), CIRC_ERR_CUDA);
     count_launches(2);
     return CIRC_OK;
 }
