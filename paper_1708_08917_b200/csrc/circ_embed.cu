@@ -362,6 +362,135 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSum a, TT* __restr
     }
 }
 
+// ---- few tokens: one launch ----
+// A thread block owns the table rows equal to its number modulo the blocks, for a slice of 2 x 32 vectors of columns, and picks its
+// tokens out of all ids in their order.  Its warps write a row each: most are zero.  A row with many tokens is left to all warps
+// together, each with an eighth of the block's tokens, added up in order.  Reading all ids in every block is what limits it to kFewTokens.
+constexpr int kFewTokens = 2048, kFewRows = 2048, kFewLong = 16;
+
+template <typename TT, typename TY, typename ID, int VEC>
+__global__ void __launch_bounds__(256, 4) embed_few_kernel(const ID* __restrict__ ids, const TY* __restrict__ dy, TT* __restrict__ dt, int tokens, int vocab,
+                                                           unsigned padding, int dim, float scale) {
+    constexpr int PARTS = 2, PER = kFewTokens / 256, WIDTH = PARTS * 32 * VEC;
+    __shared__ int tok[kFewTokens], row[kFewTokens], count[kFewRows], found[PER * 8], longs[kFewTokens / kFewLong], many;
+    __shared__ __align__(16) float sums[8][WIDTH];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const unsigned blocks = gridDim.x, b = blockIdx.x;
+    const int rows = (int)((vocab - b + blocks - 1) / blocks);
+    unsigned own[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int t = i * 256 + tid;
+        const ID id = t < tokens ? __ldg(ids + t) : (ID)-1;
+        const unsigned lo = (unsigned)id;
+        bool mine = lo < (unsigned)vocab && lo != padding;
+        if constexpr (sizeof(ID) == 8) mine = mine && (unsigned)((uint64_t)id >> 32) == 0;
+        own[i] = mine && lo % blocks == b ? lo / blocks : kNotOurs;
+    }
+    for (int i = tid; i < rows; i += 256) count[i] = 0;
+    if (tid == 0) many = 0;
+    unsigned hits[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        hits[i] = __ballot_sync(0xffffffffu, own[i] != kNotOurs);
+        if (lane == 0) found[i * 8 + warp] = __popc(hits[i]);
+    }
+    __syncthreads();
+    // places in the order of the tokens: exclusive sums over (i, warp), two a lane
+    const int f0 = found[2 * lane], f1 = found[2 * lane + 1];
+    int scan = f0 + f1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+    }
+    const int n = __shfl_sync(0xffffffffu, scan, 31), before = scan - f0 - f1;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = i * 8 + warp, at0 = __shfl_sync(0xffffffffu, before, k / 2), at1 = __shfl_sync(0xffffffffu, before + f0, k / 2);
+        if (own[i] != kNotOurs) {
+            const int at = (k % 2 ? at1 : at0) + __popc(hits[i] & ((1u << lane) - 1));
+            tok[at] = i * 256 + tid;
+            row[at] = (int)own[i];
+            atomicAdd(&count[own[i]], 1);
+        }
+    }
+    __syncthreads();
+    const int col = blockIdx.y * WIDTH + lane * VEC;
+    float sum[PARTS][VEC];
+    auto clear = [&]() {
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[c][e] = 0.f;
+    };
+    // adds the block's tokens from..to that belong to row r, up to four in flight
+    auto add_tokens = [&](int from, int to, int r) {
+        for (int base = from; base < to; base += 32) {
+            const bool in = base + lane < to && row[base + lane] == r;
+            const int mine = in ? tok[base + lane] : 0;
+            unsigned m = __ballot_sync(0xffffffffu, in);
+            while (m) {
+                RawVec<TY, VEC> raw[4][PARTS];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int k = m ? __ffs(m) - 1 : 0;
+                    const TY* src = dy + (size_t)__shfl_sync(0xffffffffu, mine, k) * dim + col;
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) {
+                        if (m && col + c * 32 * VEC < dim) raw[u][c].load(src + c * 32 * VEC);
+                        else raw[u][c].clear();
+                    }
+                    m &= m - 1;
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) sum[c][e] += raw[u][c].get(e);
+            }
+        }
+    };
+    for (int r = warp; r < rows; r += 8) {
+        const int c0 = count[r];
+        if (c0 > kFewLong) {
+            if (lane == 0) longs[atomicAdd(&many, 1)] = r;
+            continue;
+        }
+        clear();
+        if (c0) add_tokens(0, n, r);
+        TT* dst = dt + ((size_t)r * blocks + b) * dim + col;
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+            if (col + c * 32 * VEC < dim) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[c][e] *= scale;
+                store_vec_once<VEC>(dst + c * 32 * VEC, sum[c]);
+            }
+    }
+    __syncthreads();
+    const int long_rows = many;
+    for (int k = 0; k < long_rows; ++k) {
+        const int r = longs[k], per = (n + 7) / 8, from = warp * per;
+        clear();
+        add_tokens(from, from + per < n ? from + per : n, r);
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sums[warp][(c * 32 + lane) * VEC + e] = sum[c][e];
+        __syncthreads();
+        for (int i = tid; i < WIDTH; i += 256) {
+            float t = sums[0][i];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) t += sums[w][i];
+            const int c = blockIdx.y * WIDTH + i;
+            if (c < dim) store_one(dt + ((size_t)r * blocks + b) * dim + c, scale * t);
+        }
+        __syncthreads();
+    }
+}
+
 // Launch shape of a backward call and its pieces of the workspace.
 struct EmbedPlan {
     int bits, rows_per_block, blocks, vec, parts, group, slices, workers;
@@ -533,6 +662,32 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool aligned = !misaligned(grad_y, 16) && !misaligned(grad_table, 16) && e->dim % 8 == 0;
+    const int few_vec = !aligned ? 1 : e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
+    const int few_slices = (e->dim + 64 * few_vec - 1) / (64 * few_vec);
+    long few_blocks = (148L * 8 + few_slices - 1) / few_slices;                  // two rounds of blocks on the machine
+    if (few_blocks > e->vocab) few_blocks = e->vocab;
+    if (tokens <= kFewTokens && few_slices <= 65535 && (e->vocab + few_blocks - 1) / few_blocks <= kFewRows) {
+        with_dtype(e->table_dtype, [&](auto* t) {
+            with_dtype(e->y_dtype, [&](auto* o) {
+                with_index_type(e->ids_type, [&](auto* i) {
+                    using TT = tag_type<decltype(t)>;
+                    using TY = tag_type<decltype(o)>;
+                    using ID = tag_type<decltype(i)>;
+                    constexpr int WIDE = std::is_same<TY, __nv_bfloat16>::value && std::is_same<TT, __nv_bfloat16>::value ? 8 : 4;
+                    auto go = [&](auto kernel) {
+                        kernel<<<dim3((unsigned)few_blocks, few_slices), 256, 0, s>>>(static_cast<const ID*>(ids), static_cast<const TY*>(grad_y),
+                                                                                      static_cast<TT*>(grad_table), (int)tokens, e->vocab,
+                                                                                      (unsigned)e->padding, e->dim, e->scale);
+                    };
+                    few_vec == 1 ? go(embed_few_kernel<TT, TY, ID, 1>) : go(embed_few_kernel<TT, TY, ID, WIDE>);
+                });
+            });
+        });
+        CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
+        count_launches(1);
+        return CIRC_OK;
+    }
     if ((rc = ensure_scratch(e->ws, embed_bytes(e, tokens), s, "circ_embed_reserve")) != CIRC_OK) return rc;
     const EmbedPlan pl = plan_embed(e, tokens, !misaligned(grad_y, 16) && !misaligned(grad_table, 16));
     char* ws = static_cast<char*>(e->ws.ptr);

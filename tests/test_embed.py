@@ -42,10 +42,9 @@ def plain_gradient(ids, dy, vocab, scale, padding):
     keep = keep_mask(ids, vocab, padding)
     grad = torch.zeros(vocab, dy.shape[1], dtype=torch.float64)
     mag = torch.zeros_like(grad)
-    for t in range(len(ids)):
-        if keep[t]:
-            grad[ids[t]] += dy[t].double()
-            mag[ids[t]] += dy[t].double().abs()
+    for t in keep.nonzero().squeeze(1).tolist():
+        grad[ids[t]] += dy[t].double()
+        mag[ids[t]] += dy[t].double().abs()
     return scale * grad, abs(scale) * mag, torch.bincount(ids[keep], minlength=vocab).double()
 
 
@@ -81,6 +80,14 @@ def test_lookup(tokens, vocab, dim, table, y, ids_type, offset):
     (1000, 40, 1024, F32, BF16, torch.int64, 0),
     (257, 12, 2056, BF16, BF16, torch.int32, 0),
     (2500, 3, 16, F32, BF16, torch.int32, 0),
+    (2048, 5000, 72, F32, F32, torch.int64, 0),      # the most tokens of the one-launch kernel, and one more
+    (2049, 5000, 72, F32, F32, torch.int64, 0),
+    (2049, 300000, 8, BF16, F32, torch.int32, 0),    # more rows than 128 classes of the sort hold
+    (3000, 1009, 100, BF16, BF16, torch.int32, 0),
+    (5000, 300, 33, F32, BF16, torch.int64, 1),      # odd width, nothing aligned
+    (4000, 40, 1024, F32, F32, torch.int32, 0),
+    (6000, 12, 2056, F32, BF16, torch.int64, 0),
+    (20000, 500, 136, BF16, F32, torch.int64, 0),
 ])
 def test_gradient(kind, tokens, vocab, dim, table, y, ids_type, offset):
     g = rng(tokens + vocab)
@@ -147,8 +154,9 @@ def test_no_tokens_and_other_streams():
 
 
 @pytest.mark.gpu
-def test_backward_in_a_captured_graph_needs_its_workspace():
-    vocab, dim, tokens = 64, 32, 200
+@pytest.mark.parametrize("tokens", [200, 3000])
+def test_backward_in_a_captured_graph_needs_its_workspace(tokens):
+    vocab, dim = 64, 32
     h = handle(vocab, dim, F32, F32, torch.int64, 1.0)
     circ.circ_embed_reserve(h, tokens)
     ids, dy = torch.randint(vocab, (tokens,), device="cuda"), torch.randn(tokens, dim, device="cuda")
