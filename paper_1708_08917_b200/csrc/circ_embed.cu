@@ -58,9 +58,10 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict
 // counts per (warp, row) it knows the place of each of its tokens in the whole order without hearing from another block, since the
 // tokens in front of its class are those of lower classes.  (Classes and not ranges: ids are commonly handed out by frequency, and
 // a block with the first 1/128 of the ids had half of the tokens.)  Warps take consecutive parts of the tokens, so that equal ids
-// stay in the order of their positions.  The rows' order behind is (class, id); `slot` numbers the rows in that order.
+// stay in the order of their positions.  Reading the ids is what takes the time (every block reads all of them from L2), so it is done once:
+// a warp lists its tokens as it finds them.  The rows' order behind is (class, id); `slot` numbers the rows in that order.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortUnroll = 16;
-constexpr int kSortRows = 1536;      // table rows of a block: 32 warps x 1536 counts are 192 KB of shared memory
+constexpr int kSortRows = 1280, kSortListed = 160;   // table rows of a block and listed tokens of a warp: 160 + 40 KB of shared memory
 
 // The row's number within class `cls` of 2^bits classes; kNotOurs for an id of another class or for no token.  `less`: a lower class.
 // Negative ids are above every row as unsigned numbers.
@@ -77,16 +78,18 @@ __device__ __forceinline__ unsigned class_row(ID id, unsigned cls, int bits, uns
 template <typename ID>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, int vocab, unsigned padding, int bits, int rows_per_block,
                                                                   int* __restrict__ start, int* __restrict__ order, int* __restrict__ cuts) {
-    extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places
+    extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places; then the warps' lists
     __shared__ int part[kSortWarps], below[kSortWarps];
     pdl_trigger();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int per_warp = ((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
     const int begin = warp * per_warp < tokens ? warp * per_warp : tokens, end = begin + per_warp < tokens ? begin + per_warp : tokens;
     int* mine = count + warp * rows_per_block;
-    // rows of the first 16 x 32 tokens of the warp stay in registers for the second pass
-    unsigned kept[kSortUnroll];
-    auto fetch = [&](int t0, unsigned (&row)[kSortUnroll], int& less) {
+    // the warp's tokens of this class, in order: (row, token); more than the list holds are found again from the ids
+    int2* list = reinterpret_cast<int2*>(count + kSortWarps * rows_per_block) + warp * kSortListed;
+    int less = 0, listed = 0;
+    // the rows of the next 16 x 32 tokens, 0xffffffff where they are not ours
+    auto fetch = [&](int t0, unsigned (&row)[kSortUnroll]) {
         ID id[kSortUnroll];
 #pragma unroll
         for (int u = 0; u < kSortUnroll; ++u) id[u] = t0 + u * 32 + lane < end ? __ldg(ids + t0 + u * 32 + lane) : (ID)-1;
@@ -97,21 +100,24 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
             less += l;
         }
     };
-    int less = 0;
-    fetch(begin, kept, less);
     for (int i = threadIdx.x; i < kSortWarps / 4 * rows_per_block; i += kSortThreads) reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *cuts = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) cuts[threadIdx.x] = 0;
     __syncthreads();
-    auto tally = [&](const unsigned (&row)[kSortUnroll]) {
-#pragma unroll
-        for (int u = 0; u < kSortUnroll; ++u)
-            if (row[u] != kNotOurs) atomicAdd(mine + row[u], 1);
-    };
-    tally(kept);
-    for (int t0 = begin + 32 * kSortUnroll; t0 < end; t0 += 32 * kSortUnroll) {
+    for (int t0 = begin; t0 < end; t0 += 32 * kSortUnroll) {
         unsigned row[kSortUnroll];
-        fetch(t0, row, less);
-        tally(row);
+        fetch(t0, row);
+#pragma unroll
+        for (int u = 0; u < kSortUnroll; ++u) {
+            const bool ours = row[u] != kNotOurs;
+            const unsigned some = __ballot_sync(0xffffffffu, ours);
+            if (!some) continue;
+            const int at = listed + __popc(some & ((1u << lane) - 1));
+            if (ours) {
+                atomicAdd(mine + row[u], 1);
+                if (at < kSortListed) list[at] = make_int2((int)row[u], t0 + u * 32 + lane);
+            }
+            listed += __popc(some);
+        }
     }
     less = __reduce_add_sync(0xffffffffu, less);
     if (lane == 0) below[warp] = less;
@@ -149,27 +155,31 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
         if (blockIdx.x == gridDim.x - 1 && r == rows_per_block - 1) start[(size_t)gridDim.x * rows_per_block] = place;
     }
     __syncthreads();
-    auto deal = [&](int t0, const unsigned (&row)[kSortUnroll]) {
-#pragma unroll
-        for (int u = 0; u < kSortUnroll; ++u) {
-            const bool ours = row[u] != kNotOurs;
-            const unsigned some = __ballot_sync(0xffffffffu, ours);
-            if (!some) continue;
-            if (ours) {
-                const unsigned same = __match_any_sync(some, row[u]);
-                const int rank = __popc(same & ((1u << lane) - 1)), base = mine[row[u]];
-                __syncwarp(some);
-                if (rank == 0) mine[row[u]] = base + __popc(same);
-                order[base + rank] = t0 + u * 32 + lane;
-            }
-            __syncwarp();
+    // 32 tokens in their order to their rows' places; called by whole warps
+    auto deal = [&](unsigned row, int token) {
+        const bool ours = row != kNotOurs;
+        const unsigned some = __ballot_sync(0xffffffffu, ours);
+        if (ours) {
+            const unsigned same = __match_any_sync(some, row);
+            const int rank = __popc(same & ((1u << lane) - 1)), base = mine[row];
+            __syncwarp(some);
+            if (rank == 0) mine[row] = base + __popc(same);
+            order[base + rank] = token;
         }
+        __syncwarp();
     };
-    deal(begin, kept);
-    for (int t0 = begin + 32 * kSortUnroll; t0 < end; t0 += 32 * kSortUnroll) {
-        unsigned row[kSortUnroll];
-        fetch(t0, row, less);
-        deal(t0, row);
+    if (listed <= kSortListed) {
+        for (int i = 0; i < listed; i += 32) {
+            const int2 e = i + lane < listed ? list[i + lane] : make_int2(-1, 0);
+            deal((unsigned)e.x, e.y);
+        }
+    } else {
+        for (int t0 = begin; t0 < end; t0 += 32 * kSortUnroll) {
+            unsigned row[kSortUnroll];
+            fetch(t0, row);
+#pragma unroll
+            for (int u = 0; u < kSortUnroll; ++u) deal(row[u], t0 + u * 32 + lane);
+        }
     }
 }
 
@@ -177,15 +187,15 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
 // traffic per column; `workers` groups of GROUP threads take equal stretches of it, whatever the ids are.  A stretch that ends in
 // a run of more than kWholeRun tokens cuts it (the part before goes to `carry`, the part in which the row ends to `tail`); shorter
 // runs go whole to the worker they end with.
-constexpr int kWholeRun = 64;
+constexpr int kWholeRun = 64, kLongChain = 6;
 
 struct EmbedSum {
     const int* start;      // [slots + 1]
     const int* order;      // [tokens]
     float* carry;          // [workers][dim]
     float* tail;           // [workers][dim]
-    int* cuts;             // rows that are put together from parts
-    int4* cut;             // [cuts] (row, first worker that holds a part of it, the one in which it ends, 0), in any order
+    int* cuts;             // [2] rows that are put together from parts: from few, from more than kLongChain
+    int4* cut;             // [2][workers] (row, first worker that holds a part of it, the one in which it ends, 0), in any order
     int vocab, dim, workers;
     int bits, per_class, slots;     // slot = (id mod 2^bits) * per_class + id / 2^bits; those of ids >= vocab are empty
     int read_cost, row_cost;
@@ -292,7 +302,8 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
                 int q = (int)(at / (double)total * a.workers);                 // the stretch that holds the row's first read, up to rounding
                 while (q > 0 && (long)((double)total * q / a.workers) > (long)at) --q;
                 while ((long)((double)total * (q + 1) / a.workers) <= (long)at) ++q;
-                a.cut[atomicAdd(a.cuts, 1)] = make_int4(id, q, p, 0);
+                const int many = p - q > kLongChain;
+                a.cut[(size_t)many * a.workers + atomicAdd(a.cuts + many, 1)] = make_int4(id, q, p, 0);
             }
         } else if (id < a.vocab) {
             TT* row = dt + (size_t)id * a.dim + col;
@@ -315,17 +326,15 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
 // (3) Rows that were cut: carry of the stretches before, in their order, and the tail.  A warp takes 128 columns of a row; where
 // the row has many parts, a block takes 32 columns and its 8 warps share the parts, so that a row with most of the tokens is no
 // chain of loads.
-constexpr int kLongChain = 6;
 
 template <typename TT>
 __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSum a, TT* __restrict__ dt) {
     pdl_wait();
     __shared__ float parts[8][33];
-    const int cuts = *a.cuts, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int few = a.cuts[0], many = a.cuts[1], warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int slices = (a.dim + 127) / 128, thin = (a.dim + 31) / 32;
-    for (int item = blockIdx.x * 8 + warp; item < cuts * slices; item += gridDim.x * 8) {
+    for (int item = blockIdx.x * 8 + warp; item < few * slices; item += gridDim.x * 8) {
         const int4 cut = a.cut[item / slices];
-        if (cut.z - cut.y > kLongChain) continue;
         const int col = item % slices * 128 + lane;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -339,26 +348,22 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSum a, TT* __restr
         for (int e = 0; e < 4; ++e)
             if (col + 32 * e < a.dim) store_one(dt + (size_t)cut.x * a.dim + col + 32 * e, a.scale * sum[e]);
     }
-    for (int k = 0; k < cuts; ++k) {
-        const int4 cut = a.cut[k];
-        const int n = cut.z - cut.y;
-        if (n <= kLongChain) continue;
-        const int per = (n + 7) / 8;
-        for (int s = blockIdx.x; s < thin; s += gridDim.x) {
-            const int col = s * 32 + lane, from = cut.y + warp * per, to = from + per < cut.z ? from + per : cut.z;
-            float sum = 0.f;
-            if (col < a.dim)
+    for (int item = blockIdx.x; item < many * thin; item += gridDim.x) {
+        const int4 cut = a.cut[a.workers + item / thin];
+        const int col = item % thin * 32 + lane, per = (cut.z - cut.y + 7) / 8;
+        const int from = cut.y + warp * per, to = from + per < cut.z ? from + per : cut.z;
+        float sum = 0.f;
+        if (col < a.dim)
 #pragma unroll 8
-                for (int q = from; q < to; ++q) sum += a.carry[(size_t)q * a.dim + col];
-            parts[warp][lane] = sum;
-            __syncthreads();
-            if (warp == 0 && col < a.dim) {
+            for (int q = from; q < to; ++q) sum += a.carry[(size_t)q * a.dim + col];
+        parts[warp][lane] = sum;
+        __syncthreads();
+        if (warp == 0 && col < a.dim) {
 #pragma unroll
-                for (int w = 1; w < 8; ++w) sum += parts[w][lane];
-                store_one(dt + (size_t)cut.x * a.dim + col, a.scale * (sum + a.tail[(size_t)cut.z * a.dim + col]));
-            }
-            __syncthreads();
+            for (int w = 1; w < 8; ++w) sum += parts[w][lane];
+            store_one(dt + (size_t)cut.x * a.dim + col, a.scale * (sum + a.tail[(size_t)cut.z * a.dim + col]));
         }
+        __syncthreads();
     }
 }
 
@@ -511,9 +516,9 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.group = threads <= 32 ? 32 : threads <= 64 ? 64 : threads <= 128 ? 128 : 256;
     pl.slices = (threads + pl.group - 1) / pl.group;
     // stretches of equal traffic, two for each place on the machine: reads take longer than writes of the same size, and the second
-    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); a few rows each at least
+    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); some rows each at least
     long workers = 2 * 148L * kSumBlocks * 256 / pl.group / pl.slices;
-    const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 3) / 4;
+    const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 15) / 16;
     if (workers > most) workers = most;
     pl.workers = (int)(workers < 1 ? 1 : workers);
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
@@ -521,7 +526,7 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.carry_at = pl.order_at + up(sizeof(int) * (size_t)(tokens ? tokens : 1));
     pl.tail_at = pl.carry_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
     pl.cut_at = pl.tail_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
-    pl.bytes = pl.cut_at + 256 + up(sizeof(int4) * (size_t)pl.workers);
+    pl.bytes = pl.cut_at + 256 + up(2 * sizeof(int4) * (size_t)pl.workers);
     return pl;
 }
 // What a call of this many tokens needs, whatever the alignment of its pointers.
@@ -697,11 +702,11 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                      reinterpret_cast<int*>(ws + pl.cut_at), reinterpret_cast<int4*>(ws + pl.cut_at + 256), e->vocab, e->dim, pl.workers, pl.bits, pl.rows_per_block,
                      pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype),
                      (int)dtype_bytes(e->table_dtype), e->scale};
-    const size_t smem = sizeof(int) * kSortWarps * (size_t)pl.rows_per_block;
+    const size_t smem = kSortWarps * (sizeof(int) * (size_t)pl.rows_per_block + sizeof(int2) * kSortListed);
     cudaError_t err = cudaSuccess;
     with_index_type(e->ids_type, [&](auto* i) {
         using ID = tag_type<decltype(i)>;
-        err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(int) * kSortWarps * kSortRows));
+        err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSortWarps * (sizeof(int) * kSortRows + sizeof(int2) * kSortListed)));
         if (err != cudaSuccess) return;
         embed_sort_kernel<ID><<<pl.blocks, kSortThreads, smem, s>>>(static_cast<const ID*>(ids), (int)tokens, e->vocab, (unsigned)e->padding,
                                                                     pl.bits, pl.rows_per_block, start, order, a.cuts);
