@@ -35,7 +35,7 @@ struct LossArgs {
 struct Softmax {
     float top, sum;
 };
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float exp2_of(float d) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
