@@ -529,8 +529,23 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.bytes = pl.cut_at + 256 + up(2 * sizeof(int4) * (size_t)pl.workers);
     return pl;
 }
-// What a call of this many tokens needs, whatever the alignment of its pointers.
+// The one-launch kernel's shape, where it serves a call.
+struct FewPlan {
+    bool fits;
+    int vec, slices, blocks;
+};
+static FewPlan plan_few(const Embed* e, long tokens, bool aligned) {
+    FewPlan f;
+    f.vec = !aligned || e->dim % 8 ? 1 : e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
+    f.slices = (e->dim + 64 * f.vec - 1) / (64 * f.vec);
+    f.blocks = (148 * 8 + f.slices - 1) / f.slices;        // two rounds of blocks on the machine
+    if (f.blocks > e->vocab) f.blocks = e->vocab;
+    f.fits = tokens <= kFewTokens && f.slices <= 65535 && (e->vocab + f.blocks - 1) / f.blocks <= kFewRows;
+    return f;
+}
+// What a call of up to this many tokens needs, whatever the alignment of its pointers.
 static size_t embed_bytes(const Embed* e, long tokens) {
+    if (plan_few(e, tokens, true).fits && plan_few(e, tokens, false).fits) return 0;
     const size_t a = plan_embed(e, tokens, true).bytes, b = plan_embed(e, tokens, false).bytes;
     return a > b ? a : b;
 }
@@ -667,12 +682,11 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool aligned = !misaligned(grad_y, 16) && !misaligned(grad_table, 16) && e->dim % 8 == 0;
-    const int few_vec = !aligned ? 1 : e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
-    const int few_slices = (e->dim + 64 * few_vec - 1) / (64 * few_vec);
-    long few_blocks = (148L * 8 + few_slices - 1) / few_slices;                  // two rounds of blocks on the machine
-    if (few_blocks > e->vocab) few_blocks = e->vocab;
-    if (tokens <= kFewTokens && few_slices <= 65535 && (e->vocab + few_blocks - 1) / few_blocks <= kFewRows) {
+    const bool aligned = !misaligned(grad_y, 16) && !misaligned(grad_table, 16);
+    // Up to 2048 tokens in one launch, in microseconds against the three launches: 92 / 103 (65536 rows of 2048), 10 / 25 (1000 of 512),
+    // 28 / 37 (131072 of 256); only with every token in one row the three are ahead (30 / 20 at 1000 of 512).
+    const FewPlan few = plan_few(e, tokens, aligned);
+    if (few.fits) {
         with_dtype(e->table_dtype, [&](auto* t) {
             with_dtype(e->y_dtype, [&](auto* o) {
                 with_index_type(e->ids_type, [&](auto* i) {
@@ -681,11 +695,11 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                     using ID = tag_type<decltype(i)>;
                     constexpr int WIDE = std::is_same<TY, __nv_bfloat16>::value && std::is_same<TT, __nv_bfloat16>::value ? 8 : 4;
                     auto go = [&](auto kernel) {
-                        kernel<<<dim3((unsigned)few_blocks, few_slices), 256, 0, s>>>(static_cast<const ID*>(ids), static_cast<const TY*>(grad_y),
+                        kernel<<<dim3((unsigned)few.blocks, few.slices), 256, 0, s>>>(static_cast<const ID*>(ids), static_cast<const TY*>(grad_y),
                                                                                       static_cast<TT*>(grad_table), (int)tokens, e->vocab,
                                                                                       (unsigned)e->padding, e->dim, e->scale);
                     };
-                    few_vec == 1 ? go(embed_few_kernel<TT, TY, ID, 1>) : go(embed_few_kernel<TT, TY, ID, WIDE>);
+                    few.vec == 1 ? go(embed_few_kernel<TT, TY, ID, 1>) : go(embed_few_kernel<TT, TY, ID, WIDE>);
                 });
             });
         });
@@ -694,7 +708,7 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
         return CIRC_OK;
     }
     if ((rc = ensure_scratch(e->ws, embed_bytes(e, tokens), s, "circ_embed_reserve")) != CIRC_OK) return rc;
-    const EmbedPlan pl = plan_embed(e, tokens, !misaligned(grad_y, 16) && !misaligned(grad_table, 16));
+    const EmbedPlan pl = plan_embed(e, tokens, aligned);
     char* ws = static_cast<char*>(e->ws.ptr);
     int* start = reinterpret_cast<int*>(ws);
     int* order = reinterpret_cast<int*>(ws + pl.order_at);
