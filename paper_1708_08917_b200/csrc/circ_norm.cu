@@ -234,22 +234,20 @@ template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED, bool RING>
 __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
     static_assert(ALIGNED || !RING, "copies of whole vectors");
     constexpr int XB = VEC * (int)sizeof(TX), YB = VEC * (int)sizeof(TY), BYTES = 2 * XB + YB;
-    // two rows a step in the ring's form: their reductions share the barrier and hide each other's latency
-    constexpr int ROWS = RING ? 2 : 1;
-    __shared__ __align__(16) float red[2][ROWS][16];
+    __shared__ __align__(16) float red[2][16];
     pdl_trigger();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
-    for (int i = tid; i < 2 * ROWS * 16; i += threads) (&red[0][0][0])[i] = 0.f;
+    for (int i = tid; i < 2 * 16; i += threads) (&red[0][0])[i] = 0.f;
     __syncthreads();
     // dynamic shared memory: the ring; or the share of grad_gain, where rows do not start at the same column of a vector
     extern __shared__ __align__(16) unsigned char smem[];
     float* share = reinterpret_cast<float*>(smem);
     auto place = [&](int slot, int i, int off) { return smem + (size_t)(slot * ITEMS + i) * BYTES * threads + (size_t)off * threads; };
-    float acc[ITEMS][VEC];
+    Pair acc[ITEMS][VEC / 2];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[i][e] = 0.f;
+        for (int e = 0; e < VEC / 2; ++e) acc[i][e] = pair_of(0.f, 0.f);
     if (!ALIGNED && a.part) {
         for (int c = tid; c < a.dim; c += threads) share[c] = 0.f;
         __syncthreads();
@@ -288,88 +286,83 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
         }
     };
     int flip = 0;
-    for (long row0 = blockIdx.x; row0 < a.rows; row0 += ROWS * (long)gridDim.x, flip ^= 1) {
-        RawVec<TX, VEC> sr[ROWS][ITEMS], cr[ROWS][ITEMS];
-        RawVec<TY, VEC> yr[ROWS][ITEMS];
-        float rstd[ROWS], dot[ROWS];
-        if constexpr (RING) asm volatile("cp.async.wait_group %0;" ::"n"(kRowsAhead - ROWS) : "memory");
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const long row = row0 + r * (long)gridDim.x;
-            const bool live = row < a.rows;
-            const RowSpan<VEC, ALIGNED> span(live ? row : 0, live ? a.dim : 0);     // a row behind the last has no vectors
-            rstd[r] = live ? __ldg(a.rstd + row) : 0.f;
-            if constexpr (RING) {
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    sr[r][i].clear();
-                    yr[r][i].clear();
-                    cr[r][i].clear();
-                    if (!span.any(tid + i * threads)) continue;
-                    sr[r][i].load(reinterpret_cast<const TX*>(place(slot, i, 0)) + tid * VEC);
-                    yr[r][i].load(reinterpret_cast<const TY*>(place(slot, i, XB)) + tid * VEC);
-                    if (ds && dx) cr[r][i].load(reinterpret_cast<const TX*>(place(slot, i, XB + YB)) + tid * VEC);
-                }
-                slot = slot + 1 == kRowsAhead ? 0 : slot + 1;
-            } else {
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) span.load(sr[r][i], sum, tid + i * threads);
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) span.load(yr[r][i], dy, tid + i * threads);
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    if (ds && dx) span.load(cr[r][i], ds, tid + i * threads);
-                    else cr[r][i].clear();
-                }
-            }
-            dot[r] = 0.f;
+    for (long row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+        RawVec<TX, VEC> sr[ITEMS], cr[ITEMS];
+        RawVec<TY, VEC> yr[ITEMS];
+        const RowSpan<VEC, ALIGNED> span(row, a.dim);
+        const float rstd = __ldg(a.rstd + row);
+        if constexpr (RING) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRowsAhead - 1) : "memory");
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                const int v = tid + i * threads;
-                float g[VEC];
-                gain_of(span, g, v);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float h = sr[r][i].get(e) * rstd[r], d = yr[r][i].get(e);
-                    dot[r] = fmaf(d * g[e], h, dot[r]);
-                    if constexpr (ALIGNED) acc[i][e] = fmaf(d, h, acc[i][e]);
+                if (span.any(tid + i * threads)) {
+                    sr[i].load(reinterpret_cast<const TX*>(place(slot, i, 0)) + tid * VEC);
+                    yr[i].load(reinterpret_cast<const TY*>(place(slot, i, XB)) + tid * VEC);
+                } else {
+                    sr[i].clear();
+                    yr[i].clear();
                 }
-                if (!ALIGNED && a.part) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)     // a column is one thread's in each row, and rows are separated by the barrier below
-                        if (span.any(v) && e >= span.lo(v) && e < span.hi(v))
-                            share[span.col(v) + e] = fmaf(yr[r][i].get(e), sr[r][i].get(e) * rstd[r], share[span.col(v) + e]);
-                }
+                if (ds && dx && span.any(tid + i * threads)) cr[i].load(reinterpret_cast<const TX*>(place(slot, i, XB + YB)) + tid * VEC);
+                else cr[i].clear();
             }
-        }
-        if constexpr (RING)
+            slot = slot + 1 == kRowsAhead ? 0 : slot + 1;
+        } else {
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) fetch();   // these rows' vectors are in registers
+            for (int i = 0; i < ITEMS; ++i) span.load(sr[i], sum, tid + i * threads);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            dot[r] = warp_sum(dot[r]);
-            if (lane == 0) red[flip][r][tid / 32] = dot[r];
-        }
-        __syncthreads();                              // the other half of `red` serves the next rows
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const long row = row0 + r * (long)gridDim.x;
-            float mean = 0.f;
-            for (int w = 0; w < threads / 32; w += 4) {     // entries of warps that do not exist are zero
-                const float4 t = *reinterpret_cast<const float4*>(&red[flip][r][w]);
-                mean += (t.x + t.y) + (t.z + t.w);
-            }
-            mean /= (float)a.dim;
-            if (!dx || row >= a.rows) continue;
-            const RowSpan<VEC, ALIGNED> span(row, a.dim);
+            for (int i = 0; i < ITEMS; ++i) span.load(yr[i], dy, tid + i * threads);
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                float g[VEC];
-                gain_of(span, g, tid + i * threads);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) g[e] = rstd[r] * (yr[r][i].get(e) * g[e] - sr[r][i].get(e) * rstd[r] * mean) + cr[r][i].get(e);
-                span.store(dx, tid + i * threads, g);
+                if (ds && dx) span.load(cr[i], ds, tid + i * threads);
+                else cr[i].clear();
             }
+        }
+        // grad_y s once for both sums: times the gain for mean(u h), whose factor rstd waits for the end, and times rstd for grad_gain
+        Pair dots = pair_of(0.f, 0.f);
+        const Pair rs = pair_of(rstd, rstd);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int v = tid + i * threads;
+            float g[VEC];
+            gain_of(span, g, v);
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const Pair ys = pair_mul(yr[i].get2(e), sr[i].get2(e));
+                dots = pair_fma(ys, pair_of(g[e], g[e + 1]), dots);
+                if constexpr (ALIGNED) acc[i][e / 2] = pair_fma(ys, rs, acc[i][e / 2]);
+            }
+            if (!ALIGNED && a.part) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)     // a column is one thread's in each row, and rows are separated by the barrier below
+                    if (span.any(v) && e >= span.lo(v) && e < span.hi(v))
+                        share[span.col(v) + e] = fmaf(yr[i].get(e) * sr[i].get(e), rstd, share[span.col(v) + e]);
+            }
+        }
+        float lo, hi;
+        split(dots, lo, hi);
+        float dot = lo + hi;
+        if constexpr (RING) fetch();                  // this row's vectors are in registers
+        dot = warp_sum(dot);
+        if (lane == 0) red[flip][tid / 32] = dot;
+        __syncthreads();                              // the other half of `red` serves the next row
+        float mean = 0.f;
+        for (int w = 0; w < threads / 32; w += 4) {     // entries of warps that do not exist are zero
+            const float4 t = *reinterpret_cast<const float4*>(&red[flip][w]);
+            mean += (t.x + t.y) + (t.z + t.w);
+        }
+        mean *= rstd / (float)a.dim;
+        if (!dx) continue;
+        // rstd (u - h mean) + grad_sum = rstd u + (grad_sum - s (rstd rstd mean))
+        const float back = -rstd * rstd * mean;
+        const Pair bk = pair_of(back, back);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float g[VEC];
+            gain_of(span, g, tid + i * threads);
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2)
+                split(pair_fma(pair_mul(yr[i].get2(e), pair_of(g[e], g[e + 1])), rs, pair_fma(sr[i].get2(e), bk, cr[i].get2(e))), g[e], g[e + 1]);
+            span.store(dx, tid + i * threads, g);
         }
     }
     if (!a.part) return;
@@ -377,7 +370,12 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
     if constexpr (ALIGNED) {
         const RowSpan<VEC, true> span(0, a.dim);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) span.store(part, tid + i * threads, acc[i]);
+        for (int i = 0; i < ITEMS; ++i) {
+            float out[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) split(acc[i][e / 2], out[e], out[e + 1]);
+            span.store(part, tid + i * threads, out);
+        }
     } else {
         __syncthreads();
         for (int c = tid; c < a.dim; c += threads) part[c] = share[c];

@@ -157,6 +157,7 @@ struct RawVec {
                     w[e / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + e) << (e % 2 * 16);
             }
     }
+    __device__ __forceinline__ Pair get2(int e) const { return pair_of(get(e), get(e + 1)); }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (sizeof(T) == 4)
             return __uint_as_float(w[e]);
