@@ -85,17 +85,18 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[i][e] = xr[i].get(e) + rr[i].get(e);
+            for (int e = 0; e < VEC; e += 2) split(pair_add(xr[i].get2(e), rr[i].get2(e)), s[i][e], s[i][e + 1]);
     }
     if (sum)
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) span.store(sum, tid + i * threads, s[i]);
     const bool row_scale = E4M3 && a.group == a.dim;
-    float sq = 0.f, top = 0.f;
+    Pair squares = pair_of(0.f, 0.f);
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sq = fmaf(s[i][e], s[i][e], sq);
+        for (int e = 0; e < VEC; e += 2) squares = pair_fma(pair_of(s[i][e], s[i][e + 1]), pair_of(s[i][e], s[i][e + 1]), squares);
         if (row_scale) {
             float g[VEC];
             span.load_columns(g, a.gain, tid + i * threads);
@@ -103,7 +104,9 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
             for (int e = 0; e < VEC; ++e) top = max_nan(top, fabsf(s[i][e] * g[e]));
         }
     }
-    sq = warp_sum(sq);
+    float sq, odd;
+    split(squares, sq, odd);
+    sq = warp_sum(sq + odd);
     if (row_scale) top = warp_max_nan(top);
     if (threads > 32) {
         const int warps = threads / 32, lane = tid % 32;
@@ -129,7 +132,8 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
         float out[VEC];
         span.load_columns(out, a.gain, v);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) out[e] *= s[i][e] * rstd;
+        for (int e = 0; e < VEC; e += 2)
+            split(pair_mul(pair_mul(pair_of(s[i][e], s[i][e + 1]), pair_of(rstd, rstd)), pair_of(out[e], out[e + 1])), out[e], out[e + 1]);
         if constexpr (E4M3) {
             if (!row_scale) {      // the lanes of a group (32, 64 or 128 elements) are neighbours in the warp, and groups do not cross rows
                 float t = 0.f;
@@ -144,7 +148,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
             // times 1 / scale instead of a division by scale: at most the rounding of a value that lies in the middle between two
             // codes changes
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) out[e] *= inv;
+            for (int e = 0; e < VEC; e += 2) split(pair_mul(pair_of(out[e], out[e + 1]), pair_of(inv, inv)), out[e], out[e + 1]);
             uint32_t w[VEC / 4];
             pack_e4m3<VEC>(out, w);
             if (!span.any(v)) continue;
