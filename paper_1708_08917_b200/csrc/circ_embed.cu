@@ -20,33 +20,45 @@ struct Embed {
 // ---- forward -------------------------------------------------------------------------------------------------
 // Pure data movement.  The output is walked as one run of vectors (VEC elements, 16 bytes or more per access when the rows
 // allow it): a thread takes UNROLL of them, a thread block apart, so that several rows' loads are in flight behind their ids.
+// (step_rows, step_vecs): 256 vectors as whole rows and vectors, so that a thread divides once.
 template <typename TT, typename TY, typename ID, int VEC, int UNROLL>
-__global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict__ table, const ID* __restrict__ ids, TY* __restrict__ y,
-                                                            long vectors, int vec_per_row, int vocab, int dim, float scale, long padding) {
+__global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict__ table, const ID* __restrict__ ids, TY* __restrict__ y, int tokens,
+                                                            unsigned vec_per_row, unsigned step_rows, unsigned step_vecs, unsigned vocab, int dim,
+                                                            float scale, unsigned padding) {
     const long first = (long)blockIdx.x * (256 * UNROLL);
-    // one 64-bit division a thread block; the rest is small-integer arithmetic
-    const long row0 = first / vec_per_row;
-    const unsigned in_row = (unsigned)(first - row0 * vec_per_row) + threadIdx.x;
-    float v[UNROLL][VEC];
-    long at[UNROLL];
+    const long row0 = first / vec_per_row;         // the block's first vector; the rest is small-integer arithmetic
+    const unsigned k = (unsigned)(first - row0 * vec_per_row) + threadIdx.x, rows = k / vec_per_row;
+    unsigned c = k - rows * vec_per_row;
+    long t = row0 + rows;
+    RawVec<TT, VEC> raw[UNROLL];
+    unsigned col[UNROLL];
+    long token[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-        const unsigned k = in_row + u * 256u, dr = k / (unsigned)vec_per_row;
-        const long t = row0 + dr;
-        const int c = (int)(k - dr * vec_per_row) * VEC;
-        at[u] = first + u * 256 + threadIdx.x < vectors ? t * dim + c : -1;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[u][e] = 0.f;
-        if (at[u] < 0) continue;
-        const long id = (long)__ldg(ids + t);
-        if (id >= 0 && id < vocab && id != padding) load_vec<VEC>(table + id * dim + c, v[u]);
+        col[u] = c * VEC;
+        token[u] = t;
+        raw[u].clear();
+        if (t < tokens) {
+            const ID id = __ldg(ids + t);
+            const unsigned lo = (unsigned)id;
+            bool row = lo < vocab && lo != padding;
+            if constexpr (sizeof(ID) == 8) row = row && (unsigned)((uint64_t)id >> 32) == 0;
+            if (row) raw[u].load(table + (size_t)lo * dim + col[u]);
+        }
+        t += step_rows;
+        c += step_vecs;
+        if (c >= vec_per_row) {
+            c -= vec_per_row;
+            ++t;
+        }
     }
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-        if (at[u] < 0) continue;
+        if (token[u] >= tokens) break;
+        float v[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[u][e] *= scale;
-        store_vec<VEC>(y + at[u], v[u]);
+        for (int e = 0; e < VEC; ++e) v[e] = raw[u].get(e) * scale;
+        store_vec<VEC>(y + token[u] * dim + col[u], v);
     }
 }
 
@@ -652,8 +664,8 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
                 auto go = [&](auto kernel, int vec, int unroll) {
                     const int per_row = e->dim / vec;
                     const long vectors = tokens * per_row, blocks = (vectors + 256L * unroll - 1) / (256L * unroll);
-                    kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), vectors,
-                                                            per_row, e->vocab, e->dim, e->scale, e->padding);
+                    kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), (int)tokens,
+                                                            per_row, 256 / per_row, 256 % per_row, e->vocab, e->dim, e->scale, (unsigned)e->padding);
                 };
                 if (vec)
                     tokens * (e->dim / 8) <= 148L * 256 ? go(embed_forward_kernel<TT, TY, ID, 8, 1>, 8, 1)    // one vector a thread fills the machine
