@@ -77,7 +77,7 @@ __device__ __forceinline__ float piece_squares(const TG* g, int count) {
 // Pieces are walked in order here and in reverse order by the second kernel, which so finds the last ones in the L2 cache.
 __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const ClipPiece* __restrict__ pieces, int count, double* __restrict__ partial) {
     __shared__ double sums[kClipThreads / 32];
-    pdl_trigger();
+    pdl_begin();
     double total = 0.0;
     for (int i = blockIdx.x; i < count; i += gridDim.x) {
         const ClipPiece p = pieces[i];
@@ -133,7 +133,7 @@ template <int TYPES>
 __global__ void __launch_bounds__(kClipThreads, kScaleBlocks) clip_scale_kernel(const ClipPiece* __restrict__ pieces, int count, const double* __restrict__ partial,
                                                                   int partials, float max_norm, float* norm_out) {
     __shared__ double sums[kClipThreads / 32];
-    pdl_wait();
+    pdl_begin();
     double total = 0.0;
     for (int i = threadIdx.x; i < partials; i += kClipThreads) total += __ldcg(partial + i);
 #pragma unroll
@@ -283,12 +283,11 @@ int circ_clip_forward(circ_clip_handle h, float max_norm, float* norm, void* str
     const int pieces = c->count, blocks = pieces < kClipBlocks ? (pieces ? pieces : 1) : kClipBlocks;
     const ClipPiece* plan = static_cast<const ClipPiece*>(c->plan.ptr);
     double* partial = static_cast<double*>(c->partial.ptr);
-    clip_norm_kernel<<<blocks, kClipThreads, 0, s>>>(plan, pieces, partial);
-    CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
+    CIRC_CUDA_TRY(launch_row(clip_norm_kernel, dim3(blocks), dim3(kClipThreads), 0, s, plan, pieces, partial), CIRC_ERR_CUDA);
     auto* kernel = c->same_types < 0 ? clip_scale_kernel<-1> : c->same_types == 0 ? clip_scale_kernel<0> : c->same_types == 1 ? clip_scale_kernel<1>
                    : c->same_types == 2 ? clip_scale_kernel<2> : clip_scale_kernel<3>;
     const int scale_blocks = pieces < 148 * kScaleBlocks ? blocks : 148 * kScaleBlocks;
-    CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, kernel, dim3(scale_blocks), kClipThreads, 0, s, plan, pieces, partial, blocks, max_norm, norm), CIRC_ERR_CUDA);
+    CIRC_CUDA_TRY(launch_row(kernel, dim3(scale_blocks), dim3(kClipThreads), 0, s, plan, pieces, partial, blocks, max_norm, norm), CIRC_ERR_CUDA);
     count_launches(2);
     return CIRC_OK;
 }

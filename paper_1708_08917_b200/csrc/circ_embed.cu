@@ -25,6 +25,7 @@ template <typename TT, typename TY, typename ID, int VEC, int UNROLL>
 __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict__ table, const ID* __restrict__ ids, TY* __restrict__ y, int tokens,
                                                             unsigned vec_per_row, unsigned step_rows, unsigned step_vecs, unsigned vocab, int dim,
                                                             float scale, unsigned padding) {
+    pdl_begin();
     const long first = (long)blockIdx.x * (256 * UNROLL);
     const long row0 = first / vec_per_row;         // the block's first vector; the rest is small-integer arithmetic
     const unsigned k = (unsigned)(first - row0 * vec_per_row) + threadIdx.x, rows = k / vec_per_row;
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
                                                                   int* __restrict__ start, int* __restrict__ order, int* __restrict__ cuts) {
     extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places; then the warps' lists
     __shared__ int part[kSortWarps], below[kSortWarps];
-    pdl_trigger();
+    pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int per_warp = ((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
     const int begin = warp * per_warp < tokens ? warp * per_warp : tokens, end = begin + per_warp < tokens ? begin + per_warp : tokens;
@@ -251,8 +252,7 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
     constexpr int BYTES = VEC * (int)sizeof(TY), DEPTH = ring_depth(PARTS * BYTES);
     extern __shared__ __align__(16) unsigned char ring[];
     auto place = [&](int slot, int c) { return ring + ((size_t)(slot * PARTS + c) * 256 + threadIdx.x) * BYTES; };
-    pdl_trigger();
-    pdl_wait();
+    pdl_begin();
     const int p = blockIdx.x * (256 / GROUP) + threadIdx.x / GROUP, lane = threadIdx.x % 32;
     if (p >= a.workers) return;      // whole warps: GROUP is a multiple of 32
     const int col = (int)(blockIdx.y * (PARTS * GROUP) + threadIdx.x % GROUP) * VEC;
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
 
 template <typename TT>
 __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSum a, TT* __restrict__ dt) {
-    pdl_wait();
+    pdl_begin();
     __shared__ float parts[8][33];
     const int few = a.cuts[0], many = a.cuts[1], warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int slices = (a.dim + 127) / 128, thin = (a.dim + 31) / 32;
@@ -393,6 +393,7 @@ __global__ void __launch_bounds__(256, 4) embed_few_kernel(const ID* __restrict_
     __shared__ __align__(16) float sums[8][WIDTH];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const unsigned blocks = gridDim.x, b = blockIdx.x;
+    pdl_begin();
     const int rows = (int)((vocab - b + blocks - 1) / blocks);
     unsigned own[PER];
 #pragma unroll
@@ -655,6 +656,7 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool vec = e->dim % 8 == 0 && !misaligned(table, 16) && !misaligned(y, 16);
+    cudaError_t err = cudaSuccess;
     with_dtype(e->table_dtype, [&](auto* t) {
         with_dtype(e->y_dtype, [&](auto* o) {
             with_index_type(e->ids_type, [&](auto* i) {
@@ -664,8 +666,9 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
                 auto go = [&](auto kernel, int vec, int unroll) {
                     const int per_row = e->dim / vec;
                     const long vectors = tokens * per_row, blocks = (vectors + 256L * unroll - 1) / (256L * unroll);
-                    kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), (int)tokens,
-                                                            per_row, 256 / per_row, 256 % per_row, e->vocab, e->dim, e->scale, (unsigned)e->padding);
+                    err = launch_row(kernel, dim3((unsigned)blocks), dim3(256), 0, s, static_cast<const TT*>(table), static_cast<const ID*>(ids),
+                                     static_cast<TY*>(y), (int)tokens, per_row, 256 / per_row, 256 % per_row, e->vocab, e->dim, e->scale,
+                                     (unsigned)e->padding);
                 };
                 if (vec)
                     tokens * (e->dim / 8) <= 148L * 256 ? go(embed_forward_kernel<TT, TY, ID, 8, 1>, 8, 1)    // one vector a thread fills the machine
@@ -675,8 +678,8 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
             });
         });
     });
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(1);
-    CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
     return CIRC_OK;
 }
 
@@ -698,6 +701,7 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
     // Up to 2048 tokens in one launch, in microseconds against the three launches: 92 / 103 (65536 rows of 2048), 10 / 25 (1000 of 512),
     // 28 / 37 (131072 of 256); only with every token in one row the three are ahead (30 / 20 at 1000 of 512).
     const FewPlan few = plan_few(e, tokens, aligned);
+    cudaError_t err = cudaSuccess;
     if (few.fits) {
         with_dtype(e->table_dtype, [&](auto* t) {
             with_dtype(e->y_dtype, [&](auto* o) {
@@ -707,15 +711,15 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                     using ID = tag_type<decltype(i)>;
                     constexpr int WIDE = std::is_same<TY, __nv_bfloat16>::value && std::is_same<TT, __nv_bfloat16>::value ? 8 : 4;
                     auto go = [&](auto kernel) {
-                        kernel<<<dim3((unsigned)few.blocks, few.slices), 256, 0, s>>>(static_cast<const ID*>(ids), static_cast<const TY*>(grad_y),
-                                                                                      static_cast<TT*>(grad_table), (int)tokens, e->vocab,
-                                                                                      (unsigned)e->padding, e->dim, e->scale);
+                        err = launch_row(kernel, dim3((unsigned)few.blocks, few.slices), dim3(256), 0, s, static_cast<const ID*>(ids),
+                                         static_cast<const TY*>(grad_y), static_cast<TT*>(grad_table), (int)tokens, e->vocab, (unsigned)e->padding,
+                                         e->dim, e->scale);
                     };
                     few.vec == 1 ? go(embed_few_kernel<TT, TY, ID, 1>) : go(embed_few_kernel<TT, TY, ID, WIDE>);
                 });
             });
         });
-        CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
+        CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
         count_launches(1);
         return CIRC_OK;
     }
@@ -729,13 +733,12 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                      pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype),
                      (int)dtype_bytes(e->table_dtype), e->scale};
     const size_t smem = kSortWarps * (sizeof(int) * (size_t)pl.rows_per_block + sizeof(int2) * kSortListed);
-    cudaError_t err = cudaSuccess;
     with_index_type(e->ids_type, [&](auto* i) {
         using ID = tag_type<decltype(i)>;
         err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSortWarps * (sizeof(int) * kSortRows + sizeof(int2) * kSortListed)));
         if (err != cudaSuccess) return;
-        embed_sort_kernel<ID><<<pl.blocks, kSortThreads, smem, s>>>(static_cast<const ID*>(ids), (int)tokens, e->vocab, (unsigned)e->padding,
-                                                                    pl.bits, pl.rows_per_block, start, order, a.cuts);
+        err = launch_row(embed_sort_kernel<ID>, dim3(pl.blocks), dim3(kSortThreads), smem, s, static_cast<const ID*>(ids), (int)tokens, e->vocab,
+                         (unsigned)e->padding, pl.bits, pl.rows_per_block, start, order, a.cuts);
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     with_dtype(e->table_dtype, [&](auto* t) {
@@ -746,7 +749,7 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
             auto go = [&](auto kernel) {
                 const int per_block = 256 / pl.group, bytes = pl.parts * pl.vec * (int)sizeof(TY);
                 const size_t ring = (size_t)ring_depth(bytes) * bytes * 256;
-                err = launch_kernel(PDL_EARLY, kernel, dim3((pl.workers + per_block - 1) / per_block, pl.slices), 256, ring, s, a,
+                err = launch_row(kernel, dim3((pl.workers + per_block - 1) / per_block, pl.slices), dim3(256), ring, s, a,
                                     static_cast<const TY*>(grad_y), static_cast<TT*>(grad_table));
             };
             auto by_group = [&](auto vec, auto parts) {
@@ -763,7 +766,7 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                 pl.vec == 1 ? by_group(One{}, Two{}) : by_group(Wide{}, Two{});
         });
         if (err == cudaSuccess && tokens > kWholeRun)
-            err = launch_kernel(PDL_EARLY, embed_join_kernel<TT>, dim3(148), 256, 0, s, a, static_cast<TT*>(grad_table));
+            err = launch_row(embed_join_kernel<TT>, dim3(148), dim3(256), 0, s, a, static_cast<TT*>(grad_table));
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(2 + (tokens > kWholeRun));

@@ -223,7 +223,7 @@ __device__ __forceinline__ int targets_of(const LossArgs& a, const ID* __restric
 template <typename ID>
 __global__ void __launch_bounds__(1024) loss_count_kernel(LossArgs a, const ID* __restrict__ targets) {
     __shared__ int part[32];
-    pdl_trigger();
+    pdl_begin();
     const int n = __reduce_add_sync(0xffffffffu, targets_of(a, targets, threadIdx.x, 1024));
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = n;
     __syncthreads();
@@ -276,6 +276,7 @@ __device__ __forceinline__ void finish_mean(const LossArgs& a, const ID* __restr
 template <typename T, typename ID, int VEC, int ITEMS, bool ALIGNED, bool GRAD>
 __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
     __shared__ int part[8];
+    pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 8 + warp;
     const bool live = row < a.rows;
     const RowSpan<VEC, ALIGNED> span(live ? row : 0, live ? a.classes : 0, a.ld);
@@ -300,10 +301,7 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) run.take(s[i]);
     const Softmax all = warp_join(run.done());
-    if (GRAD && a.count) {
-        pdl_wait();
-        count = __ldcg(a.count);
-    }
+    if (GRAD && a.count) count = __ldcg(a.count);
     if (live) {
         const RowResult r = finish_row(a, row, all, target, target_score, count, lane == 0);
         if constexpr (GRAD) {
@@ -360,6 +358,7 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
     __shared__ Softmax part[2][16];
     __shared__ Softmax peers[2][8];
     __shared__ int counts[16];
+    pdl_begin();
     const int threads = blockDim.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = threads / 32;
     const int rank = blockIdx.x % cluster, rows_apart = gridDim.x / cluster;
     T* kept = reinterpret_cast<T*>(held) + (size_t)tid * VEC;
@@ -439,12 +438,7 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
             all = warp_join(lane < cluster ? peers[flip][lane] : Softmax{-INFINITY, 0.f});
         }
         if (GRAD && count == 0) {
-            if (a.count) {
-                pdl_wait();
-                count = __ldcg(a.count);
-            } else {
-                count = __reduce_add_sync(0xffffffffu, lane < warps ? counts[lane] : 0);
-            }
+            count = a.count ? __ldcg(a.count) : __reduce_add_sync(0xffffffffu, lane < warps ? counts[lane] : 0);
             count = count < 1 ? 1 : count;
         }
         const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
@@ -515,6 +509,7 @@ template <typename T, typename ID>
 __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
     __shared__ Softmax part[16];
     __shared__ int counts[16];
+    pdl_begin();
     const int row = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const T* zr = z + (size_t)row * a.ld;
     Running run;
@@ -536,10 +531,7 @@ __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __r
     __syncthreads();         // every thread has read the target's score: grad may be z
     all = warp_join(lane < 16 ? part[lane] : Softmax{-INFINITY, 0.f});
     int count = __reduce_add_sync(0xffffffffu, lane < 16 ? counts[lane] : 0);
-    if (grad && a.count) {
-        pdl_wait();
-        count = __ldcg(a.count);
-    }
+    if (grad && a.count) count = __ldcg(a.count);
     const RowResult r = finish_row(a, row, all, target, target_score, count, tid == 0);
     if (grad) {
         T* gr = grad + (size_t)row * a.grad_ld;
@@ -558,7 +550,7 @@ constexpr size_t kLossHeld = 110 * 1024;           // bytes of a row that a bloc
 constexpr size_t kLossMost = 216 * 1024;           // one block an SM
 
 template <typename... KArgs, typename... Args>
-static cudaError_t launch_loss(bool dependent, int cluster, void (*kernel)(KArgs...), unsigned blocks, int threads, size_t smem, cudaStream_t s, Args... args) {
+static cudaError_t launch_loss(int cluster, void (*kernel)(KArgs...), unsigned blocks, int threads, size_t smem, cudaStream_t s, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(threads);
@@ -566,10 +558,8 @@ static cudaError_t launch_loss(bool dependent, int cluster, void (*kernel)(KArgs
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     int n = 0;
-    if (dependent) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
     if (cluster > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
         attr[n].val.clusterDim.x = cluster;
@@ -585,7 +575,6 @@ static cudaError_t launch_loss(bool dependent, int cluster, void (*kernel)(KArgs
 template <typename T, typename ID>
 static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const LossArgs& a, cudaStream_t s) {
     constexpr int VEC = 16 / (int)sizeof(T);
-    const bool dependent = a.count != nullptr;
     cudaError_t err = cudaErrorNotSupported;
     auto with_rows = [&](auto aligned, auto gradient) {
         constexpr bool ALIGNED = decltype(aligned)::value, GRAD = decltype(gradient)::value;
@@ -593,7 +582,7 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
         if (vectors <= 128) {
             const unsigned blocks = (unsigned)((a.rows + 7L) / 8);
             auto go = [&](auto items) {
-                err = launch_loss(dependent, 1, loss_warp_kernel<T, ID, VEC, decltype(items)::value, ALIGNED, GRAD>, blocks, 256, 0, s, z, targets, grad, a);
+                err = launch_loss(1, loss_warp_kernel<T, ID, VEC, decltype(items)::value, ALIGNED, GRAD>, blocks, 256, 0, s, z, targets, grad, a);
             };
             vectors <= 32 ? go(std::integral_constant<int, 1>{}) : vectors <= 64 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
             return;
@@ -610,7 +599,7 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
         int per_sm = 1;
         if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, GRAD ? bytes() : 0)) != cudaSuccess) return;
         const long wave = 148L * (per_sm < 1 ? 1 : per_sm) / cluster, walkers = wave < 1 ? 1 : a.rows < wave ? a.rows : wave;
-        err = launch_loss(dependent, cluster, kernel, (unsigned)(walkers * cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
+        err = launch_loss(cluster, kernel, (unsigned)(walkers * cluster), threads, GRAD ? bytes() : 0, s, z, targets, grad, a, cluster);
     };
     auto with_alignment = [&](auto gradient) {
         if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) return;
@@ -618,7 +607,7 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
         else with_rows(std::false_type{}, gradient);
     };
     grad ? with_alignment(std::true_type{}) : with_alignment(std::false_type{});
-    if (err == cudaErrorNotSupported) err = launch_loss(dependent, 1, loss_any_kernel<T, ID>, (unsigned)a.rows, 512, 0, s, z, targets, grad, a);
+    if (err == cudaErrorNotSupported) err = launch_loss(1, loss_any_kernel<T, ID>, (unsigned)a.rows, 512, 0, s, z, targets, grad, a);
     return err;
 }
 
@@ -674,8 +663,7 @@ static int run_loss(Loss* l, const void* z, long ld, const void* targets, float*
             using ID = tag_type<decltype(i)>;
             const ID* ids = static_cast<const ID*>(targets);
             if (count_alone) {
-                loss_count_kernel<ID><<<1, 1024, 0, s>>>(a, ids);
-                if ((err = cudaGetLastError()) != cudaSuccess) return;
+                if ((err = launch_row(loss_count_kernel<ID>, dim3(1), dim3(1024), 0, s, a, ids)) != cudaSuccess) return;
             }
             err = dispatch_loss<T, ID>(static_cast<const T*>(z), ids, static_cast<T*>(grad), a, s);
         });

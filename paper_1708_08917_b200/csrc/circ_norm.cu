@@ -66,6 +66,7 @@ template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED>
 __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX* residual, TX* sum, TY* y, NormForward a) {
     constexpr bool E4M3 = std::is_same<TY, uint8_t>::value;
     __shared__ float red[2][16];
+    pdl_begin();
     const int threads = blockDim.x, tid = threadIdx.x;
     const long row = (long)blockIdx.x * blockDim.y + threadIdx.y;
     if (row >= a.rows) return;       // whole warps; blocks of several rows have one warp a row and no barrier
@@ -174,6 +175,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const TX* x, const TX
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(512) norm_forward_any_kernel(const TX* x, const TX* residual, TX* sum, TY* y, NormForward a) {
     __shared__ float red[33];
+    pdl_begin();
     const int dim = a.dim, group = a.group;
     const size_t row = blockIdx.x, base = row * dim;
     auto value = [&](int c) { return to_float(x[base + c]) + (residual ? to_float(residual[base + c]) : 0.f); };
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
     static_assert(ALIGNED || !RING, "copies of whole vectors");
     constexpr int XB = VEC * (int)sizeof(TX), YB = VEC * (int)sizeof(TY), BYTES = 2 * XB + YB;
     __shared__ __align__(16) float red[2][16];
-    pdl_trigger();
+    pdl_begin();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
     for (int i = tid; i < 2 * 16; i += threads) (&red[0][0])[i] = 0.f;
     __syncthreads();
@@ -389,6 +391,7 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(512) norm_backward_any_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
     __shared__ float red[33];
+    pdl_begin();
     const int dim = a.dim;
     const size_t row = blockIdx.x, base = row * dim;
     const float rstd = a.rstd[row];
@@ -401,7 +404,7 @@ __global__ void __launch_bounds__(512) norm_backward_any_kernel(const TX* __rest
 }
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(256) norm_gain_any_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, NormBackward a) {
-    pdl_trigger();
+    pdl_begin();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= a.dim) return;
     float acc = 0.f;
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__(256) norm_gain_any_kernel(const TX* __restrict
 // grad_gain[c] = part[0][c] + part[1][c] + ...: a block has 32 columns, its warps take consecutive parts.
 __global__ void __launch_bounds__(512) norm_gain_kernel(const float* __restrict__ part, float* __restrict__ dgain, int parts, int dim) {
     __shared__ float sums[16][33];
-    pdl_wait();
+    pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = blockIdx.x * 32 + lane;
     const int per = (parts + 15) / 16, from = warp * per, to = from + per < parts ? from + per : parts;
     float s = 0.f;
@@ -454,6 +457,7 @@ static void with_items(int items, F&& f) {
 template <typename TO>
 __global__ void __launch_bounds__(256) norm_unpack_kernel(const uint8_t* __restrict__ y, const float* __restrict__ scale, TO* __restrict__ out,
                                                           long count, int group) {
+    pdl_begin();
     for (long i = blockIdx.x * (long)blockDim.x + threadIdx.x; i < count; i += (long)gridDim.x * blockDim.x)
         store_one(out + i, from_e4m3(y[i]) * scale[i / group]);
 }
@@ -548,6 +552,7 @@ int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, c
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t err = cudaSuccess;
     const NormForward a{gain, y_scale, rstd, rows, n->dim, norm_group(n), n->group == 32 ? 5 : n->group == 64 ? 6 : 7, n->eps};
     with_dtype(n->x_dtype, [&](auto* t) {
         using TX = tag_type<decltype(t)>;
@@ -566,22 +571,22 @@ int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, c
                 if (!shape.items) return false;
                 const int per_block = shape.threads == 32 ? (rows < 148 * 4 ? 1 : 4) : 1;
                 with_items(shape.items, [&](auto items) {
-                    norm_forward_kernel<TX, TY, VEC, decltype(items)::value, ALIGNED>
-                        <<<(unsigned)((rows + per_block - 1) / per_block), dim3(shape.threads, per_block), 0, s>>>(xs, rs, ss, ys, a);
+                    err = launch_row(norm_forward_kernel<TX, TY, VEC, decltype(items)::value, ALIGNED>, dim3((unsigned)((rows + per_block - 1) / per_block)),
+                                     dim3(shape.threads, per_block), 0, s, xs, rs, ss, ys, a);
                 });
                 return true;
             };
             const bool bases = !misaligned(x, 16) && !misaligned(residual, 16) && !misaligned(sum, 16) && !misaligned(y, 16);
             const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : launch(std::false_type{}));
-            if (!done) norm_forward_any_kernel<TX, TY><<<(unsigned)rows, 512, 0, s>>>(xs, rs, ss, ys, a);
+            if (!done) err = launch_row(norm_forward_any_kernel<TX, TY>, dim3((unsigned)rows), dim3(512), 0, s, xs, rs, ss, ys, a);
         };
         if (e4m3)
             go(static_cast<uint8_t*>(nullptr));
         else
             with_dtype(n->y_dtype, go);
     });
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(1);
-    CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
     return CIRC_OK;
 }
 
@@ -635,7 +640,7 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
                     if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, shape.threads, smem)) != cudaSuccess) return;
                     const long wave = 148L * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm), some = (rows + 3) / 4 > 148 ? (rows + 3) / 4 : rows < 148 ? rows : 148;
                     parts = (int)(some < wave ? some : wave);
-                    kernel<<<parts, shape.threads, smem, s>>>(ss, ys, cs, xs, a);
+                    err = launch_row(kernel, dim3(parts), dim3(shape.threads), smem, s, ss, ys, cs, xs, a);
                     ++launches;
                 });
                 return true;
@@ -644,19 +649,19 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
             const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : n->dim <= 16384 && launch(std::false_type{}));
             if (done || err != cudaSuccess) return;
             if (grad_x) {
-                norm_backward_any_kernel<TX, TY><<<(unsigned)rows, 512, 0, s>>>(ss, ys, cs, xs, a);
+                err = launch_row(norm_backward_any_kernel<TX, TY>, dim3((unsigned)rows), dim3(512), 0, s, ss, ys, cs, xs, a);
                 ++launches;
             }
-            if (grad_gain) {
+            if (grad_gain && err == cudaSuccess) {
                 parts = rows < 64 ? (int)rows : 64;
-                norm_gain_any_kernel<TX, TY><<<dim3((n->dim + 255) / 256, parts), 256, 0, s>>>(ss, ys, a);
+                err = launch_row(norm_gain_any_kernel<TX, TY>, dim3((n->dim + 255) / 256, parts), dim3(256), 0, s, ss, ys, a);
                 ++launches;
             }
         });
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     if (grad_gain) {
-        CIRC_CUDA_TRY(launch_kernel(PDL_EARLY, norm_gain_kernel, dim3((n->dim + 31) / 32), 512, 0, s, a.part, grad_gain, parts, n->dim), CIRC_ERR_CUDA);
+        CIRC_CUDA_TRY(launch_row(norm_gain_kernel, dim3((n->dim + 31) / 32), dim3(512), 0, s, a.part, grad_gain, parts, n->dim), CIRC_ERR_CUDA);
         ++launches;
     }
     count_launches(launches);
@@ -674,13 +679,14 @@ int circ_norm_unpack(circ_norm_handle h, const void* y, const float* y_scale, vo
     }
     const long count = rows * n->dim, need = (count + 255) / 256;
     const unsigned blocks = (unsigned)(need < 148L * 32 ? need : 148L * 32);
+    cudaError_t err = cudaSuccess;
     with_dtype(out_dtype, [&](auto* o) {
         using TO = tag_type<decltype(o)>;
-        norm_unpack_kernel<TO><<<blocks, 256, 0, static_cast<cudaStream_t>(stream)>>>(static_cast<const uint8_t*>(y), y_scale, static_cast<TO*>(out),
-                                                                                      count, norm_group(n));
+        err = launch_row(norm_unpack_kernel<TO>, dim3(blocks), dim3(256), 0, static_cast<cudaStream_t>(stream), static_cast<const uint8_t*>(y), y_scale,
+                         static_cast<TO*>(out), count, norm_group(n));
     });
+    CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(1);
-    CIRC_CUDA_TRY(cudaGetLastError(), CIRC_ERR_CUDA);
     return CIRC_OK;
 }
 

@@ -10,6 +10,17 @@
 
 namespace circ {
 
+// Every kernel of these operators starts with pdl_begin() and is launched by launch_row: its blocks may be scheduled while the stream's
+// previous kernel still runs (which hides the launch), and touch global memory only once that one has finished.
+__device__ __forceinline__ void pdl_begin() {
+    pdl_wait();
+    pdl_trigger();
+}
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_row(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args&&... args) {
+    return launch_kernel(PDL_EARLY, kernel, grid, block, smem, stream, args...);
+}
+
 inline size_t dtype_bytes(int dtype) { return dtype == CIRC_F32 ? 4 : dtype == CIRC_BF16 ? 2 : 1; }
 inline bool float_dtype(int dtype) { return dtype == CIRC_F32 || dtype == CIRC_BF16; }
 inline bool misaligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
