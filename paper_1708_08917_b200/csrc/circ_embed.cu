@@ -568,8 +568,8 @@ static int check_embed(const Embed* e, long tokens) {
         set_error(CIRC_ERR_ARG, "handle is NULL");
         return CIRC_ERR_ARG;
     }
-    if (tokens < 0 || tokens > INT32_MAX) {
-        set_error(CIRC_ERR_SHAPE, "tokens=%ld must be in [0, 2^31)", tokens);
+    if (tokens < 0 || tokens > (1L << 30)) {
+        set_error(CIRC_ERR_SHAPE, "tokens=%ld must be in [0, 2^30]", tokens);
         return CIRC_ERR_SHAPE;
     }
     return CIRC_OK;
@@ -582,8 +582,8 @@ using namespace circ;
 extern "C" {
 
 circ_embed_handle circ_embed_create(int vocab, int dim) {
-    if (vocab < 1 || dim < 1) {
-        set_error(CIRC_ERR_SHAPE, "vocab=%d and dim=%d must be >= 1", vocab, dim);
+    if (vocab < 1 || vocab > (1 << 30) || dim < 1 || dim > (1 << 24)) {
+        set_error(CIRC_ERR_SHAPE, "vocab=%d must be in [1, 2^30], dim=%d in [1, 2^24]", vocab, dim);
         return nullptr;
     }
     int device;
@@ -650,7 +650,7 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
         set_error(CIRC_ERR_ARG, "table, ids and y must be aligned to their element sizes");
         return CIRC_ERR_ARG;
     }
-    if (tokens > (1L << 48) / e->dim) {
+    if (tokens > (1L << 41) / e->dim) {      // thread blocks of 2048 elements at least
         set_error(CIRC_ERR_SHAPE, "tokens=%ld of %d elements are too many", tokens, e->dim);
         return CIRC_ERR_SHAPE;
     }

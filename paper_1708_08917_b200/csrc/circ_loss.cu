@@ -587,7 +587,6 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
             vectors <= 32 ? go(std::integral_constant<int, 1>{}) : vectors <= 64 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
             return;
         }
-        if (vectors > (1 << 26)) return;
         // blocks a row: enough to hold it, and more while the rows do not fill the machine (4 vectors a thread left at least)
         int cluster = 1;
         auto bytes = [&]() { return (size_t)((vectors + cluster - 1) / cluster) * 16; };
@@ -631,8 +630,8 @@ static int run_loss(Loss* l, const void* z, long ld, const void* targets, float*
         set_error(CIRC_ERR_ARG, "handle is NULL");
         return CIRC_ERR_ARG;
     }
-    if (rows < 0 || rows > INT32_MAX || ld < l->classes || (grad && grad_ld < l->classes)) {
-        set_error(CIRC_ERR_SHAPE, "rows=%ld must be in [0, 2^31) and the strides (%ld, %ld) at least classes=%d", rows, ld, grad_ld, l->classes);
+    if (rows < 0 || rows > (1L << 30) || ld < l->classes || (grad && grad_ld < l->classes)) {
+        set_error(CIRC_ERR_SHAPE, "rows=%ld must be in [0, 2^30] and the strides (%ld, %ld) at least classes=%d", rows, ld, grad_ld, l->classes);
         return CIRC_ERR_SHAPE;
     }
     if (rows == 0) {
@@ -680,8 +679,8 @@ using namespace circ;
 extern "C" {
 
 circ_loss_handle circ_loss_create(int classes) {
-    if (classes < 1) {
-        set_error(CIRC_ERR_SHAPE, "classes=%d must be >= 1", classes);
+    if (classes < 1 || classes > (1 << 28)) {
+        set_error(CIRC_ERR_SHAPE, "classes=%d must be in [1, 2^28]", classes);
         return nullptr;
     }
     int device;
@@ -721,7 +720,7 @@ int circ_loss_set_ignore(circ_loss_handle h, long ignore) {
 
 int circ_loss_reserve(circ_loss_handle h, long max_rows) {
     Loss* l = reinterpret_cast<Loss*>(h);
-    if (!l || max_rows < 0 || max_rows > INT32_MAX) {
+    if (!l || max_rows < 0 || max_rows > (1L << 30)) {
         set_error(CIRC_ERR_ARG, "bad handle or max_rows %ld", max_rows);
         return CIRC_ERR_ARG;
     }

@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(512) norm_gain_kernel(const float* __restrict_
     }
 }
 
-constexpr int kNormParts = 148 * 4;   // blocks of a backward call at most
+constexpr int kNormParts = 148 * 4, kGainParts = 64;      // shares of grad_gain: of rows in registers at most, and of others
+constexpr int kNormLongest = 32768;                       // longest row that a block's registers hold (512 threads x 8 vectors x 8 elements)
 
 // Launch shape of a row kernel: `items` vectors a thread (1, 2, 4 or 8), `threads` a multiple of 32 (at most 512); items 0: the row
 // does not fit.  Rows of one warp are put several in a block.
@@ -474,6 +475,7 @@ static int check_norm(const Norm* n, long rows) {
     return CIRC_OK;
 }
 static int norm_group(const Norm* n) { return n->group ? n->group : n->dim; }
+static size_t norm_scratch(const Norm* n) { return sizeof(float) * (size_t)(n->dim <= kNormLongest ? kNormParts : kGainParts) * n->dim; }
 
 }  // namespace circ
 
@@ -482,8 +484,8 @@ using namespace circ;
 extern "C" {
 
 circ_norm_handle circ_norm_create(int dim, float eps) {
-    if (dim < 1) {
-        set_error(CIRC_ERR_SHAPE, "dim=%d must be >= 1", dim);
+    if (dim < 1 || dim > (1 << 24)) {
+        set_error(CIRC_ERR_SHAPE, "dim=%d must be in [1, 2^24]", dim);
         return nullptr;
     }
     if (!(eps >= 0.f) || isinf(eps)) {
@@ -532,7 +534,7 @@ int circ_norm_set_group(circ_norm_handle h, int group) {
 int circ_norm_reserve(circ_norm_handle h) {
     Norm* n = reinterpret_cast<Norm*>(h);
     const int rc = check_norm(n, 0);
-    return rc != CIRC_OK ? rc : ensure_scratch(n->ws, sizeof(float) * kNormParts * (size_t)n->dim, 0, "circ_norm_reserve");
+    return rc != CIRC_OK ? rc : ensure_scratch(n->ws, norm_scratch(n), 0, "circ_norm_reserve");
 }
 
 int circ_norm_forward(circ_norm_handle h, const void* x, const void* residual, const float* gain, void* sum, void* y, float* y_scale,
@@ -611,7 +613,7 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    if (grad_gain && (rc = ensure_scratch(n->ws, sizeof(float) * kNormParts * (size_t)n->dim, s, "circ_norm_reserve")) != CIRC_OK) return rc;
+    if (grad_gain && (rc = ensure_scratch(n->ws, norm_scratch(n), s, "circ_norm_reserve")) != CIRC_OK) return rc;
     const NormBackward a{gain, rstd, grad_gain ? static_cast<float*>(n->ws.ptr) : nullptr, rows, n->dim};
     int parts = 0, launches = 0;
     cudaError_t err = cudaSuccess;
@@ -653,7 +655,7 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
                 ++launches;
             }
             if (grad_gain && err == cudaSuccess) {
-                parts = rows < 64 ? (int)rows : 64;
+                parts = rows < kGainParts ? (int)rows : kGainParts;
                 err = launch_row(norm_gain_any_kernel<TX, TY>, dim3((n->dim + 255) / 256, parts), dim3(256), 0, s, ss, ys, a);
                 ++launches;
             }

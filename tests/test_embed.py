@@ -182,6 +182,7 @@ def refused(code, call, *args):
 def test_refusals_before_any_device_call():
     refused(circ.CIRC_ERR_SHAPE, circ.circ_embed_create, 0, 8)
     refused(circ.CIRC_ERR_SHAPE, circ.circ_embed_create, 8, 0)
+    refused(circ.CIRC_ERR_SHAPE, circ.circ_embed_create, 8, (1 << 24) + 1)
     for call, args in ((circ.circ_embed_forward, (None, 64, 64, 128, 1)), (circ.circ_embed_backward, (None, 64, 64, 128, 1)),
                        (circ.circ_embed_set_dtypes, (None, 0, 0, 0)), (circ.circ_embed_set_scale, (None, 1.0)),
                        (circ.circ_embed_set_padding, (None, 0)), (circ.circ_embed_reserve, (None, 1))):

@@ -11,7 +11,7 @@ import paper_1708_08917_b200 as circ
 from row_helpers import CODE, U, device, guarded, rng, rounding, small, within
 
 F32, BF16 = torch.float32, torch.bfloat16
-SHAPES = [(1, 1), (1, 7), (5, 32), (3, 1000), (40, 257), (2, 50001), (1, 131072), (130, 2056), (9, 16384), (200, 8), (3, 70003)]
+SHAPES = [(1, 1), (1, 7), (5, 32), (3, 1000), (40, 257), (2, 50001), (1, 131072), (130, 2056), (9, 16384), (200, 8), (3, 70003), (1500, 40), (1100, 3001), (1, 500000)]
 
 
 def handle(classes, dtype, ids, ignore=-100):
@@ -204,8 +204,8 @@ def test_gradient_is_the_derivative_of_the_mean():
 
 
 @pytest.mark.gpu
-def test_captured_graph():
-    rows, classes = 50, 1000
+@pytest.mark.parametrize("rows,classes", [(50, 1000), (3, 70003), (1200, 300), (1030, 3000)])
+def test_captured_graph(rows, classes):
     z, targets = draw(rows, classes, F32, 9)
     zd, td = device(z), device(targets)
     h = handle(classes, F32, torch.int64)

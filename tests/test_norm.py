@@ -12,7 +12,7 @@ from row_helpers import CODE, U, device, guarded, rng, rounding, small, within
 
 F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
 EPS = 1e-5
-SHAPES = [(1, 1), (1, 4096), (3, 31), (5, 64), (2, 250), (17, 1001), (9, 1024), (4, 2056), (3, 8200), (2, 20000), (300, 96)]
+SHAPES = [(1, 1), (1, 4096), (3, 31), (5, 64), (2, 250), (17, 1001), (9, 1024), (4, 2056), (3, 8200), (2, 20000), (300, 96), (3, 40000), (700, 2048)]
 
 
 def handle(dim, x, y, group=0, eps=EPS):
