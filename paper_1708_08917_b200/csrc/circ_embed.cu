@@ -73,26 +73,52 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict
 // a block with the first 1/128 of the ids had half of the tokens.)  Warps take consecutive parts of the tokens, so that equal ids
 // stay in the order of their positions.  Reading the ids is what takes the time (every block reads all of them from L2), so it is done once:
 // a warp lists its tokens as it finds them.  The rows' order behind is (class, id); `slot` numbers the rows in that order.
+// (2) The work is the list of all rows, each with its reads and then its write, laid out on a line whose unit is a byte of
+// traffic per column; `workers` groups of GROUP threads take equal stretches of it, whatever the ids are.  A stretch that ends in
+// a run of more than kWholeRun tokens cuts it (the part before goes to `carry`, the part in which the row ends to `tail`); shorter
+// runs go whole to the worker they end with.  Where a stretch begins is found by the sort, by the block that knows its row.
+constexpr int kWholeRun = 64, kLongChain = 6;
+
+struct Bound {
+    int row, read;         // reads before `read` and slots before `row` lie before the bound
+};
+struct EmbedSum {
+    int* start;            // [slots + 1] first sorted token of a slot
+    int* order;            // [tokens]
+    Bound* bound;          // [workers + 1]
+    long* stretch;         // [1] length of a stretch: worker p begins at p * stretch
+    float* carry;          // [workers][dim]
+    float* tail;           // [workers][dim]
+    int* cuts;             // [2] rows that are put together from parts: from few, from more than kLongChain
+    int4* cut;             // [2][workers] (row, first worker that holds a part of it, the one in which it ends, 0), in any order
+    int vocab, dim, workers;
+    int bits, per_class, slots;     // slot = (id mod 2^bits) * per_class + id / 2^bits; those of ids >= vocab are empty
+    int read_cost, row_cost;
+    float scale;
+};
+__device__ __forceinline__ int slot_id(const EmbedSum& a, int slot) { return ((slot % a.per_class) << a.bits) + slot / a.per_class; }
+
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortUnroll = 16;
 constexpr int kSortRows = 1280, kSortListed = 160;   // table rows of a block and listed tokens of a warp: 160 + 40 KB of shared memory
 
-// The row's number within class `cls` of 2^bits classes; kNotOurs for an id of another class or for no token.  `less`: a lower class.
-// Negative ids are above every row as unsigned numbers.
+// The row's number within class `cls` of 2^bits classes; kNotOurs for an id of another class or for no token.  `less`, `all`: counts of
+// tokens of lower classes and of all classes.  Negative ids are above every row as unsigned numbers.
 constexpr unsigned kNotOurs = 0xffffffffu;
 template <typename ID>
-__device__ __forceinline__ unsigned class_row(ID id, unsigned cls, int bits, unsigned vocab, unsigned padding, bool& less) {
+__device__ __forceinline__ unsigned class_row(ID id, unsigned cls, int bits, unsigned vocab, unsigned padding, int& less, int& all) {
     const unsigned lo = (unsigned)id, own = lo & ((1u << bits) - 1);
     bool token = lo < vocab && lo != padding;
     if constexpr (sizeof(ID) == 8) token = token && (unsigned)((uint64_t)id >> 32) == 0;
-    less = token && own < cls;
+    less += token && own < cls;
+    all += token;
     return token && own == cls ? lo >> bits : kNotOurs;
 }
 
 template <typename ID>
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, int vocab, unsigned padding, int bits, int rows_per_block,
-                                                                  int* __restrict__ start, int* __restrict__ order, int* __restrict__ cuts) {
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, unsigned padding, EmbedSum a) {
+    const int rows_per_block = a.per_class;
     extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places; then the warps' lists
-    __shared__ int part[kSortWarps], below[kSortWarps];
+    __shared__ int part[kSortWarps], below[kSortWarps], valid[kSortWarps];
     pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int per_warp = ((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
@@ -100,21 +126,17 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
     int* mine = count + warp * rows_per_block;
     // the warp's tokens of this class, in order: (row, token); more than the list holds are found again from the ids
     int2* list = reinterpret_cast<int2*>(count + kSortWarps * rows_per_block) + warp * kSortListed;
-    int less = 0, listed = 0;
+    int less = 0, all = 0, listed = 0;
     // the rows of the next 16 x 32 tokens, 0xffffffff where they are not ours
     auto fetch = [&](int t0, unsigned (&row)[kSortUnroll]) {
         ID id[kSortUnroll];
 #pragma unroll
         for (int u = 0; u < kSortUnroll; ++u) id[u] = t0 + u * 32 + lane < end ? __ldg(ids + t0 + u * 32 + lane) : (ID)-1;
 #pragma unroll
-        for (int u = 0; u < kSortUnroll; ++u) {
-            bool l;
-            row[u] = class_row(id[u], blockIdx.x, bits, (unsigned)vocab, padding, l);
-            less += l;
-        }
+        for (int u = 0; u < kSortUnroll; ++u) row[u] = class_row(id[u], blockIdx.x, a.bits, (unsigned)a.vocab, padding, less, all);
     };
     for (int i = threadIdx.x; i < kSortWarps / 4 * rows_per_block; i += kSortThreads) reinterpret_cast<int4*>(count)[i] = make_int4(0, 0, 0, 0);
-    if (blockIdx.x == 0 && threadIdx.x < 2) cuts[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.cuts[threadIdx.x] = 0;
     __syncthreads();
     for (int t0 = begin; t0 < end; t0 += 32 * kSortUnroll) {
         unsigned row[kSortUnroll];
@@ -133,7 +155,11 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
         }
     }
     less = __reduce_add_sync(0xffffffffu, less);
-    if (lane == 0) below[warp] = less;
+    all = __reduce_add_sync(0xffffffffu, all);
+    if (lane == 0) {
+        below[warp] = less;
+        valid[warp] = all;
+    }
     __syncthreads();
     // exclusive sums over the block's rows; a thread takes consecutive ones
     const int rpt = (rows_per_block + kSortThreads - 1) / kSortThreads;
@@ -153,19 +179,41 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
     if (lane == 31) part[warp] = scan;
     __syncthreads();
     int place = scan - sum + __reduce_add_sync(0xffffffffu, below[lane] + (lane < warp ? part[lane] : 0));
+    const long total = (long)__reduce_add_sync(0xffffffffu, valid[lane]) * a.read_cost + (long)a.slots * a.row_cost, stretch = total / a.workers + 1;
     for (int i = 0; i < rpt; ++i) {
-        const int r = threadIdx.x * rpt + i;
-        if (r >= rows_per_block) break;
-        start[(size_t)blockIdx.x * rows_per_block + r] = place;
-        int n[kSortWarps];
+        const int r = threadIdx.x * rpt + i, slot = blockIdx.x * rows_per_block + r, first = place;
+        const bool row = r < rows_per_block;
+        long p0 = 0, p1 = 0;                    // the stretches that begin in this slot, which is [from, to) on the line
+        if (row) {
+            a.start[slot] = first;
+            int n[kSortWarps];
 #pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) n[w] = count[w * rows_per_block + r];
+            for (int w = 0; w < kSortWarps; ++w) n[w] = count[w * rows_per_block + r];
 #pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) {
-            count[w * rows_per_block + r] = place;
-            place += n[w];
+            for (int w = 0; w < kSortWarps; ++w) {
+                count[w * rows_per_block + r] = place;
+                place += n[w];
+            }
+            const long from = (long)first * a.read_cost + (long)slot * a.row_cost, to = (long)place * a.read_cost + (long)(slot + 1) * a.row_cost;
+            p0 = (from + stretch - 1) / stretch;
+            p1 = (to + stretch - 1) / stretch;
+            if (slot == a.slots - 1) {          // the end of the line, and stretches behind it
+                a.start[a.slots] = place;
+                for (long p = p1; p <= a.workers; ++p) a.bound[p] = Bound{a.slots, place};
+                *a.stretch = stretch;
+            }
         }
-        if (blockIdx.x == gridDim.x - 1 && r == rows_per_block - 1) start[(size_t)gridDim.x * rows_per_block] = place;
+        // a slot with many stretches has the whole warp's help
+        for (unsigned left = __ballot_sync(0xffffffffu, p1 > p0); left; left &= left - 1) {
+            const int src = __ffs(left) - 1, sl = __shfl_sync(0xffffffffu, slot, src), s0 = __shfl_sync(0xffffffffu, first, src);
+            const int cnt = __shfl_sync(0xffffffffu, place, src) - s0;
+            const long q0 = __shfl_sync(0xffffffffu, p0, src), q1 = __shfl_sync(0xffffffffu, p1, src);
+            const long from = (long)s0 * a.read_cost + (long)sl * a.row_cost;
+            for (long p = q0 + lane; p < q1; p += 32) {
+                const long into = (p * stretch - from + a.read_cost - 1) >> (a.read_cost == 4 ? 2 : 1);     // a read costs 2 or 4
+                a.bound[p] = Bound{sl, cnt <= kWholeRun ? s0 : s0 + (int)(into < cnt ? into : cnt)};
+            }
+        }
     }
     __syncthreads();
     // 32 tokens in their order to their rows' places; called by whole warps
@@ -177,7 +225,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
             const int rank = __popc(same & ((1u << lane) - 1)), base = mine[row];
             __syncwarp(some);
             if (rank == 0) mine[row] = base + __popc(same);
-            order[base + rank] = token;
+            a.order[base + rank] = token;
         }
         __syncwarp();
     };
@@ -196,52 +244,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
     }
 }
 
-// (2) The work is the list of all rows, each with its reads and then its write, laid out on a line whose unit is a byte of
-// traffic per column; `workers` groups of GROUP threads take equal stretches of it, whatever the ids are.  A stretch that ends in
-// a run of more than kWholeRun tokens cuts it (the part before goes to `carry`, the part in which the row ends to `tail`); shorter
-// runs go whole to the worker they end with.
-constexpr int kWholeRun = 64, kLongChain = 6;
-
-struct EmbedSum {
-    const int* start;      // [slots + 1]
-    const int* order;      // [tokens]
-    float* carry;          // [workers][dim]
-    float* tail;           // [workers][dim]
-    int* cuts;             // [2] rows that are put together from parts: from few, from more than kLongChain
-    int4* cut;             // [2][workers] (row, first worker that holds a part of it, the one in which it ends, 0), in any order
-    int vocab, dim, workers;
-    int bits, per_class, slots;     // slot = (id mod 2^bits) * per_class + id / 2^bits; those of ids >= vocab are empty
-    int read_cost, row_cost;
-    float scale;
-};
-struct Bound {
-    int row, read;         // reads before `read` and slots before `row` lie before the bound
-};
-__device__ __forceinline__ int slot_id(const EmbedSum& a, int slot) { return ((slot % a.per_class) << a.bits) + slot / a.per_class; }
-// The bounds at x0 <= x1, one search in each half of the warp; all lanes call this with the same arguments and get the same answer.
-__device__ __forceinline__ void embed_bounds(const EmbedSum& a, long x0, long x1, Bound& b0, Bound& b1) {
-    const int lane = threadIdx.x % 32, half = lane / 16, probe = lane % 16;
-    const long x = half ? x1 : x0;
-    auto line = [&](int v, int s) { return (long)s * a.read_cost + (long)v * a.row_cost; };
-    // the last slot v in [0, slots] with line(v) <= x: 16 probes a step, of which the first always holds
-    int lo = 0;
-    for (int n = a.slots + 1; n > 1;) {
-        const int step = (n + 15) / 16, v = lo + probe * step;
-        const bool before = v <= a.slots && line(v, __ldg(a.start + v)) <= x;
-        const unsigned hits = __ballot_sync(0xffffffffu, before) >> (half * 16) & 0xffffu;
-        lo += (31 - __clz(hits)) * step;
-        n = step;
-    }
-    const int s = __ldg(a.start + lo), cnt = lo < a.slots ? __ldg(a.start + lo + 1) - s : 0;
-    int read = s;
-    if (cnt > kWholeRun) {
-        const long into = (x - line(lo, s) + a.read_cost - 1) / a.read_cost;
-        read += (int)(into < cnt ? into : cnt);
-    }
-    b0 = Bound{__shfl_sync(0xffffffffu, lo, 0), __shfl_sync(0xffffffffu, read, 0)};
-    b1 = Bound{__shfl_sync(0xffffffffu, lo, 16), __shfl_sync(0xffffffffu, read, 16)};
-}
-
 // A thread has PARTS vectors of a row, GROUP vectors apart: enough bytes a row that the walk over rows costs little next to them.
 constexpr int kSumBlocks = 4;        // resident blocks of 256 threads on an SM, 48 KB of ring each
 constexpr int ring_depth(int bytes) { return bytes <= 16 ? 12 : 6; }
@@ -256,9 +258,7 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
     const int p = blockIdx.x * (256 / GROUP) + threadIdx.x / GROUP, lane = threadIdx.x % 32;
     if (p >= a.workers) return;      // whole warps: GROUP is a multiple of 32
     const int col = (int)(blockIdx.y * (PARTS * GROUP) + threadIdx.x % GROUP) * VEC;
-    const long total = (long)__ldg(a.start + a.slots) * a.read_cost + (long)a.slots * a.row_cost;
-    Bound from, to;
-    embed_bounds(a, (long)((double)total * p / a.workers), p + 1 == a.workers ? total : (long)((double)total * (p + 1) / a.workers), from, to);
+    const Bound from = a.bound[p], to = a.bound[p + 1];
     int j = from.read, ahead = j, tokens = 0, slot = 0, slot_in = 0;      // `tokens`: 32 sorted tokens, one a lane, of which `ahead` is next
     auto fetch = [&]() {
         if (ahead < to.read) {
@@ -310,10 +310,8 @@ __global__ void __launch_bounds__(256, kSumBlocks) embed_sum_kernel(EmbedSum a, 
             if (open) break;
             begun = false;
             if (blockIdx.y == 0 && threadIdx.x % GROUP == 0) {
-                const double at = (double)__ldg(a.start + v) * a.read_cost + (double)v * a.row_cost;
-                int q = (int)(at / (double)total * a.workers);                 // the stretch that holds the row's first read, up to rounding
-                while (q > 0 && (long)((double)total * q / a.workers) > (long)at) --q;
-                while ((long)((double)total * (q + 1) / a.workers) <= (long)at) ++q;
+                // the stretch that holds the row's first read
+                const int q = (int)(((long)__ldg(a.start + v) * a.read_cost + (long)v * a.row_cost) / *a.stretch);
                 const int many = p - q > kLongChain;
                 a.cut[(size_t)many * a.workers + atomicAdd(a.cuts + many, 1)] = make_int4(id, q, p, 0);
             }
@@ -512,7 +510,7 @@ __global__ void __launch_bounds__(256, 4) embed_few_kernel(const ID* __restrict_
 // Launch shape of a backward call and its pieces of the workspace.
 struct EmbedPlan {
     int bits, rows_per_block, blocks, vec, parts, group, slices, workers;
-    size_t order_at, carry_at, tail_at, cut_at, bytes;
+    size_t order_at, bound_at, carry_at, tail_at, cut_at, bytes;
 };
 static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     EmbedPlan pl;
@@ -536,7 +534,8 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.workers = (int)(workers < 1 ? 1 : workers);
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
     pl.order_at = up(sizeof(int) * ((size_t)pl.blocks * pl.rows_per_block + 1));
-    pl.carry_at = pl.order_at + up(sizeof(int) * (size_t)(tokens ? tokens : 1));
+    pl.bound_at = pl.order_at + up(sizeof(int) * (size_t)(tokens ? tokens : 1));
+    pl.carry_at = pl.bound_at + up(sizeof(Bound) * ((size_t)pl.workers + 1));
     pl.tail_at = pl.carry_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
     pl.cut_at = pl.tail_at + up(sizeof(float) * (size_t)pl.workers * e->dim);
     pl.bytes = pl.cut_at + 256 + up(2 * sizeof(int4) * (size_t)pl.workers);
@@ -726,19 +725,17 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
     if ((rc = ensure_scratch(e->ws, embed_bytes(e, tokens), s, "circ_embed_reserve")) != CIRC_OK) return rc;
     const EmbedPlan pl = plan_embed(e, tokens, aligned);
     char* ws = static_cast<char*>(e->ws.ptr);
-    int* start = reinterpret_cast<int*>(ws);
-    int* order = reinterpret_cast<int*>(ws + pl.order_at);
-    const EmbedSum a{start, order, reinterpret_cast<float*>(ws + pl.carry_at), reinterpret_cast<float*>(ws + pl.tail_at),
-                     reinterpret_cast<int*>(ws + pl.cut_at), reinterpret_cast<int4*>(ws + pl.cut_at + 256), e->vocab, e->dim, pl.workers, pl.bits, pl.rows_per_block,
-                     pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype),
-                     (int)dtype_bytes(e->table_dtype), e->scale};
+    const EmbedSum a{reinterpret_cast<int*>(ws), reinterpret_cast<int*>(ws + pl.order_at), reinterpret_cast<Bound*>(ws + pl.bound_at),
+                     reinterpret_cast<long*>(ws + pl.cut_at + 16), reinterpret_cast<float*>(ws + pl.carry_at), reinterpret_cast<float*>(ws + pl.tail_at),
+                     reinterpret_cast<int*>(ws + pl.cut_at), reinterpret_cast<int4*>(ws + pl.cut_at + 256), e->vocab, e->dim, pl.workers, pl.bits,
+                     pl.rows_per_block, pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype), (int)dtype_bytes(e->table_dtype), e->scale};
     const size_t smem = kSortWarps * (sizeof(int) * (size_t)pl.rows_per_block + sizeof(int2) * kSortListed);
     with_index_type(e->ids_type, [&](auto* i) {
         using ID = tag_type<decltype(i)>;
         err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSortWarps * (sizeof(int) * kSortRows + sizeof(int2) * kSortListed)));
         if (err != cudaSuccess) return;
-        err = launch_row(embed_sort_kernel<ID>, dim3(pl.blocks), dim3(kSortThreads), smem, s, static_cast<const ID*>(ids), (int)tokens, e->vocab,
-                         (unsigned)e->padding, pl.bits, pl.rows_per_block, start, order, a.cuts);
+        err = launch_row(embed_sort_kernel<ID>, dim3(pl.blocks), dim3(kSortThreads), smem, s, static_cast<const ID*>(ids), (int)tokens,
+                         (unsigned)e->padding, a);
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     with_dtype(e->table_dtype, [&](auto* t) {
