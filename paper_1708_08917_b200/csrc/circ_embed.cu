@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict
 // traffic per column; `workers` groups of GROUP threads take equal stretches of it, whatever the ids are.  A stretch that ends in
 // a run of more than kWholeRun tokens cuts it (the part before goes to `carry`, the part in which the row ends to `tail`); shorter
 // runs go whole to the worker they end with.  Where a stretch begins is found by the sort, by the block that knows its row.
-constexpr int kWholeRun = 64, kLongChain = 6;
+constexpr int kWholeRun = 16, kLongChain = 6;
 
 struct Bound {
     int row, read;         // reads before `read` and slots before `row` lie before the bound
@@ -99,7 +99,8 @@ struct EmbedSum {
 __device__ __forceinline__ int slot_id(const EmbedSum& a, int slot) { return ((slot % a.per_class) << a.bits) + slot / a.per_class; }
 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortUnroll = 16;
-constexpr int kSortRows = 1280, kSortListed = 160;   // table rows of a block and listed tokens of a warp: 160 + 40 KB of shared memory
+constexpr int kSortRows = 1280;              // table rows of a block at most: 32 warps x 1280 counts are 160 KB of shared memory
+constexpr size_t kSortShared = 200 * 1024;   // what the counts leave of it holds the warps' lists of tokens
 
 // The row's number within class `cls` of 2^bits classes; kNotOurs for an id of another class or for no token.  `less`, `all`: counts of
 // tokens of lower classes and of all classes.  Negative ids are above every row as unsigned numbers.
@@ -115,7 +116,7 @@ __device__ __forceinline__ unsigned class_row(ID id, unsigned cls, int bits, uns
 }
 
 template <typename ID>
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, unsigned padding, EmbedSum a) {
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __restrict__ ids, int tokens, unsigned padding, int room, EmbedSum a) {
     const int rows_per_block = a.per_class;
     extern __shared__ __align__(16) int count[];   // [warp][rows_per_block], first counts, then places; then the warps' lists
     __shared__ int part[kSortWarps], below[kSortWarps], valid[kSortWarps];
@@ -124,8 +125,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
     const int per_warp = ((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
     const int begin = warp * per_warp < tokens ? warp * per_warp : tokens, end = begin + per_warp < tokens ? begin + per_warp : tokens;
     int* mine = count + warp * rows_per_block;
-    // the warp's tokens of this class, in order: (row, token); more than the list holds are found again from the ids
-    int2* list = reinterpret_cast<int2*>(count + kSortWarps * rows_per_block) + warp * kSortListed;
+    // the warp's tokens of this class, in order: (row, token); where they are more than the list has room for they are found again
+    int2* list = reinterpret_cast<int2*>(count + kSortWarps * rows_per_block) + warp * room;
     int less = 0, all = 0, listed = 0;
     // the rows of the next 16 x 32 tokens, 0xffffffff where they are not ours
     auto fetch = [&](int t0, unsigned (&row)[kSortUnroll]) {
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
             const int at = listed + __popc(some & ((1u << lane) - 1));
             if (ours) {
                 atomicAdd(mine + row[u], 1);
-                if (at < kSortListed) list[at] = make_int2((int)row[u], t0 + u * 32 + lane);
+                if (at < room) list[at] = make_int2((int)row[u], t0 + u * 32 + lane);
             }
             listed += __popc(some);
         }
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(const ID* __re
         }
         __syncwarp();
     };
-    if (listed <= kSortListed) {
+    if (listed <= room) {
         for (int i = 0; i < listed; i += 32) {
             const int2 e = i + lane < listed ? list[i + lane] : make_int2(-1, 0);
             deal((unsigned)e.x, e.y);
@@ -527,9 +528,9 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.group = threads <= 32 ? 32 : threads <= 64 ? 64 : threads <= 128 ? 128 : 256;
     pl.slices = (threads + pl.group - 1) / pl.group;
     // stretches of equal traffic, two for each place on the machine: reads take longer than writes of the same size, and the second
-    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); some rows each at least
+    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); a few rows each at least
     long workers = 2 * 148L * kSumBlocks * 256 / pl.group / pl.slices;
-    const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 15) / 16;
+    const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 3) / 4;
     if (workers > most) workers = most;
     pl.workers = (int)(workers < 1 ? 1 : workers);
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
@@ -729,13 +730,16 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                      reinterpret_cast<long*>(ws + pl.cut_at + 16), reinterpret_cast<float*>(ws + pl.carry_at), reinterpret_cast<float*>(ws + pl.tail_at),
                      reinterpret_cast<int*>(ws + pl.cut_at), reinterpret_cast<int4*>(ws + pl.cut_at + 256), e->vocab, e->dim, pl.workers, pl.bits,
                      pl.rows_per_block, pl.blocks * pl.rows_per_block, (int)dtype_bytes(e->y_dtype), (int)dtype_bytes(e->table_dtype), e->scale};
-    const size_t smem = kSortWarps * (sizeof(int) * (size_t)pl.rows_per_block + sizeof(int2) * kSortListed);
+    const int per_warp = (int)((tokens + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
+    int room = (int)((kSortShared - sizeof(int) * kSortWarps * pl.rows_per_block) / (sizeof(int2) * kSortWarps));
+    if (room > per_warp) room = per_warp;
+    const size_t smem = kSortWarps * (sizeof(int) * (size_t)pl.rows_per_block + sizeof(int2) * room);
     with_index_type(e->ids_type, [&](auto* i) {
         using ID = tag_type<decltype(i)>;
-        err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSortWarps * (sizeof(int) * kSortRows + sizeof(int2) * kSortListed)));
+        err = cudaFuncSetAttribute(embed_sort_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSortShared);
         if (err != cudaSuccess) return;
         err = launch_row(embed_sort_kernel<ID>, dim3(pl.blocks), dim3(kSortThreads), smem, s, static_cast<const ID*>(ids), (int)tokens,
-                         (unsigned)e->padding, a);
+                         (unsigned)e->padding, room, a);
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     with_dtype(e->table_dtype, [&](auto* t) {
@@ -763,7 +767,7 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
                 pl.vec == 1 ? by_group(One{}, Two{}) : by_group(Wide{}, Two{});
         });
         if (err == cudaSuccess && tokens > kWholeRun)
-            err = launch_row(embed_join_kernel<TT>, dim3(148), dim3(256), 0, s, a, static_cast<TT*>(grad_table));
+            err = launch_row(embed_join_kernel<TT>, dim3(148 * 4), dim3(256), 0, s, a, static_cast<TT*>(grad_table));
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(2 + (tokens > kWholeRun));
