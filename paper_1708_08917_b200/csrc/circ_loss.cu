@@ -25,7 +25,8 @@ struct LossArgs {
     long ld, grad_ld;
     float *row_loss, *lse, *mean;
     int* count;          // rows with a target, from loss_count_kernel; NULL: the block counts them itself
-    unsigned* done;      // blocks that have written their row losses (0 before and after a call)
+    unsigned* done;      // blocks that have written their sums (0 before and after a call)
+    double2* sums;       // [blocks] sum of a block's row losses, and its rows with a target
     float grad_mean;
     int rows, classes;
     long ignore;
@@ -169,18 +170,20 @@ struct RowResult {
     float factor;      // gradient = exponential * factor, less `hot` at the target
     float hot;
     bool zero;         // no gradient
+    bool valid;        // has a target
+    float loss;        // 0 without one
 };
 template <typename ID>
 __device__ __forceinline__ RowResult finish_row(const LossArgs& a, int row, Softmax all, ID target, float target_score, int count, bool writes) {
-    RowResult r{Exponent(all.top), 0.f, 0.f, false};
-    const bool valid = has_target(target, a.classes, a.ignore);
+    RowResult r{Exponent(all.top), 0.f, 0.f, false, has_target(target, a.classes, a.ignore), 0.f};
     if (writes) {
         const float log_sum = logf(all.sum), lse = r.ex.top + log_sum;
-        if (a.lse) a.lse[row] = lse;
         // the difference of the two scores first: it is small where both are large
-        if (a.row_loss) a.row_loss[row] = !valid ? 0.f : target_score == -INFINITY && lse == lse ? INFINITY : (r.ex.top - target_score) + log_sum;
+        if (r.valid) r.loss = target_score == -INFINITY && lse == lse ? INFINITY : (r.ex.top - target_score) + log_sum;
+        if (a.lse) a.lse[row] = lse;
+        if (a.row_loss) a.row_loss[row] = r.loss;
     }
-    r.zero = !valid || all.sum == 0.f;
+    r.zero = !r.valid || all.sum == 0.f;
     r.hot = a.grad_mean / (float)(count < 1 ? 1 : count);
     r.factor = r.hot / (all.sum * exp2_of(r.ex.shift));
     return r;
@@ -233,41 +236,43 @@ __global__ void __launch_bounds__(1024) loss_count_kernel(LossArgs a, const ID* 
     }
 }
 
-// The block that is last to write its losses adds all of them up, in the order of the rows and in float64.  All threads call it.
-template <typename ID>
-__device__ __forceinline__ void finish_mean(const LossArgs& a, const ID* __restrict__ targets, unsigned blocks) {
+// The mean: every block leaves the sum of its rows' losses and the number of its rows with a target (`loss` and `rows` of thread 0), and
+// the block that is last to do so adds them up in the blocks' order, in float64.  All threads call it.
+__device__ __forceinline__ void finish_mean(const LossArgs& a, unsigned block, unsigned blocks, double loss, int rows) {
     __shared__ bool last;
-    __shared__ double sums[32];
-    __shared__ int counts[32];
+    __shared__ double part[2][32];
     if (!a.mean) return;
-    __syncthreads();
     if (threadIdx.x == 0) {
+        a.sums[block] = make_double2(loss, (double)rows);
         __threadfence();
         last = atomicAdd(a.done, 1u) == blocks - 1;
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
-    double s = 0.0;
-    int n = 0;
-    for (int r = threadIdx.x; r < a.rows; r += blockDim.x) {
-        s += (double)__ldcg(a.row_loss + r);      // 0 for a row without a target
-        n += has_target(targets[r], a.classes, a.ignore);
+    double s = 0.0, n = 0.0;
+#pragma unroll 8
+    for (unsigned b = threadIdx.x; b < blocks; b += blockDim.x) {
+        const double2 v = __ldcg(a.sums + b);
+        s += v.x;
+        n += v.y;
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    n = __reduce_add_sync(0xffffffffu, n);
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        n += __shfl_xor_sync(0xffffffffu, n, o);
+    }
     if (threadIdx.x % 32 == 0) {
-        sums[threadIdx.x / 32] = s;
-        counts[threadIdx.x / 32] = n;
+        part[0][threadIdx.x / 32] = s;
+        part[1][threadIdx.x / 32] = n;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < (int)blockDim.x / 32; ++w) {
-            sums[0] += sums[w];
-            counts[0] += counts[w];
+            s += part[0][w];
+            n += part[1][w];
         }
-        *a.mean = counts[0] ? (float)(sums[0] / counts[0]) : 0.f;
+        *a.mean = n > 0.0 ? (float)(s / n) : 0.f;
         *a.done = 0;
     }
 }
@@ -276,6 +281,8 @@ __device__ __forceinline__ void finish_mean(const LossArgs& a, const ID* __restr
 template <typename T, typename ID, int VEC, int ITEMS, bool ALIGNED, bool GRAD>
 __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
     __shared__ int part[8];
+    __shared__ float losses[8];
+    __shared__ int valid[8];
     pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 8 + warp;
     const bool live = row < a.rows;
@@ -302,8 +309,16 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
     for (int i = 0; i < ITEMS; ++i) run.take(s[i]);
     const Softmax all = warp_join(run.done());
     if (GRAD && a.count) count = __ldcg(a.count);
+    if (lane == 0) {
+        losses[warp] = 0.f;
+        valid[warp] = 0;
+    }
     if (live) {
         const RowResult r = finish_row(a, row, all, target, target_score, count, lane == 0);
+        if (lane == 0) {
+            losses[warp] = r.loss;
+            valid[warp] = r.valid;
+        }
         if constexpr (GRAD) {
             const size_t first = (size_t)row * a.grad_ld + span.shift;
             __syncwarp();      // every lane has its scores and the target's: grad may be z
@@ -312,7 +327,14 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
                 if (span.any(lane + i * 32)) write_gradient<T, VEC>(span, grad, first, lane + i * 32, s[i], r, (int)target);
         }
     }
-    finish_mean(a, targets, gridDim.x);
+    __syncthreads();
+    double sum = 0.0;
+    int rows = 0;
+    for (int w = 0; w < 8; ++w) {
+        sum += (double)losses[w];
+        rows += valid[w];
+    }
+    finish_mean(a, blockIdx.x, gridDim.x, sum, rows);
 }
 
 // ---- long rows: a block, or the blocks of a cluster, hold one ----
@@ -376,7 +398,8 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
         const int n = a.count ? 0 : __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, threads));
         if (lane == 0) counts[warp] = n;
     }
-    int count = 0, flip = 0;
+    int count = 0, flip = 0, valid = 0;
+    double losses = 0.0;
     for (int row = blockIdx.x / cluster; row < a.rows; row += rows_apart, flip ^= 1) {
         const LossPart<VEC> p(a, row, rank, cluster);
         // the vectors that are not whole: the row's first block's thread 0 or 1 has one, or -1
@@ -442,6 +465,8 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
             count = count < 1 ? 1 : count;
         }
         const RowResult r = finish_row(a, row, all, target, target_score, count, rank == 0 && tid == 0);
+        losses += (double)r.loss;
+        valid += r.valid;
         if constexpr (GRAD) {
             const size_t first = (size_t)row * a.grad_ld + p.span.shift;
             T* dst = grad + first + (size_t)(p.from + tid) * VEC;
@@ -501,39 +526,40 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
             }
         }
     }
-    if (rank == 0) finish_mean(a, targets, rows_apart);
+    if (rank == 0) finish_mean(a, blockIdx.x / cluster, rows_apart, losses, valid);
 }
 
 // ---- anything else (unaligned tensors, strides of the two matrices that do not go together, rows longer than a cluster holds) ----
 template <typename T, typename ID>
 __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
-    __shared__ Softmax part[16];
+    __shared__ Softmax part[2][16];
     __shared__ int counts[16];
     pdl_begin();
-    const int row = blockIdx.x, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const T* zr = z + (size_t)row * a.ld;
-    Running run;
-    for (int c0 = tid; c0 < a.classes; c0 += 512 * 8) {
-        float s[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = c0 + e * 512 < a.classes ? to_float(zr[c0 + e * 512]) : -INFINITY;
-        run.take(s);
-    }
-    const ID target = targets[row];
-    const bool valid = has_target(target, a.classes, a.ignore);
-    const float target_score = valid ? to_float(zr[target]) : 0.f;
-    Softmax all = warp_join(run.done());
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int n = grad && !a.count ? __reduce_add_sync(0xffffffffu, targets_of(a, targets, tid, 512)) : 0;
-    if (lane == 0) {
-        part[warp] = all;
-        counts[warp] = n;
-    }
-    __syncthreads();         // every thread has read the target's score: grad may be z
-    all = warp_join(lane < 16 ? part[lane] : Softmax{-INFINITY, 0.f});
-    int count = __reduce_add_sync(0xffffffffu, lane < 16 ? counts[lane] : 0);
-    if (grad && a.count) count = __ldcg(a.count);
-    const RowResult r = finish_row(a, row, all, target, target_score, count, tid == 0);
-    if (grad) {
+    if (lane == 0) counts[warp] = n;
+    int flip = 0, valid = 0;
+    double losses = 0.0;
+    for (int row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+        const T* zr = z + (size_t)row * a.ld;
+        Running run;
+        for (int c0 = tid; c0 < a.classes; c0 += 512 * 8) {
+            float s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = c0 + e * 512 < a.classes ? to_float(zr[c0 + e * 512]) : -INFINITY;
+            run.take(s);
+        }
+        const ID target = targets[row];
+        const float target_score = has_target(target, a.classes, a.ignore) ? to_float(zr[target]) : 0.f;
+        Softmax all = warp_join(run.done());
+        if (lane == 0) part[flip][warp] = all;
+        __syncthreads();         // every thread has read the target's score: grad may be z
+        all = warp_join(lane < 16 ? part[flip][lane] : Softmax{-INFINITY, 0.f});
+        const int count = a.count ? __ldcg(a.count) : __reduce_add_sync(0xffffffffu, lane < 16 ? counts[lane] : 0);
+        const RowResult r = finish_row(a, row, all, target, target_score, count, tid == 0);
+        losses += (double)r.loss;
+        valid += r.valid;
+        if (!grad) continue;
         T* gr = grad + (size_t)row * a.grad_ld;
         for (int c = tid; c < a.classes; c += 512) {
             const float s[1] = {to_float(zr[c])};
@@ -542,9 +568,10 @@ __global__ void __launch_bounds__(512) loss_any_kernel(const T* z, const ID* __r
             store_one(gr + c, g[0]);
         }
     }
-    finish_mean(a, targets, gridDim.x);
+    finish_mean(a, blockIdx.x, gridDim.x, losses, valid);
 }
 
+constexpr int kLossWalkers = 148 * 16;             // blocks that walk over long rows, at most
 constexpr int kCountAlone = 1024;                  // rows from which on a kernel of its own counts the targets
 constexpr size_t kLossHeld = 110 * 1024;           // bytes of a row that a block holds: two blocks an SM
 constexpr size_t kLossMost = 216 * 1024;           // one block an SM
@@ -606,13 +633,14 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
         else with_rows(std::false_type{}, gradient);
     };
     grad ? with_alignment(std::true_type{}) : with_alignment(std::false_type{});
-    if (err == cudaErrorNotSupported) err = launch_loss(1, loss_any_kernel<T, ID>, (unsigned)a.rows, 512, 0, s, z, targets, grad, a);
+    if (err == cudaErrorNotSupported) err = launch_loss(1, loss_any_kernel<T, ID>, (unsigned)(a.rows < kLossWalkers ? a.rows : kLossWalkers), 512, 0, s, z, targets, grad, a);
     return err;
 }
 
-// Workspace: the counters (256 bytes), then a row of losses for calls that want their mean alone.
+// Workspace: the counters (256 bytes), then the blocks' sums.
 static int ensure_loss(Loss* l, long rows, cudaStream_t s) {
-    const size_t need = 256 + sizeof(float) * (size_t)rows;
+    const long blocks = (rows + 7) / 8 > kLossWalkers ? (rows + 7) / 8 : kLossWalkers;
+    const size_t need = 256 + sizeof(double2) * (size_t)blocks;
     if (l->ws.bytes >= need) return CIRC_OK;
     const int rc = ensure_scratch(l->ws, need, s, "circ_loss_reserve");
     if (rc != CIRC_OK) return rc;
@@ -649,11 +677,11 @@ static int run_loss(Loss* l, const void* z, long ld, const void* targets, float*
         return CIRC_ERR_ARG;
     }
     const bool count_alone = grad && rows > kCountAlone;
-    const int rc = ensure_loss(l, mean && !row_loss ? rows : 0, s);
+    const int rc = ensure_loss(l, rows, s);
     if (rc != CIRC_OK) return rc;
     unsigned* words = static_cast<unsigned*>(l->ws.ptr);
-    if (mean && !row_loss) row_loss = reinterpret_cast<float*>(static_cast<char*>(l->ws.ptr) + 256);
-    const LossArgs a{ld, grad_ld, row_loss, lse, mean, count_alone ? reinterpret_cast<int*>(words + 1) : nullptr, words, grad_mean, (int)rows,
+    const LossArgs a{ld, grad_ld, row_loss, lse, mean, count_alone ? reinterpret_cast<int*>(words + 1) : nullptr, words,
+                     reinterpret_cast<double2*>(static_cast<char*>(l->ws.ptr) + 256), grad_mean, (int)rows,
                      l->classes, l->ignore};
     cudaError_t err = cudaSuccess;
     with_dtype(l->dtype, [&](auto* t) {

@@ -233,31 +233,28 @@ struct NormBackward {
 };
 
 // A row's reduction waits for all of its loads, so the loads of the next rows must be in flight meanwhile.  RING (rows of at most 16 KB
-// a tensor, aligned): they go to a ring of kRowsAhead rows in shared memory, in which every thread copies and reads its own vectors.
+// a tensor): they go to a ring of kRowsAhead rows in shared memory, in which every thread copies and reads its own vectors.
+// Rows that are not aligned: the blocks are a multiple of VEC, so all rows of a block start at the same place within a vector, and a
+// thread has the same columns in each of them.  A vector that is shared with the neighbouring row is copied whole, and what is not the
+// row's own is cleared when it is read; only the tensor's last vector, which may end behind it, goes by element.
 constexpr int kRowsAhead = 4;
 
 template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED, bool RING>
 __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
-    static_assert(ALIGNED || !RING, "copies of whole vectors");
     constexpr int XB = VEC * (int)sizeof(TX), YB = VEC * (int)sizeof(TY), BYTES = 2 * XB + YB;
     __shared__ __align__(16) float red[2][16];
     pdl_begin();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
     for (int i = tid; i < 2 * 16; i += threads) (&red[0][0])[i] = 0.f;
     __syncthreads();
-    // dynamic shared memory: the ring; or the share of grad_gain, where rows do not start at the same column of a vector
-    extern __shared__ __align__(16) unsigned char smem[];
-    float* share = reinterpret_cast<float*>(smem);
+    extern __shared__ __align__(16) unsigned char smem[];      // the ring
     auto place = [&](int slot, int i, int off) { return smem + (size_t)(slot * ITEMS + i) * BYTES * threads + (size_t)off * threads; };
     Pair acc[ITEMS][VEC / 2];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
         for (int e = 0; e < VEC / 2; ++e) acc[i][e] = pair_of(0.f, 0.f);
-    if (!ALIGNED && a.part) {
-        for (int c = tid; c < a.dim; c += threads) share[c] = 0.f;
-        __syncthreads();
-    }
+    const size_t size = (size_t)a.rows * a.dim;
     long ahead = blockIdx.x;
     int slot_in = 0, slot = 0;
     auto fetch = [&]() {
@@ -266,7 +263,7 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
                 const int v = tid + i * threads;
-                if (!span.any(v)) continue;
+                if (!span.any(v) || (!ALIGNED && span.at(v) + VEC > size)) continue;
                 copy_async<XB>(place(slot_in, i, 0) + tid * XB, sum + span.at(v));
                 copy_async<YB>(place(slot_in, i, XB) + tid * YB, dy + span.at(v));
                 if (ds && dx) copy_async<XB>(place(slot_in, i, XB + YB) + tid * XB, ds + span.at(v));
@@ -279,10 +276,10 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
     if constexpr (RING)
 #pragma unroll 1
         for (int u = 0; u < kRowsAhead; ++u) fetch();
-    // the gain's columns are the same for every aligned row: they stay in registers where a thread has one vector
+    // a thread's columns of the gain are the same for every row: they stay in registers where it has one vector
     constexpr bool KEEP = RING && ITEMS == 1;
     float kept[VEC];
-    if constexpr (KEEP) RowSpan<VEC, ALIGNED>(0, a.dim).load_columns(kept, a.gain, tid);
+    if constexpr (KEEP) RowSpan<VEC, ALIGNED>(blockIdx.x, a.dim).load_columns(kept, a.gain, tid);
     auto gain_of = [&](const RowSpan<VEC, ALIGNED>& span, float (&g)[VEC], int v) {
         if constexpr (KEEP) {
 #pragma unroll
@@ -301,15 +298,22 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
             asm volatile("cp.async.wait_group %0;" ::"n"(kRowsAhead - 1) : "memory");
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                if (span.any(tid + i * threads)) {
-                    sr[i].load(reinterpret_cast<const TX*>(place(slot, i, 0)) + tid * VEC);
-                    yr[i].load(reinterpret_cast<const TY*>(place(slot, i, XB)) + tid * VEC);
-                } else {
-                    sr[i].clear();
-                    yr[i].clear();
+                const int v = tid + i * threads;
+                if (!span.any(v) || (!ALIGNED && span.at(v) + VEC > size)) {
+                    span.load(sr[i], sum, v);
+                    span.load(yr[i], dy, v);
+                    if (ds && dx) span.load(cr[i], ds, v);
+                    else cr[i].clear();
+                    continue;
                 }
-                if (ds && dx && span.any(tid + i * threads)) cr[i].load(reinterpret_cast<const TX*>(place(slot, i, XB + YB)) + tid * VEC);
+                sr[i].load(reinterpret_cast<const TX*>(place(slot, i, 0)) + tid * VEC);
+                yr[i].load(reinterpret_cast<const TY*>(place(slot, i, XB)) + tid * VEC);
+                if (ds && dx) cr[i].load(reinterpret_cast<const TX*>(place(slot, i, XB + YB)) + tid * VEC);
                 else cr[i].clear();
+                if (!span.whole(v)) {
+                    sr[i].keep(span.lo(v), span.hi(v));
+                    yr[i].keep(span.lo(v), span.hi(v));
+                }
             }
             slot = slot + 1 == kRowsAhead ? 0 : slot + 1;
         } else {
@@ -335,13 +339,7 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
             for (int e = 0; e < VEC; e += 2) {
                 const Pair ys = pair_mul(yr[i].get2(e), sr[i].get2(e));
                 dots = pair_fma(ys, pair_of(g[e], g[e + 1]), dots);
-                if constexpr (ALIGNED) acc[i][e / 2] = pair_fma(ys, rs, acc[i][e / 2]);
-            }
-            if (!ALIGNED && a.part) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)     // a column is one thread's in each row, and rows are separated by the barrier below
-                    if (span.any(v) && e >= span.lo(v) && e < span.hi(v))
-                        share[span.col(v) + e] = fmaf(yr[i].get(e) * sr[i].get(e), rstd, share[span.col(v) + e]);
+                acc[i][e / 2] = pair_fma(ys, rs, acc[i][e / 2]);
             }
         }
         float lo, hi;
@@ -373,18 +371,21 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
     }
     if (!a.part) return;
     float* part = a.part + (size_t)blockIdx.x * a.dim;
-    if constexpr (ALIGNED) {
-        const RowSpan<VEC, true> span(0, a.dim);
+    const RowSpan<VEC, ALIGNED> span(blockIdx.x, a.dim);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            float out[VEC];
+    for (int i = 0; i < ITEMS; ++i) {
+        const int v = tid + i * threads;
+        if (!span.any(v)) continue;
+        float out[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; e += 2) split(acc[i][e / 2], out[e], out[e + 1]);
-            span.store(part, tid + i * threads, out);
+        for (int e = 0; e < VEC; e += 2) split(acc[i][e / 2], out[e], out[e + 1]);
+        if constexpr (ALIGNED) {
+            store_vec<VEC>(part + span.col(v), out);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e >= span.lo(v) && e < span.hi(v)) part[span.col(v) + e] = out[e];
         }
-    } else {
-        __syncthreads();
-        for (int c = tid; c < a.dim; c += threads) part[c] = share[c];
     }
 }
 
@@ -455,12 +456,33 @@ static void with_items(int items, F&& f) {
     else f(std::integral_constant<int, 8>{});
 }
 
+// Sixteen values a thread where the tensors allow it; those of a group of 32 or more share their scale.
 template <typename TO>
 __global__ void __launch_bounds__(256) norm_unpack_kernel(const uint8_t* __restrict__ y, const float* __restrict__ scale, TO* __restrict__ out,
-                                                          long count, int group) {
+                                                          long count, int group_bits) {
     pdl_begin();
-    for (long i = blockIdx.x * (long)blockDim.x + threadIdx.x; i < count; i += (long)gridDim.x * blockDim.x)
-        store_one(out + i, from_e4m3(y[i]) * scale[i / group]);
+    const long v = blockIdx.x * 256L + threadIdx.x;
+    if (v * 16 >= count) return;
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(y) + v);
+    const float s = __ldg(scale + (v * 16 >> group_bits));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = from_e4m3((uint8_t)(w[e / 4] >> (e % 4 * 8))) * s;
+    store_vec<16>(out + v * 16, x);
+}
+// Whole-row scales, or tensors that are not aligned.
+template <typename TO>
+__global__ void __launch_bounds__(256) norm_unpack_any_kernel(const uint8_t* __restrict__ y, const float* __restrict__ scale, TO* __restrict__ out,
+                                                              long rows, int dim, int group) {
+    pdl_begin();
+    for (long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const uint8_t* src = y + row * dim;
+        const float* sc = scale + row * (dim / group);
+        TO* dst = out + row * dim;
+#pragma unroll 4
+        for (int c = threadIdx.x; c < dim; c += 256) store_one(dst + c, from_e4m3(src[c]) * __ldg(sc + c / group));
+    }
 }
 
 static int check_norm(const Norm* n, long rows) {
@@ -632,23 +654,24 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
                 if (!shape.items) return false;
                 with_items(shape.items, [&](auto items) {
                     constexpr int ITEMS = decltype(items)::value;
-                    constexpr bool RING = ALIGNED && ITEMS <= 2;
+                    constexpr bool RING = ITEMS <= 2;
                     constexpr int BYTES = VEC * (2 * (int)sizeof(TX) + (int)sizeof(TY));
                     auto kernel = norm_backward_kernel<TX, TY, VEC, ITEMS, ALIGNED, RING>;
-                    const size_t smem = RING ? (size_t)kRowsAhead * ITEMS * BYTES * shape.threads : ALIGNED || !grad_gain ? 0 : sizeof(float) * (size_t)n->dim;
+                    const size_t smem = RING ? (size_t)kRowsAhead * ITEMS * BYTES * shape.threads : 0;
                     // a wave of blocks that walk the rows, some rows each, and no more shares than kNormParts
                     int per_sm = 1;
                     if ((err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024)) != cudaSuccess) return;
                     if ((err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, shape.threads, smem)) != cudaSuccess) return;
                     const long wave = 148L * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm), some = (rows + 3) / 4 > 148 ? (rows + 3) / 4 : rows < 148 ? rows : 148;
                     parts = (int)(some < wave ? some : wave);
+                    if (!ALIGNED && parts < rows) parts = parts / VEC * VEC;
                     err = launch_row(kernel, dim3(parts), dim3(shape.threads), smem, s, ss, ys, cs, xs, a);
                     ++launches;
                 });
                 return true;
             };
             const bool bases = !misaligned(sum, 16) && !misaligned(grad_y, 16) && !misaligned(grad_sum, 16) && !misaligned(grad_x, 16);
-            const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : n->dim <= 16384 && launch(std::false_type{}));
+            const bool done = bases && (n->dim % VEC == 0 && !misaligned(gain, 16) ? launch(std::true_type{}) : launch(std::false_type{}));
             if (done || err != cudaSuccess) return;
             if (grad_x) {
                 err = launch_row(norm_backward_any_kernel<TX, TY>, dim3((unsigned)rows), dim3(512), 0, s, ss, ys, cs, xs, a);
@@ -679,13 +702,19 @@ int circ_norm_unpack(circ_norm_handle h, const void* y, const float* y_scale, vo
         set_error(CIRC_ERR_ARG, "y, y_scale and out must be non-NULL and aligned to their element sizes, out_dtype CIRC_F32 or CIRC_BF16");
         return CIRC_ERR_ARG;
     }
-    const long count = rows * n->dim, need = (count + 255) / 256;
-    const unsigned blocks = (unsigned)(need < 148L * 32 ? need : 148L * 32);
+    const long count = rows * n->dim;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t err = cudaSuccess;
     with_dtype(out_dtype, [&](auto* o) {
         using TO = tag_type<decltype(o)>;
-        err = launch_row(norm_unpack_kernel<TO>, dim3(blocks), dim3(256), 0, static_cast<cudaStream_t>(stream), static_cast<const uint8_t*>(y), y_scale,
-                         static_cast<TO*>(out), count, norm_group(n));
+        const uint8_t* q = static_cast<const uint8_t*>(y);
+        TO* x = static_cast<TO*>(out);
+        if (n->group && !misaligned(y, 16) && !misaligned(out, 16) && count / 16 < (1L << 31) * 256)
+            err = launch_row(norm_unpack_kernel<TO>, dim3((unsigned)((count / 16 + 255) / 256)), dim3(256), 0, s, q, y_scale, x, count,
+                             n->group == 32 ? 5 : n->group == 64 ? 6 : 7);
+        else
+            err = launch_row(norm_unpack_any_kernel<TO>, dim3((unsigned)(rows < 148 * 8 ? rows : 148 * 8)), dim3(256), 0, s, q, y_scale, x, rows, n->dim,
+                             norm_group(n));
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(1);

@@ -168,6 +168,17 @@ struct RawVec {
                     w[e / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + e) << (e % 2 * 16);
             }
     }
+    // Keeps elements lo <= e < hi of a whole vector, zeros beside them.
+    __device__ __forceinline__ void keep(int lo, int hi) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e < lo || e >= hi) {
+                if constexpr (sizeof(T) == 4)
+                    w[e] = 0;
+                else
+                    w[e / 2] &= e % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+    }
     __device__ __forceinline__ Pair get2(int e) const { return pair_of(get(e), get(e + 1)); }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (sizeof(T) == 4)
@@ -238,6 +249,18 @@ struct RowSpan {
                 const float4 t = __ldg(reinterpret_cast<const float4*>(p + col(v) + e));
                 g[e] = t.x; g[e + 1] = t.y; g[e + 2] = t.z; g[e + 3] = t.w;
             }
+        } else if (whole(v) && col(v) + VEC + 3 <= dim && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+            // aligned loads around the vector, turned by what its first column is behind a boundary: the same for the whole row
+            float t[VEC + 4];
+            const int turn = col(v) & 3;
+            const float* q = p + col(v) - turn;
+#pragma unroll
+            for (int e = 0; e < VEC + 4; e += 4) {
+                const float4 f = __ldg(reinterpret_cast<const float4*>(q + e));
+                t[e] = f.x; t[e + 1] = f.y; t[e + 2] = f.z; t[e + 3] = f.w;
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) g[e] = turn == 0 ? t[e] : turn == 1 ? t[e + 1] : turn == 2 ? t[e + 2] : t[e + 3];
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
