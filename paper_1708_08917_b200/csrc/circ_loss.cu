@@ -219,7 +219,7 @@ __device__ __forceinline__ void write_gradient(const SPAN& span, T* grad, size_t
 template <typename ID>
 __device__ __forceinline__ int targets_of(const LossArgs& a, const ID* __restrict__ targets, int from, int step) {
     int n = 0;
-#pragma unroll 4
+#pragma unroll 16
     for (int r = from; r < a.rows; r += step) n += has_target(targets[r], a.classes, a.ignore);
     return n;
 }

@@ -232,20 +232,21 @@ struct NormBackward {
     int dim;
 };
 
-// A row's reduction waits for all of its loads, so the loads of the next rows must be in flight meanwhile.  RING (rows of at most 16 KB
-// a tensor): they go to a ring of kRowsAhead rows in shared memory, in which every thread copies and reads its own vectors.
+// A row's reduction waits for all of its loads, so the loads of the next rows must be in flight meanwhile.  RING (a vector a thread, rows
+// of at most 16 KB a tensor): they go to a ring of kRowsAhead rows in shared memory, in which every thread copies and reads its own vectors.
 // Rows that are not aligned: the blocks are a multiple of VEC, so all rows of a block start at the same place within a vector, and a
 // thread has the same columns in each of them.  A vector that is shared with the neighbouring row is copied whole, and what is not the
 // row's own is cleared when it is read; only the tensor's last vector, which may end behind it, goes by element.
 constexpr int kRowsAhead = 4;
 
 template <typename TX, typename TY, int VEC, int ITEMS, bool ALIGNED, bool RING>
-__global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
+__global__ void __launch_bounds__(RING ? 1024 : 512) norm_backward_kernel(const TX* __restrict__ sum, const TY* __restrict__ dy, const TX* ds, TX* dx, NormBackward a) {
     constexpr int XB = VEC * (int)sizeof(TX), YB = VEC * (int)sizeof(TY), BYTES = 2 * XB + YB;
-    __shared__ __align__(16) float red[2][16];
+    static_assert(!RING || ITEMS == 1, "a vector a thread");
+    __shared__ __align__(16) float red[2][32];
     pdl_begin();
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid % 32;
-    for (int i = tid; i < 2 * 16; i += threads) (&red[0][0])[i] = 0.f;
+    for (int i = tid; i < 2 * 32; i += threads) (&red[0][0])[i] = 0.f;
     __syncthreads();
     extern __shared__ __align__(16) unsigned char smem[];      // the ring
     auto place = [&](int slot, int i, int off) { return smem + (size_t)(slot * ITEMS + i) * BYTES * threads + (size_t)off * threads; };
@@ -277,11 +278,10 @@ __global__ void __launch_bounds__(512, RING && ITEMS == 1 ? 2 : 1) norm_backward
 #pragma unroll 1
         for (int u = 0; u < kRowsAhead; ++u) fetch();
     // a thread's columns of the gain are the same for every row: they stay in registers where it has one vector
-    constexpr bool KEEP = RING && ITEMS == 1;
     float kept[VEC];
-    if constexpr (KEEP) RowSpan<VEC, ALIGNED>(blockIdx.x, a.dim).load_columns(kept, a.gain, tid);
+    if constexpr (RING) RowSpan<VEC, ALIGNED>(blockIdx.x, a.dim).load_columns(kept, a.gain, tid);
     auto gain_of = [&](const RowSpan<VEC, ALIGNED>& span, float (&g)[VEC], int v) {
-        if constexpr (KEEP) {
+        if constexpr (RING) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) g[e] = kept[e];
         } else {
@@ -650,11 +650,11 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
             auto launch = [&](auto aligned) {
                 constexpr bool ALIGNED = decltype(aligned)::value;
                 const int vectors = RowSpan<VEC, ALIGNED>::most(n->dim);
-                const RowShape shape = row_shape(vectors, 1);
+                const RowShape shape = vectors <= 1024 ? RowShape{1, (vectors + 31) / 32 * 32} : row_shape(vectors, 4);
                 if (!shape.items) return false;
-                with_items(shape.items, [&](auto items) {
+                auto go = [&](auto items) {
                     constexpr int ITEMS = decltype(items)::value;
-                    constexpr bool RING = ITEMS <= 2;
+                    constexpr bool RING = ITEMS == 1;
                     constexpr int BYTES = VEC * (2 * (int)sizeof(TX) + (int)sizeof(TY));
                     auto kernel = norm_backward_kernel<TX, TY, VEC, ITEMS, ALIGNED, RING>;
                     const size_t smem = RING ? (size_t)kRowsAhead * ITEMS * BYTES * shape.threads : 0;
@@ -667,7 +667,8 @@ int circ_norm_backward(circ_norm_handle h, const void* sum, const float* gain, c
                     if (!ALIGNED && parts < rows) parts = parts / VEC * VEC;
                     err = launch_row(kernel, dim3(parts), dim3(shape.threads), smem, s, ss, ys, cs, xs, a);
                     ++launches;
-                });
+                };
+                shape.items == 1 ? go(std::integral_constant<int, 1>{}) : shape.items == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
                 return true;
             };
             const bool bases = !misaligned(sum, 16) && !misaligned(grad_y, 16) && !misaligned(grad_sum, 16) && !misaligned(grad_x, 16);
