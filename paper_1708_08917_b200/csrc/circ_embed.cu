@@ -63,6 +63,32 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const TT* __restrict
     }
 }
 
+// Rows that do not lie on 16-byte boundaries: a block has a stretch of one row, by element, eight in flight a thread.
+template <typename TT, typename TY, typename ID>
+__global__ void __launch_bounds__(256) embed_forward_any_kernel(const TT* __restrict__ table, const ID* __restrict__ ids, TY* __restrict__ y, unsigned chunks,
+                                                                unsigned vocab, int dim, float scale, unsigned padding) {
+    pdl_begin();
+    const unsigned t = blockIdx.x / chunks;
+    const int c0 = (int)(blockIdx.x - t * chunks) * (8 * blockDim.x) + threadIdx.x;
+    const ID id = __ldg(ids + t);
+    const unsigned lo = (unsigned)id;
+    bool row = lo < vocab && lo != padding;
+    if constexpr (sizeof(ID) == 8) row = row && (unsigned)((uint64_t)id >> 32) == 0;
+    const TT* src = table + (size_t)(row ? lo : 0) * dim;
+    TY* dst = y + (size_t)t * dim;
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int c = c0 + u * (int)blockDim.x;
+        v[u] = row && c < dim ? to_float(src[c]) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int c = c0 + u * (int)blockDim.x;
+        if (c < dim) store_one(dst + c, v[u] * scale);
+    }
+}
+
 // ---- backward ------------------------------------------------------------------------------------------------
 // The tokens are sorted by id (1), then every table row is the sum of its run of sorted tokens (2), and runs that were
 // cut for balance are put together (3).  Nothing is added through atomics: the order of every sum follows from the ids.
@@ -650,7 +676,7 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
         set_error(CIRC_ERR_ARG, "table, ids and y must be aligned to their element sizes");
         return CIRC_ERR_ARG;
     }
-    if (tokens > (1L << 41) / e->dim) {      // thread blocks of 2048 elements at least
+    if (tokens * ((e->dim + 2047) / 2048) > INT32_MAX) {      // thread blocks: of 1024 vectors of 8 elements, or of a row's 2048 elements
         set_error(CIRC_ERR_SHAPE, "tokens=%ld of %d elements are too many", tokens, e->dim);
         return CIRC_ERR_SHAPE;
     }
@@ -673,8 +699,13 @@ int circ_embed_forward(circ_embed_handle h, const void* table, const void* ids, 
                 if (vec)
                     tokens * (e->dim / 8) <= 148L * 256 ? go(embed_forward_kernel<TT, TY, ID, 8, 1>, 8, 1)    // one vector a thread fills the machine
                                                         : go(embed_forward_kernel<TT, TY, ID, 8, 4>, 8, 4);
-                else
-                    go(embed_forward_kernel<TT, TY, ID, 1, 8>, 1, 8);
+                else {
+                    const int threads = e->dim >= 2048 ? 256 : (e->dim + 255) / 256 * 32;
+                    const long chunks = (e->dim + 8L * threads - 1) / (8L * threads);
+                    err = launch_row(embed_forward_any_kernel<TT, TY, ID>, dim3((unsigned)(tokens * chunks)), dim3(threads), 0, s,
+                                     static_cast<const TT*>(table), static_cast<const ID*>(ids), static_cast<TY*>(y), (unsigned)chunks, e->vocab, e->dim,
+                                     e->scale, (unsigned)e->padding);
+                }
             });
         });
     });
