@@ -549,7 +549,7 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     const int wide = e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
     pl.vec = aligned && e->dim % 8 == 0 ? wide : 1;
     const int vectors = (e->dim + pl.vec - 1) / pl.vec;
-    pl.parts = vectors > 32 ? 2 : 1;
+    pl.parts = vectors <= 32 ? 1 : pl.vec == 1 ? 4 : 2;      // single elements: more of them a thread
     const int threads = (vectors + pl.parts - 1) / pl.parts;
     pl.group = threads <= 32 ? 32 : threads <= 64 ? 64 : threads <= 128 ? 128 : 256;
     pl.slices = (threads + pl.group - 1) / pl.group;
@@ -576,7 +576,8 @@ struct FewPlan {
 static FewPlan plan_few(const Embed* e, long tokens, bool aligned) {
     FewPlan f;
     f.vec = !aligned || e->dim % 8 ? 1 : e->y_dtype == CIRC_BF16 && e->table_dtype == CIRC_BF16 ? 8 : 4;
-    f.slices = (e->dim + 64 * f.vec - 1) / (64 * f.vec);
+    const int width = 64 * f.vec;                           // columns of a block: 32 lanes, 2 vectors each
+    f.slices = (e->dim + width - 1) / width;
     f.blocks = (148 * 8 + f.slices - 1) / f.slices;        // two rounds of blocks on the machine
     if (f.blocks > e->vocab) f.blocks = e->vocab;
     f.fits = tokens <= kFewTokens && f.slices <= 65535 && (e->vocab + f.blocks - 1) / f.blocks <= kFewRows;
@@ -729,8 +730,8 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool aligned = !misaligned(grad_y, 16) && !misaligned(grad_table, 16);
-    // Up to 2048 tokens in one launch, in microseconds against the three launches: 92 / 103 (65536 rows of 2048), 10 / 25 (1000 of 512),
-    // 28 / 37 (131072 of 256); only with every token in one row the three are ahead (30 / 20 at 1000 of 512).
+    // Up to 2048 tokens in one launch, in microseconds against the three launches: 92 / 100 (65536 rows of 2048), 10 / 18 (1000 of 512),
+    // 28 / 34 (131072 of 256); only with every token in one row the three are ahead (30 / 17 at 1000 of 512).
     const FewPlan few = plan_few(e, tokens, aligned);
     cudaError_t err = cudaSuccess;
     if (few.fits) {
@@ -791,11 +792,12 @@ int circ_embed_backward(circ_embed_handle h, const void* ids, const void* grad_y
             };
             using One = std::integral_constant<int, 1>;
             using Two = std::integral_constant<int, 2>;
+            using Four = std::integral_constant<int, 4>;
             using Wide = std::integral_constant<int, WIDE>;
             if (pl.parts == 1)     // at most 32 vectors a row
                 pl.vec == 1 ? go(embed_sum_kernel<TT, TY, 1, 1, 32>) : go(embed_sum_kernel<TT, TY, WIDE, 1, 32>);
             else
-                pl.vec == 1 ? by_group(One{}, Two{}) : by_group(Wide{}, Two{});
+                pl.vec == 1 ? by_group(One{}, Four{}) : by_group(Wide{}, Two{});
         });
         if (err == cudaSuccess && tokens > kWholeRun)
             err = launch_row(embed_join_kernel<TT>, dim3(148 * 4), dim3(256), 0, s, a, static_cast<TT*>(grad_table));
