@@ -278,6 +278,7 @@ __device__ __forceinline__ void finish_mean(const LossArgs& a, unsigned block, u
 }
 
 // ---- short rows: a warp holds one in registers ----
+// 65536 x 1000 bfloat16: 88 us with gradient, 48 without; a row of 2 KB does not keep a warp's loads in flight for long.
 template <typename T, typename ID, int VEC, int ITEMS, bool ALIGNED, bool GRAD>
 __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __restrict__ targets, T* grad, LossArgs a) {
     __shared__ int part[8];
@@ -341,7 +342,8 @@ __global__ void __launch_bounds__(256) loss_warp_kernel(const T* z, const ID* __
 // GRAD: the row is copied to shared memory as it arrives, summed up from there, and read there a second time for the gradient, so that
 // it crosses the memory bus once.  Every thread copies and reads its own vectors, so a vector's place is free for the next row's as
 // soon as its gradient is out: the blocks walk over the rows, and the next row streams in behind the gradient of this one.  Without a
-// gradient nothing is kept.  What bounds it next to the bus: two exponentials an element, at 16 a cycle on an SM.  The loops run over
+// gradient nothing is kept.  What bounds it next to the bus: two exponentials an element, at 16 a cycle on an SM (8192 x 50001 bfloat16: 358 us,
+// 4.6 TB/s, XU pipe 56 % busy; 306 us without any exponential; 174 us for the loss alone).  The loops run over
 // whole vectors; a row's first and last elements beside them (odd strides) are one thread's each.
 constexpr int kLossChunk = 4;     // vectors a thread in a group of copies
 
