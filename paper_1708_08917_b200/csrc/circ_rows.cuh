@@ -69,40 +69,8 @@ __device__ __forceinline__ Pair pair_mul(Pair a, Pair b) {
     return r;
 }
 
-// VEC consecutive elements <-> float32 registers: 16-byte accesses (the address must be 16-byte aligned), or VEC = 1.
-template <int VEC>
-__device__ __forceinline__ void load_vec(const float* p, float (&v)[VEC]) {
-    if constexpr (VEC == 1) {
-        v[0] = *p;
-    } else {
-#pragma unroll
-        for (int r = 0; r < VEC; r += 4) {
-            const float4 t = *reinterpret_cast<const float4*>(p + r);
-            v[r] = t.x; v[r + 1] = t.y; v[r + 2] = t.z; v[r + 3] = t.w;
-        }
-    }
-}
-template <int VEC>
-__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&v)[VEC]) {
-    if constexpr (VEC == 1) {
-        v[0] = __bfloat162float(*p);
-    } else if constexpr (VEC == 4) {      // 8 bytes
-        const uint2 t = *reinterpret_cast<const uint2*>(p);
-        v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xffff0000u);
-        v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int r = 0; r < VEC; r += 8) {
-            const uint4 t = *reinterpret_cast<const uint4*>(p + r);
-            const uint32_t u[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {     // a bfloat16 is the upper half of a float32
-                v[r + 2 * h] = __uint_as_float(u[h] << 16);
-                v[r + 2 * h + 1] = __uint_as_float(u[h] & 0xffff0000u);
-            }
-        }
-    }
-}
+// VEC float32 registers to consecutive elements: 16-byte accesses (the address must be 16-byte aligned; 8 bytes for four bfloat16), or
+// VEC = 1.
 template <int VEC, typename T>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[VEC]) {
     if constexpr (VEC == 1)

@@ -130,6 +130,16 @@ def test_nothing_but_empty_tensors_and_a_captured_graph():
     circ.circ_clip_destroy(h)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 2])
+def test_a_plan_that_cannot_be_allocated(n):
+    try:
+        circ.circ_debug_fail_alloc_after(n)
+        refused(circ.CIRC_ERR_ALLOC, circ.circ_clip_create, [100, 5], circ.CIRC_F32, circ.CIRC_F32)
+    finally:
+        circ.circ_debug_fail_alloc_after(0)
+
+
 def refused(code, call, *args):
     with pytest.raises(circ.CircError) as e:
         call(*args)

@@ -173,6 +173,25 @@ def test_backward_in_a_captured_graph_needs_its_workspace(tokens):
     circ.circ_embed_destroy(h)
 
 
+@pytest.mark.gpu
+def test_a_workspace_that_cannot_be_allocated():
+    vocab, dim, tokens = 300, 64, 3000
+    ids, dy, out = torch.randint(vocab, (tokens,), device="cuda"), torch.randn(tokens, dim, device="cuda"), torch.empty(vocab, dim, device="cuda")
+    h = handle(vocab, dim, F32, F32, torch.int64, 1.0)
+    try:
+        circ.circ_debug_fail_alloc_after(1)
+        refused(circ.CIRC_ERR_ALLOC, circ.circ_embed_backward, h, ids, dy, out, tokens, torch.cuda.current_stream())
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_embed_backward(h, ids, dy, out, tokens, torch.cuda.current_stream())     # the handle serves the next call
+        torch.cuda.synchronize()
+        assert torch.allclose(out.double(), torch.zeros(vocab, dim, device="cuda", dtype=torch.float64).index_add_(0, ids, dy.double()), atol=1e-4)
+        circ.circ_debug_fail_alloc_after(1)
+        refused(circ.CIRC_ERR_ALLOC, circ.circ_embed_reserve, h, 1 << 20)
+    finally:
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_embed_destroy(h)
+
+
 def refused(code, call, *args):
     with pytest.raises(circ.CircError) as e:
         call(*args)

@@ -223,6 +223,19 @@ def test_captured_graph(rows, classes):
     circ.circ_loss_destroy(h)
 
 
+@pytest.mark.gpu
+def test_a_workspace_that_cannot_be_allocated():
+    h = handle(64, F32, torch.int64)
+    try:
+        circ.circ_debug_fail_alloc_after(1)
+        refused(circ.CIRC_ERR_ALLOC, circ.circ_loss_reserve, h, 10)
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_loss_reserve(h, 10)
+    finally:
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_loss_destroy(h)
+
+
 def refused(code, call, *args):
     with pytest.raises(circ.CircError) as e:
         call(*args)

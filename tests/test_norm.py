@@ -264,6 +264,19 @@ def test_captured_graph():
     circ.circ_norm_destroy(h)
 
 
+@pytest.mark.gpu
+def test_a_workspace_that_cannot_be_allocated():
+    h = handle(64, F32, F32)
+    try:
+        circ.circ_debug_fail_alloc_after(1)
+        refused(circ.CIRC_ERR_ALLOC, circ.circ_norm_reserve, h)
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_norm_reserve(h)
+    finally:
+        circ.circ_debug_fail_alloc_after(0)
+        circ.circ_norm_destroy(h)
+
+
 def refused(code, call, *args):
     with pytest.raises(circ.CircError) as e:
         call(*args)
