@@ -387,6 +387,8 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
     const int rank = blockIdx.x % cluster, rows_apart = gridDim.x / cluster;
     T* kept = reinterpret_cast<T*>(held) + (size_t)tid * VEC;
     const int step = threads * VEC;
+    // the peers' shared memory may be written once their blocks run: arrived here, waited for in front of the first such write
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (lane == 0) counts[warp] = 0;
     if constexpr (GRAD) {
         const LossPart<VEC> p(a, blockIdx.x / cluster, rank, cluster);
@@ -454,6 +456,7 @@ __global__ void __launch_bounds__(512, GRAD ? 2 : 3) loss_block_kernel(const T* 
         __syncthreads();                    // the other halves of `part` and `peers` serve the next row
         all = warp_join(lane < warps ? part[flip][lane] : Softmax{-INFINITY, 0.f});
         if (cluster > 1) {
+            if (row == (int)blockIdx.x / cluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             if (tid < cluster) {            // this block's pair to every block of the cluster
                 uint32_t dst;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"((uint32_t)__cvta_generic_to_shared(&peers[flip][rank])), "r"(tid));

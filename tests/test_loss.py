@@ -137,6 +137,16 @@ def test_gradient_in_place_and_scaled(rows, classes, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes,dtype,extra", [(400, 30000, F32, 0), (400, 30001, F32, 2), (310, 60003, BF16, 0), (170, 60001, F32, 0), (90, 131073, F32, 3)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clusters_that_walk_over_several_rows(rows, classes, dtype, extra, in_place):
+    """Rows of 2, 4 and 8 blocks, two or more for each cluster that the machine holds at once: the copies of a row run behind the
+    gradient of the one before, and the places for the peers' sums are used again."""
+    z, targets = draw(rows, classes, dtype, rows)
+    check(z, targets, dtype, run(z, targets, dtype, torch.int64, classes + extra, in_place=in_place))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("masked", [-torch.inf, "lowest"])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_masked_classes_and_impossible_targets(masked, dtype):
