@@ -176,19 +176,21 @@ template <int VEC, bool ALIGNED>
 struct RowSpan {
     size_t first;      // element index of vector 0 in the tensor
     int shift, dim;    // column of its first element, <= 0
-    __device__ __forceinline__ RowSpan(long row, int d) : RowSpan(row, d, d) {}
-    __device__ __forceinline__ RowSpan(long row, int d, long stride) {
+    __host__ __device__ __forceinline__ RowSpan(long row, int d) : RowSpan(row, d, d) {}
+    __host__ __device__ __forceinline__ RowSpan(long row, int d, long stride) {
         const size_t base = (size_t)row * stride;
         first = ALIGNED ? base : base / VEC * VEC;
         shift = ALIGNED ? 0 : -(int)(base - first);
         dim = d;
     }
-    __device__ __forceinline__ int col(int v) const { return v * VEC + shift; }
-    __device__ __forceinline__ size_t at(int v) const { return first + (size_t)v * VEC; }
-    __device__ __forceinline__ bool any(int v) const { return col(v) < dim; }
-    __device__ __forceinline__ bool whole(int v) const { return ALIGNED || (col(v) >= 0 && col(v) + VEC <= dim); }
-    __device__ __forceinline__ int lo(int v) const { return col(v) < 0 ? -col(v) : 0; }
-    __device__ __forceinline__ int hi(int v) const { return dim - col(v) < VEC ? dim - col(v) : VEC; }
+    __host__ __device__ __forceinline__ int col(int v) const { return v * VEC + shift; }
+    __host__ __device__ __forceinline__ size_t at(int v) const { return first + (size_t)v * VEC; }
+    __host__ __device__ __forceinline__ bool any(int v) const { return col(v) < dim; }
+    __host__ __device__ __forceinline__ bool whole(int v) const { return ALIGNED || (col(v) >= 0 && col(v) + VEC <= dim); }
+    __host__ __device__ __forceinline__ int lo(int v) const { return col(v) < 0 ? -col(v) : 0; }
+    __host__ __device__ __forceinline__ int hi(int v) const { return dim - col(v) < VEC ? dim - col(v) : VEC; }
+    // The aligned loads of VEC + 4 columns around a vector, from its first column down to a multiple of 4, stay within the row's columns.
+    __host__ __device__ __forceinline__ bool turns(int v) const { return whole(v) && (col(v) & ~3) + VEC + 4 <= dim; }
     template <typename T>
     __device__ __forceinline__ void load(RawVec<T, VEC>& r, const T* p, int v) const {
         if (!any(v)) r.clear();
@@ -217,7 +219,7 @@ struct RowSpan {
                 const float4 t = __ldg(reinterpret_cast<const float4*>(p + col(v) + e));
                 g[e] = t.x; g[e + 1] = t.y; g[e + 2] = t.z; g[e + 3] = t.w;
             }
-        } else if (whole(v) && col(v) + VEC + 3 <= dim && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+        } else if (turns(v) && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
             // aligned loads around the vector, turned by what its first column is behind a boundary: the same for the whole row
             float t[VEC + 4];
             const int turn = col(v) & 3;
