@@ -111,6 +111,28 @@ def test_gradient(kind, tokens, vocab, dim, table, y, ids_type, offset):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,vocab,dim,share,table,y,ids_type", [(40000, 300, 24, 0.7, F32, BF16, torch.int64), (33000, 1000, 33, 1.0, F32, F32, torch.int32),
+                                                                     (50000, 2, 40, 0.8, BF16, BF16, torch.int64), (60000, 3000, 136, 0.9, BF16, F32, torch.int32)])
+def test_gradient_with_more_tokens_of_a_class_than_a_warp_lists(tokens, vocab, dim, share, table, y, ids_type):
+    """A `share` of the tokens has one id: more of a sort block's tokens than its warps have room for (800 each at most)."""
+    g = rng(tokens)
+    ids = torch.where(torch.rand(tokens, generator=g) < share, min(130, vocab - 1), torch.randint(vocab, (tokens,), generator=g))
+    dy = torch.randn(tokens, dim, generator=g).to(y)
+    scale = 0.3
+    h = handle(vocab, dim, table, y, ids_type, scale)
+    out, untouched = guarded((vocab, dim), table)
+    circ.circ_embed_backward(h, device(ids.to(ids_type)), device(dy), out, tokens, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_embed_destroy(h)
+    untouched()
+    s = float(torch.tensor(scale, dtype=F32))
+    zero = torch.zeros(vocab, dim, dtype=torch.float64)
+    ref, mag = s * zero.index_add(0, ids, dy.double()), s * zero.index_add(0, ids, dy.double().abs())
+    n = torch.bincount(ids, minlength=vocab).double()
+    within(out, ref, (n[:, None] + 2) * U * mag + rounding(table) * ref.abs() + small(table))
+
+
+@pytest.mark.gpu
 def test_gradient_is_the_derivative_of_the_lookup():
     tokens, vocab, dim, scale = 40, 11, 24, 1.5
     g = rng(5)

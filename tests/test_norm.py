@@ -143,6 +143,33 @@ def test_backward(rows, dim, x_dtype, y_dtype, carry, gain, offset):
     within(dg, terms.sum(0), (rows + 4) * U * terms.abs().sum(0) + 1e-40)
 
 
+# Rows enough that a launch has four of them in a block (at least 592), that a thread has 2, 4 or 8 vectors of a row (more than 148 rows, or
+# long ones), and that a block of the backward pass walks over more rows than its ring holds (4 rows, at most 592 blocks).
+MANY = [(700, 96), (700, 97), (700, 31), (200, 300), (200, 301), (200, 1001), (200, 2047), (150, 9001), (150, 16001), (150, 20001)]
+WALKS = [(5000, 96), (5000, 97), (3000, 1001), (2600, 2056), (1500, 2047), (150, 5001), (200, 8201), (150, 9001), (150, 20001)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim", MANY)
+@pytest.mark.parametrize("x_dtype,y_dtype,residual,gain", [(F32, F32, True, True), (BF16, BF16, True, True), (BF16, F32, False, False)])
+def test_forward_of_many_rows(rows, dim, x_dtype, y_dtype, residual, gain):
+    test_forward(rows, dim, x_dtype, y_dtype, residual, gain, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,group", [(700, 96, 32), (700, 97, 0), (700, 64, 64), (200, 1001, 0), (200, 2048, 128), (150, 9001, 0), (150, 20001, 0)])
+@pytest.mark.parametrize("x_dtype", [BF16, F32])
+def test_eight_bits_of_many_rows(rows, dim, group, x_dtype):
+    test_eight_bits(rows, dim, group, x_dtype, True, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim", WALKS)
+@pytest.mark.parametrize("x_dtype,y_dtype,carry,gain", [(F32, F32, True, True), (BF16, BF16, True, True), (BF16, F32, False, True)])
+def test_backward_of_many_rows(rows, dim, x_dtype, y_dtype, carry, gain):
+    test_backward(rows, dim, x_dtype, y_dtype, carry, gain, 0)
+
+
 @pytest.mark.gpu
 def test_gradients_are_the_derivatives_of_the_forward_pass():
     rows, dim = 6, 50
@@ -203,6 +230,25 @@ def test_gradient_in_the_place_of_the_one_that_flows_past():
     torch.cuda.synchronize()
     circ.circ_norm_destroy(h)
     assert torch.equal(dx, carry)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,dtype", [(5000, 97, BF16), (3000, 1001, F32), (200, 8201, BF16)])
+def test_gradient_of_shared_vectors_in_the_place_of_the_one_that_flows_past(rows, dim, dtype):
+    """Neighbouring rows share a vector, and other blocks have them."""
+    g = rng(4)
+    s, dy, ds = (torch.randn(rows, dim, generator=g).to(dtype) for _ in range(3))
+    rstd = torch.rsqrt((s.float() ** 2).mean(1) + EPS)
+    w = 1 + 0.2 * torch.randn(dim, generator=g)
+    h = handle(dim, dtype, dtype)
+    dx, carry = torch.empty(rows, dim, device="cuda", dtype=dtype), device(ds)
+    dg, dg2 = torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    args = (device(s), device(w), device(rstd), device(dy))
+    circ.circ_norm_backward(h, *args, carry, dx, dg, rows, torch.cuda.current_stream())
+    circ.circ_norm_backward(h, *args, carry, carry, dg2, rows, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_norm_destroy(h)
+    assert torch.equal(dx, carry) and torch.equal(dg, dg2)
 
 
 @pytest.mark.gpu
