@@ -343,7 +343,8 @@ CIRC_API int circ_pool_forward(const void* x, void* y, int N, int H, int W, int 
  *     caller, aligned to its element size.  16-byte aligned rows are the fast case, any other works.
  *   - A handle holds the sizes, the types and a workspace, no tensor.  Each handle is used by one stream at a time.
  *   - Calls only enqueue on `stream`.  A workspace that a call needs is allocated by its first call, or before by the
- *     handle's reserve call (needed before stream capture; CIRC_ERR_UNSUPPORTED otherwise).
+ *     handle's reserve call (needed before stream capture; CIRC_ERR_UNSUPPORTED otherwise).  A captured call keeps the workspace
+ *     that it was captured with, whatever later calls need, until the handle is destroyed; a replay of it is a use of the handle.
  *   - Zero rows are served (nothing is read; sums over no row are written as 0).
  *   - Sums are taken in float32 or float64 in an order that follows from the sizes, strides, alignment and ids alone: the same call
  *     gives the same bits.

@@ -195,7 +195,7 @@ circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_
     if (!current_device(&device)) return nullptr;
     Clip* c = nullptr;
     try {
-        c = new Clip{device, {}, {}, {}, 0, -1, false, {nullptr, 0}, {nullptr, 0}};
+        c = new Clip{device, {}, {}, {}, 0, -1, false, {}, {}};
         c->sizes.assign(sizes, sizes + count);
         for (int i = 0; i < count; ++i) c->types.push_back((grad_dtypes[i] == CIRC_BF16 ? 1 : 0) | (out_dtypes[i] == CIRC_BF16 ? 2 : 0));
         c->pieces.resize(pieces);

@@ -619,7 +619,7 @@ circ_embed_handle circ_embed_create(int vocab, int dim) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Embed* e = new (std::nothrow) Embed{device, vocab, dim, CIRC_F32, CIRC_F32, CIRC_I64, 1.f, -1, {nullptr, 0}};
+    Embed* e = new (std::nothrow) Embed{device, vocab, dim, CIRC_F32, CIRC_F32, CIRC_I64, 1.f, -1, {}};
     if (!e) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_embed_handle>(e);
 }

@@ -646,11 +646,13 @@ static cudaError_t dispatch_loss(const T* z, const ID* targets, T* grad, const L
 static int ensure_loss(Loss* l, long rows, cudaStream_t s) {
     const long blocks = (rows + 7) / 8 > kLossWalkers ? (rows + 7) / 8 : kLossWalkers;
     const size_t need = 256 + sizeof(double2) * (size_t)blocks;
-    if (l->ws.bytes >= need) return CIRC_OK;
+    const bool fresh = l->ws.bytes < need;
     const int rc = ensure_scratch(l->ws, need, s, "circ_loss_reserve");
-    if (rc != CIRC_OK) return rc;
+    if (rc != CIRC_OK || !fresh) return rc;
     if (cudaMemsetAsync(l->ws.ptr, 0, 256, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
-        free_on(l->device, l->ws);
+        cudaFree(l->ws.ptr);      // this one alone: graphs may hold earlier ones
+        l->ws.ptr = nullptr;
+        l->ws.bytes = 0;
         set_error(CIRC_ERR_CUDA, "clearing the workspace failed: %s", cudaGetErrorString(cudaGetLastError()));
         return CIRC_ERR_CUDA;
     }
@@ -718,7 +720,7 @@ circ_loss_handle circ_loss_create(int classes) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Loss* l = new (std::nothrow) Loss{device, classes, CIRC_F32, CIRC_I64, -100, {nullptr, 0}};
+    Loss* l = new (std::nothrow) Loss{device, classes, CIRC_F32, CIRC_I64, -100, {}};
     if (!l) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_loss_handle>(l);
 }

@@ -519,7 +519,7 @@ circ_norm_handle circ_norm_create(int dim, float eps) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Norm* n = new (std::nothrow) Norm{device, dim, eps, CIRC_F32, CIRC_F32, 0, {nullptr, 0}};
+    Norm* n = new (std::nothrow) Norm{device, dim, eps, CIRC_F32, CIRC_F32, 0, {}};
     if (!n) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_norm_handle>(n);
 }

@@ -3,6 +3,7 @@
 #pragma once
 #include <math.h>
 
+#include <new>
 #include <type_traits>
 
 #include "circ_common.cuh"
@@ -271,17 +272,32 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
     return warp_sum(v);
 }
 
-// A workspace that a handle owns: grows when a call needs more, never while the stream is being captured.
+// A workspace that a handle owns: grows when a call needs more, never while the stream is being captured.  One that a captured graph
+// holds is not freed when it is outgrown, since replays of the graph write there: it stays until the handle is destroyed.
 struct Scratch {
     void* ptr;
     size_t bytes;
+    bool in_graph;      // a call that was captured uses it
+    Scratch* outgrown;  // earlier ones that graphs hold
 };
 inline int ensure_scratch(Scratch& s, size_t need, cudaStream_t stream, const char* reserve_call) {
-    if (s.bytes >= need) return CIRC_OK;
-    if (stream_is_capturing(stream)) {
+    const bool capturing = stream_is_capturing(stream);
+    if (s.bytes >= need) {
+        s.in_graph = s.in_graph || capturing;
+        return CIRC_OK;
+    }
+    if (capturing) {
         set_error(CIRC_ERR_UNSUPPORTED, "the workspace (%zu bytes) is too small for this call (%zu bytes) and the stream is being "
                   "captured: call %s before the capture", s.bytes, need, reserve_call);
         return CIRC_ERR_UNSUPPORTED;
+    }
+    if (s.in_graph) {
+        Scratch* old = new (std::nothrow) Scratch(s);
+        if (!old) {
+            set_error(CIRC_ERR_ALLOC, "host allocation failed");
+            return CIRC_ERR_ALLOC;
+        }
+        s = Scratch{nullptr, 0, false, old};
     }
     cudaFree(s.ptr);   // implicit synchronisation: earlier calls have finished with it
     s.ptr = nullptr;
@@ -297,14 +313,18 @@ inline int ensure_scratch(Scratch& s, size_t need, cudaStream_t stream, const ch
 }
 // Frees what a handle owns on the device it was created on.
 inline void free_on(int device, Scratch& s) {
-    if (!s.ptr) return;
+    if (!s.ptr && !s.outgrown) return;
     int prev = -1;
     cudaGetDevice(&prev);
     if (prev != device) cudaSetDevice(device);
     cudaFree(s.ptr);
+    while (Scratch* old = s.outgrown) {
+        cudaFree(old->ptr);
+        s.outgrown = old->outgrown;
+        delete old;
+    }
     if (prev != device && prev >= 0) cudaSetDevice(prev);
-    s.ptr = nullptr;
-    s.bytes = 0;
+    s = Scratch{};
 }
 // The current device for a new handle; false (with the error set) when there is none.
 inline bool current_device(int* device) {

@@ -196,6 +196,32 @@ def test_backward_in_a_captured_graph_needs_its_workspace(tokens):
 
 
 @pytest.mark.gpu
+def test_a_captured_graph_keeps_its_workspace():
+    """Calls behind the capture need more and more, and other memory takes what they leave."""
+    vocab, dim, tokens = 500, 64, 3000
+    h = handle(vocab, dim, F32, F32, torch.int64, 1.0)
+    circ.circ_embed_reserve(h, tokens)
+    ids, dy = torch.randint(vocab, (tokens,), device="cuda"), torch.randn(tokens, dim, device="cuda")
+    want, out = torch.empty(vocab, dim, device="cuda"), torch.zeros(vocab, dim, device="cuda")
+    circ.circ_embed_backward(h, ids, dy, want, tokens, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        circ.circ_embed_backward(h, ids, dy, out, tokens, torch.cuda.current_stream())
+    for more in (50000, 200000, 800000):
+        ids2, dy2 = torch.randint(vocab, (more,), device="cuda"), torch.randn(more, dim, device="cuda")
+        first, again = torch.empty(vocab, dim, device="cuda"), torch.empty(vocab, dim, device="cuda")
+        circ.circ_embed_backward(h, ids2, dy2, first, more, torch.cuda.current_stream())
+        out.zero_()
+        graph.replay()
+        circ.circ_embed_backward(h, ids2, dy2, again, more, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(first, again)
+    del graph
+    circ.circ_embed_destroy(h)
+
+
+@pytest.mark.gpu
 def test_a_workspace_that_cannot_be_allocated():
     vocab, dim, tokens = 300, 64, 3000
     ids, dy, out = torch.randint(vocab, (tokens,), device="cuda"), torch.randn(tokens, dim, device="cuda"), torch.empty(vocab, dim, device="cuda")

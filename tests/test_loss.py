@@ -234,6 +234,36 @@ def test_captured_graph(rows, classes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(50, 1000), (1200, 300), (30, 70003)])
+def test_a_captured_graph_keeps_its_workspace(rows, classes):
+    """Calls behind the capture need more, and other memory takes what they leave."""
+    z, targets = draw(rows, classes, F32, 19)
+    zd, td = device(z), device(targets)
+    h = handle(classes, F32, torch.int64)
+    circ.circ_loss_reserve(h, rows)
+    mean, grad = torch.zeros(1, device="cuda"), torch.zeros_like(zd)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        circ.circ_loss_backward(h, zd, classes, td, None, None, mean, grad, classes, 1.0, rows, torch.cuda.current_stream())
+    ref = plain(z, targets)
+    for more in (20000, 400000, 1600000):                # blocks of 8 rows: 2500, 50000, 200000 sums
+        circ.circ_loss_reserve(h, more)
+        other = torch.full((more,), float("nan"), device="cuda")
+        for _ in range(2):
+            mean.zero_()
+            grad.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert abs(float(mean) - float(ref[2])) <= 1e-5 * float(ref[2]) and torch.allclose(grad.double().cpu(), ref[3], atol=1e-7)
+        eager = torch.zeros(1, device="cuda")
+        circ.circ_loss_backward(h, zd, classes, td, None, None, eager, grad, classes, 1.0, rows, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(eager, mean) and bool(other.isnan().all())
+    del graph
+    circ.circ_loss_destroy(h)
+
+
+@pytest.mark.gpu
 def test_a_workspace_that_cannot_be_allocated():
     h = handle(64, F32, torch.int64)
     try:
