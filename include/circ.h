@@ -438,7 +438,8 @@ CIRC_API void circ_loss_destroy(circ_loss_handle h);
  *   circ_clip_create      : `count` tensors of sizes[i] elements (0 is allowed); grad_dtypes[i], out_dtypes[i]: CIRC_F32 or
  *                           CIRC_BF16.  The arrays are HOST memory, read during the call.
  *   circ_clip_set_tensors : HOST arrays of `count` device addresses; outs NULL, or outs[i] = grads[i]: in place.  Must be called once
- *                           before circ_clip_forward and again when an address changes; ordered on `stream`.
+ *                           before circ_clip_forward and again when an address changes; ordered on `stream`.  A captured
+ *                           circ_clip_forward clips the tensors that were set last before its replay, wherever they are.
  *   circ_clip_forward     : norm: DEVICE float32 [1], NULL to skip.  max_norm >= 0.
  * A norm that is not finite follows the formula: NaN makes every output NaN, infinity makes them 0 (NaN where g is infinite).
  */

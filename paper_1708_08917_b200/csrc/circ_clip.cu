@@ -28,7 +28,6 @@ struct Clip {
     std::vector<long> sizes;
     std::vector<int> types;
     std::vector<ClipPiece> pieces;
-    int count;     // pieces in use
     int same_types;     // ClipPiece::types of every tensor, or -1
     bool set;
     Scratch plan, partial;
@@ -36,8 +35,10 @@ struct Clip {
 
 // A piece is a block's unit of work: 256 threads take 32 elements each, in 16-byte vectors of the gradients that are all in flight
 // together.  Pieces start on 16-byte boundaries of their tensor's gradient, but for its first one, which has up to 7 elements more in
-// front.
+// front.  A tensor's number of pieces follows from its size alone (the last one may be empty), so that a captured call stays valid for
+// other addresses.
 constexpr int kPieceElems = 8192;
+static long pieces_of(long size) { return (size + kPieceElems - 1) / kPieceElems; }
 
 // Elements in front of the first 16-byte boundary.
 template <typename T>
@@ -185,7 +186,7 @@ circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_
             set_error(CIRC_ERR_ARG, "bad dtype codes (%d, %d) of tensor %d", grad_dtypes[i], out_dtypes[i], i);
             return nullptr;
         }
-        pieces += (sizes[i] + kPieceElems - 1) / kPieceElems;
+        pieces += pieces_of(sizes[i]);
     }
     if (pieces > INT32_MAX) {
         set_error(CIRC_ERR_SHAPE, "too many elements");
@@ -195,7 +196,7 @@ circ_clip_handle circ_clip_create(int count, const long* sizes, const int* grad_
     if (!current_device(&device)) return nullptr;
     Clip* c = nullptr;
     try {
-        c = new Clip{device, {}, {}, {}, 0, -1, false, {}, {}};
+        c = new Clip{device, {}, {}, {}, -1, false, {}, {}};
         c->sizes.assign(sizes, sizes + count);
         for (int i = 0; i < count; ++i) c->types.push_back((grad_dtypes[i] == CIRC_BF16 ? 1 : 0) | (out_dtypes[i] == CIRC_BF16 ? 2 : 0));
         c->pieces.resize(pieces);
@@ -251,19 +252,19 @@ int circ_clip_set_tensors(circ_clip_handle h, const void* const* grads, void* co
             return CIRC_ERR_ARG;
         }
     }
-    size_t n = 0;      // at most the pieces that circ_clip_create made room for: a first piece is longer than the others, never shorter
+    size_t n = 0;
     for (int i = 0; i < count; ++i) {
         const size_t gb = c->types[i] & 1 ? 2 : 4, ob = c->types[i] & 2 ? 2 : 4;
         const char* g = static_cast<const char*>(grads[i]);
         char* o = outs ? static_cast<char*>(outs[i]) : const_cast<char*>(g);
-        long most = kPieceElems + (long)((16 - reinterpret_cast<uintptr_t>(g) % 16) % 16 / gb);
-        for (long at = 0; at < c->sizes[i]; ++n, most = kPieceElems) {
+        const long pieces = pieces_of(c->sizes[i]);
+        long most = kPieceElems + (long)((16 - reinterpret_cast<uintptr_t>(g) % 16) % 16 / gb), at = 0;
+        for (long k = 0; k < pieces; ++k, ++n, most = kPieceElems) {
             const long left = c->sizes[i] - at, len = left < most ? left : most;
             c->pieces[n] = ClipPiece{g + at * gb, o + at * ob, (int)len, c->types[i]};
             at += len;
         }
     }
-    c->count = (int)n;
     c->set = false;
     if (n) CIRC_CUDA_TRY(cudaMemcpyAsync(c->plan.ptr, c->pieces.data(), sizeof(ClipPiece) * n, cudaMemcpyHostToDevice, s), CIRC_ERR_CUDA);
     c->set = true;
@@ -281,7 +282,7 @@ int circ_clip_forward(circ_clip_handle h, float max_norm, float* norm, void* str
         return CIRC_ERR_ARG;
     }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int pieces = c->count, blocks = pieces < kClipBlocks ? (pieces ? pieces : 1) : kClipBlocks;
+    const int pieces = (int)c->pieces.size(), blocks = pieces < kClipBlocks ? (pieces ? pieces : 1) : kClipBlocks;
     const ClipPiece* plan = static_cast<const ClipPiece*>(c->plan.ptr);
     double* partial = static_cast<double*>(c->partial.ptr);
     CIRC_CUDA_TRY(launch_row(clip_norm_kernel, dim3(blocks), dim3(kClipThreads), 0, s, plan, pieces, partial), CIRC_ERR_CUDA);

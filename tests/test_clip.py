@@ -131,6 +131,37 @@ def test_nothing_but_empty_tensors_and_a_captured_graph():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("first,then", [(3, 0), (0, 3), (1, 5), (0, 0)])
+def test_a_captured_call_clips_the_tensors_that_were_set_last(dtype, first, then):
+    """Other addresses and other alignments, which cut the tensors at other places: sizes just above 8192 and 2 x 8192 elements have a
+    piece more or less."""
+    sizes = [8195, 8193, 16385, 100, 0, 8192]
+    h = circ.circ_clip_create(sizes, CODE[dtype], CODE[dtype])
+    norm = torch.empty(1, device="cuda")
+    graph = None
+    kept = []                              # every tensor stays allocated, also what an old plan would reach
+    for seed, offset in enumerate((first, then, first)):
+        g = rng(seed)
+        tensors = [torch.randn(n, generator=g).to(dtype) for n in sizes]
+        held, out = [device(t, offset) for t in tensors], [guarded((n,), dtype, offset) for n in sizes]
+        kept += held + [o[0] for o in out]
+        max_norm = 40.0
+        circ.circ_clip_set_tensors(h, held, [o[0] for o in out], torch.cuda.current_stream())
+        if graph is None:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                circ.circ_clip_forward(h, max_norm, norm, torch.cuda.current_stream())
+        graph.replay()
+        torch.cuda.synchronize()
+        for _, ok in out:
+            ok()
+        check([o[0] for o in out], tensors, [dtype] * len(sizes), float(norm), *plain(tensors, max_norm))
+    del graph
+    circ.circ_clip_destroy(h)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 2])
 def test_a_plan_that_cannot_be_allocated(n):
     try:
