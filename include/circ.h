@@ -441,6 +441,7 @@ CIRC_API void circ_loss_destroy(circ_loss_handle h);
  *                           before circ_clip_forward and again when an address changes; ordered on `stream`.  A captured
  *                           circ_clip_forward clips the tensors that were set last before its replay, wherever they are.
  *   circ_clip_forward     : norm: DEVICE float32 [1], NULL to skip.  max_norm >= 0.
+ * Elements whose squares leave float32's range count in full: the norm is what float32 holds of the formula's.
  * A norm that is not finite follows the formula: NaN makes every output NaN, infinity makes them 0 (NaN where g is infinite).
  */
 typedef struct circ_clip* circ_clip_handle;

@@ -47,13 +47,18 @@ __device__ __forceinline__ int head_of(const T* p) {
     return (int)((VEC - (unsigned)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) % VEC) % VEC);
 }
 
-// The sum of squares of a thread's elements of a piece; consecutive threads take consecutive vectors.
+// The sum of squares of a thread's elements of a piece; consecutive threads take consecutive vectors.  Squares that float32 does not hold
+// (a sum beyond its range, or so small that squares below the normal numbers count) are taken again of the elements times 2^-96 or
+// 2^96, which are still in registers.
+constexpr float kSquareFactor = 7.9228162514264338e28f;      // 2^96
+constexpr float kSquaresLow = 1.2621774483536189e-29f;       // 2^-96: what subnormal squares lose is below 2^-45 of a sum from here on
+
 template <typename TG>
-__device__ __forceinline__ float piece_squares(const TG* g, int count) {
+__device__ __forceinline__ double piece_squares(const TG* g, int count) {
     constexpr int VEC = 16 / (int)sizeof(TG), DEPTH = kPieceElems / kClipThreads / VEC;
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
     const int tid = threadIdx.x, front = head_of(g), head = front < count ? front : count;
-    if (tid < head) part[0] = to_float(g[tid]) * to_float(g[tid]);
+    const float first = tid < head ? to_float(g[tid]) : 0.f;
+    float last = 0.f;
     g += head;
     count -= head;
     RawVec<TG, VEC> raw[DEPTH];
@@ -67,13 +72,22 @@ __device__ __forceinline__ float piece_squares(const TG* g, int count) {
             if (u * kClipThreads + tid < whole) raw[u].load(g + (u * kClipThreads + tid) * VEC);
             else raw[u].clear();
         }
-        if (c < count) part[1] = to_float(g[c]) * to_float(g[c]);
+        if (c < count) last = to_float(g[c]);
     }
+    float part[4] = {first * first, last * last, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < DEPTH; ++u)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) part[e % 4] = fmaf(raw[u].get(e), raw[u].get(e), part[e % 4]);
-    return (part[0] + part[1]) + (part[2] + part[3]);
+    const float sum = (part[0] + part[1]) + (part[2] + part[3]);
+    if (sum >= kSquaresLow && sum < INFINITY) return (double)sum;
+    const float k = sum < 1.f ? kSquareFactor : 1.f / kSquareFactor;
+    float again = first * k * (first * k) + last * k * (last * k);
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) again = fmaf(raw[u].get(e) * k, raw[u].get(e) * k, again);
+    return (double)again / ((double)k * (double)k);
 }
 
 // Pieces are walked in order here and in reverse order by the second kernel, which so finds the last ones in the L2 cache.

@@ -162,6 +162,59 @@ def test_a_captured_call_clips_the_tensors_that_were_set_last(dtype, first, then
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("grads,outs", [(F32, F32), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("size", [1e25, 3e30, 1e19, 1e-12, 1e-20, 1e-25, 1e-38])
+@pytest.mark.parametrize("alone", [False, True])
+def test_values_whose_squares_are_no_float32(grads, outs, size, alone):
+    """All of this size, or one element of it among smaller ones: the squares overflow or vanish in float32, the norm does not."""
+    sizes = [5, 70000, 8192]
+    g = rng(17)
+    tensors = [torch.randn(n, generator=g) * size * (1e-6 if alone else 1.0) for n in sizes]
+    if alone:
+        tensors[1][12345] = size
+    tensors = [t.to(grads) for t in tensors]
+    want = plain(tensors, 0.0)[0]
+    max_norm = float(torch.tensor(want / 3, dtype=F32))
+    h = circ.circ_clip_create(sizes, CODE[grads], CODE[outs])
+    held, out = [device(t) for t in tensors], [guarded((n,), outs) for n in sizes]
+    norm = torch.empty(1, device="cuda")
+    circ.circ_clip_set_tensors(h, held, [o[0] for o in out], torch.cuda.current_stream())
+    circ.circ_clip_forward(h, max_norm, norm, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_clip_destroy(h)
+    for _, ok in out:
+        ok()
+    _, factor = plain(tensors, max_norm)
+    # a factor below float32's normal numbers has an absolute error of 2^-150
+    for o, t in zip(out, tensors):
+        ref = t.double() * factor
+        bound = (NORM + 5 * U + rounding(outs)) * ref.abs() + 2.0 ** -150 * t.double().abs() + small(outs)
+        assert bool(((o[0].double().cpu() - ref).abs() <= bound).all())
+    assert abs(float(norm) - want) <= NORM * want + 2.0 ** -150
+
+
+@pytest.mark.gpu
+def test_the_norm_adds_few_squares_in_float32():
+    """A thread adds 32 squares (33 with those in front of a boundary and behind the last vector) in four chains of at most 9 float32
+    multiply-adds and joins them by 2 additions: at most 11 roundings, all terms positive, so 11 u of the sum; float64 from there on
+    (2^-40 covers it).  The norm has half of that, and its own rounding: 6.5 u."""
+    n = 1 << 20
+    g = rng(23)
+    h = circ.circ_clip_create([n, 77777], circ.CIRC_F32, circ.CIRC_F32)
+    norm = torch.empty(1, device="cuda")
+    for scale in (1.0, 1e-4):
+        for tensors in ([scale * torch.rand(n, generator=g), scale * torch.randn(77777, generator=g)], [torch.full((n,), 0.1 * scale), torch.zeros(77777)]):
+            held = [device(t) for t in tensors]
+            out = [torch.empty_like(t) for t in held]
+            circ.circ_clip_set_tensors(h, held, out, torch.cuda.current_stream())
+            circ.circ_clip_forward(h, 1.0, norm, torch.cuda.current_stream())
+            torch.cuda.synchronize()
+            want = plain(tensors, 1.0)[0]
+            assert abs(float(norm) - want) <= (6.5 * U + 2.0 ** -40) * want
+    circ.circ_clip_destroy(h)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [1, 2])
 def test_a_plan_that_cannot_be_allocated(n):
     try:
