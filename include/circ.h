@@ -391,6 +391,9 @@ CIRC_API void circ_embed_destroy(circ_embed_handle h);
  *   circ_norm_backward   : gradients from grad_y = dL/dy and, where s is used elsewhere too, grad_sum = dL/ds (NULL: 0).
  *       grad_x    : dL/dx = dL/dresidual, may be grad_sum; NULL to skip.    grad_gain : float32 [dim], overwritten; NULL to skip.
  *       sum, rstd : of the forward pass (sum is x where there was no residual).
+ *   Both passes are float32: rows whose root mean square lies between 1e-15 (any below, where eps is larger than its square) and 1e15
+ *   keep all digits.  Beyond, digits of the gradient go first; a row whose sum of squares is no float32 has rstd 0, like a row with an
+ *   infinity.
  *   circ_norm_unpack     : out = y_scale * y of an 8-bit y, float32 or bfloat16 (out_dtype).
  *   circ_norm_reserve    : workspace of the backward calls.
  */

@@ -279,6 +279,74 @@ def test_rows_of_zeros_and_values_that_are_not_finite():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,offset", [(6, 31, 0), (6, 1024, 0), (700, 64, 0), (200, 1001, 0), (5, 4096, 1), (2, 40000, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,eps", [(1e15, 1e-5), (1e-15, 0.0), (1e-24, 1e-30)])
+def test_large_and_small_rows(rows, dim, offset, dtype, size, eps):
+    """Every second row of this size, the others of size 1."""
+    x, r, w = inputs(rows, dim, F32, True, True, dim)
+    x[::2] *= size
+    r[::2] *= size
+    x, r = x.to(dtype), r.to(dtype)
+    h = handle(dim, dtype, F32, eps=eps)
+    y, s, rstd = torch.empty(rows, dim, device="cuda"), guarded((rows, dim), dtype, offset)[0], torch.empty(rows, device="cuda")
+    circ.circ_norm_forward(h, device(x, offset), device(r, offset), device(w), s, y, None, rstd, rows, torch.cuda.current_stream())
+    h8 = handle(dim, dtype, E4M3, eps=eps)
+    q, scale, out = torch.empty(rows, dim, device="cuda", dtype=E4M3), torch.empty(rows, 1, device="cuda"), torch.empty(rows, dim, device="cuda")
+    circ.circ_norm_forward(h8, device(x, offset), device(r, offset), device(w), None, q, scale, None, rows, torch.cuda.current_stream())
+    circ.circ_norm_unpack(h8, q, scale, out, circ.CIRC_F32, rows, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_norm_destroy(h)
+    circ.circ_norm_destroy(h8)
+    _, rstd_ref, y_ref = plain_forward(x, r, w, eps)
+    c = chain(dim) / 2 + 6 * U
+    within(rstd, rstd_ref, c * rstd_ref)
+    within(y, y_ref, (c + 4 * U + rounding(F32)) * y_ref.abs() + small(F32))
+    within(out, y_ref, 1 / 16 * (1 + 2.0 ** -10) * y_ref.abs() + y_ref.abs().amax(1, keepdim=True) / 448 * 2.0 ** -9)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [31, 1024, 40000])
+def test_rows_beyond_the_range_of_their_squares(dim):
+    """A sum of squares that float32 does not hold is infinite: rstd and the row are 0."""
+    x = torch.randn(3, dim, generator=rng(9))
+    x[1] *= 1e25
+    h = handle(dim, F32, F32)
+    y, rstd = torch.empty(3, dim, device="cuda"), torch.empty(3, device="cuda")
+    circ.circ_norm_forward(h, device(x), None, None, None, y, None, rstd, 3, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_norm_destroy(h)
+    assert float(rstd[1]) == 0 and bool((y[1] == 0).all()) and bool((rstd[::2] > 0.3).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,offset", [(6, 31, 0), (6, 1024, 0), (5, 4096, 1), (700, 1001, 0), (3, 9001, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [1e12, 1e15, 1e-12, 1e-15])
+def test_gradients_of_large_and_small_rows(rows, dim, offset, dtype, size):
+    g = rng(dim + 5)
+    s = torch.randn(rows, dim, generator=g)
+    s[::2] *= size
+    s = s.to(dtype)
+    dy, w = torch.randn(rows, dim, generator=g).to(dtype), 1 + 0.2 * torch.randn(dim, generator=g)
+    rstd = (1 / torch.sqrt((s.double() ** 2).mean(1))).float()
+    h = handle(dim, dtype, dtype, eps=0.0)
+    dx, dg = torch.empty(rows, dim, device="cuda", dtype=dtype), torch.empty(dim, device="cuda")
+    circ.circ_norm_backward(h, device(s, offset), device(w), device(rstd), device(dy, offset), None, dx, dg, rows, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_norm_destroy(h)
+    k = rstd.double()[:, None]
+    unit = s.double() * k
+    u = dy.double() * w.double()
+    mean = (u * unit).mean(1, keepdim=True)
+    ref = k * (u - unit * mean)
+    bound = k * (6 * U * u.abs() + unit.abs() * (8 * U * mean.abs() + (chain(dim) + 4 * U) * (u * unit).abs().mean(1, keepdim=True)))   # as above
+    within(dx, ref, bound + 2 * U * ref.abs() + rounding(dtype) * ref.abs() + small(dtype))
+    terms = dy.double() * unit
+    within(dg, terms.sum(0), (rows + 4) * U * terms.abs().sum(0) + 1e-40)
+
+
+@pytest.mark.gpu
 def test_no_rows():
     h = handle(64, F32, F32)
     circ.circ_norm_forward(h, None, None, None, None, None, None, None, 0)
