@@ -387,7 +387,9 @@ CIRC_API void circ_embed_destroy(circ_embed_handle h);
  *       sum  : receives s, may be x or residual; NULL to skip.     rstd : float32 [rows], for the backward pass; NULL to skip.
  *       y    : [rows][dim]; the norm is taken of s before it is rounded to x_dtype.
  *       y_scale : float32 [rows][dim / group], 8-bit y only: scale = max|y| / 448 over the group (at least 2^-126; 1 where all are 0,
- *              NaN where one is not finite), y / scale rounded to the nearest e4m3 value; the value stored stands for y_scale * y.
+ *              NaN where one is not finite); y times the float32 inverse of scale (off by at most one unit of its last place), rounded
+ *              to the nearest e4m3 value: a quotient that lies within 2^-22 of the middle of two may go to either.  What is stored
+ *              stands for y_scale * y.
  *   circ_norm_backward   : gradients from grad_y = dL/dy and, where s is used elsewhere too, grad_sum = dL/ds (NULL: 0).
  *       grad_x    : dL/dx = dL/dresidual, may be grad_sum; NULL to skip.    grad_gain : float32 [dim], overwritten; NULL to skip.
  *       sum, rstd : of the forward pass (sum is x where there was no residual).

@@ -106,6 +106,24 @@ def test_eight_bits(rows, dim, group, x_dtype, residual, offset):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,dim,group", [(64, 4096, 128), (100, 1001, 0), (200, 64, 32), (2, 20000, 32)])
+@pytest.mark.parametrize("x_dtype,offset", [(BF16, 0), (F32, 1)])
+def test_eight_bits_are_the_nearest(rows, dim, group, x_dtype, offset):
+    """Codes lie at half their spacing from the quotient at most, but for what the norm (c) and the inverse of the scale are off by."""
+    x, r, w = inputs(rows, dim, x_dtype, True, True, dim)
+    h = handle(dim, x_dtype, E4M3, group)
+    width = group or dim
+    q, scale = torch.empty(rows, dim, device="cuda", dtype=E4M3), torch.empty(rows, dim // width, device="cuda")
+    circ.circ_norm_forward(h, device(x, offset), device(r, offset), device(w), None, q, scale, None, rows, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_norm_destroy(h)
+    _, _, y = plain_forward(x, r, w)
+    ratio = y.view(rows, -1, width) / scale.double().cpu()[:, :, None]
+    half = torch.exp2(torch.floor(torch.log2(ratio.abs().clamp(min=2.0 ** -6))) - 4)        # 3 bits behind the point; 2^-10 below 2^-6
+    within(q.float().view_as(ratio), ratio, half + (chain(dim) / 2 + 12 * U) * ratio.abs())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,dim", SHAPES)
 @pytest.mark.parametrize("x_dtype,y_dtype,carry,gain,offset", [(F32, F32, True, True, 0), (BF16, BF16, True, True, 0), (BF16, F32, False, True, 0),
                                                                (F32, BF16, False, False, 1), (F32, E4M3, True, True, 0)])
