@@ -281,7 +281,8 @@ CIRC_API int circ_set_spectrum_dtype(circ_handle h, int dtype);
 CIRC_API int circ_set_variant(circ_handle h, int variant);
 
 /* circ_reserve -- size the workspace for forwards up to `max_batch` samples (FC) or pixels
- * N*H*W (CONV), so that later forwards allocate nothing. */
+ * N*H*W (CONV), so that later forwards allocate nothing.  A larger workspace takes the place of the one before: a graph
+ * captured with a layer must be captured again when the layer's workspace grows (here, or in a larger call). */
 CIRC_API int circ_reserve(circ_handle h, long max_batch);
 
 /* circ_workspace_bytes -- bytes of device workspace currently held by the handle. */

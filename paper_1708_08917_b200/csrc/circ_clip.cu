@@ -3,7 +3,7 @@
 // Two launches: sums of squares (one partial sum per thread block), then the scaled copies; every block of the second
 // adds the partial sums up itself, in the same fixed order.  A norm that is not finite follows the formula (a NaN makes
 // every output NaN, an infinity makes them 0 and NaN): the caller sees it in `norm`.  Bound by memory with two reads: 676 million bfloat16 into
-// float32 in 208 + 640 us (6.5 and 6.3 TB/s); 21 million float32, half of whose second read comes from L2, in 15 + 24 us.
+// float32 in 215 + 640 us (6.3 TB/s both); 21 million float32, half of whose second read comes from L2, in 15 + 24 us.
 #include <new>
 #include <type_traits>
 #include <vector>

@@ -558,7 +558,7 @@ static EmbedPlan plan_embed(const Embed* e, long tokens, bool aligned) {
     pl.group = threads <= 32 ? 32 : threads <= 64 ? 64 : threads <= 128 ? 128 : 256;
     pl.slices = (threads + pl.group - 1) / pl.group;
     // stretches of equal traffic, two for each place on the machine: reads take longer than writes of the same size, and the second
-    // round evens that out (one / two / four rounds: 164 / 155 / 154 us at 32768 tokens of 2048, 65536 rows); a few rows each at least
+    // round evens that out (one / two / four rounds: 160 / 144 / 138 us at 32768 tokens of 2048, 65536 rows); a few rows each at least
     long workers = 2 * 148L * kSumBlocks * 256 / pl.group / pl.slices;
     const long most = (tokens + (long)pl.blocks * pl.rows_per_block + 3) / 4;
     if (workers > most) workers = most;

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(512) norm_forward_any_kernel(const TX* x, cons
 // One pass over the tensors gives both gradients: a block walks rows blockIdx.x, + gridDim.x, ..., holds a row in registers while its
 // mean(u h) is summed up, and adds grad_y h to its own columns' share of grad_gain, in registers.  The shares of the blocks go to
 // `part` [blocks][dim], and a second kernel adds them up in the blocks' order.  16384 x 4096 bfloat16 with grad_sum: 89 us, 6.0 TB/s, issue slots
-// 72 % busy; the second kernel takes 6 us more.  16384 x 4095: 121 us together.
+// two thirds busy; the second kernel takes 6 us more.  16384 x 4095: 121 us together.
 struct NormBackward {
     const float* gain;
     const float* rstd;
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(512) norm_gain_kernel(const float* __restrict_
 }
 
 constexpr int kNormParts = 148 * 4, kGainParts = 64;      // shares of grad_gain: of rows in registers at most, and of others
-constexpr int kNormLongest = 32768;                       // longest row that a block's registers hold (512 threads x 8 vectors x 8 elements)
+constexpr int kNormLongest = 32768;                       // longest row that a block's registers hold (512 threads x 8 vectors x 8 elements; 4 beside float32)
 
 // Launch shape of a row kernel: `items` vectors a thread (1, 2, 4 or 8), `threads` a multiple of 32 (at most 512); items 0: the row
 // does not fit.  Rows of one warp are put several in a block.
