@@ -20,6 +20,7 @@ CIRC_ERR_ARG, CIRC_ERR_SHAPE, CIRC_ERR_ALLOC, CIRC_ERR_CUDA, CIRC_ERR_DEVICE_TIM
 CIRC_F32, CIRC_BF16, CIRC_E4M3 = 0, 1, 2
 CIRC_I32, CIRC_I64 = 0, 1
 CIRC_POOL_MAX, CIRC_POOL_AVG, CIRC_POOL_L2 = 0, 1, 2
+CIRC_ACT_NONE, CIRC_ACT_RELU, CIRC_ACT_SILU = 0, 1, 2
 CIRC_VARIANT_AUTO, CIRC_VARIANT_FUSED, CIRC_VARIANT_STAGED, CIRC_VARIANT_TENSOR = 0, 1, 2, 3
 # include/circ_debug.h
 CIRC_STAGE_INPUT_FFT, CIRC_STAGE_CONTRACTION, CIRC_STAGE_OUTPUT_IFFT, CIRC_STAGE_FUSED = 0, 1, 2, 3
@@ -100,6 +101,28 @@ SIGNATURES = {
     "circ_clip_set_tensors": (_ci, [_vp, _vp, _vp, _vp]),
     "circ_clip_forward": (_ci, [_vp, _cf, _vp, _vp]),
     "circ_clip_destroy": (None, [_vp]),
+    "circ_top_create": (_vp, [_ci, _ci]),
+    "circ_top_set_dtypes": (_ci, [_vp, _ci, _ci]),
+    "circ_top_set_temperature": (_ci, [_vp, _cf]),
+    "circ_top_reserve": (_ci, [_vp, _cl]),
+    "circ_top_forward": (_ci, [_vp, _vp, _cl, _vp, _vp, _vp, _cl, _vp]),
+    "circ_top_destroy": (None, [_vp]),
+    "circ_distill_create": (_vp, [_ci, _ci]),
+    "circ_distill_set_dtypes": (_ci, [_vp, _ci, _ci, _ci]),
+    "circ_distill_set_temperature": (_ci, [_vp, _cf]),
+    "circ_distill_set_rest": (_ci, [_vp, _ci]),
+    "circ_distill_set_add": (_ci, [_vp, _ci]),
+    "circ_distill_reserve": (_ci, [_vp, _cl]),
+    "circ_distill_forward": (_ci, [_vp, _vp, _cl, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _cl, _vp]),
+    "circ_distill_backward": (_ci, [_vp, _vp, _cl, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _cl, _cf, _cl, _vp]),
+    "circ_distill_destroy": (None, [_vp]),
+    "circ_gnorm_create": (_vp, [_ci, _ci, _cf]),
+    "circ_gnorm_set_dtypes": (_ci, [_vp, _ci, _ci]),
+    "circ_gnorm_set_activation": (_ci, [_vp, _ci]),
+    "circ_gnorm_reserve": (_ci, [_vp, _ci, _ci, _ci]),
+    "circ_gnorm_forward": (_ci, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _vp]),
+    "circ_gnorm_backward": (_ci, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _vp]),
+    "circ_gnorm_destroy": (None, [_vp]),
     "circ_last_error": (ctypes.c_char_p, []),
     "circ_last_code": (_ci, []),
 }
@@ -468,6 +491,108 @@ def circ_clip_forward(h: int, max_norm: float, norm, stream=None) -> None:
 
 def circ_clip_destroy(h: int | None) -> None:
     load().circ_clip_destroy(h)
+
+
+# ---- operators that train a compressed network in the place of an uncompressed one ---------------------
+
+def circ_top_create(classes: int, count: int) -> int:
+    return _made(load().circ_top_create(classes, count))
+
+
+def circ_top_set_dtypes(h: int, logits_dtype: int, ids_type: int) -> None:
+    _check(load().circ_top_set_dtypes(h, logits_dtype, ids_type))
+
+
+def circ_top_set_temperature(h: int, temperature: float) -> None:
+    _check(load().circ_top_set_temperature(h, temperature))
+
+
+def circ_top_reserve(h: int, max_rows: int) -> None:
+    _check(load().circ_top_reserve(h, max_rows))
+
+
+def circ_top_forward(h: int, logits, stride: int, values, ids, lse, rows: int, stream=None) -> None:
+    """Enqueue the selection of each row's largest logits, descending, and log sum exp(logits / temperature); results that are None are skipped."""
+    _check(load().circ_top_forward(h, _rows_ptr(logits), stride, _ptr(values), _ptr(ids), _ptr(lse), rows, _stream(stream)))
+
+
+def circ_top_destroy(h: int | None) -> None:
+    load().circ_top_destroy(h)
+
+
+def circ_distill_create(classes: int, count: int) -> int:
+    return _made(load().circ_distill_create(classes, count))
+
+
+def circ_distill_set_dtypes(h: int, logits_dtype: int, values_dtype: int, ids_type: int) -> None:
+    _check(load().circ_distill_set_dtypes(h, logits_dtype, values_dtype, ids_type))
+
+
+def circ_distill_set_temperature(h: int, temperature: float) -> None:
+    _check(load().circ_distill_set_temperature(h, temperature))
+
+
+def circ_distill_set_rest(h: int, rest: int) -> None:
+    """1: the classes outside a list count as one class more (the calls need the teacher's lse then)."""
+    _check(load().circ_distill_set_rest(h, int(rest)))
+
+
+def circ_distill_set_add(h: int, add: int) -> None:
+    """1: gradients are added to what ``grad_logits`` holds."""
+    _check(load().circ_distill_set_add(h, int(add)))
+
+
+def circ_distill_reserve(h: int, max_rows: int) -> None:
+    _check(load().circ_distill_reserve(h, max_rows))
+
+
+def circ_distill_forward(h: int, logits, stride: int, values, ids, lse, weights, row_loss, student_lse, mean, rows: int, stream=None) -> None:
+    """Enqueue the divergence from the teacher's lists ``values``, ``ids`` [rows][count]; ``lse``, ``weights`` and any result may be None."""
+    _check(load().circ_distill_forward(h, _rows_ptr(logits), stride, _ptr(values), _ptr(ids), _ptr(lse), _ptr(weights), _ptr(row_loss),
+                                       _ptr(student_lse), _ptr(mean), rows, _stream(stream)))
+
+
+def circ_distill_backward(h: int, logits, stride: int, values, ids, lse, weights, row_loss, student_lse, mean, grad_logits, grad_stride: int,
+                          grad_mean: float, rows: int, stream=None) -> None:
+    """``circ_distill_forward`` and the gradient of ``grad_mean * mean`` with respect to the logits (may replace them)."""
+    _check(load().circ_distill_backward(h, _rows_ptr(logits), stride, _ptr(values), _ptr(ids), _ptr(lse), _ptr(weights), _ptr(row_loss),
+                                        _ptr(student_lse), _ptr(mean), _rows_ptr(grad_logits), grad_stride, grad_mean, rows, _stream(stream)))
+
+
+def circ_distill_destroy(h: int | None) -> None:
+    load().circ_distill_destroy(h)
+
+
+def circ_gnorm_create(channels: int, groups: int, eps: float) -> int:
+    return _made(load().circ_gnorm_create(channels, groups, eps))
+
+
+def circ_gnorm_set_dtypes(h: int, x_dtype: int, y_dtype: int) -> None:
+    _check(load().circ_gnorm_set_dtypes(h, x_dtype, y_dtype))
+
+
+def circ_gnorm_set_activation(h: int, activation: int) -> None:
+    """``activation``: CIRC_ACT_NONE, CIRC_ACT_RELU or CIRC_ACT_SILU."""
+    _check(load().circ_gnorm_set_activation(h, activation))
+
+
+def circ_gnorm_reserve(h: int, N: int, H: int, W: int) -> None:
+    _check(load().circ_gnorm_reserve(h, N, H, W))
+
+
+def circ_gnorm_forward(h: int, x, gain, bias, y, mean, rstd, N: int, H: int, W: int, stream=None) -> None:
+    """Enqueue ``y = act(gain (x - mean) rstd + bias)`` on ``x[N][H][W][channels]``; ``gain``, ``bias``, ``mean``, ``rstd`` may be None."""
+    _check(load().circ_gnorm_forward(h, _ptr(x), _ptr(gain), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), N, H, W, _stream(stream)))
+
+
+def circ_gnorm_backward(h: int, x, gain, bias, mean, rstd, grad_y, grad_x, grad_gain, grad_bias, N: int, H: int, W: int, stream=None) -> None:
+    """Enqueue the gradients of the group norm; any of ``grad_x``, ``grad_gain``, ``grad_bias`` may be None."""
+    _check(load().circ_gnorm_backward(h, _ptr(x), _ptr(gain), _ptr(bias), _ptr(mean), _ptr(rstd), _ptr(grad_y), _ptr(grad_x), _ptr(grad_gain),
+                                      _ptr(grad_bias), N, H, W, _stream(stream)))
+
+
+def circ_gnorm_destroy(h: int | None) -> None:
+    load().circ_gnorm_destroy(h)
 
 
 # ---- include/circ_debug.h: test and measurement aids ------------------------------------------------
