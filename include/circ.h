@@ -469,7 +469,9 @@ CIRC_API void circ_clip_destroy(circ_clip_handle h);
  *   circ_top_forward         : logits [rows] of `stride` elements (>= classes).  Any of the three results may be NULL:
  *       values : [rows][count], descending        ids : [rows][count], their classes; equal scores: the lower class first
  *       lse    : float32 [rows], log sum exp(logits / temperature) over all classes
- * A NaN counts as larger than anything else.  Classes masked with -inf come last, in their order.
+ *   circ_top_reserve         : workspace for calls of up to max_rows rows.
+ * A NaN counts as larger than anything else.  Classes masked with -inf come last, in their order.  Equal zeros of either sign are +0 in
+ * values.
  */
 typedef struct circ_top* circ_top_handle;
 CIRC_API circ_top_handle circ_top_create(int classes, int count);
