@@ -36,20 +36,22 @@ struct DistillArgs {
     float *row_loss, *student_lse, *mean;
     float grad_mean;
     int rows;
-    int pieces, per;          // pieces a row, vectors a piece
+    int pieces, per;          // pieces a row, vectors a piece (0: all)
     bool add;
     // workspace
-    unsigned* done;           // rows that are finished (0 before and after a call)
-    double* weight_sum;
+    unsigned* done;           // groups of rows that are finished (0 before and after a call)
+    double *weight_sum, *weight_total;      // found with the mean; found beforehand
     unsigned* arrived;        // [rows] pieces that are summed up (0 before and after a call)
+    unsigned* grouped;        // [rows / 64] rows that are finished (0 before and after a call)
     double2* sums;            // [rows] weight loss, weight
+    double2* group_sums;      // [rows / 64]
     RowPlan* plans;           // [rows]
     Listed* listed;           // [rows][count]
     Softmax* parts;           // [rows][pieces]
 };
 
 constexpr int kPieceBits = 32768;        // classes a piece, at most: a bit each says which are listed
-constexpr int kPieceThreads = 256;
+constexpr int kPieceThreads = 256;       // of the gradient's pieces
 
 template <int VEC>
 struct Piece {
@@ -58,7 +60,7 @@ struct Piece {
     __device__ __forceinline__ Piece(const DistillArgs& a, long row, int piece) : span(row, a.side.classes, a.ld) {
         const int vectors = (a.side.classes - span.shift + VEC - 1) / VEC;
         from = piece * a.per;
-        to = min(vectors, from + a.per);
+        to = a.per ? min(vectors, from + a.per) : vectors;
     }
     // Place of a class in the piece, or -1.
     __device__ __forceinline__ int place(long id) const {
@@ -66,6 +68,438 @@ struct Piece {
         return id >= 0 && id < span.dim && at >= 0 && at < (long)(to - from) * VEC ? (int)at : -1;
     }
 };
+template <int VEC>
+__device__ __forceinline__ unsigned marks_of(const uint32_t* marks, int v) {       // v: vector of the piece
+    if constexpr (VEC == 8) return reinterpret_cast<const unsigned char*>(marks)[v];
+    else return (marks[v * VEC / 32] >> (v * VEC % 32)) & ((1u << VEC) - 1);
+}
+// The marked elements of a vector become -inf.
+template <typename T, int VEC>
+__device__ __forceinline__ void strike(RawVec<T, VEC>& raw, unsigned m) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        if (m >> e & 1) {
+            if constexpr (sizeof(T) == 4) raw.w[e] = 0xff800000u;
+            else raw.w[e / 2] = e % 2 ? (raw.w[e / 2] & 0xffffu) | 0xff800000u : (raw.w[e / 2] & 0xffff0000u) | 0xff80u;
+        }
+}
+
+// The mean: every row leaves weight * loss and weight; the warp that is last in a group of 64 rows adds up the group's, the one that is last of
+// all the groups', in their order, in float64.  All lanes of one warp call it.
+constexpr int kMeanGroup = 64;
+__device__ __forceinline__ void finish_mean(const DistillArgs& a, int row, double loss, double weight) {
+    const int lane = threadIdx.x % 32, group = row / kMeanGroup, groups = (a.rows + kMeanGroup - 1) / kMeanGroup;
+    bool last = false;
+    if (lane == 0) {
+        a.sums[row] = make_double2(weight * loss, weight);
+        __threadfence();
+        const unsigned size = min(kMeanGroup, a.rows - group * kMeanGroup);
+        last = atomicAdd(a.grouped + group, 1u) == size - 1;
+        if (last) a.grouped[group] = 0;
+    }
+    if (!__shfl_sync(0xffffffffu, last, 0)) return;
+    __threadfence();
+    double s = 0.0, w = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMeanGroup; i += 32)
+        if (group * kMeanGroup + i + lane < a.rows) {
+            const double2 v = __ldcg(a.sums + group * kMeanGroup + i + lane);
+            s += v.x;
+            w += v.y;
+        }
+    s = warp_sum(s);
+    w = warp_sum(w);
+    if (lane == 0) {
+        a.group_sums[group] = make_double2(s, w);
+        __threadfence();
+        last = atomicAdd(a.done, 1u) == (unsigned)groups - 1;
+        if (last) *a.done = 0;
+    }
+    if (!__shfl_sync(0xffffffffu, last, 0)) return;
+    __threadfence();
+    s = w = 0.0;
+#pragma unroll 8
+    for (int i = lane; i < groups; i += 32) {
+        const double2 v = __ldcg(a.group_sums + i);
+        s += v.x;
+        w += v.y;
+    }
+    s = warp_sum(s);
+    w = warp_sum(w);
+    if (lane == 0) {
+        if (a.mean) *a.mean = w > 0.0 ? (float)(s / w) : 0.f;
+        *a.weight_sum = w;
+    }
+}
+// The sum of the weights above 0, for a gradient that is written along with the losses.
+__global__ void __launch_bounds__(1024) distill_weights_kernel(DistillArgs a) {
+    __shared__ double part[32];
+    pdl_begin();
+    double w = 0.0;
+#pragma unroll 8
+    for (int r = threadIdx.x; r < a.rows; r += 1024) {
+        const float v = a.weights[r];
+        w += v > 0.f ? (double)v : 0.0;
+    }
+    w = warp_sum(w);
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = w;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        w = warp_sum(part[threadIdx.x]);
+        if (threadIdx.x == 0) *a.weight_total = w;
+    }
+}
+constexpr int kWeightsAlone = 512;       // rows from which on a kernel of its own adds up the weights
+// The factor that a row's gradients share; one warp calls it.
+__device__ __forceinline__ float shared_factor(const DistillArgs& a, float weight) {
+    double total = (double)a.rows;
+    if (a.weights && a.rows > kWeightsAlone) {
+        total = __ldcg(a.weight_total);
+    } else if (a.weights) {
+        total = 0.0;
+#pragma unroll 4
+        for (int r = threadIdx.x % 32; r < a.rows; r += 32) {
+            const float v = a.weights[r];
+            total += v > 0.f ? (double)v : 0.0;
+        }
+        total = warp_sum(total);
+    }
+    return (float)((double)a.grad_mean * (double)weight / total * a.side.inv_tau);
+}
+
+// Gradients of a vector: exponentials * factor, on top of what is there if `add`.
+template <bool PLAIN, typename T, int VEC>
+__device__ __forceinline__ void slopes(const RawVec<T, VEC>& raw, const Exponent& ex, float factor, bool add, const T* old, float (&g)[VEC]) {
+    float s[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[e] = raw.get(e);
+    ex.powers<PLAIN>(s, g);
+    if (add) {
+        RawVec<T, VEC> was;
+        was.load(old);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) g[e] = fmaf(g[e], factor, was.get(e));
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) g[e] *= factor;
+    }
+}
+
+// ---- rows, or pieces of them, a block each ----
+// THREADS threads sum up the classes that are not listed, four vectors at a time (the first four are on their way before the list is known); one more
+// warp has the list: it marks its classes, works out the teacher's side meanwhile, and then the row's loss.  GRAD: the row is read a second time, from
+// L2, where its block's neighbours have left room for it, and the gradient written; the list's own elements follow behind a barrier.
+// PIECES: the warp that is last to finish a row's pieces works out its loss, and with `plans` what distill_grad_kernel needs.
+template <int WARPS, int ITEMS>
+struct RowSpace {
+    uint32_t table[ITEMS * 64];
+    Softmax part[WARPS];
+    float top, factor;
+    bool zero;
+};
+constexpr int kAhead = 4;
+
+template <typename T, typename V, typename ID, int VEC, int THREADS, int ITEMS, bool GRAD, bool PIECES>
+__global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 32))
+    distill_rows_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, T* grad, DistillArgs a) {
+    static_assert(!(GRAD && PIECES) && (VEC > 1 || PIECES), "");
+    constexpr int WARPS = THREADS / 32;
+    extern __shared__ __align__(16) uint32_t marks[];
+    __shared__ RowSpace<WARPS, ITEMS> space;
+    pdl_begin();
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int row = PIECES ? blockIdx.x / a.pieces : blockIdx.x, piece = PIECES ? blockIdx.x % a.pieces : 0;
+    const float weight = a.weights ? a.weights[row] : 1.f;
+    const bool live = weight > 0.f;
+    const Piece<VEC> p(a, row, piece);
+    const int w0 = p.span.whole(p.from) ? p.from : p.from + 1, w1 = p.to > w0 && !p.span.whole(p.to - 1) ? p.to - 1 : p.to, whole = w1 - w0;
+    const T* zr = z + (size_t)row * a.ld;
+    // the vectors that are not whole: one for each of the first two threads, or -1
+    const int rest = tid == 0 && w0 > p.from ? p.from : tid == 1 && w1 < p.to ? p.to - 1 : -1;
+    if (warp == WARPS) {
+        TeacherList<ITEMS> list;
+        float old[ITEMS];
+        if (live) {
+            list.fetch(a.side, values, ids, (size_t)row, zr);
+            if (GRAD && a.add)
+#pragma unroll
+                for (int j = 0; j < ITEMS; ++j) old[j] = list.id[j] >= 0 ? to_float(grad[(size_t)row * a.grad_ld + list.id[j]]) : 0.f;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+                const int at = list.id[j] >= 0 ? p.place(list.id[j]) : -1;
+                if (at >= 0) atomicOr(marks + at / 32, 1u << at % 32);
+            }
+            __syncthreads();
+            list.prepare(a.side, space.table);
+        }
+        const float scale = GRAD && live ? shared_factor(a, weight) : 0.f;
+        double loss = 0.0, lse = 0.0;
+        RowPlan plan{-INFINITY, 0.f, 0.f, 0};
+        float q[ITEMS];
+        bool zero = true;
+        if (live || PIECES) {
+            Softmax outside{-INFINITY, 0.f};
+            if (live) {
+                __syncthreads();
+                outside = warp_join(lane < WARPS ? space.part[lane] : outside, a.side.scale);
+            }
+            if (PIECES && a.pieces > 1) {
+                bool last = false;
+                if (lane == 0) {
+                    a.parts[(size_t)row * a.pieces + piece] = outside;
+                    __threadfence();
+                    last = atomicAdd(a.arrived + row, 1u) == (unsigned)a.pieces - 1;
+                    if (last) a.arrived[row] = 0;
+                }
+                if (!__shfl_sync(0xffffffffu, last, 0)) return;
+                __threadfence();
+                outside = Softmax{-INFINITY, 0.f};
+                for (int i = lane; i < a.pieces; i += 32) {
+                    const float2 other = __ldcg(reinterpret_cast<const float2*>(a.parts) + (size_t)row * a.pieces + i);
+                    outside = join(outside, Softmax{other.x, other.y}, a.side.scale);
+                }
+                outside = warp_join(outside, a.side.scale);
+            }
+            if (live) {
+                const ListRow r = list.finish(a.side, outside, q);
+                loss = r.loss;
+                lse = r.lse;
+                zero = r.zero;
+                if (GRAD && lane == 0) {
+                    space.top = outside.top;
+                    space.factor = r.factor * scale;
+                    space.zero = zero;
+                }
+                if (GRAD) __syncthreads();
+                if (PIECES && a.plans) {
+                    int n = 0;
+#pragma unroll
+                    for (int j = 0; j < ITEMS; ++j) {
+                        const unsigned have = __ballot_sync(0xffffffffu, list.id[j] >= 0);
+                        if (list.id[j] >= 0) a.listed[(size_t)row * a.side.count + n + __popc(have & ((1u << lane) - 1))] = Listed{list.id[j], q[j]};
+                        n += __popc(have);
+                    }
+                    plan = RowPlan{outside.top, r.factor, zero ? 0.f : weight, n};
+                }
+            }
+        }
+        if (lane == 0) {
+            if (a.row_loss) a.row_loss[row] = (float)loss;
+            if (a.student_lse) a.student_lse[row] = (float)lse;
+            if (PIECES && a.plans) a.plans[row] = plan;
+        }
+        finish_mean(a, row, loss, live ? (double)weight : 0.0);
+        if (GRAD && live) {
+            __syncthreads();
+            if (!zero)
+#pragma unroll
+                for (int j = 0; j < ITEMS; ++j)
+                    if (list.id[j] >= 0) store_one(grad + (size_t)row * a.grad_ld + list.id[j], a.add ? fmaf(q[j], scale, old[j]) : q[j] * scale);
+        }
+        return;
+    }
+    const T* src = z + p.span.at(w0) + (size_t)tid * VEC;
+    if (live) {
+        RawVec<T, VEC> raw[kAhead];
+        const bool full = tid + (kAhead - 1) * THREADS < whole;
+        if (full)
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) raw[u].load(src + u * THREADS * VEC);
+        for (int i = tid; i < ((p.to - p.from) * VEC + 31) / 32; i += THREADS) marks[i] = 0;
+        __syncthreads();
+        __syncthreads();      // the list is marked
+        Running run(a.side.scale);
+        auto take = [&](auto& some) {
+            if constexpr (VEC > 1) {
+                run.take(some);
+            } else {
+                float s[sizeof(some) / sizeof(some[0])];
+#pragma unroll
+                for (int u = 0; u < (int)(sizeof(some) / sizeof(some[0])); ++u) s[u] = some[u].get(0);
+                run.take(s);
+            }
+        };
+        int i = tid;
+        for (bool ready = full; i + (kAhead - 1) * THREADS < whole; i += kAhead * THREADS, ready = false) {
+            if (!ready)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) raw[u].load(src + (size_t)(i - tid + u * THREADS) * VEC);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const unsigned m = marks_of<VEC>(marks, w0 - p.from + i + u * THREADS);
+                if (m) strike(raw[u], m);
+            }
+            take(raw);
+        }
+        for (; i < whole; i += THREADS) {
+            RawVec<T, VEC> one[1];
+            one[0].load(src + (size_t)(i - tid) * VEC);
+            const unsigned m = marks_of<VEC>(marks, w0 - p.from + i);
+            if (m) strike(one[0], m);
+            take(one);
+        }
+        if (rest >= 0) {
+            RawVec<T, VEC> one;
+            float s[VEC];
+            p.span.load(one, z, rest);
+            strike(one, marks_of<VEC>(marks, rest - p.from));
+            scores(p.span, rest, one, s);
+            run.take(s);
+        }
+        const Softmax all = warp_join(run.done(), a.side.scale);
+        if (lane == 0) space.part[warp] = all;
+        __syncthreads();
+    }
+    if constexpr (GRAD) {
+        bool zero = true;
+        float factor = 0.f;
+        Exponent ex(-INFINITY, a.side.scale);
+        if (live) {
+            __syncthreads();
+            zero = space.zero;
+            factor = space.factor;
+            ex = Exponent(space.top, a.side.scale);
+        }
+        T* const g0 = grad + (size_t)row * a.grad_ld + p.span.shift;
+        T* dst = g0 + (size_t)(w0 + tid) * VEC;
+        if (zero) {
+            if (!a.add) {
+                const float none[VEC] = {};
+                for (int i = tid; i < whole; i += THREADS) store_vec_once<VEC>(dst + (size_t)(i - tid) * VEC, none);
+            }
+        } else {
+            auto put = [&](auto plain) {
+                int i = tid;
+                for (; i + (kAhead - 1) * THREADS < whole; i += kAhead * THREADS) {
+                    RawVec<T, VEC> raw[kAhead];
+                    const size_t o = (size_t)(i - tid) * VEC;
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) raw[u].load(src + o + u * THREADS * VEC);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        float g[VEC];
+                        slopes<decltype(plain)::value>(raw[u], ex, factor, a.add, dst + o + u * THREADS * VEC, g);
+                        store_vec_once<VEC>(dst + o + u * THREADS * VEC, g);
+                    }
+                }
+                for (; i < whole; i += THREADS) {
+                    RawVec<T, VEC> raw;
+                    float g[VEC];
+                    const size_t o = (size_t)(i - tid) * VEC;
+                    raw.load(src + o);
+                    slopes<decltype(plain)::value>(raw, ex, factor, a.add, dst + o, g);
+                    store_vec_once<VEC>(dst + o, g);
+                }
+            };
+            if (ex.plain) put(std::true_type{});
+            else put(std::false_type{});
+        }
+        if (rest >= 0 && !(zero && a.add)) {
+            RawVec<T, VEC> raw;
+            float s[VEC], g[VEC];
+            if (zero) raw.clear();
+            else p.span.load(raw, z, rest);
+            scores(p.span, rest, raw, s);
+            ex.of(s, g);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e >= p.span.lo(rest) && e < p.span.hi(rest)) {
+                    T* at = g0 + (size_t)rest * VEC + e;
+                    store_one(at, zero ? 0.f : a.add ? fmaf(g[e], factor, to_float(*at)) : g[e] * factor);
+                }
+        }
+        if (live) __syncthreads();
+    }
+}
+
+// ---- short rows: a warp holds one in registers, and its list ----
+template <typename T, typename V, typename ID, int VEC, int N, int ITEMS, bool GRAD>
+__global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, T* grad, DistillArgs a) {
+    __shared__ uint32_t marks_of_warp[4][N * VEC], tables[4][ITEMS * 64];
+    pdl_begin();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 4 + warp;
+    if (row >= a.rows) return;
+    uint32_t* marks = marks_of_warp[warp];
+    const float weight = a.weights ? a.weights[row] : 1.f;
+    const bool live = weight > 0.f;
+    const Piece<VEC> p(a, row, 0);
+    const auto& span = p.span;
+    T* const gr = GRAD ? grad + (size_t)row * a.grad_ld : nullptr;
+    double loss = 0.0, lse = 0.0;
+    bool zero = true;
+    if (live) {
+        RawVec<T, VEC> raw[N];
+        float s[N][VEC];
+        TeacherList<ITEMS> list;
+        list.fetch(a.side, values, ids, (size_t)row, z + (size_t)row * a.ld);
+#pragma unroll
+        for (int i = 0; i < N; ++i) span.load(raw[i], z, i * 32 + lane);
+        for (int i = lane; i < N * VEC; i += 32) marks[i] = 0;
+        __syncwarp();
+        float old[ITEMS];
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j)
+            if (list.id[j] >= 0) {
+                const int at = p.place(list.id[j]);
+                atomicOr(marks + at / 32, 1u << at % 32);
+                if (GRAD && a.add) old[j] = to_float(gr[list.id[j]]);
+            }
+        __syncwarp();
+        Running run(a.side.scale);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int v = i * 32 + lane;
+            scores(span, v, raw[i], s[i]);
+            const unsigned m = marks_of<VEC>(marks, v);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (m >> e & 1) s[i][e] = -INFINITY;
+            run.take(s[i]);
+        }
+        const Softmax outside = warp_join(run.done(), a.side.scale);
+        list.prepare(a.side, tables[warp]);
+        float q[ITEMS];
+        const ListRow r = list.finish(a.side, outside, q);
+        loss = r.loss;
+        lse = r.lse;
+        zero = r.zero;
+        if (GRAD && !zero) {
+            const float scale = shared_factor(a, weight), factor = r.factor * scale;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int v = i * 32 + lane;
+                if (!span.any(v)) continue;
+                float g[VEC];
+                r.ex.of(s[i], g);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const bool in = e >= span.lo(v) && e < span.hi(v);
+                    g[e] = a.add && in ? fmaf(g[e], factor, to_float(gr[span.col(v) + e])) : g[e] * factor;
+                }
+                if (span.whole(v)) {
+                    store_vec_once<VEC>(gr + span.col(v), g);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (e >= span.lo(v) && e < span.hi(v)) store_one(gr + span.col(v) + e, g[e]);
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j)
+                if (list.id[j] >= 0) store_one(gr + list.id[j], a.add ? fmaf(q[j], scale, old[j]) : q[j] * scale);
+        }
+    }
+    if (GRAD && zero && !a.add)
+        for (int c = lane; c < a.side.classes; c += 32) store_one(gr + c, 0.f);
+    if (lane == 0) {
+        if (a.row_loss) a.row_loss[row] = (float)loss;
+        if (a.student_lse) a.student_lse[row] = (float)lse;
+    }
+    finish_mean(a, row, loss, live ? (double)weight : 0.0);
+}
+
 // One bit for each listed class of the piece.
 template <int VEC, typename ID>
 __device__ __forceinline__ void mark_listed(const DistillArgs& a, const Piece<VEC>& p, const ID* __restrict__ ids, size_t row, uint32_t* marks) {
@@ -76,118 +510,6 @@ __device__ __forceinline__ void mark_listed(const DistillArgs& a, const Piece<VE
         if (at >= 0) atomicOr(marks + at / 32, 1u << at % 32);
     }
     __syncthreads();
-}
-template <int VEC>
-__device__ __forceinline__ unsigned marks_of(const uint32_t* marks, int v) {       // v: vector of the piece
-    return (marks[v * VEC / 32] >> (v * VEC % 32)) & ((1u << VEC) - 1);
-}
-
-// Pieces of rows, summed up without the listed classes; the block that is last to finish a row's pieces works out its loss, and the one
-// that is last to finish a row the mean.
-template <typename T, typename V, typename ID, int VEC, int ITEMS>
-__global__ void __launch_bounds__(kPieceThreads) distill_sum_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, DistillArgs a) {
-    __shared__ uint32_t marks[kPieceBits / 32];
-    __shared__ Softmax part[kPieceThreads / 32];
-    __shared__ bool last;
-    __shared__ double2 red[kPieceThreads / 32];
-    pdl_begin();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
-    const float weight = a.weights ? a.weights[row] : 1.f;
-    const bool live = weight > 0.f;
-    if (live) {
-        const Piece<VEC> p(a, row, piece);
-        mark_listed(a, p, ids, (size_t)row, marks);
-        Running run(a.side.scale);
-        for (int v = p.from + tid; v < p.to; v += kPieceThreads) {
-            RawVec<T, VEC> raw;
-            float s[VEC];
-            p.span.load(raw, z, v);
-            scores(p.span, v, raw, s);
-            const unsigned m = marks_of<VEC>(marks, v - p.from);
-            if (m)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (m >> e & 1) s[e] = -INFINITY;
-            run.take(s);
-        }
-        const Softmax all = warp_join(run.done(), a.side.scale);
-        if (lane == 0) part[warp] = all;
-        __syncthreads();
-        if (warp == 0) {
-            const Softmax block = warp_join(lane < kPieceThreads / 32 ? part[lane] : Softmax{-INFINITY, 0.f}, a.side.scale);
-            if (lane == 0) a.parts[(size_t)row * a.pieces + piece] = block;
-        }
-    }
-    if (tid == 0) {
-        __threadfence();
-        last = a.pieces == 1 || atomicAdd(a.arrived + row, 1u) == (unsigned)a.pieces - 1;
-        if (last && a.pieces > 1) a.arrived[row] = 0;
-    }
-    __syncthreads();
-    if (!last) return;
-    if (warp == 0) {
-        __threadfence();
-        RowPlan plan{-INFINITY, 0.f, 0.f, 0};
-        double loss = 0.0, lse = 0.0;
-        if (live) {
-            Softmax outside{-INFINITY, 0.f};
-            for (int i = lane; i < a.pieces; i += 32) {
-                const float2 other = __ldcg(reinterpret_cast<const float2*>(a.parts) + (size_t)row * a.pieces + i);
-                outside = join(outside, Softmax{other.x, other.y}, a.side.scale);
-            }
-            outside = warp_join(outside, a.side.scale);
-            TeacherList<ITEMS> list;
-            list.load(a.side, values, ids, (size_t)row, marks);
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j) list.s[j] = list.id[j] >= 0 ? to_float(z[(size_t)row * a.ld + list.id[j]]) : -INFINITY;
-            float q[ITEMS];
-            const ListRow r = list.finish(a.side, outside, q);
-            loss = r.loss;
-            lse = r.lse;
-            if (a.plans) {
-                int n = 0;
-#pragma unroll
-                for (int j = 0; j < ITEMS; ++j) {
-                    const unsigned have = __ballot_sync(0xffffffffu, list.id[j] >= 0);
-                    if (list.id[j] >= 0) a.listed[(size_t)row * a.side.count + n + __popc(have & ((1u << lane) - 1))] = Listed{list.id[j], q[j]};
-                    n += __popc(have);
-                }
-                plan = RowPlan{outside.top, r.factor, r.zero ? 0.f : weight, n};
-            }
-        }
-        if (lane == 0) {
-            if (a.row_loss) a.row_loss[row] = (float)loss;
-            if (a.student_lse) a.student_lse[row] = (float)lse;
-            if (a.plans) a.plans[row] = plan;
-            a.sums[row] = live ? make_double2(weight * loss, (double)weight) : make_double2(0.0, 0.0);
-            __threadfence();
-            last = atomicAdd(a.done, 1u) == (unsigned)a.rows - 1;
-        }
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double s = 0.0, w = 0.0;
-    for (int r = tid; r < a.rows; r += kPieceThreads) {
-        const double2 v = __ldcg(a.sums + r);
-        s += v.x;
-        w += v.y;
-    }
-    s = warp_sum(s);
-    w = warp_sum(w);
-    if (lane == 0) red[warp] = make_double2(s, w);
-    __syncthreads();
-    if (tid == 0) {
-        s = w = 0.0;
-        for (int i = 0; i < kPieceThreads / 32; ++i) {
-            s += red[i].x;
-            w += red[i].y;
-        }
-        if (a.mean) *a.mean = w > 0.0 ? (float)(s / w) : 0.f;
-        *a.weight_sum = w;
-        *a.done = 0;
-    }
 }
 
 // The gradient of pieces of rows, from the rows' plans.
@@ -249,7 +571,7 @@ constexpr long kPieceTarget = 148 * 8;      // blocks that fill the machine
 static int pieces_of(long rows, int classes, int vec, int* per) {
     const long vectors = ((long)classes + 2 * vec - 2) / vec, most = kPieceBits / vec;
     long pieces = (vectors + most - 1) / most;
-    const long want = (kPieceTarget + rows - 1) / rows, can = vectors / (4 * kPieceThreads);
+    const long want = (kPieceTarget / 2 + rows - 1) / rows, can = vectors / (kAhead * kPieceThreads);
     const long split = want < can ? want : can;
     if (split > pieces) pieces = split;
     if (pieces < 1) pieces = 1;
@@ -259,15 +581,17 @@ static int pieces_of(long rows, int classes, int vec, int* per) {
 
 // Workspace: counters (256 bytes), the rows' counters, their sums, plans and lists, and the pieces' sums, for `rows` rows.
 struct DistillSpace {
-    size_t arrived, sums, plans, listed, parts, bytes;
+    size_t arrived, grouped, sums, group_sums, plans, listed, parts, bytes;
 };
 static DistillSpace space_of(const Distill* d, long rows) {
     DistillSpace s;
     const size_t least = ((size_t)d->classes + kPieceBits / 2 - 1) / (kPieceBits / 2) + 1;      // pieces a row where rows fill the machine
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     s.arrived = 256;
-    s.sums = s.arrived + up(sizeof(unsigned) * rows);
-    s.plans = s.sums + up(sizeof(double2) * rows);
+    s.grouped = s.arrived + up(sizeof(unsigned) * rows);
+    s.sums = s.grouped + up(sizeof(unsigned) * (rows / kMeanGroup + 1));
+    s.group_sums = s.sums + up(sizeof(double2) * rows);
+    s.plans = s.group_sums + up(sizeof(double2) * (rows / kMeanGroup + 1));
     s.listed = s.plans + up(sizeof(RowPlan) * rows);
     s.parts = s.listed + up(sizeof(Listed) * rows * d->count);
     s.bytes = s.parts + up(sizeof(Softmax) * (rows * least + 2 * kPieceTarget));
@@ -289,29 +613,70 @@ static int ensure_distill(Distill* d, long rows, cudaStream_t s) {
     return CIRC_OK;
 }
 
+// The kernel for a call, by the rows' length, their number and the alignment.
 template <typename T, typename V, typename ID>
 static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, T* grad, DistillArgs a, cudaStream_t s, int* launches) {
     constexpr int VEC = 16 / (int)sizeof(T);
     cudaError_t err = cudaSuccess;
-    auto split = [&](auto vec) {
-        constexpr int N = decltype(vec)::value;
-        a.pieces = pieces_of(a.rows, a.side.classes, N, &a.per);
-        const long blocks = (long)a.rows * a.pieces;
+    auto go = [&](auto kernel, long blocks, int threads, size_t smem, auto... args) {
+        if (err != cudaSuccess) return;
         if (blocks >= 1L << 31) {
             err = cudaErrorInvalidConfiguration;
             return;
         }
-        auto sum = [&](auto items) {
-            err = launch_row(distill_sum_kernel<T, V, ID, N, decltype(items)::value>, dim3((unsigned)blocks), dim3(kPieceThreads), 0, s, z, values, ids, a);
-        };
-        a.side.count <= 64 ? sum(std::integral_constant<int, 2>{}) : sum(std::integral_constant<int, kListLanes>{});
-        *launches = 1;
-        if (err != cudaSuccess || !grad) return;
-        err = launch_row(distill_grad_kernel<T, ID, N>, dim3((unsigned)blocks), dim3(kPieceThreads), 0, s, z, ids, grad, a);
-        *launches = 2;
+        if (smem > 32 * 1024) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err == cudaSuccess) err = launch_row(kernel, dim3((unsigned)blocks), dim3(threads), smem, s, args..., a);
+        ++*launches;
     };
-    if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) split(std::integral_constant<int, 1>{});
-    else split(std::integral_constant<int, VEC>{});
+    auto with_items = [&](auto f) {
+        if (a.side.count <= 64) f(std::integral_constant<int, 2>{});
+        else f(std::integral_constant<int, kListLanes>{});
+    };
+    auto in_pieces = [&](auto vec) {
+        constexpr int N = decltype(vec)::value;
+        a.pieces = pieces_of(a.rows, a.side.classes, N, &a.per);
+        const long blocks = (long)a.rows * a.pieces;
+        with_items([&](auto items) {
+            go(distill_rows_kernel<T, V, ID, N, kPieceThreads, decltype(items)::value, false, true>, blocks, kPieceThreads + 32,
+               ((size_t)a.per * N + 31) / 32 * 4, z, values, ids, static_cast<T*>(nullptr));
+        });
+        if (grad) go(distill_grad_kernel<T, ID, N>, blocks, kPieceThreads, 0, z, ids, grad);
+    };
+    if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) {
+        in_pieces(std::integral_constant<int, 1>{});
+        return err;
+    }
+    const int vectors = RowSpan<VEC, false>::most(a.side.classes);
+    const size_t marks = ((size_t)vectors * VEC + 31) / 32 * 4, bytes = (size_t)vectors * 16;
+    const bool few = vectors > 128 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < 148 * 2;
+    if (few || marks > 48 * 1024) {
+        in_pieces(std::integral_constant<int, VEC>{});
+        return err;
+    }
+    a.pieces = 1;
+    a.per = 0;
+    auto with_grad = [&](auto gradient) {
+        constexpr bool GRAD = decltype(gradient)::value;
+        if (GRAD && a.weights && a.rows > kWeightsAlone) go(distill_weights_kernel, 1, 1024, 0);
+        with_items([&](auto items) {
+            constexpr int ITEMS = decltype(items)::value;
+            auto rows = [&](auto threads) {
+                constexpr int THREADS = decltype(threads)::value;
+                go(distill_rows_kernel<T, V, ID, VEC, THREADS, ITEMS, GRAD, false>, a.rows, THREADS + 32, marks, z, values, ids, grad);
+            };
+            auto warps = [&](auto n) {
+                go(distill_warp_kernel<T, V, ID, VEC, decltype(n)::value, ITEMS, GRAD>, (a.rows + 3L) / 4, 128, 0, z, values, ids, grad);
+            };
+            if (vectors <= 32) warps(std::integral_constant<int, 1>{});
+            else if (vectors <= 64) warps(std::integral_constant<int, 2>{});
+            else if (vectors <= 128) warps(std::integral_constant<int, 4>{});
+            // small blocks, whose waits overlap; with a gradient no more of them than L2 holds the rows of
+            else if (!GRAD || bytes <= 32 * 1024) rows(std::integral_constant<int, 128>{});
+            else if (bytes <= 64 * 1024) rows(std::integral_constant<int, 256>{});
+            else rows(std::integral_constant<int, 512>{});
+        });
+    };
+    grad ? with_grad(std::true_type{}) : with_grad(std::false_type{});
     return err;
 }
 
@@ -360,6 +725,9 @@ static int run_distill(Distill* d, const void* z, long ld, const void* values, c
     a.add = d->add;
     a.done = reinterpret_cast<unsigned*>(ws);
     a.weight_sum = reinterpret_cast<double*>(ws + 8);
+    a.weight_total = reinterpret_cast<double*>(ws + 16);
+    a.grouped = reinterpret_cast<unsigned*>(ws + space.grouped);
+    a.group_sums = reinterpret_cast<double2*>(ws + space.group_sums);
     a.arrived = reinterpret_cast<unsigned*>(ws + space.arrived);
     a.sums = reinterpret_cast<double2*>(ws + space.sums);
     a.plans = grad ? reinterpret_cast<RowPlan*>(ws + space.plans) : nullptr;

@@ -50,27 +50,34 @@ template <int ITEMS>
 struct TeacherList {
     int id[ITEMS];          // -1: does not count
     double p[ITEMS];
-    float s[ITEMS];         // the student's logits, of the entries that count
+    float t[ITEMS], s[ITEMS];      // the teacher's values, the student's logits
+    float given;            // the teacher's lse
     double mass, own, left; // sum p, sum p (t / tau - T), p_rest
     bool none;              // no teacher
 
-    // `table`: list_table(count) words of shared memory of this warp's own.
-    template <typename V, typename ID>
-    __device__ __forceinline__ void load(const ListSide& a, const V* __restrict__ values, const ID* __restrict__ ids, size_t row, uint32_t* table) {
-        const int lane = threadIdx.x % 32, slots = list_table(a.count);
-        float t[ITEMS];
+    // The list as it lies in memory, with the student's logits of it; an id outside the classes does not count.
+    template <typename T, typename V, typename ID>
+    __device__ __forceinline__ void fetch(const ListSide& a, const V* __restrict__ values, const ID* __restrict__ ids, size_t row, const T* zr) {
+        const int lane = threadIdx.x % 32;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) {
             const int k = j * 32 + lane;
             id[j] = -1;
-            t[j] = -INFINITY;
+            t[j] = s[j] = -INFINITY;
             if (k < a.count) {
                 const ID c = ids[row * a.count + k];
                 if (c >= 0 && c < (ID)a.classes) id[j] = (int)c;
                 t[j] = to_float(values[row * a.count + k]);
             }
         }
-        const double given = a.rest ? (double)a.lse[row] : 0.0;
+        given = a.rest ? a.lse[row] : 0.f;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j)
+            if (id[j] >= 0) s[j] = to_float(zr[id[j]]);
+    }
+    // The teacher's side.  `table`: list_table(count) words of shared memory of this warp's own.
+    __device__ __forceinline__ void prepare(const ListSide& a, uint32_t* table) {
+        const int lane = threadIdx.x % 32, slots = list_table(a.count);
         __syncwarp();       // the row before is done with the table
         for (int i = lane; i < slots; i += 32) table[i] = kNoId;
         __syncwarp();
@@ -109,7 +116,7 @@ struct TeacherList {
         }
         sum = warp_sum(sum);
         // e / exp(T - base / tau)
-        const double log_all = a.rest ? given - base * a.inv_tau : log(sum), part = a.rest ? exp(-log_all) : 1.0 / sum;
+        const double log_all = a.rest ? (double)given - base * a.inv_tau : log(sum), part = a.rest ? exp(-log_all) : 1.0 / sum;
         none = a.rest ? given == -INFINITY : sum == 0.0;
         mass = own = 0.0;
 #pragma unroll
