@@ -263,15 +263,14 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
             }
             if (live) {
                 const ListRow r = list.finish(a.side, outside, q);
-                loss = r.loss;
-                lse = r.lse;
                 zero = r.zero;
                 if (GRAD && lane == 0) {
-                    space.top = outside.top;
+                    space.top = r.top;
                     space.factor = r.factor * scale;
                     space.zero = zero;
                 }
                 if (GRAD) __syncthreads();
+                list.losses(a.side, r, loss, lse);
                 if (PIECES && a.plans) {
                     int n = 0;
 #pragma unroll
@@ -280,7 +279,7 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
                         if (list.id[j] >= 0) a.listed[(size_t)row * a.side.count + n + __popc(have & ((1u << lane) - 1))] = Listed{list.id[j], q[j]};
                         n += __popc(have);
                     }
-                    plan = RowPlan{outside.top, r.factor, zero ? 0.f : weight, n};
+                    plan = RowPlan{r.top, r.factor, zero ? 0.f : weight, n};
                 }
             }
         }
@@ -332,12 +331,19 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
             }
             take(raw);
         }
-        for (; i < whole; i += THREADS) {
-            RawVec<T, VEC> one[1];
-            one[0].load(src + (size_t)(i - tid) * VEC);
-            const unsigned m = marks_of<VEC>(marks, w0 - p.from + i);
-            if (m) strike(one[0], m);
-            take(one);
+        if (i < whole) {      // the last vectors together too
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                raw[u].fill_lowest();
+                if (i + u * THREADS < whole) raw[u].load(src + (size_t)(i - tid + u * THREADS) * VEC);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (i + u * THREADS < whole) {
+                    const unsigned m = marks_of<VEC>(marks, w0 - p.from + i + u * THREADS);
+                    if (m) strike(raw[u], m);
+                }
+            take(raw);
         }
         if (rest >= 0) {
             RawVec<T, VEC> one;
@@ -383,13 +389,19 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
                         store_vec_once<VEC>(dst + o + u * THREADS * VEC, g);
                     }
                 }
-                for (; i < whole; i += THREADS) {
-                    RawVec<T, VEC> raw;
-                    float g[VEC];
+                if (i < whole) {
+                    RawVec<T, VEC> raw[kAhead];
                     const size_t o = (size_t)(i - tid) * VEC;
-                    raw.load(src + o);
-                    slopes<decltype(plain)::value>(raw, ex, factor, a.add, dst + o, g);
-                    store_vec_once<VEC>(dst + o, g);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        if (i + u * THREADS < whole) raw[u].load(src + o + u * THREADS * VEC);
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        if (i + u * THREADS < whole) {
+                            float g[VEC];
+                            slopes<decltype(plain)::value>(raw[u], ex, factor, a.add, dst + o + u * THREADS * VEC, g);
+                            store_vec_once<VEC>(dst + o + u * THREADS * VEC, g);
+                        }
                 }
             };
             if (ex.plain) put(std::true_type{});
@@ -461,17 +473,17 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* 
         list.prepare(a.side, tables[warp]);
         float q[ITEMS];
         const ListRow r = list.finish(a.side, outside, q);
-        loss = r.loss;
-        lse = r.lse;
+        list.losses(a.side, r, loss, lse);
         zero = r.zero;
         if (GRAD && !zero) {
             const float scale = shared_factor(a, weight), factor = r.factor * scale;
+            const Exponent ex(r.top, a.side.scale);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int v = i * 32 + lane;
                 if (!span.any(v)) continue;
                 float g[VEC];
-                r.ex.of(s[i], g);
+                ex.of(s[i], g);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const bool in = e >= span.lo(v) && e < span.hi(v);
@@ -672,7 +684,7 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
             else if (vectors <= 128) warps(std::integral_constant<int, 4>{});
             // small blocks, whose waits overlap; with a gradient no more of them than L2 holds the rows of
             else if (!GRAD || bytes <= 32 * 1024) rows(std::integral_constant<int, 128>{});
-            else if (bytes <= 64 * 1024) rows(std::integral_constant<int, 256>{});
+            else if (bytes <= 128 * 1024) rows(std::integral_constant<int, 256>{});
             else rows(std::integral_constant<int, 512>{});
         });
     };

@@ -37,12 +37,14 @@ struct ListSide {
     bool rest;
 };
 
-// What one row's loss and gradient need; the same in every lane.
+// What a row's gradient needs, and its loss further on; the same in every lane.
 struct ListRow {
-    double loss, lse;
-    Exponent ex;            // of the classes outside the list ...
-    float factor;           // ... whose gradient is exponential * factor, before grad_mean weight / (sum of weights tau)
+    float top;              // of the classes outside the list ...
+    float factor;           // ... whose gradient is 2^(s scale - base) * factor (Exponent), before grad_mean weight / (sum of weights tau)
     bool zero;              // no gradient
+    bool empty;             // nothing outside the list
+    float base, total, sum; // exponentials relative to base, all of them; of those outside relative to their own top
+    double p_rest, all;
 };
 
 // ITEMS: entries a lane (the list has at most 32 ITEMS).
@@ -134,7 +136,7 @@ struct TeacherList {
         left = a.rest && !none && !(mass >= 1.0) ? 1.0 - mass : 0.0;
     }
 
-    // `outside`: the student's classes outside the list; s holds its logits on the list.
+    // `outside`: the student's classes outside the list; s holds its logits on the list.  q: the list's own gradients, before the same factor.
     __device__ __forceinline__ ListRow finish(const ListSide& a, Softmax outside, float (&q)[ITEMS]) const {
         float top = outside.top;
 #pragma unroll
@@ -142,44 +144,52 @@ struct TeacherList {
             if (id[j] >= 0) top = fmaxf(top, s[j]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float base = top == -INFINITY ? 0.f : top;
+        ListRow r;
+        r.base = top == -INFINITY ? 0.f : top;
         float listed = 0.f;
-        double cross = 0.0;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) {
             q[j] = 0.f;
             if (j * 32 >= a.count) break;
-            if (id[j] >= 0) {
-                q[j] = exp2_of((s[j] - base) * a.scale);
-                if (p[j] != 0.0) cross += p[j] * ((double)s[j] - (double)base);
-            }
+            if (id[j] >= 0) q[j] = exp2_of((s[j] - r.base) * a.scale);
             listed += q[j];
         }
         listed = warp_sum(listed);
-        cross = warp_sum(cross) * a.inv_tau;
-        const float rest = outside.top == -INFINITY && outside.sum == 0.f ? 0.f : outside.sum * exp2_of((outside.top - base) * a.scale);
-        const float total = rest + listed;
-        ListRow r{0.0, 0.0, Exponent(outside.top, a.scale), 0.f, false};
-        const double log_total = log((double)total);
-        r.lse = (double)base * a.inv_tau + log_total;
-        const bool empty = outside.sum == 0.f;                       // its term is left out
-        const double p_rest = empty ? 0.0 : left, all = mass + p_rest;
-        r.zero = none || total == 0.f || all == 0.0;
-        if (none || all == 0.0) {
-            r.loss = 0.0;
-        } else if (total == 0.f) {
-            r.loss = INFINITY;
-        } else {
-            r.loss = own - cross + log_total * mass;
-            if (p_rest != 0.0) r.loss += p_rest * (log(p_rest) - log((double)outside.sum) - ((double)outside.top - (double)base) * a.inv_tau + log_total);
-        }
+        const float rest = outside.top == -INFINITY && outside.sum == 0.f ? 0.f : outside.sum * exp2_of((outside.top - r.base) * a.scale);
+        r.top = outside.top;
+        r.sum = outside.sum;
+        r.total = rest + listed;
+        r.empty = outside.sum == 0.f;                       // its term is left out
+        r.p_rest = r.empty ? 0.0 : left;
+        r.all = mass + r.p_rest;
+        r.zero = none || r.total == 0.f || r.all == 0.0;
+        r.factor = 0.f;
         if (!r.zero) {
-            const float inv = 1.f / total;
-            r.factor = empty ? 0.f : (float)(all * (double)(rest / total) - p_rest) / (outside.sum * exp2_of(r.ex.shift));
+            const float inv = 1.f / r.total;
+            if (!r.empty) r.factor = (float)(r.all * (double)(rest / r.total) - r.p_rest) / (outside.sum * exp2_of(Exponent(outside.top, a.scale).shift));
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) q[j] = (float)(all * (double)(q[j] * inv) - p[j]);
+            for (int j = 0; j < ITEMS; ++j) q[j] = (float)(r.all * (double)(q[j] * inv) - p[j]);
         }
         return r;
+    }
+    __device__ __forceinline__ void losses(const ListSide& a, const ListRow& r, double& loss, double& lse) const {
+        const double log_total = log((double)r.total);
+        lse = (double)r.base * a.inv_tau + log_total;
+        double cross = 0.0;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            if (j * 32 >= a.count) break;
+            if (id[j] >= 0 && p[j] != 0.0) cross += p[j] * ((double)s[j] - (double)r.base);
+        }
+        cross = warp_sum(cross) * a.inv_tau;
+        if (none || r.all == 0.0) {
+            loss = 0.0;
+        } else if (r.total == 0.f) {
+            loss = INFINITY;
+        } else {
+            loss = own - cross + log_total * mass;
+            if (r.p_rest != 0.0) loss += r.p_rest * (log(r.p_rest) - log((double)r.sum) - ((double)r.top - (double)r.base) * a.inv_tau + log_total);
+        }
     }
 };
 

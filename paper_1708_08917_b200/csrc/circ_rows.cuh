@@ -111,6 +111,10 @@ struct RawVec {
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) w[i] = 0;
     }
+    __device__ __forceinline__ void fill_lowest() {      // -inf
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    }
     __device__ __forceinline__ void load(const T* p) {
         if constexpr (VEC == 1) {
             w[0] = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)*reinterpret_cast<const uint16_t*>(p);

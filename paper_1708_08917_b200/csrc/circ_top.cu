@@ -478,36 +478,28 @@ __global__ void __launch_bounds__(THREADS, PIECES ? 1 : kRowThreads / THREADS) t
     Running run(a.scale);
     for (int i = tid; i < whole; i += kKept * THREADS) {
         const T* from = src + (size_t)(i - tid) * VEC;
+        RawVec<T, VEC> raw[kKept];
         if (i + (kKept - 1) * THREADS < whole) {
-            RawVec<T, VEC> raw[kKept];
 #pragma unroll
             for (int u = 0; u < kKept; ++u) raw[u].load(from + u * THREADS * VEC);
-            float most = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < kKept; ++u) {
-                const float one = most_nan(raw[u]);
-                best[u] = max_nan(best[u], one);
-                most = max_nan(most, one);
-            }
-            if (a.lse) {
-                run.rise(most);
-                if (run.ex.plain) run.template add<true>(raw);
-                else run.template add<false>(raw);
-            }
         } else {
 #pragma unroll
-            for (int u = 0; u < kKept; ++u)
-                if (i + u * THREADS < whole) {
-                    RawVec<T, VEC> raw[1];
-                    raw[0].load(from + u * THREADS * VEC);
-                    const float one = most_nan(raw[0]);
-                    best[u] = max_nan(best[u], one);
-                    if (a.lse) {
-                        run.rise(one);
-                        if (run.ex.plain) run.template add<true>(raw);
-                        else run.template add<false>(raw);
-                    }
-                }
+            for (int u = 0; u < kKept; ++u) {
+                raw[u].fill_lowest();
+                if (i + u * THREADS < whole) raw[u].load(from + u * THREADS * VEC);
+            }
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) {
+            const float one = most_nan(raw[u]);
+            best[u] = max_nan(best[u], one);
+            most = max_nan(most, one);
+        }
+        if (a.lse) {
+            run.rise(most);
+            if (run.ex.plain) run.template add<true>(raw);
+            else run.template add<false>(raw);
         }
     }
     // the first and last elements beside the whole vectors
