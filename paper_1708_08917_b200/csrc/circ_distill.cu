@@ -190,22 +190,23 @@ __device__ __forceinline__ void slopes(const RawVec<T, VEC>& raw, const Exponent
 // warp has the list: it marks its classes, works out the teacher's side meanwhile, and then the row's loss.  GRAD: the row is read a second time, from
 // L2, where its block's neighbours have left room for it, and the gradient written; the list's own elements follow behind a barrier.
 // PIECES: the warp that is last to finish a row's pieces works out its loss, and with `plans` what distill_grad_kernel needs.
-template <int WARPS, int ITEMS>
+template <int WARPS, int MOST, bool PIECES>
 struct RowSpace {
-    uint32_t table[ITEMS * 64];
+    ListSpace<MOST> list;
+    uint32_t table[PIECES ? 2 * MOST : 1];
     Softmax part[WARPS];
     float top, factor;
     bool zero;
 };
 constexpr int kAhead = 4;
 
-template <typename T, typename V, typename ID, int VEC, int THREADS, int ITEMS, bool GRAD, bool PIECES>
+template <typename T, typename V, typename ID, int VEC, int THREADS, int MOST, bool GRAD, bool PIECES>
 __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 32))
     distill_rows_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, T* grad, DistillArgs a) {
     static_assert(!(GRAD && PIECES) && (VEC > 1 || PIECES), "");
     constexpr int WARPS = THREADS / 32;
     extern __shared__ __align__(16) uint32_t marks[];
-    __shared__ RowSpace<WARPS, ITEMS> space;
+    __shared__ RowSpace<WARPS, MOST, PIECES> space;
     pdl_begin();
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int row = PIECES ? blockIdx.x / a.pieces : blockIdx.x, piece = PIECES ? blockIdx.x % a.pieces : 0;
@@ -217,26 +218,28 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
     // the vectors that are not whole: one for each of the first two threads, or -1
     const int rest = tid == 0 && w0 > p.from ? p.from : tid == 1 && w1 < p.to ? p.to - 1 : -1;
     if (warp == WARPS) {
-        TeacherList<ITEMS> list;
-        float old[ITEMS];
+        TeacherList<MOST> list(space.list);
         if (live) {
             list.fetch(a.side, values, ids, (size_t)row, zr);
-            if (GRAD && a.add)
-#pragma unroll
-                for (int j = 0; j < ITEMS; ++j) old[j] = list.id[j] >= 0 ? to_float(grad[(size_t)row * a.grad_ld + list.id[j]]) : 0.f;
             __syncthreads();
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                const int at = list.id[j] >= 0 ? p.place(list.id[j]) : -1;
-                if (at >= 0) atomicOr(marks + at / 32, 1u << at % 32);
+            auto mark = [&](int id) {      // false: it is marked already
+                const int at = p.place(id);
+                return at >= 0 && !(atomicOr(marks + at / 32, 1u << at % 32) >> at % 32 & 1);
+            };
+            if constexpr (PIECES) {        // the marks are those of the piece
+                for (int k = lane; k < a.side.count; k += 32) mark(list.at.id[k]);
+                __syncthreads();
+                list.keep_first(a.side, space.table);
+            } else {
+                list.keep_first(a.side, mark);
+                __syncthreads();
             }
-            __syncthreads();
-            list.prepare(a.side, space.table);
+            list.prepare(a.side);
         }
         const float scale = GRAD && live ? shared_factor(a, weight) : 0.f;
         double loss = 0.0, lse = 0.0;
         RowPlan plan{-INFINITY, 0.f, 0.f, 0};
-        float q[ITEMS];
+        ListRow r{};
         bool zero = true;
         if (live || PIECES) {
             Softmax outside{-INFINITY, 0.f};
@@ -262,21 +265,24 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
                 outside = warp_join(outside, a.side.scale);
             }
             if (live) {
-                const ListRow r = list.finish(a.side, outside, q);
+                r = list.finish(a.side, outside);
                 zero = r.zero;
                 if (GRAD && lane == 0) {
                     space.top = r.top;
                     space.factor = r.factor * scale;
                     space.zero = zero;
                 }
+                if (GRAD && a.add && !zero)      // what is there now, before the others write over it
+                    for (int k = lane; k < a.side.count; k += 32)
+                        if (list.at.id[k] >= 0) list.at.t[k] = fmaf(list.slope(r, k), scale, to_float(grad[(size_t)row * a.grad_ld + list.at.id[k]]));
                 if (GRAD) __syncthreads();
                 list.losses(a.side, r, loss, lse);
                 if (PIECES && a.plans) {
                     int n = 0;
-#pragma unroll
-                    for (int j = 0; j < ITEMS; ++j) {
-                        const unsigned have = __ballot_sync(0xffffffffu, list.id[j] >= 0);
-                        if (list.id[j] >= 0) a.listed[(size_t)row * a.side.count + n + __popc(have & ((1u << lane) - 1))] = Listed{list.id[j], q[j]};
+                    for (int k0 = 0; k0 < a.side.count; k0 += 32) {
+                        const int k = k0 + lane, id = k < a.side.count ? list.at.id[k] : -1;
+                        const unsigned have = __ballot_sync(0xffffffffu, id >= 0);
+                        if (id >= 0) a.listed[(size_t)row * a.side.count + n + __popc(have & ((1u << lane) - 1))] = Listed{id, list.slope(r, k)};
                         n += __popc(have);
                     }
                     plan = RowPlan{r.top, r.factor, zero ? 0.f : weight, n};
@@ -292,9 +298,8 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
         if (GRAD && live) {
             __syncthreads();
             if (!zero)
-#pragma unroll
-                for (int j = 0; j < ITEMS; ++j)
-                    if (list.id[j] >= 0) store_one(grad + (size_t)row * a.grad_ld + list.id[j], a.add ? fmaf(q[j], scale, old[j]) : q[j] * scale);
+                for (int k = lane; k < a.side.count; k += 32)
+                    if (list.at.id[k] >= 0) store_one(grad + (size_t)row * a.grad_ld + list.at.id[k], a.add ? list.at.t[k] : list.slope(r, k) * scale);
         }
         return;
     }
@@ -425,10 +430,11 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
     }
 }
 
-// ---- short rows: a warp holds one in registers, and its list ----
-template <typename T, typename V, typename ID, int VEC, int N, int ITEMS, bool GRAD>
+// ---- short rows: a warp holds one in registers ----
+template <typename T, typename V, typename ID, int VEC, int N, int MOST, bool GRAD>
 __global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, T* grad, DistillArgs a) {
-    __shared__ uint32_t marks_of_warp[4][N * VEC], tables[4][ITEMS * 64];
+    __shared__ uint32_t marks_of_warp[4][N * VEC];
+    __shared__ ListSpace<MOST> lists[4];
     pdl_begin();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 4 + warp;
     if (row >= a.rows) return;
@@ -442,48 +448,44 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* 
     bool zero = true;
     if (live) {
         RawVec<T, VEC> raw[N];
-        float s[N][VEC];
-        TeacherList<ITEMS> list;
-        list.fetch(a.side, values, ids, (size_t)row, z + (size_t)row * a.ld);
 #pragma unroll
         for (int i = 0; i < N; ++i) span.load(raw[i], z, i * 32 + lane);
         for (int i = lane; i < N * VEC; i += 32) marks[i] = 0;
+        TeacherList<MOST> list(lists[warp]);
+        list.fetch(a.side, values, ids, (size_t)row, z + (size_t)row * a.ld);
         __syncwarp();
-        float old[ITEMS];
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j)
-            if (list.id[j] >= 0) {
-                const int at = p.place(list.id[j]);
-                atomicOr(marks + at / 32, 1u << at % 32);
-                if (GRAD && a.add) old[j] = to_float(gr[list.id[j]]);
-            }
+        list.keep_first(a.side, [&](int id) {
+            const int at = p.place(id);
+            return !(atomicOr(marks + at / 32, 1u << at % 32) >> at % 32 & 1);
+        });
         __syncwarp();
         Running run(a.side.scale);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int v = i * 32 + lane;
-            scores(span, v, raw[i], s[i]);
-            const unsigned m = marks_of<VEC>(marks, v);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (m >> e & 1) s[i][e] = -INFINITY;
-            run.take(s[i]);
+            if (span.any(v)) strike(raw[i], marks_of<VEC>(marks, v));
+            float s[VEC];
+            scores(span, v, raw[i], s);
+            run.take(s);
         }
         const Softmax outside = warp_join(run.done(), a.side.scale);
-        list.prepare(a.side, tables[warp]);
-        float q[ITEMS];
-        const ListRow r = list.finish(a.side, outside, q);
+        list.prepare(a.side);
+        const ListRow r = list.finish(a.side, outside);
         list.losses(a.side, r, loss, lse);
         zero = r.zero;
         if (GRAD && !zero) {
             const float scale = shared_factor(a, weight), factor = r.factor * scale;
             const Exponent ex(r.top, a.side.scale);
+            for (int k = lane; k < a.side.count; k += 32)
+                if (list.at.id[k] >= 0) list.at.t[k] = a.add ? fmaf(list.slope(r, k), scale, to_float(gr[list.at.id[k]])) : list.slope(r, k) * scale;
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int v = i * 32 + lane;
                 if (!span.any(v)) continue;
-                float g[VEC];
-                ex.of(s[i], g);
+                float s[VEC], g[VEC];
+                scores(span, v, raw[i], s);
+                ex.of(s, g);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const bool in = e >= span.lo(v) && e < span.hi(v);
@@ -498,9 +500,8 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* 
                 }
             }
             __syncwarp();
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j)
-                if (list.id[j] >= 0) store_one(gr + list.id[j], a.add ? fmaf(q[j], scale, old[j]) : q[j] * scale);
+            for (int k = lane; k < a.side.count; k += 32)
+                if (list.at.id[k] >= 0) store_one(gr + list.at.id[k], list.at.t[k]);
         }
     }
     if (GRAD && zero && !a.add)
@@ -640,16 +641,16 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
         if (err == cudaSuccess) err = launch_row(kernel, dim3((unsigned)blocks), dim3(threads), smem, s, args..., a);
         ++*launches;
     };
-    auto with_items = [&](auto f) {
-        if (a.side.count <= 64) f(std::integral_constant<int, 2>{});
-        else f(std::integral_constant<int, kListLanes>{});
+    auto with_list = [&](auto f) {
+        if (a.side.count <= 64) f(std::integral_constant<int, 64>{});
+        else f(std::integral_constant<int, kListMost>{});
     };
     auto in_pieces = [&](auto vec) {
         constexpr int N = decltype(vec)::value;
         a.pieces = pieces_of(a.rows, a.side.classes, N, &a.per);
         const long blocks = (long)a.rows * a.pieces;
-        with_items([&](auto items) {
-            go(distill_rows_kernel<T, V, ID, N, kPieceThreads, decltype(items)::value, false, true>, blocks, kPieceThreads + 32,
+        with_list([&](auto most) {
+            go(distill_rows_kernel<T, V, ID, N, kPieceThreads, decltype(most)::value, false, true>, blocks, kPieceThreads + 32,
                ((size_t)a.per * N + 31) / 32 * 4, z, values, ids, static_cast<T*>(nullptr));
         });
         if (grad) go(distill_grad_kernel<T, ID, N>, blocks, kPieceThreads, 0, z, ids, grad);
@@ -670,14 +671,14 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
     auto with_grad = [&](auto gradient) {
         constexpr bool GRAD = decltype(gradient)::value;
         if (GRAD && a.weights && a.rows > kWeightsAlone) go(distill_weights_kernel, 1, 1024, 0);
-        with_items([&](auto items) {
-            constexpr int ITEMS = decltype(items)::value;
+        with_list([&](auto most) {
+            constexpr int MOST = decltype(most)::value;
             auto rows = [&](auto threads) {
                 constexpr int THREADS = decltype(threads)::value;
-                go(distill_rows_kernel<T, V, ID, VEC, THREADS, ITEMS, GRAD, false>, a.rows, THREADS + 32, marks, z, values, ids, grad);
+                go(distill_rows_kernel<T, V, ID, VEC, THREADS, MOST, GRAD, false>, a.rows, THREADS + 32, marks, z, values, ids, grad);
             };
             auto warps = [&](auto n) {
-                go(distill_warp_kernel<T, V, ID, VEC, decltype(n)::value, ITEMS, GRAD>, (a.rows + 3L) / 4, 128, 0, z, values, ids, grad);
+                go(distill_warp_kernel<T, V, ID, VEC, decltype(n)::value, MOST, GRAD>, (a.rows + 3L) / 4, 128, 0, z, values, ids, grad);
             };
             if (vectors <= 32) warps(std::integral_constant<int, 1>{});
             else if (vectors <= 64) warps(std::integral_constant<int, 2>{});

@@ -13,7 +13,6 @@
 namespace circ {
 
 constexpr int kListMost = 256;                   // entries
-constexpr int kListLanes = kListMost / 32;       // a lane's entries: lane, lane + 32, ...
 constexpr uint32_t kNoId = 0xffffffffu;
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -47,112 +46,134 @@ struct ListRow {
     double p_rest, all;
 };
 
-// ITEMS: entries a lane (the list has at most 32 ITEMS).
-template <int ITEMS>
+// A list in shared memory; a lane of its warp works on the entries lane, lane + 32, ...  (In registers they cost the kernel's other warps
+// occupancy, and where those were spilled, every use of one a trip through an L1 cache that the rows stream through: 5000 to 17000 cycles a row.)
+template <int MOST>
+struct ListSpace {
+    double p[MOST];
+    float t[MOST], s[MOST];     // the teacher's values (later the entries' gradients), the student's logits
+    int id[MOST];               // -1: does not count
+};
+
+template <int MOST>
 struct TeacherList {
-    int id[ITEMS];          // -1: does not count
-    double p[ITEMS];
-    float t[ITEMS], s[ITEMS];      // the teacher's values, the student's logits
-    float given;            // the teacher's lse
-    double mass, own, left; // sum p, sum p (t / tau - T), p_rest
-    bool none;              // no teacher
+    ListSpace<MOST>& at;
+    double mass, own, left;     // sum p, this lane's part of sum p (t / tau - T), p_rest
+    float given;                // the teacher's lse
+    bool none;                  // no teacher
+    __device__ __forceinline__ explicit TeacherList(ListSpace<MOST>& space) : at(space) {}
 
     // The list as it lies in memory, with the student's logits of it; an id outside the classes does not count.
     template <typename T, typename V, typename ID>
     __device__ __forceinline__ void fetch(const ListSide& a, const V* __restrict__ values, const ID* __restrict__ ids, size_t row, const T* zr) {
         const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            const int k = j * 32 + lane;
-            id[j] = -1;
-            t[j] = s[j] = -INFINITY;
-            if (k < a.count) {
-                const ID c = ids[row * a.count + k];
-                if (c >= 0 && c < (ID)a.classes) id[j] = (int)c;
-                t[j] = to_float(values[row * a.count + k]);
-            }
-        }
+        constexpr int N = MOST / 32;
+        int c[N];
+        float t[N], s[N];
         given = a.rest ? a.lse[row] : 0.f;
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j)
-            if (id[j] >= 0) s[j] = to_float(zr[id[j]]);
-    }
-    // The teacher's side.  `table`: list_table(count) words of shared memory of this warp's own.
-    __device__ __forceinline__ void prepare(const ListSide& a, uint32_t* table) {
-        const int lane = threadIdx.x % 32, slots = list_table(a.count);
-        __syncwarp();       // the row before is done with the table
-        for (int i = lane; i < slots; i += 32) table[i] = kNoId;
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            if (j * 32 >= a.count) break;
-            const unsigned same = __match_any_sync(0xffffffffu, id[j]);
-            bool first = false;
-            if (id[j] >= 0 && lane == __ffs(same) - 1) {
-                uint32_t slot = ((uint32_t)id[j] * 2654435761u) >> 16;
-                for (int tries = 0; tries < slots; ++tries) {     // the table is at most half full
-                    slot &= (uint32_t)slots - 1;
-                    const uint32_t old = atomicCAS(table + slot, kNoId, (uint32_t)id[j]);
-                    first = old == kNoId;
-                    if (first || old == (uint32_t)id[j]) break;
-                    ++slot;
-                }
+        for (int j = 0; j < N; ++j) {
+            c[j] = -1;
+            if (j * 32 + lane < a.count) {
+                const ID i = ids[row * a.count + j * 32 + lane];
+                if (i >= 0 && i < (ID)a.classes) c[j] = (int)i;
+                t[j] = to_float(values[row * a.count + j * 32 + lane]);
             }
-            __syncwarp();   // earlier entries come first
-            if (!first) id[j] = -1;
         }
-        float top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j)
-            if (id[j] >= 0) top = fmaxf(top, t[j]);
+        for (int j = 0; j < N; ++j)
+            if (c[j] >= 0) s[j] = to_float(zr[c[j]]);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j * 32 + lane < a.count) {
+                at.id[j * 32 + lane] = c[j];
+                at.t[j * 32 + lane] = t[j];
+                at.s[j * 32 + lane] = c[j] >= 0 ? s[j] : -INFINITY;
+            }
+    }
+    // Calls take(id), by the first lane of each id, for the entries in their order; the entries that it does not want, and those behind a first one,
+    // no longer count.
+    template <typename F>
+    __device__ __forceinline__ void keep_first(const ListSide& a, F take) {
+        const int lane = threadIdx.x % 32;
+        for (int k0 = 0; k0 < a.count; k0 += 32) {
+            const int k = k0 + lane, id = k < a.count ? at.id[k] : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, id);
+            bool first = false;
+            if (id >= 0 && lane == __ffs(same) - 1) first = take(id);
+            __syncwarp();
+            if (id >= 0 && !first) at.id[k] = -1;
+        }
+    }
+    // The same by a table of list_table(count) words of shared memory.
+    __device__ __forceinline__ void keep_first(const ListSide& a, uint32_t* table) {
+        const int slots = list_table(a.count);
+        for (int i = threadIdx.x % 32; i < slots; i += 32) table[i] = kNoId;
+        __syncwarp();
+        keep_first(a, [&](int id) {
+            uint32_t slot = ((uint32_t)id * 2654435761u) >> 16;
+            for (int tries = 0; tries < slots; ++tries, ++slot) {      // the table is at most half full
+                slot &= (uint32_t)slots - 1;
+                const uint32_t old = atomicCAS(table + slot, kNoId, (uint32_t)id);
+                if (old == kNoId) return true;
+                if (old == (uint32_t)id) return false;
+            }
+            return false;
+        });
+    }
+    // The teacher's side.
+    __device__ __forceinline__ void prepare(const ListSide& a) {
+        const int lane = threadIdx.x % 32;
+        float top = -INFINITY;
+        for (int k = lane; k < a.count; k += 32)
+            if (at.id[k] >= 0) top = fmaxf(top, at.t[k]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        double e[ITEMS], sum = 0.0;
         const double base = top == -INFINITY ? 0.0 : (double)top;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            e[j] = 0.0;
-            if (j * 32 >= a.count) break;
-            if (id[j] >= 0) e[j] = exp(((double)t[j] - base) * a.inv_tau);
-            sum += e[j];
+        double sum = 0.0;
+        for (int k = lane; k < a.count; k += 32) {
+            const double e = at.id[k] >= 0 ? exp(((double)at.t[k] - base) * a.inv_tau) : 0.0;
+            at.p[k] = e;
+            sum += e;
         }
-        sum = warp_sum(sum);
         // e / exp(T - base / tau)
-        const double log_all = a.rest ? (double)given - base * a.inv_tau : log(sum), part = a.rest ? exp(-log_all) : 1.0 / sum;
-        none = a.rest ? given == -INFINITY : sum == 0.0;
+        double log_all, part;
+        if (a.rest) {
+            log_all = (double)given - base * a.inv_tau;
+            part = exp(-log_all);
+            none = given == -INFINITY;
+        } else {
+            sum = warp_sum(sum);
+            log_all = log(sum);
+            part = 1.0 / sum;
+            none = sum == 0.0;
+        }
         mass = own = 0.0;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            p[j] = 0.0;
-            if (j * 32 >= a.count) break;
-            if (id[j] >= 0 && !none && e[j] != 0.0) {
-                p[j] = e[j] * part;
-                mass += p[j];
-                own += p[j] * (((double)t[j] - base) * a.inv_tau - log_all);
-            }
+        for (int k = lane; k < a.count; k += 32) {
+            const double e = at.p[k], p = e != 0.0 && !none ? e * part : 0.0;
+            at.p[k] = p;
+            mass += p;
+            if (p != 0.0) own += p * (((double)at.t[k] - base) * a.inv_tau - log_all);
         }
         mass = warp_sum(mass);
-        own = warp_sum(own);
         left = a.rest && !none && !(mass >= 1.0) ? 1.0 - mass : 0.0;
     }
 
-    // `outside`: the student's classes outside the list; s holds its logits on the list.  q: the list's own gradients, before the same factor.
-    __device__ __forceinline__ ListRow finish(const ListSide& a, Softmax outside, float (&q)[ITEMS]) const {
+    // `outside`: the student's classes outside the list.  The entries' own gradients, before the same factor, take the place of the teacher's values.
+    __device__ __forceinline__ ListRow finish(const ListSide& a, Softmax outside) const {
+        const int lane = threadIdx.x % 32;
         float top = outside.top;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j)
-            if (id[j] >= 0) top = fmaxf(top, s[j]);
+        for (int k = lane; k < a.count; k += 32)
+            if (at.id[k] >= 0) top = fmaxf(top, at.s[k]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         ListRow r;
         r.base = top == -INFINITY ? 0.f : top;
         float listed = 0.f;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            q[j] = 0.f;
-            if (j * 32 >= a.count) break;
-            if (id[j] >= 0) q[j] = exp2_of((s[j] - r.base) * a.scale);
-            listed += q[j];
+        for (int k = lane; k < a.count; k += 32) {
+            const float q = at.id[k] >= 0 ? exp2_of((at.s[k] - r.base) * a.scale) : 0.f;
+            at.t[k] = q;
+            listed += q;
         }
         listed = warp_sum(listed);
         const float rest = outside.top == -INFINITY && outside.sum == 0.f ? 0.f : outside.sum * exp2_of((outside.top - r.base) * a.scale);
@@ -164,31 +185,25 @@ struct TeacherList {
         r.all = mass + r.p_rest;
         r.zero = none || r.total == 0.f || r.all == 0.0;
         r.factor = 0.f;
-        if (!r.zero) {
-            const float inv = 1.f / r.total;
-            if (!r.empty) r.factor = (float)(r.all * (double)(rest / r.total) - r.p_rest) / (outside.sum * exp2_of(Exponent(outside.top, a.scale).shift));
-#pragma unroll
-            for (int j = 0; j < ITEMS; ++j) q[j] = (float)(r.all * (double)(q[j] * inv) - p[j]);
-        }
+        if (!r.zero && !r.empty) r.factor = (float)(r.all * (double)(rest / r.total) - r.p_rest) / (outside.sum * exp2_of(Exponent(outside.top, a.scale).shift));
         return r;
     }
+    // The gradient of entry k, before the factor that all rows share.
+    __device__ __forceinline__ float slope(const ListRow& r, int k) const { return (float)(r.all * (double)(at.t[k] / r.total) - at.p[k]); }
     __device__ __forceinline__ void losses(const ListSide& a, const ListRow& r, double& loss, double& lse) const {
         const double log_total = log((double)r.total);
         lse = (double)r.base * a.inv_tau + log_total;
-        double cross = 0.0;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) {
-            if (j * 32 >= a.count) break;
-            if (id[j] >= 0 && p[j] != 0.0) cross += p[j] * ((double)s[j] - (double)r.base);
-        }
-        cross = warp_sum(cross) * a.inv_tau;
+        double mine = 0.0;
+        for (int k = threadIdx.x % 32; k < a.count; k += 32)
+            if (at.p[k] != 0.0) mine += at.p[k] * ((double)at.s[k] - (double)r.base);
+        mine = warp_sum(own - mine * a.inv_tau);
         if (none || r.all == 0.0) {
             loss = 0.0;
         } else if (r.total == 0.f) {
             loss = INFINITY;
         } else {
-            loss = own - cross + log_total * mass;
-            if (r.p_rest != 0.0) loss += r.p_rest * (log(r.p_rest) - log((double)r.sum) - ((double)r.top - (double)r.base) * a.inv_tau + log_total);
+            loss = mine + log_total * mass;
+            if (r.p_rest != 0.0) loss += r.p_rest * (log(r.p_rest * ((double)r.total / (double)r.sum)) - ((double)r.top - (double)r.base) * a.inv_tau);
         }
     }
 };
