@@ -3,6 +3,7 @@
 // and its gradients, with u = (x - mean) rstd and g = grad_y act'(v):
 //   grad_x = rstd (gain g - (A + u B) / m), A = sum of gain g over the group, B = sum of gain g u
 //   grad_gain_c = sum of g u, grad_bias_c = sum of g over images and pixels.
+#include <algorithm>
 #include <new>
 #include <type_traits>
 
@@ -16,7 +17,7 @@ struct Gnorm {
     float eps;
     int x_dtype, y_dtype, act;
     Scratch ws;
-    int images_held;        // images that the workspace is laid out for
+    long images_held, tasks_held;        // that the workspace is laid out for
 };
 
 struct GnormArgs {
@@ -25,10 +26,14 @@ struct GnormArgs {
     int channels, groups, depth;      // depth: channels a group
     int images, pixels;
     float eps;
+    double inv_m;             // 1 / (pixels depth)
     // a block's part: `columns` vectors of channels (all, or a tile of them), and pixels of one image
     int columns, tiles, pieces, per;
+    int act;
+    int image0;               // of a launch's images
     // workspace
     unsigned* arrived;        // [N] parts of an image that are summed up (0 before and after a call)
+    float2* group_parts;      // [N][pieces][groups] the tasks' sums of the groups
     float2* parts;            // [N][pieces][C] forward: mean, less the channel's first value, and sum of squares around it; backward: sum of g, of g u
     float2* totals;           // [N][C] backward: the same over the image
     float2* means;            // [N][groups] backward: A / m, B / m
@@ -36,13 +41,26 @@ struct GnormArgs {
 
 constexpr int kGnormThreads = 256;
 
-__device__ __forceinline__ float sigmoid_of(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// 1 / (1 + exp(-v)): one exponential, one reciprocal.  Below -87 the exponential is infinite and the sigmoid 0.
+__device__ __forceinline__ float sigmoid_of(float v) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
+}
 
 template <int ACT>
 __device__ __forceinline__ float activate(float v) {
-    if constexpr (ACT == CIRC_ACT_RELU) return v > 0.f ? v : v != v ? v : 0.f;
+    if constexpr (ACT == CIRC_ACT_RELU) return max_nan(v, 0.f);
     if constexpr (ACT == CIRC_ACT_SILU) return v * sigmoid_of(v);
     return v;
+}
+
+template <typename F>
+__device__ __forceinline__ void with_act_of(int act, F&& f) {
+    if (act == CIRC_ACT_RELU) f(std::integral_constant<int, CIRC_ACT_RELU>{});
+    else if (act == CIRC_ACT_SILU) f(std::integral_constant<int, CIRC_ACT_SILU>{});
+    else f(std::integral_constant<int, CIRC_ACT_NONE>{});
 }
 
 // What a channel's values go through: v = (x - mean) (rstd gain) + bias.
@@ -66,8 +84,56 @@ struct Channel {
     }
 };
 
-// Which vectors of channels and which pixels a thread works on.
+// The same for a vector of channels, arithmetic in pairs.
 template <int VEC>
+struct Channels {
+    static constexpr int N = VEC > 1 ? VEC / 2 : 1;
+    Pair mean[N], rstd[N], gain[N], bias[N];       // mean: less than 0
+    __device__ __forceinline__ void set(int e, float m, float r, float g, float b) {
+        put(mean[e / 2], e % 2, -m);
+        put(rstd[e / 2], e % 2, r);
+        put(gain[e / 2], e % 2, g);
+        put(bias[e / 2], e % 2, b);
+    }
+    __device__ __forceinline__ static void put(Pair& p, int half, float v) {
+        float lo, hi;
+        split(p, lo, hi);
+        p = half ? pair_of(lo, v) : pair_of(v, VEC > 1 ? hi : 0.f);
+    }
+    // u and g = grad_y act'(v) of two values.
+    template <int ACT>
+    __device__ __forceinline__ void slopes(int i, Pair x, Pair grad_y, Pair& u, Pair& g) const {
+        u = pair_mul(pair_add(x, mean[i]), rstd[i]);
+        g = grad_y;
+        if constexpr (ACT == CIRC_ACT_NONE) return;
+        const Pair t = pair_mul(u, gain[i]), v = pair_add(t, bias[i]);
+        float v0, v1;
+        split(v, v0, v1);
+        if constexpr (ACT == CIRC_ACT_RELU) {
+            float t0, t1, b0, b1, g0, g1;
+            split(t, t0, t1);
+            split(bias[i], b0, b1);
+            split(g, g0, g1);
+            bool on0 = v0 > 0.f, on1 = v1 > 0.f;
+            if (fabsf(v0) <= 1e-6f * (fabsf(t0) + fabsf(b0)) || fabsf(v1) <= 1e-6f * (fabsf(t1) + fabsf(b1))) {
+                float x0, x1, m0, m1, r0, r1, a0, a1;
+                split(x, x0, x1);
+                split(mean[i], m0, m1);
+                split(rstd[i], r0, r1);
+                split(gain[i], a0, a1);
+                on0 = ((double)x0 + (double)m0) * ((double)r0 * (double)a0) + (double)b0 > 0.0;
+                on1 = ((double)x1 + (double)m1) * ((double)r1 * (double)a1) + (double)b1 > 0.0;
+            }
+            g = pair_of(on0 ? g0 : v0 != v0 ? v0 : 0.f, on1 ? g1 : v1 != v1 ? v1 : 0.f);
+        } else {
+            const Pair s = pair_of(sigmoid_of(v0), VEC > 1 ? sigmoid_of(v1) : 0.f), one = pair_of(1.f, 1.f);
+            g = pair_mul(g, pair_mul(s, pair_fma(v, pair_fma(s, pair_of(-1.f, -1.f), one), one)));
+        }
+    }
+};
+
+// ---- any tensor: a thread a channel, two launches ----
+// Which channel and which pixels a thread works on.
 struct GnormPlace {
     int image, piece, tile, column, lane, lanes, from, to;      // pixels from + lane, + lanes, ... below `to`
     bool live;
@@ -81,14 +147,12 @@ struct GnormPlace {
         column = tile * a.columns + threadIdx.x % a.columns;
         from = piece * a.per;
         to = min(a.pixels, from + a.per);
-        live = lane < lanes && column * VEC < a.channels;
+        live = lane < lanes && column < a.channels;
     }
-    __device__ __forceinline__ size_t at(const GnormArgs& a, int pixel) const {
-        return ((size_t)image * a.pixels + pixel) * a.channels + (size_t)column * VEC;
-    }
-    __device__ __forceinline__ Channel channel(const GnormArgs& a, int e) const {
-        const int c = column * VEC + e, g = c / a.depth;
-        return Channel{a.mean[(size_t)image * a.groups + g], a.rstd[(size_t)image * a.groups + g], a.gain ? a.gain[c] : 1.f, a.bias ? a.bias[c] : 0.f};
+    __device__ __forceinline__ size_t at(const GnormArgs& a, int pixel) const { return ((size_t)image * a.pixels + pixel) * a.channels + column; }
+    __device__ __forceinline__ Channel channel(const GnormArgs& a) const {
+        const size_t g = (size_t)image * a.groups + column / a.depth;
+        return Channel{a.mean[g], a.rstd[g], a.gain ? a.gain[column] : 1.f, a.bias ? a.bias[column] : 0.f};
     }
 };
 
@@ -99,8 +163,8 @@ __device__ __forceinline__ bool last_of_image(const GnormArgs& a, int image) {
     if (threadIdx.x == 0) {
         __threadfence();
         const unsigned parts = (unsigned)(a.pieces * a.tiles);
-        last = parts == 1 || atomicAdd(a.arrived + image, 1u) == parts - 1;
-        if (last && parts > 1) a.arrived[image] = 0;
+        last = atomicAdd(a.arrived + image, 1u) == parts - 1;
+        if (last) a.arrived[image] = 0;
     }
     __syncthreads();
     if (last) __threadfence();
@@ -109,45 +173,33 @@ __device__ __forceinline__ bool last_of_image(const GnormArgs& a, int image) {
 
 // A thread's sums of a channel run around the thread's first value, which bounds what the difference of the two sums loses; means are kept as
 // differences from the channel's first value in the image, so that a large offset costs no digits, until they are joined in float64.
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* __restrict__ x, GnormArgs a) {
-    __shared__ float2 sums[kGnormThreads * VEC];
+template <typename T>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_any_stats_kernel(const T* __restrict__ x, GnormArgs a) {
+    __shared__ float2 sums[kGnormThreads];
     pdl_begin();
-    const GnormPlace<VEC> at(a);
-    float pivot[VEC], s1[VEC], s2[VEC];
-    int n = 0;
+    const GnormPlace at(a);
     if (at.live) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) pivot[e] = s1[e] = s2[e] = 0.f;
+        float pivot = 0.f, s1 = 0.f, s2 = 0.f;
+        int n = 0;
+#pragma unroll 4
         for (int p = at.from + at.lane; p < at.to; p += at.lanes, ++n) {
-            RawVec<T, VEC> raw;
-            raw.load(x + at.at(a, p));
-            if (n == 0)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) pivot[e] = raw.get(e);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = raw.get(e) - pivot[e];
-                s1[e] += d;
-                s2[e] = fmaf(d, d, s2[e]);
-            }
+            const float v = to_float(x[at.at(a, p)]);
+            if (n == 0) pivot = v;
+            const float d = v - pivot;
+            s1 += d;
+            s2 = fmaf(d, d, s2);
         }
         const float inv = n ? 1.f / (float)n : 0.f;
-        RawVec<T, VEC> first;
-        first.load(x + at.at(a, 0));
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            sums[(at.lane * a.columns + threadIdx.x % a.columns) * VEC + e] = make_float2(fmaf(s1[e], inv, pivot[e] - first.get(e)), s2[e] - s1[e] * s1[e] * inv);
+        sums[threadIdx.x] = make_float2(fmaf(s1, inv, pivot - to_float(x[at.at(a, 0)])), s2 - s1 * s1 * inv);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.columns * VEC; i += kGnormThreads) {
-        const int c = at.tile * a.columns * VEC + i;
-        if (c >= a.channels) continue;
+    const int c = at.tile * a.columns + threadIdx.x;
+    if ((int)threadIdx.x < a.columns && c < a.channels) {
         float count = 0.f, mean = 0.f, m2 = 0.f;
         for (int l = 0; l < at.lanes; ++l) {
             const int mine = (at.to - at.from - l + at.lanes - 1) / at.lanes;
             if (mine <= 0) break;
-            const float2 v = sums[l * a.columns * VEC + i];
+            const float2 v = sums[l * a.columns + threadIdx.x];
             const float all = count + (float)mine, d = v.x - mean, part = (float)mine / all;
             mean = fmaf(d, part, mean);
             m2 += v.y + d * d * count * part;
@@ -185,89 +237,56 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* __r
         }
     }
 }
-
-template <typename T, typename U, int VEC, int ACT>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
+template <typename T, typename U>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_any_apply_kernel(const T* x, U* y, GnormArgs a) {
     pdl_begin();
-    const GnormPlace<VEC> at(a);
+    const GnormPlace at(a);
     if (!at.live) return;
-    float mean[VEC], scale[VEC], bias[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const Channel c = at.channel(a, e);
-        mean[e] = c.mean;
-        scale[e] = c.rstd * c.gain;
-        bias[e] = c.bias;
-    }
-    for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
-        RawVec<T, VEC> raw;
-        float v[VEC];
-        raw.load(x + at.at(a, p));
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = activate<ACT>(fmaf(raw.get(e) - mean[e], scale[e], bias[e]));
-        store_vec<VEC>(y + at.at(a, p), v);
-    }
+    const Channel c = at.channel(a);
+    const float scale = c.rstd * c.gain;
+    with_act_of(a.act, [&](auto act) {
+#pragma unroll 4
+        for (int p = at.from + at.lane; p < at.to; p += at.lanes)
+            store_one(y + at.at(a, p), activate<decltype(act)::value>(fmaf(to_float(x[at.at(a, p)]) - c.mean, scale, c.bias)));
+    });
 }
-
-template <typename T, typename U, int VEC, int ACT>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* __restrict__ x, const U* __restrict__ grad_y, GnormArgs a) {
-    __shared__ float2 sums[kGnormThreads * VEC];
+template <typename T, typename U>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_any_sums_kernel(const T* __restrict__ x, const U* __restrict__ grad_y, GnormArgs a) {
+    __shared__ float2 sums[kGnormThreads];
     pdl_begin();
-    const GnormPlace<VEC> at(a);
+    const GnormPlace at(a);
     if (at.live) {
-        Channel ch[VEC];
-        float s1[VEC], s2[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            ch[e] = at.channel(a, e);
-            s1[e] = s2[e] = 0.f;
-        }
-        for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
-            RawVec<T, VEC> raw;
-            RawVec<U, VEC> graw;
-            raw.load(x + at.at(a, p));
-            graw.load(grad_y + at.at(a, p));
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float v = raw.get(e), u = ch[e].unit(v), g = graw.get(e) * ch[e].template slope<ACT>(v, u);
-                s1[e] += g;
-                s2[e] = fmaf(g, u, s2[e]);
+        const Channel ch = at.channel(a);
+        float s1 = 0.f, s2 = 0.f;
+        with_act_of(a.act, [&](auto act) {
+#pragma unroll 4
+            for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
+                const float v = to_float(x[at.at(a, p)]), u = ch.unit(v), g = to_float(grad_y[at.at(a, p)]) * ch.template slope<decltype(act)::value>(v, u);
+                s1 += g;
+                s2 = fmaf(g, u, s2);
             }
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) sums[(at.lane * a.columns + threadIdx.x % a.columns) * VEC + e] = make_float2(s1[e], s2[e]);
+        });
+        sums[threadIdx.x] = make_float2(s1, s2);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.columns * VEC; i += kGnormThreads) {
-        const int c = at.tile * a.columns * VEC + i;
-        if (c >= a.channels) continue;
+    const int c = at.tile * a.columns + threadIdx.x;
+    if ((int)threadIdx.x < a.columns && c < a.channels) {
         float2 s = make_float2(0.f, 0.f);
         for (int l = 0; l < at.lanes; ++l) {
-            const float2 v = sums[l * a.columns * VEC + i];
-            s.x += v.x;
-            s.y += v.y;
+            s.x += sums[l * a.columns + threadIdx.x].x;
+            s.y += sums[l * a.columns + threadIdx.x].y;
         }
         a.parts[((size_t)at.image * a.pieces + at.piece) * a.channels + c] = s;
     }
     if (!last_of_image(a, at.image)) return;
-    for (int c = threadIdx.x; c < a.channels; c += kGnormThreads) {
-        double s1 = 0.0, s2 = 0.0;
-        for (int piece = 0; piece < a.pieces; ++piece) {
-            const float2 v = __ldcg(a.parts + ((size_t)at.image * a.pieces + piece) * a.channels + c);
-            s1 += (double)v.x;
-            s2 += (double)v.y;
-        }
-        a.totals[(size_t)at.image * a.channels + c] = make_float2((float)s1, (float)s2);
-    }
-    __syncthreads();
-    const int lane = threadIdx.x % 32;
+    const int lane = threadIdx.x % 32, entries = a.pieces * a.depth;
     const double m = (double)a.pixels * a.depth;
     for (int g = threadIdx.x / 32; g < a.groups; g += kGnormThreads / 32) {
         double s1 = 0.0, s2 = 0.0;
-        for (int i = lane; i < a.depth; i += 32) {
-            const int c = g * a.depth + i;
-            const float2 v = a.totals[(size_t)at.image * a.channels + c];
-            const double gain = a.gain ? (double)a.gain[c] : 1.0;
+        for (int i = lane; i < entries; i += 32) {
+            const int k = g * a.depth + i % a.depth;
+            const float2 v = __ldcg(a.parts + ((size_t)at.image * a.pieces + i / a.depth) * a.channels + k);
+            const double gain = a.gain ? (double)a.gain[k] : 1.0;
             s1 += gain * v.x;
             s2 += gain * v.y;
         }
@@ -279,117 +298,470 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* __re
         if (lane == 0) a.means[(size_t)at.image * a.groups + g] = make_float2((float)(s1 / m), (float)(s2 / m));
     }
 }
-
-// The blocks behind those of the pixels add up the gain's and the bias's gradients over the images, 32 channels each.
-template <typename T, typename U, int VEC, int ACT>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_grad_kernel(const T* x, const U* grad_y, T* grad_x, float* grad_gain, float* grad_bias, GnormArgs a) {
-    __shared__ double2 red[kGnormThreads / 32][32];
+template <typename T, typename U>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
     pdl_begin();
-    const unsigned blocks = grad_x ? (unsigned)a.images * a.pieces * a.tiles : 0;
-    if (blockIdx.x >= blocks) {
-        const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = (int)(blockIdx.x - blocks) * 32 + lane;
-        double2 s = make_double2(0.0, 0.0);
-        if (c < a.channels)
-            for (int n = warp; n < a.images; n += kGnormThreads / 32) {
-                const float2 v = a.totals[(size_t)n * a.channels + c];
-                s.x += (double)v.x;
-                s.y += (double)v.y;
-            }
-        red[warp][lane] = s;
-        __syncthreads();
-        if (warp == 0 && c < a.channels) {
-            for (int w = 1; w < kGnormThreads / 32; ++w) {
-                s.x += red[w][lane].x;
-                s.y += red[w][lane].y;
-            }
-            if (grad_bias) grad_bias[c] = (float)s.x;
-            if (grad_gain) grad_gain[c] = (float)s.y;
-        }
-        return;
-    }
-    const GnormPlace<VEC> at(a);
+    const GnormPlace at(a);
     if (!at.live) return;
-    Channel ch[VEC];
-    float mean_a[VEC], mean_b[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        ch[e] = at.channel(a, e);
-        const float2 m = a.means[(size_t)at.image * a.groups + (at.column * VEC + e) / a.depth];
-        mean_a[e] = m.x;
-        mean_b[e] = m.y;
+    const Channel ch = at.channel(a);
+    const float2 m = a.means[(size_t)at.image * a.groups + at.column / a.depth];
+    with_act_of(a.act, [&](auto act) {
+#pragma unroll 4
+        for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
+            const float v = to_float(x[at.at(a, p)]), u = ch.unit(v), g = to_float(grad_y[at.at(a, p)]) * ch.template slope<decltype(act)::value>(v, u);
+            store_one(grad_x + at.at(a, p), ch.rstd * (fmaf(g, ch.gain, -m.x) - u * m.y));
+        }
+    });
+}
+
+// ---- tensors up to 256 vectors of channels wide ----
+// Two launches: the sums of pieces of the images (the block that is last to finish an image's joins them), and the output, which takes the images in reverse
+// order: the last ones read are still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
+// (One launch, whose blocks took sums and outputs from a counter and waited for an image's sums, read every image once, but an image's counting, waiting
+// and joining by small tasks cost more than the second reading: 145 us for 32 x 112 x 112 x 256 bfloat16.)
+// Pieces run through the images as `per` pixels each; `chunk` images from `image0` on are one launch's.
+template <int VEC>
+struct Stretch {
+    int image, piece, lanes, lane, column, here, mine;      // `here` pixels of the piece, `mine` of this thread: lane, lane + lanes, ...
+    bool live;
+    size_t at, step;                                       // element of the first, and between two
+    __device__ __forceinline__ Stretch(const GnormArgs& a, unsigned block) {
+        image = a.image0 + block / a.pieces;
+        piece = block % a.pieces;
+        lanes = kGnormThreads / a.columns;
+        lane = threadIdx.x / a.columns;
+        column = threadIdx.x % a.columns;
+        live = lane < lanes;
+        const int from = piece * a.per;
+        here = min(a.per, a.pixels - from);
+        mine = live ? (here - lane + lanes - 1) / lanes : 0;
+        at = ((size_t)image * a.pixels + from + lane) * a.channels + (size_t)column * VEC;
+        step = (size_t)lanes * a.channels;
     }
-    for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
-        RawVec<T, VEC> raw;
-        RawVec<U, VEC> graw;
-        float out[VEC];
-        raw.load(x + at.at(a, p));
-        graw.load(grad_y + at.at(a, p));
+};
+// Sums over an image's parts for every group: f(group, sum of x-terms, sum of y-terms), in float64.  `red`: [kGnormThreads] double2.
+template <typename TERM, typename F>
+__device__ __forceinline__ void join_groups(const GnormArgs& a, int image, double2* red, TERM term, F f) {
+    const int wide = min(a.groups, kGnormThreads), rows = kGnormThreads / wide, r = threadIdx.x / wide;
+    for (int g0 = 0; g0 < a.groups; g0 += wide) {
+        const int g = g0 + threadIdx.x % wide;
+        double2 s = make_double2(0.0, 0.0);
+        if (r < rows && g < a.groups) {
+            const float2* p = a.group_parts + (size_t)image * a.pieces * a.groups + g;
+#pragma unroll 4
+            for (int t = r; t < a.pieces; t += rows) {
+                const double2 v = term(t, __ldcg(p + (size_t)t * a.groups));
+                s.x += v.x;
+                s.y += v.y;
+            }
+        }
+        __syncthreads();
+        red[threadIdx.x] = s;
+        __syncthreads();
+        if (r == 0 && g < a.groups) {
+            for (int i = 1; i < rows; ++i) {
+                s.x += red[i * wide + threadIdx.x].x;
+                s.y += red[i * wide + threadIdx.x].y;
+            }
+            f(g, s);
+        }
+    }
+}
+// Every group's channels in shared memory, by as many lanes of a warp as there are channels in one: f(group, lane of that many, their number, whether
+// the group is one).
+template <typename F>
+__device__ __forceinline__ void each_group(const GnormArgs& a, F f) {
+    int shift = 0;
+    while (1 << shift < a.depth && shift < 5) ++shift;
+    for (int g0 = 0; g0 < a.groups; g0 += kGnormThreads >> shift) {
+        const int g = g0 + (threadIdx.x >> shift);
+        f(g, threadIdx.x & ((1 << shift) - 1), 1 << shift, g < a.groups);
+    }
+}
+__device__ __forceinline__ float lanes_sum(float v, int wide) {
+    for (int o = wide / 2; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Pair two(const RawVec<T, VEC>& r, int i) {
+    if constexpr (VEC > 1) return r.get2(2 * i);
+    else return pair_of(r.get(0), 0.f);
+}
+__device__ __forceinline__ float half(Pair p, int e) {
+    float lo, hi;
+    split(p, lo, hi);
+    return e % 2 ? hi : lo;
+}
+// Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.
+template <int R, typename LOAD, typename TAKE>
+__device__ __forceinline__ void walk_pixels(int mine, size_t at, size_t step, LOAD load, TAKE take) {
+    for (; mine >= R; mine -= R, at += R * step) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) load(i, at + i * step);
+#pragma unroll
+        for (int i = 0; i < R; ++i) take(i, at + i * step);
+    }
+    if (mine <= 0) return;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (i < mine) load(i, at + i * step);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (i < mine) take(i, at + i * step);
+}
+
+// A piece's sums: a thread's, around the channel's value at its first pixel (which bounds what the difference of the two sums loses), those of the
+// threads that share a channel, and those of a group's channels, each around their joint mean.  Means are kept as differences from the image's first
+// pixel, so that a large offset costs no digits.
+template <typename T, int VEC, int R>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, GnormArgs a) {
+    constexpr int N = Channels<VEC>::N;
+    __shared__ float2 sums[kGnormThreads * VEC];
+    __shared__ float firsts[kGnormThreads * VEC];
+    __shared__ double2 red[kGnormThreads];
+    pdl_begin();
+    const Stretch<VEC> st(a, blockIdx.x);
+    const T* first = x + (size_t)st.image * a.pixels * a.channels;
+    if (st.live) {
+        RawVec<T, VEC> raw[R], zero, own;
+        zero.load(first + st.column * VEC);
+        own.load(st.mine > 0 ? x + st.at : first + st.column * VEC);
+        Pair pivot[N], s1[N], s2[N];       // pivot: less than 0
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            pivot[i] = pair_mul(two(own, i), pair_of(-1.f, -1.f));
+            s1[i] = s2[i] = pair_of(0.f, 0.f);
+        }
+        walk_pixels<R>(st.mine, st.at, st.step, [&](int i, size_t o) { raw[i].load(x + o); },
+                       [&](int i, size_t) {
+#pragma unroll
+                           for (int k = 0; k < N; ++k) {
+                               const Pair d = pair_add(two(raw[i], k), pivot[k]);
+                               s1[k] = pair_add(s1[k], d);
+                               s2[k] = pair_fma(d, d, s2[k]);
+                           }
+                       });
+        const float inv = st.mine > 0 ? 1.f / (float)st.mine : 0.f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const float v = raw.get(e), u = ch[e].unit(v), g = graw.get(e) * ch[e].template slope<ACT>(v, u);
-            out[e] = ch[e].rstd * (fmaf(g, ch[e].gain, -mean_a[e]) - u * mean_b[e]);
+            const float f = zero.get(e), sum = half(s1[e / 2], e), square = half(s2[e / 2], e);
+            sums[(st.lane * a.columns + st.column) * VEC + e] = make_float2(fmaf(sum, inv, -half(pivot[e / 2], e) - f), square - sum * sum * inv);
+            if (st.lane == 0) firsts[st.column * VEC + e] = f;
         }
-        store_vec<VEC>(grad_x + at.at(a, p), out);
+    }
+    __syncthreads();
+    const int least = st.here / st.lanes, more = st.here - least * st.lanes;      // pixels of lane l: least + (l < more)
+    for (int c = threadIdx.x; c < a.channels; c += kGnormThreads) {
+        float s = 0.f, q = 0.f;
+        for (int l = 0; l < st.lanes; ++l)
+            if (least > 0 || l < more) s = fmaf((float)(least + (l < more)), sums[l * a.channels + c].x, s);
+        const float mean = s / (float)st.here;
+        for (int l = 0; l < st.lanes; ++l)
+            if (least > 0 || l < more) {
+                const float2 v = sums[l * a.channels + c];
+                const float d = v.x - mean;
+                q += fmaf(d * d, (float)(least + (l < more)), v.y);
+            }
+        sums[c] = make_float2(mean, q);
+    }
+    __syncthreads();
+    each_group(a, [&](int g, int l, int wide, bool one) {
+        const int c0 = g * a.depth, end = one ? a.depth : 0;
+        const float f = one ? firsts[c0] : 0.f;
+        float s = 0.f, q = 0.f;
+        for (int i = l; i < end; i += wide) s += sums[c0 + i].x + (firsts[c0 + i] - f);
+        const float mean = lanes_sum(s, wide) / (float)a.depth;
+        for (int i = l; i < end; i += wide) {
+            const float2 v = sums[c0 + i];
+            const float d = v.x + (firsts[c0 + i] - f) - mean;
+            q += fmaf(d * d, (float)st.here, v.y);
+        }
+        q = lanes_sum(q, wide);
+        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_float2(mean, q);
+    });
+    if (!last_of_image(a, st.image)) return;
+    join_groups(a, st.image, red,
+                [&](int t, float2 v) {
+                    const double k = (double)(min(a.per, a.pixels - t * a.per) * a.depth), mean = (double)v.x;
+                    return make_double2(k * mean, (double)v.y + k * mean * mean);
+                },
+                [&](int g, double2 s) {
+                    const double mean = s.x * a.inv_m, var = s.y * a.inv_m - mean * mean;
+                    a.mean[(size_t)st.image * a.groups + g] = (float)(mean + (double)to_float(first[g * a.depth]));
+                    a.rstd[(size_t)st.image * a.groups + g] = 1.f / sqrtf((var < 0.0 ? 0.f : (float)var) + a.eps);
+                });
+}
+
+template <typename T, typename U, int VEC, int R>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
+    pdl_begin();
+    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x);
+    if (!st.live) return;
+    Channels<VEC> ch;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const int c = st.column * VEC + e;
+        const size_t g = (size_t)st.image * a.groups + c / a.depth;
+        ch.set(e, a.mean[g], a.rstd[g] * (a.gain ? __ldg(a.gain + c) : 1.f), 1.f, a.bias ? __ldg(a.bias + c) : 0.f);
+    }
+    with_act_of(a.act, [&](auto act) {
+        RawVec<T, VEC> raw[R];
+        walk_pixels<R>(st.mine, st.at, st.step, [&](int i, size_t o) { raw[i].load(x + o); },
+                       [&](int i, size_t o) {
+                           float v[VEC > 1 ? VEC : 2], out[VEC];
+#pragma unroll
+                           for (int k = 0; k < Channels<VEC>::N; ++k)
+                               split(pair_fma(pair_add(two(raw[i], k), ch.mean[k]), ch.rstd[k], ch.bias[k]), v[2 * k], v[2 * k + 1]);
+#pragma unroll
+                           for (int e = 0; e < VEC; ++e) out[e] = activate<decltype(act)::value>(v[e]);
+                           store_vec_once<VEC>(y + o, out);
+                       });
+    });
+}
+
+// Backward: the channels' sums of the pieces go to `parts`; the gain's and the bias's gradients are added up from them by gnorm_total_kernel.
+template <int VEC>
+__device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<VEC>& st, Channels<VEC>& ch) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const int c = st.column * VEC + e;
+        const size_t g = (size_t)st.image * a.groups + c / a.depth;
+        ch.set(e, __ldg(a.mean + g), __ldg(a.rstd + g), a.gain ? __ldg(a.gain + c) : 1.f, a.bias ? __ldg(a.bias + c) : 0.f);
+    }
+}
+template <typename T, typename U, int VEC, int R>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* x, const U* grad_y, GnormArgs a) {
+    constexpr int N = Channels<VEC>::N;
+    __shared__ float2 sums[kGnormThreads * VEC];
+    __shared__ double2 red[kGnormThreads];
+    pdl_begin();
+    const Stretch<VEC> st(a, blockIdx.x);
+    if (st.live) {
+        Channels<VEC> ch;
+        load_channels(a, st, ch);
+        Pair s1[N], s2[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) s1[i] = s2[i] = pair_of(0.f, 0.f);
+        with_act_of(a.act, [&](auto act) {
+            RawVec<T, VEC> raw[R];
+            RawVec<U, VEC> graw[R];
+            walk_pixels<R>(st.mine, st.at, st.step,
+                           [&](int i, size_t o) {
+                               raw[i].load(x + o);
+                               graw[i].load(grad_y + o);
+                           },
+                           [&](int i, size_t) {
+#pragma unroll
+                               for (int k = 0; k < N; ++k) {
+                                   Pair u, g;
+                                   ch.template slopes<decltype(act)::value>(k, two(raw[i], k), two(graw[i], k), u, g);
+                                   s1[k] = pair_add(s1[k], g);
+                                   s2[k] = pair_fma(g, u, s2[k]);
+                               }
+                           });
+        });
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sums[(st.lane * a.columns + st.column) * VEC + e] = make_float2(half(s1[e / 2], e), half(s2[e / 2], e));
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.channels; c += kGnormThreads) {
+        float2 s = sums[c];
+        for (int l = 1; l < st.lanes; ++l) {
+            s.x += sums[l * a.channels + c].x;
+            s.y += sums[l * a.channels + c].y;
+        }
+        sums[c] = s;
+        a.parts[((size_t)st.image * a.pieces + st.piece) * a.channels + c] = s;
+    }
+    __syncthreads();
+    each_group(a, [&](int g, int l, int wide, bool one) {
+        float s = 0.f, q = 0.f;
+        for (int i = l; i < (one ? a.depth : 0); i += wide) {
+            const int c = g * a.depth + i;
+            const float gain = a.gain ? __ldg(a.gain + c) : 1.f;
+            s = fmaf(gain, sums[c].x, s);
+            q = fmaf(gain, sums[c].y, q);
+        }
+        s = lanes_sum(s, wide);
+        q = lanes_sum(q, wide);
+        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_float2(s, q);
+    });
+    if (!last_of_image(a, st.image)) return;
+    join_groups(a, st.image, red, [&](int, float2 v) { return make_double2((double)v.x, (double)v.y); },
+                [&](int g, double2 s) { a.means[(size_t)st.image * a.groups + g] = make_float2((float)(s.x * a.inv_m), (float)(s.y * a.inv_m)); });
+}
+template <typename T, typename U, int VEC, int R>
+__global__ void __launch_bounds__(kGnormThreads) gnorm_grad_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
+    constexpr int N = Channels<VEC>::N;
+    pdl_begin();
+    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x);
+    if (!st.live) return;
+    Channels<VEC> ch;
+    load_channels(a, st, ch);
+    Pair mean_a[N], mean_b[N];       // less than 0
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const float2 m = a.means[(size_t)st.image * a.groups + (st.column * VEC + e) / a.depth];
+        Channels<VEC>::put(mean_a[e / 2], e % 2, -m.x);
+        Channels<VEC>::put(mean_b[e / 2], e % 2, -m.y);
+    }
+    with_act_of(a.act, [&](auto act) {
+        RawVec<T, VEC> raw[R];
+        RawVec<U, VEC> graw[R];
+        walk_pixels<R>(st.mine, st.at, st.step,
+                       [&](int i, size_t o) {
+                           raw[i].load(x + o);
+                           graw[i].load(grad_y + o);
+                       },
+                       [&](int i, size_t o) {
+                           float v[VEC > 1 ? VEC : 2], out[VEC];
+#pragma unroll
+                           for (int k = 0; k < N; ++k) {
+                               Pair u, g;
+                               ch.template slopes<decltype(act)::value>(k, two(raw[i], k), two(graw[i], k), u, g);
+                               split(pair_mul(ch.rstd[k], pair_fma(u, mean_b[k], pair_fma(g, ch.gain[k], mean_a[k]))), v[2 * k], v[2 * k + 1]);
+                           }
+#pragma unroll
+                           for (int e = 0; e < VEC; ++e) out[e] = v[e];
+                           store_vec_once<VEC>(grad_x + o, out);
+                       });
+    });
+}
+// Channel sums over `rows` rows of float2 [C], 32 channels and a stretch of `per` rows a block: into out [stretches][C], or the gradients where the
+// stretch is all of them.
+constexpr int kTotalThreads = 1024;
+template <bool LAST>
+__global__ void __launch_bounds__(kTotalThreads) gnorm_total_kernel(const float2* __restrict__ in, float2* out, float* grad_gain, float* grad_bias, int rows,
+                                                                    int per, int channels) {
+    __shared__ double2 red[kTotalThreads / 32][32];
+    pdl_begin();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = (int)blockIdx.x * 32 + lane, from = blockIdx.y * per, to = min(rows, from + per);
+    double2 s = make_double2(0.0, 0.0);
+    if (c < channels)
+#pragma unroll 8
+        for (int r = from + warp; r < to; r += kTotalThreads / 32) {
+            const float2 v = in[(size_t)r * channels + c];
+            s.x += (double)v.x;
+            s.y += (double)v.y;
+        }
+    red[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || c >= channels) return;
+    for (int w = 1; w < kTotalThreads / 32; ++w) {
+        s.x += red[w][lane].x;
+        s.y += red[w][lane].y;
+    }
+    if constexpr (LAST) {
+        if (grad_bias) grad_bias[c] = (float)s.x;
+        if (grad_gain) grad_gain[c] = (float)s.y;
+    } else {
+        out[(size_t)blockIdx.y * channels + c] = make_float2((float)s.x, (float)s.y);
     }
 }
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
+constexpr int kFewTasks = 1184;             // blocks below which their pieces are made smaller
 
-static void lay_out(GnormArgs& a, int vec) {
-    const int vectors = a.channels / vec;
-    a.columns = vectors < kGnormThreads ? vectors : kGnormThreads;
-    a.tiles = (vectors + a.columns - 1) / a.columns;
-    const int lanes = kGnormThreads / a.columns;
-    const long want = (kGnormTarget + (long)a.images * a.tiles - 1) / ((long)a.images * a.tiles), can = (a.pixels + 4L * lanes - 1) / (4L * lanes);
-    const long pieces = want < can ? want : can;
-    a.per = (int)((a.pixels + pieces - 1) / pieces);
-    a.pieces = (a.pixels + a.per - 1) / a.per;
+// How a call is run.
+struct GnormPlan {
+    int vec, r;             // elements a vector, pixels a thread; vec 0: any tensor
+    int columns, tiles, pieces, per;
+};
+static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, uintptr_t addresses) {
+    const size_t xb = dtype_bytes(g->x_dtype), yb = dtype_bytes(g->y_dtype), small = xb < yb ? xb : yb;
+    GnormPlan p{};
+    const int widest = small == 2 ? 8 : 4;
+    for (int vec : {widest, 4, 1})       // 16 bytes of the smaller type, 4 elements, or single ones
+        if (g->channels % vec == 0 && g->channels / vec <= kGnormThreads && addresses % (vec * small) == 0 && addresses % (vec * xb < 16 ? vec * xb : 16) == 0 &&
+            addresses % (vec * yb < 16 ? vec * yb : 16) == 0) {
+            p.vec = vec;
+            break;
+        }
+    if (p.vec) {
+        p.columns = g->channels / p.vec;
+        p.tiles = 1;
+        const int lanes = kGnormThreads / p.columns;
+        p.r = backward || (p.vec == 8 && xb == 4) ? 4 : 8;
+        auto tasks = [&](int n) { return (long)images * ((pixels + lanes * n - 1) / (lanes * n)); };      // of n pixels a thread
+        int each = 16 * p.r;
+        while (each > 1 && tasks(each) < kFewTasks) each /= 2;
+        if (each == 1) p.r = 1;
+        p.per = lanes * each;
+    } else {
+        p.columns = kGnormThreads < g->channels ? kGnormThreads : g->channels;
+        p.tiles = (g->channels + p.columns - 1) / p.columns;
+        const int lanes = kGnormThreads / p.columns;
+        const long want = (kGnormTarget + (long)images * p.tiles - 1) / ((long)images * p.tiles), can = (pixels + 8L * lanes - 1) / (8L * lanes);
+        const long pieces = want < can ? want : can;
+        p.per = (int)((pixels + pieces - 1) / pieces);
+    }
+    p.pieces = (pixels + p.per - 1) / p.per;
+    return p;
+}
+// Tasks that any call of up to `images` images of up to `pixels` pixels has at most.
+static long tasks_of(const Gnorm* g, long images, long pixels) {
+    long most = 0;
+    for (int vec : {8, 4, 1})
+        for (int r : {8, 4}) {
+            if (g->channels % vec || g->channels / vec > kGnormThreads) continue;
+            const long l = kGnormThreads / (g->channels / vec), n = images * ((pixels + l * r - 1) / (l * r));
+            most = n > most ? n : most;
+        }
+    const long small = 8 * kFewTasks + images, any = kGnormTarget + images;       // of one pixel a thread; of any tensor
+    return std::max({most, small, any});
 }
 
-// Workspace: the images' counters, the parts' sums, the images' totals, the groups' means, and mean and rstd where the caller keeps none.
+// Workspace: the images' counters, the tasks' sums, sums of many tasks, the groups' means, and mean and rstd where the caller keeps
+// none.
+constexpr int kStretches = 1024;
 struct GnormSpace {
-    size_t parts, totals, means, stats, bytes;
+    size_t group_parts, parts, totals, means, stats, bytes;
 };
-static GnormSpace space_of(const Gnorm* g, long images) {
+static GnormSpace space_of(const Gnorm* g, long images, long tasks) {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     GnormSpace s;
-    s.parts = up(sizeof(unsigned) * images);
-    s.totals = s.parts + up(sizeof(float2) * (images * g->channels + kGnormTarget * (long)(g->channels < kGnormThreads * 8 ? g->channels : kGnormThreads * 8)));
-    s.means = s.totals + up(sizeof(float2) * images * g->channels);
+    s.group_parts = up(sizeof(unsigned) * images);
+    s.parts = s.group_parts + up(sizeof(float2) * tasks * g->groups);
+    s.totals = s.parts + up(sizeof(float2) * tasks * g->channels);
+    s.means = s.totals + up(sizeof(float2) * kStretches * g->channels);
     s.stats = s.means + up(sizeof(float2) * images * g->groups);
     s.bytes = s.stats + up(2 * sizeof(float) * images * g->groups);
     return s;
 }
-static int ensure_gnorm(Gnorm* g, int images, cudaStream_t s) {
-    if (images <= g->images_held) return ensure_scratch(g->ws, space_of(g, g->images_held).bytes, s, "circ_gnorm_reserve");
-    const int rc = ensure_scratch(g->ws, space_of(g, images).bytes, s, "circ_gnorm_reserve");
-    g->images_held = rc == CIRC_OK ? images : g->ws.ptr ? g->images_held : 0;
-    if (rc != CIRC_OK) return rc;
-    if (cudaMemsetAsync(g->ws.ptr, 0, space_of(g, images).parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+static int ensure_gnorm(Gnorm* g, long images, long tasks, cudaStream_t s) {
+    if (images <= g->images_held && tasks <= g->tasks_held) return ensure_scratch(g->ws, space_of(g, g->images_held, g->tasks_held).bytes, s, "circ_gnorm_reserve");
+    images = std::max(images, g->images_held);
+    tasks = std::max(tasks, g->tasks_held);
+    const int rc = ensure_scratch(g->ws, space_of(g, images, tasks).bytes, s, "circ_gnorm_reserve");
+    if (rc != CIRC_OK) {
+        if (!g->ws.ptr) g->images_held = g->tasks_held = 0;
+        return rc;
+    }
+    g->images_held = images;
+    g->tasks_held = tasks;
+    if (cudaMemsetAsync(g->ws.ptr, 0, space_of(g, images, tasks).group_parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaFree(g->ws.ptr);      // this one alone: graphs may hold earlier ones
         g->ws.ptr = nullptr;
         g->ws.bytes = 0;
-        g->images_held = 0;
+        g->images_held = g->tasks_held = 0;
         set_error(CIRC_ERR_CUDA, "clearing the workspace failed: %s", cudaGetErrorString(cudaGetLastError()));
         return CIRC_ERR_CUDA;
     }
     return CIRC_OK;
 }
 
-template <typename F>
-static void with_act(int act, F&& f) {
-    if (act == CIRC_ACT_RELU) f(std::integral_constant<int, CIRC_ACT_RELU>{});
-    else if (act == CIRC_ACT_SILU) f(std::integral_constant<int, CIRC_ACT_SILU>{});
-    else f(std::integral_constant<int, CIRC_ACT_NONE>{});
+// Calls f(vector elements, pixels a thread) as constants.
+template <typename T, bool BACKWARD, typename F>
+static void with_plan(const GnormPlan& p, F&& f) {
+    auto with_r = [&](auto vec) {
+        constexpr int VEC = decltype(vec)::value, R = BACKWARD || (VEC == 8 && sizeof(T) == 4) ? 4 : 8;
+        if (p.r == 1) f(vec, std::integral_constant<int, 1>{});
+        else f(vec, std::integral_constant<int, R>{});
+    };
+    if (p.vec == 8) with_r(std::integral_constant<int, 8>{});
+    else if (p.vec == 4) with_r(std::integral_constant<int, 4>{});
+    else with_r(std::integral_constant<int, 1>{});
 }
-// Vectors of 8 elements (4 where both tensors are float32) where every one of them is aligned, else single elements.
-template <typename T, typename U, typename F>
-static void with_vectors(bool aligned, int channels, F&& f) {
-    constexpr int VEC = sizeof(T) == 4 && sizeof(U) == 4 ? 4 : 8;
-    if (aligned && channels % VEC == 0) f(std::integral_constant<int, VEC>{});
-    else f(std::integral_constant<int, 1>{});
-}
-
 static int check_gnorm(const Gnorm* g, int N, int H, int W) {
     if (!g) {
         set_error(CIRC_ERR_ARG, "handle is NULL");
@@ -401,8 +773,43 @@ static int check_gnorm(const Gnorm* g, int N, int H, int W) {
     }
     return CIRC_OK;
 }
-static GnormArgs args_of(const Gnorm* g, const float* gain, const float* bias, const float* mean, const float* rstd, int N, int H, int W) {
-    const GnormSpace space = space_of(g, g->images_held);
+template <typename T, typename U>
+static cudaError_t run_forward(const GnormPlan& p, const GnormArgs& a, const T* x, U* y, cudaStream_t s) {
+    cudaError_t err = cudaSuccess;
+    if (p.vec == 0) {
+        const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles));
+        if ((err = launch_row(gnorm_any_stats_kernel<T>, grid, dim3(kGnormThreads), 0, s, x, a)) == cudaSuccess)
+            err = launch_row(gnorm_any_apply_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, y, a);
+        return err;
+    }
+    with_plan<T, false>(p, [&](auto vec, auto r) {
+        constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
+        const dim3 grid((unsigned)((long)a.images * a.pieces));
+        if ((err = launch_row(gnorm_stats_kernel<T, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, a)) == cudaSuccess)
+            err = launch_row(gnorm_apply_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, y, a);
+    });
+    return err;
+}
+template <typename T, typename U>
+static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T* x, const U* grad_y, T* grad_x, cudaStream_t s) {
+    cudaError_t err = cudaSuccess;
+    if (p.vec == 0) {
+        const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles));
+        if ((err = launch_row(gnorm_any_sums_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, grad_y, a)) == cudaSuccess && grad_x)
+            err = launch_row(gnorm_any_grad_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, grad_y, grad_x, a);
+        return err;
+    }
+    with_plan<T, true>(p, [&](auto vec, auto r) {
+        constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
+        const dim3 grid((unsigned)((long)a.images * a.pieces));
+        if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, grad_y, a)) == cudaSuccess && grad_x)
+            err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, grad_y, grad_x, a);
+    });
+    return err;
+}
+
+static GnormArgs args_of(const Gnorm* g, const GnormPlan& p, const float* gain, const float* bias, const float* mean, const float* rstd, int N, int pixels) {
+    const GnormSpace space = space_of(g, g->images_held, g->tasks_held);
     char* ws = static_cast<char*>(g->ws.ptr);
     GnormArgs a{};
     a.gain = gain;
@@ -414,14 +821,22 @@ static GnormArgs args_of(const Gnorm* g, const float* gain, const float* bias, c
     a.groups = g->groups;
     a.depth = g->channels / g->groups;
     a.images = N;
-    a.pixels = H * W;
+    a.pixels = pixels;
     a.eps = g->eps;
+    a.inv_m = 1.0 / ((double)pixels * a.depth);
+    a.columns = p.columns;
+    a.tiles = p.tiles;
+    a.pieces = p.pieces;
+    a.per = p.per;
+    a.act = g->act;
     a.arrived = reinterpret_cast<unsigned*>(ws);
+    a.group_parts = reinterpret_cast<float2*>(ws + space.group_parts);
     a.parts = reinterpret_cast<float2*>(ws + space.parts);
     a.totals = reinterpret_cast<float2*>(ws + space.totals);
     a.means = reinterpret_cast<float2*>(ws + space.means);
     return a;
 }
+static uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
 }  // namespace circ
 
@@ -436,7 +851,7 @@ circ_gnorm_handle circ_gnorm_create(int channels, int groups, float eps) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Gnorm* g = new (std::nothrow) Gnorm{device, channels, groups, eps, CIRC_F32, CIRC_F32, CIRC_ACT_NONE, {}, 0};
+    Gnorm* g = new (std::nothrow) Gnorm{device, channels, groups, eps, CIRC_F32, CIRC_F32, CIRC_ACT_NONE, {}, 0, 0};
     if (!g) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_gnorm_handle>(g);
 }
@@ -472,7 +887,7 @@ int circ_gnorm_set_activation(circ_gnorm_handle h, int activation) {
 int circ_gnorm_reserve(circ_gnorm_handle h, int N, int H, int W) {
     Gnorm* g = reinterpret_cast<Gnorm*>(h);
     const int rc = check_gnorm(g, N, H, W);
-    return rc != CIRC_OK || N == 0 ? rc : ensure_gnorm(g, N, 0);
+    return rc != CIRC_OK || N == 0 ? rc : ensure_gnorm(g, N, tasks_of(g, N, (long)H * W), 0);
 }
 
 int circ_gnorm_forward(circ_gnorm_handle h, const void* x, const float* gain, const float* bias, void* y, float* mean, float* rstd, int N, int H,
@@ -490,23 +905,15 @@ int circ_gnorm_forward(circ_gnorm_handle h, const void* x, const float* gain, co
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    if ((rc = ensure_gnorm(g, N, s)) != CIRC_OK) return rc;
-    GnormArgs a = args_of(g, gain, bias, mean, rstd, N, H, W);
+    const GnormPlan p = plan_of(g, N, H * W, false, address(x) | address(y));
+    if ((rc = ensure_gnorm(g, N, (long)N * p.pieces, s)) != CIRC_OK) return rc;
+    const GnormArgs a = args_of(g, p, gain, bias, mean, rstd, N, H * W);
     cudaError_t err = cudaSuccess;
     with_dtype(g->x_dtype, [&](auto* t) {
         with_dtype(g->y_dtype, [&](auto* u) {
             using T = tag_type<decltype(t)>;
             using U = tag_type<decltype(u)>;
-            with_vectors<T, U>(!misaligned(x, 16) && !misaligned(y, 16), a.channels, [&](auto vec) {
-                constexpr int VEC = decltype(vec)::value;
-                lay_out(a, VEC);
-                const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles));
-                if ((err = launch_row(gnorm_stats_kernel<T, VEC>, grid, dim3(kGnormThreads), 0, s, static_cast<const T*>(x), a)) != cudaSuccess) return;
-                with_act(g->act, [&](auto act) {
-                    err = launch_row(gnorm_apply_kernel<T, U, VEC, decltype(act)::value>, grid, dim3(kGnormThreads), 0, s, static_cast<const T*>(x),
-                                     static_cast<U*>(y), a);
-                });
-            });
+            err = run_forward(p, a, static_cast<const T*>(x), static_cast<U*>(y), s);
         });
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
@@ -537,30 +944,37 @@ int circ_gnorm_backward(circ_gnorm_handle h, const void* x, const float* gain, c
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    if ((rc = ensure_gnorm(g, N, s)) != CIRC_OK) return rc;
-    GnormArgs a = args_of(g, gain, bias, mean, rstd, N, H, W);
+    const GnormPlan p = plan_of(g, N, H * W, true, address(x) | address(grad_y) | address(grad_x));
+    if ((rc = ensure_gnorm(g, N, (long)N * p.pieces, s)) != CIRC_OK) return rc;
+    const GnormArgs a = args_of(g, p, gain, bias, mean, rstd, N, H * W);
     cudaError_t err = cudaSuccess;
+    int launches = grad_x ? 2 : 1;
     with_dtype(g->x_dtype, [&](auto* t) {
         with_dtype(g->y_dtype, [&](auto* u) {
             using T = tag_type<decltype(t)>;
             using U = tag_type<decltype(u)>;
-            with_vectors<T, U>(!misaligned(x, 16) && !misaligned(grad_y, 16) && !misaligned(grad_x, 16), a.channels, [&](auto vec) {
-                constexpr int VEC = decltype(vec)::value;
-                lay_out(a, VEC);
-                with_act(g->act, [&](auto act) {
-                    constexpr int ACT = decltype(act)::value;
-                    const unsigned blocks = (unsigned)((long)a.images * a.pieces * a.tiles), sums = grad_gain || grad_bias ? (a.channels + 31) / 32 : 0;
-                    err = launch_row(gnorm_sums_kernel<T, U, VEC, ACT>, dim3(blocks), dim3(kGnormThreads), 0, s, static_cast<const T*>(x),
-                                     static_cast<const U*>(grad_y), a);
-                    if (err != cudaSuccess) return;
-                    err = launch_row(gnorm_grad_kernel<T, U, VEC, ACT>, dim3((grad_x ? blocks : 0) + sums), dim3(kGnormThreads), 0, s,
-                                     static_cast<const T*>(x), static_cast<const U*>(grad_y), static_cast<T*>(grad_x), grad_gain, grad_bias, a);
-                });
-            });
+            err = run_backward(p, a, static_cast<const T*>(x), static_cast<const U*>(grad_y), static_cast<T*>(grad_x), s);
         });
     });
+    if (err == cudaSuccess && (grad_gain || grad_bias)) {      // over all tasks; where they are many, over stretches of them first
+        const long tasks = (long)N * p.pieces;
+        const unsigned columns = (unsigned)(g->channels + 31) / 32;
+        const float2* in = a.parts;
+        int rows = (int)tasks;
+        if (tasks > 2048) {
+            const int per = (int)std::max(256L, (tasks + kStretches - 1) / kStretches);
+            rows = (int)((tasks + per - 1) / per);
+            err = launch_row(gnorm_total_kernel<false>, dim3(columns, (unsigned)rows), dim3(kTotalThreads), 0, s, in, a.totals, static_cast<float*>(nullptr),
+                             static_cast<float*>(nullptr), (int)tasks, per, g->channels);
+            in = a.totals;
+            ++launches;
+        }
+        if (err == cudaSuccess)
+            err = launch_row(gnorm_total_kernel<true>, dim3(columns), dim3(kTotalThreads), 0, s, in, a.totals, grad_gain, grad_bias, rows, rows, g->channels);
+        ++launches;
+    }
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
-    count_launches(2);
+    count_launches(launches);
     return CIRC_OK;
 }
 

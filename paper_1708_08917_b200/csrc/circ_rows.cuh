@@ -118,6 +118,8 @@ struct RawVec {
     __device__ __forceinline__ void load(const T* p) {
         if constexpr (VEC == 1) {
             w[0] = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)*reinterpret_cast<const uint16_t*>(p);
+        } else if constexpr (WORDS == 1) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
         } else if constexpr (WORDS == 2) {
             const uint2 t = *reinterpret_cast<const uint2*>(p);
             w[0] = t.x; w[1] = t.y;
