@@ -17,7 +17,7 @@ struct Gnorm {
     float eps;
     int x_dtype, y_dtype, act;
     Scratch ws;
-    long images_held, tasks_held;        // that the workspace is laid out for
+    long images_held;       // that the workspace is laid out for
 };
 
 struct GnormArgs {
@@ -30,12 +30,10 @@ struct GnormArgs {
     // a block's part: `columns` vectors of channels (all, or a tile of them), and pixels of one image
     int columns, tiles, pieces, per;
     int act;
-    int image0;               // of a launch's images
     // workspace
     unsigned* arrived;        // [N] parts of an image that are summed up (0 before and after a call)
     float2* group_parts;      // [N][pieces][groups] the tasks' sums of the groups
     float2* parts;            // [N][pieces][C] forward: mean, less the channel's first value, and sum of squares around it; backward: sum of g, of g u
-    float2* totals;           // [N][C] backward: the same over the image
     float2* means;            // [N][groups] backward: A / m, B / m
 };
 
@@ -160,6 +158,7 @@ struct GnormPlace {
 __device__ __forceinline__ bool last_of_image(const GnormArgs& a, int image) {
     __shared__ bool last;
     __syncthreads();
+    if (a.pieces * a.tiles == 1) return true;
     if (threadIdx.x == 0) {
         __threadfence();
         const unsigned parts = (unsigned)(a.pieces * a.tiles);
@@ -319,24 +318,35 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* 
 // order: the last ones read are still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
 // (One launch, whose blocks took sums and outputs from a counter and waited for an image's sums, read every image once, but an image's counting, waiting
 // and joining by small tasks cost more than the second reading: 145 us for 32 x 112 x 112 x 256 bfloat16.)
-// Pieces run through the images as `per` pixels each; `chunk` images from `image0` on are one launch's.
+// A piece takes every pieces-th round of `per` pixels (R of each thread): the blocks that run at once read neighbouring memory.
+struct PieceSize {
+    int full, rest;      // whole rounds, and pixels of one that is not
+    __device__ __forceinline__ PieceSize(const GnormArgs& a, int piece) {
+        const int whole = a.pixels / a.per;
+        full = piece < whole ? (whole - piece + a.pieces - 1) / a.pieces : 0;
+        rest = whole % a.pieces == piece ? a.pixels - whole * a.per : 0;
+    }
+    __device__ __forceinline__ int pixels(const GnormArgs& a) const { return full * a.per + rest; }
+};
 template <int VEC>
 struct Stretch {
-    int image, piece, lanes, lane, column, here, mine;      // `here` pixels of the piece, `mine` of this thread: lane, lane + lanes, ...
+    int image, piece, lanes, lane, column;
+    PieceSize size;
+    int last, mine;           // this thread's pixels: of the round that is not whole, and all
     bool live;
-    size_t at, step;                                       // element of the first, and between two
-    __device__ __forceinline__ Stretch(const GnormArgs& a, unsigned block) {
-        image = a.image0 + block / a.pieces;
+    size_t at, step, jump;    // element of the first, between two pixels, between two rounds
+    __device__ __forceinline__ Stretch(const GnormArgs& a, unsigned block, int r) : size(a, block % a.pieces) {
+        image = block / a.pieces;
         piece = block % a.pieces;
         lanes = kGnormThreads / a.columns;
         lane = threadIdx.x / a.columns;
         column = threadIdx.x % a.columns;
         live = lane < lanes;
-        const int from = piece * a.per;
-        here = min(a.per, a.pixels - from);
-        mine = live ? (here - lane + lanes - 1) / lanes : 0;
-        at = ((size_t)image * a.pixels + from + lane) * a.channels + (size_t)column * VEC;
+        last = live ? (size.rest - lane + lanes - 1) / lanes : 0;
+        mine = live ? size.full * r + last : 0;
+        at = ((size_t)image * a.pixels + (size_t)piece * a.per + lane) * a.channels + (size_t)column * VEC;
         step = (size_t)lanes * a.channels;
+        jump = (size_t)a.pieces * a.per * a.channels;
     }
 };
 // Sums over an image's parts for every group: f(group, sum of x-terms, sum of y-terms), in float64.  `red`: [kGnormThreads] double2.
@@ -392,22 +402,32 @@ __device__ __forceinline__ float half(Pair p, int e) {
     split(p, lo, hi);
     return e % 2 ? hi : lo;
 }
-// Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.
-template <int R, typename LOAD, typename TAKE>
-__device__ __forceinline__ void walk_pixels(int mine, size_t at, size_t step, LOAD load, TAKE take) {
-    for (; mine >= R; mine -= R, at += R * step) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) load(i, at + i * step);
-#pragma unroll
-        for (int i = 0; i < R; ++i) take(i, at + i * step);
+// The threads' sums of a channel lie `columns` apart and those of a vector's elements a block's threads apart, so that neither side's accesses meet in a
+// bank.  Calls f(channel, element, column) for a block's channels, by one thread each.
+template <int VEC, typename F>
+__device__ __forceinline__ void each_channel(const GnormArgs& a, F f) {
+    for (int i = threadIdx.x; i < a.channels; i += kGnormThreads) {
+        const int e = i / a.columns, column = i - e * a.columns;
+        f(column * VEC + e, e, column);
     }
-    if (mine <= 0) return;
+}
+// Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.
+template <int R, int VEC, typename LOAD, typename TAKE>
+__device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, TAKE take) {
+    size_t at = st.at;
+    for (int n = 0; n < st.size.full; ++n, at += st.jump) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) load(i, at + i * st.step);
+#pragma unroll
+        for (int i = 0; i < R; ++i) take(i, at + i * st.step);
+    }
+    if (st.last <= 0) return;
 #pragma unroll
     for (int i = 0; i < R; ++i)
-        if (i < mine) load(i, at + i * step);
+        if (i < st.last) load(i, at + i * st.step);
 #pragma unroll
     for (int i = 0; i < R; ++i)
-        if (i < mine) take(i, at + i * step);
+        if (i < st.last) take(i, at + i * st.step);
 }
 
 // A piece's sums: a thread's, around the channel's value at its first pixel (which bounds what the difference of the two sums loses), those of the
@@ -416,11 +436,11 @@ __device__ __forceinline__ void walk_pixels(int mine, size_t at, size_t step, LO
 template <typename T, int VEC, int R>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
-    __shared__ float2 sums[kGnormThreads * VEC];
+    __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ float firsts[kGnormThreads * VEC];
     __shared__ double2 red[kGnormThreads];
     pdl_begin();
-    const Stretch<VEC> st(a, blockIdx.x);
+    const Stretch<VEC> st(a, blockIdx.x, R);
     const T* first = x + (size_t)st.image * a.pixels * a.channels;
     if (st.live) {
         RawVec<T, VEC> raw[R], zero, own;
@@ -432,7 +452,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, 
             pivot[i] = pair_mul(two(own, i), pair_of(-1.f, -1.f));
             s1[i] = s2[i] = pair_of(0.f, 0.f);
         }
-        walk_pixels<R>(st.mine, st.at, st.step, [&](int i, size_t o) { raw[i].load(x + o); },
+        walk_pixels<R>(st, [&](int i, size_t o) { raw[i].load(x + o); },
                        [&](int i, size_t) {
 #pragma unroll
                            for (int k = 0; k < N; ++k) {
@@ -445,36 +465,37 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, 
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const float f = zero.get(e), sum = half(s1[e / 2], e), square = half(s2[e / 2], e);
-            sums[(st.lane * a.columns + st.column) * VEC + e] = make_float2(fmaf(sum, inv, -half(pivot[e / 2], e) - f), square - sum * sum * inv);
+            sums[e * kGnormThreads + threadIdx.x] = make_float2(fmaf(sum, inv, -half(pivot[e / 2], e) - f), square - sum * sum * inv);
             if (st.lane == 0) firsts[st.column * VEC + e] = f;
         }
     }
     __syncthreads();
-    const int least = st.here / st.lanes, more = st.here - least * st.lanes;      // pixels of lane l: least + (l < more)
-    for (int c = threadIdx.x; c < a.channels; c += kGnormThreads) {
+    const int here = st.size.pixels(a), least = st.size.full * R + st.size.rest / st.lanes, more = st.size.rest % st.lanes;      // pixels of lane l: least + (l < more)
+    const float inv_here = 1.f / (float)here;
+    each_channel<VEC>(a, [&](int c, int e, int column) {
+        const float2* v = sums + e * kGnormThreads + column;
         float s = 0.f, q = 0.f;
         for (int l = 0; l < st.lanes; ++l)
-            if (least > 0 || l < more) s = fmaf((float)(least + (l < more)), sums[l * a.channels + c].x, s);
-        const float mean = s / (float)st.here;
+            if (least > 0 || l < more) s = fmaf((float)(least + (l < more)), v[l * a.columns].x, s);
+        const float mean = s * inv_here;
         for (int l = 0; l < st.lanes; ++l)
             if (least > 0 || l < more) {
-                const float2 v = sums[l * a.channels + c];
-                const float d = v.x - mean;
-                q += fmaf(d * d, (float)(least + (l < more)), v.y);
+                const float d = v[l * a.columns].x - mean;
+                q += fmaf(d * d, (float)(least + (l < more)), v[l * a.columns].y);
             }
-        sums[c] = make_float2(mean, q);
-    }
+        joined[c] = make_float2(mean, q);
+    });
     __syncthreads();
     each_group(a, [&](int g, int l, int wide, bool one) {
         const int c0 = g * a.depth, end = one ? a.depth : 0;
         const float f = one ? firsts[c0] : 0.f;
         float s = 0.f, q = 0.f;
-        for (int i = l; i < end; i += wide) s += sums[c0 + i].x + (firsts[c0 + i] - f);
+        for (int i = l; i < end; i += wide) s += joined[c0 + i].x + (firsts[c0 + i] - f);
         const float mean = lanes_sum(s, wide) / (float)a.depth;
         for (int i = l; i < end; i += wide) {
-            const float2 v = sums[c0 + i];
+            const float2 v = joined[c0 + i];
             const float d = v.x + (firsts[c0 + i] - f) - mean;
-            q += fmaf(d * d, (float)st.here, v.y);
+            q += fmaf(d * d, (float)here, v.y);
         }
         q = lanes_sum(q, wide);
         if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_float2(mean, q);
@@ -482,7 +503,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, 
     if (!last_of_image(a, st.image)) return;
     join_groups(a, st.image, red,
                 [&](int t, float2 v) {
-                    const double k = (double)(min(a.per, a.pixels - t * a.per) * a.depth), mean = (double)v.x;
+                    const double k = (double)PieceSize(a, t).pixels(a) * a.depth, mean = (double)v.x;
                     return make_double2(k * mean, (double)v.y + k * mean * mean);
                 },
                 [&](int g, double2 s) {
@@ -492,21 +513,56 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, 
                 });
 }
 
+// VEC channels' values of a vector of one a channel (NULL: `none`), and of one a group.
+template <int VEC>
+__device__ __forceinline__ void of_channels(const float* p, int c, float none, float (&v)[VEC]) {
+    if (VEC >= 4 && p && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e + 3 < VEC; e += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(p + c + e));
+            v[e] = f.x; v[e + 1] = f.y; v[e + 2] = f.z; v[e + 3] = f.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = p ? __ldg(p + c + e) : none;
+}
+template <int VEC, typename V, typename F>
+__device__ __forceinline__ void of_groups(const GnormArgs& a, const Stretch<VEC>& st, const V* p, F set) {
+    p += (size_t)st.image * a.groups;
+    const int c = st.column * VEC, g = c / a.depth;
+    if (a.depth % VEC == 0) {
+        const V v = p[g];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) set(e, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) set(e, p[(c + e) / a.depth]);
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<VEC>& st, Channels<VEC>& ch) {
+    float gain[VEC], bias[VEC], mean[VEC], rstd[VEC];
+    of_channels<VEC>(a.gain, st.column * VEC, 1.f, gain);
+    of_channels<VEC>(a.bias, st.column * VEC, 0.f, bias);
+    of_groups<VEC>(a, st, a.mean, [&](int e, float v) { mean[e] = v; });
+    of_groups<VEC>(a, st, a.rstd, [&](int e, float v) { rstd[e] = v; });
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) ch.set(e, mean[e], rstd[e], gain[e], bias[e]);
+}
+
 template <typename T, typename U, int VEC, int R>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
     pdl_begin();
-    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x);
+    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x, R);
     if (!st.live) return;
     Channels<VEC> ch;
+    load_channels(a, st, ch);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const int c = st.column * VEC + e;
-        const size_t g = (size_t)st.image * a.groups + c / a.depth;
-        ch.set(e, a.mean[g], a.rstd[g] * (a.gain ? __ldg(a.gain + c) : 1.f), 1.f, a.bias ? __ldg(a.bias + c) : 0.f);
-    }
+    for (int k = 0; k < Channels<VEC>::N; ++k) ch.rstd[k] = pair_mul(ch.rstd[k], ch.gain[k]);
     with_act_of(a.act, [&](auto act) {
         RawVec<T, VEC> raw[R];
-        walk_pixels<R>(st.mine, st.at, st.step, [&](int i, size_t o) { raw[i].load(x + o); },
+        walk_pixels<R>(st, [&](int i, size_t o) { raw[i].load(x + o); },
                        [&](int i, size_t o) {
                            float v[VEC > 1 ? VEC : 2], out[VEC];
 #pragma unroll
@@ -519,23 +575,14 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, 
     });
 }
 
-// Backward: the channels' sums of the pieces go to `parts`; the gain's and the bias's gradients are added up from them by gnorm_total_kernel.
-template <int VEC>
-__device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<VEC>& st, Channels<VEC>& ch) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const int c = st.column * VEC + e;
-        const size_t g = (size_t)st.image * a.groups + c / a.depth;
-        ch.set(e, __ldg(a.mean + g), __ldg(a.rstd + g), a.gain ? __ldg(a.gain + c) : 1.f, a.bias ? __ldg(a.bias + c) : 0.f);
-    }
-}
+// Backward: the channels' sums of the pieces go to `parts`; the gain's and the bias's gradients are added up from them.
 template <typename T, typename U, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* x, const U* grad_y, GnormArgs a) {
+__global__ void __launch_bounds__(kGnormThreads, 2) gnorm_sums_kernel(const T* x, const U* grad_y, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
-    __shared__ float2 sums[kGnormThreads * VEC];
+    __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ double2 red[kGnormThreads];
     pdl_begin();
-    const Stretch<VEC> st(a, blockIdx.x);
+    const Stretch<VEC> st(a, blockIdx.x, R);
     if (st.live) {
         Channels<VEC> ch;
         load_channels(a, st, ch);
@@ -545,7 +592,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* x, c
         with_act_of(a.act, [&](auto act) {
             RawVec<T, VEC> raw[R];
             RawVec<U, VEC> graw[R];
-            walk_pixels<R>(st.mine, st.at, st.step,
+            walk_pixels<R>(st,
                            [&](int i, size_t o) {
                                raw[i].load(x + o);
                                graw[i].load(grad_y + o);
@@ -561,26 +608,27 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* x, c
                            });
         });
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sums[(st.lane * a.columns + st.column) * VEC + e] = make_float2(half(s1[e / 2], e), half(s2[e / 2], e));
+        for (int e = 0; e < VEC; ++e) sums[e * kGnormThreads + threadIdx.x] = make_float2(half(s1[e / 2], e), half(s2[e / 2], e));
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < a.channels; c += kGnormThreads) {
-        float2 s = sums[c];
+    each_channel<VEC>(a, [&](int c, int e, int column) {
+        const float2* v = sums + e * kGnormThreads + column;
+        float2 s = v[0];
         for (int l = 1; l < st.lanes; ++l) {
-            s.x += sums[l * a.channels + c].x;
-            s.y += sums[l * a.channels + c].y;
+            s.x += v[l * a.columns].x;
+            s.y += v[l * a.columns].y;
         }
-        sums[c] = s;
+        joined[c] = s;
         a.parts[((size_t)st.image * a.pieces + st.piece) * a.channels + c] = s;
-    }
+    });
     __syncthreads();
     each_group(a, [&](int g, int l, int wide, bool one) {
         float s = 0.f, q = 0.f;
         for (int i = l; i < (one ? a.depth : 0); i += wide) {
             const int c = g * a.depth + i;
             const float gain = a.gain ? __ldg(a.gain + c) : 1.f;
-            s = fmaf(gain, sums[c].x, s);
-            q = fmaf(gain, sums[c].y, q);
+            s = fmaf(gain, joined[c].x, s);
+            q = fmaf(gain, joined[c].y, q);
         }
         s = lanes_sum(s, wide);
         q = lanes_sum(q, wide);
@@ -590,25 +638,52 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_sums_kernel(const T* x, c
     join_groups(a, st.image, red, [&](int, float2 v) { return make_double2((double)v.x, (double)v.y); },
                 [&](int g, double2 s) { a.means[(size_t)st.image * a.groups + g] = make_float2((float)(s.x * a.inv_m), (float)(s.y * a.inv_m)); });
 }
+// The gradients of kTotalWide channels of the gain and the bias, by one block, from all pieces' sums.
+constexpr int kTotalWide = 8;
+__device__ __forceinline__ void total_of_channels(const GnormArgs& a, int block, float* grad_gain, float* grad_bias, double2* red) {
+    const int c = block * kTotalWide + threadIdx.x % kTotalWide, r = threadIdx.x / kTotalWide, rows = a.images * a.pieces;
+    double2 s = make_double2(0.0, 0.0);
+    if (c < a.channels)
+#pragma unroll 8
+        for (int t = r; t < rows; t += kGnormThreads / kTotalWide) {
+            const float2 v = a.parts[(size_t)t * a.channels + c];
+            s.x += (double)v.x;
+            s.y += (double)v.y;
+        }
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (r != 0 || c >= a.channels) return;
+    for (int i = 1; i < kGnormThreads / kTotalWide; ++i) {
+        s.x += red[i * kTotalWide + threadIdx.x].x;
+        s.y += red[i * kTotalWide + threadIdx.x].y;
+    }
+    if (grad_bias) grad_bias[c] = (float)s.x;
+    if (grad_gain) grad_gain[c] = (float)s.y;
+}
+
+// Its first `totals` blocks add up the gradients of the gain and the bias meanwhile.
 template <typename T, typename U, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_grad_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
+__global__ void __launch_bounds__(kGnormThreads, 2) gnorm_grad_kernel(const T* x, const U* grad_y, T* grad_x, float* grad_gain, float* grad_bias, int totals, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
+    __shared__ double2 red[kGnormThreads];
     pdl_begin();
-    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x);
+    if ((int)blockIdx.x < totals) {
+        total_of_channels(a, blockIdx.x, grad_gain, grad_bias, red);
+        return;
+    }
+    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x, R);
     if (!st.live) return;
     Channels<VEC> ch;
     load_channels(a, st, ch);
     Pair mean_a[N], mean_b[N];       // less than 0
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const float2 m = a.means[(size_t)st.image * a.groups + (st.column * VEC + e) / a.depth];
+    of_groups<VEC>(a, st, a.means, [&](int e, float2 m) {
         Channels<VEC>::put(mean_a[e / 2], e % 2, -m.x);
         Channels<VEC>::put(mean_b[e / 2], e % 2, -m.y);
-    }
+    });
     with_act_of(a.act, [&](auto act) {
         RawVec<T, VEC> raw[R];
         RawVec<U, VEC> graw[R];
-        walk_pixels<R>(st.mine, st.at, st.step,
+        walk_pixels<R>(st,
                        [&](int i, size_t o) {
                            raw[i].load(x + o);
                            graw[i].load(grad_y + o);
@@ -627,40 +702,16 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_grad_kernel(const T* x, c
                        });
     });
 }
-// Channel sums over `rows` rows of float2 [C], 32 channels and a stretch of `per` rows a block: into out [stretches][C], or the gradients where the
-// stretch is all of them.
-constexpr int kTotalThreads = 1024;
-template <bool LAST>
-__global__ void __launch_bounds__(kTotalThreads) gnorm_total_kernel(const float2* __restrict__ in, float2* out, float* grad_gain, float* grad_bias, int rows,
-                                                                    int per, int channels) {
-    __shared__ double2 red[kTotalThreads / 32][32];
+
+__global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_gain, float* grad_bias, GnormArgs a) {
+    __shared__ double2 red[kGnormThreads];
     pdl_begin();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = (int)blockIdx.x * 32 + lane, from = blockIdx.y * per, to = min(rows, from + per);
-    double2 s = make_double2(0.0, 0.0);
-    if (c < channels)
-#pragma unroll 8
-        for (int r = from + warp; r < to; r += kTotalThreads / 32) {
-            const float2 v = in[(size_t)r * channels + c];
-            s.x += (double)v.x;
-            s.y += (double)v.y;
-        }
-    red[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || c >= channels) return;
-    for (int w = 1; w < kTotalThreads / 32; ++w) {
-        s.x += red[w][lane].x;
-        s.y += red[w][lane].y;
-    }
-    if constexpr (LAST) {
-        if (grad_bias) grad_bias[c] = (float)s.x;
-        if (grad_gain) grad_gain[c] = (float)s.y;
-    } else {
-        out[(size_t)blockIdx.y * channels + c] = make_float2((float)s.x, (float)s.y);
-    }
+    total_of_channels(a, blockIdx.x, grad_gain, grad_bias, red);
 }
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
-constexpr int kFewTasks = 1184;             // blocks below which their pieces are made smaller
+constexpr double kEndRounds = 3.0;
+constexpr int kFewPieces = 222;             // rounds below which they are made shorter
 
 // How a call is run.
 struct GnormPlan {
@@ -682,11 +733,22 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.tiles = 1;
         const int lanes = kGnormThreads / p.columns;
         p.r = backward || (p.vec == 8 && xb == 4) ? 4 : 8;
-        auto tasks = [&](int n) { return (long)images * ((pixels + lanes * n - 1) / (lanes * n)); };      // of n pixels a thread
-        int each = 16 * p.r;
-        while (each > 1 && tasks(each) < kFewTasks) each /= 2;
-        if (each == 1) p.r = 1;
-        p.per = lanes * each;
+        // a round of loads a piece at least, and no more pieces than fill the machine twice over; with few of them, shorter rounds
+        auto rounds = [&](int r) { return (pixels + lanes * r - 1) / (lanes * r); };
+        if ((long)images * rounds(p.r) < kFewPieces) p.r = 1;
+        p.per = lanes * p.r;
+        // As many pieces an image as take the least time: blocks that run at once (three an SM, two backward) take the pieces in turns, and a block's
+        // beginning and end take as long as some rounds.
+        const long slots = 148 * (backward ? 2 : 3), most = std::min((long)rounds(p.r), (kGnormTarget + images) / (long)images);
+        double best = 0.0;
+        p.pieces = 1;
+        for (long k = 1; k <= most; ++k) {
+            const double cost = (double)((images * k + slots - 1) / slots) * ((double)((rounds(p.r) + k - 1) / k) + kEndRounds);
+            if (k == 1 || cost < best) {
+                best = cost;
+                p.pieces = (int)k;
+            }
+        }
     } else {
         p.columns = kGnormThreads < g->channels ? kGnormThreads : g->channels;
         p.tiles = (g->channels + p.columns - 1) / p.columns;
@@ -694,56 +756,42 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         const long want = (kGnormTarget + (long)images * p.tiles - 1) / ((long)images * p.tiles), can = (pixels + 8L * lanes - 1) / (8L * lanes);
         const long pieces = want < can ? want : can;
         p.per = (int)((pixels + pieces - 1) / pieces);
+        p.pieces = (pixels + p.per - 1) / p.per;
     }
-    p.pieces = (pixels + p.per - 1) / p.per;
     return p;
 }
-// Tasks that any call of up to `images` images of up to `pixels` pixels has at most.
-static long tasks_of(const Gnorm* g, long images, long pixels) {
-    long most = 0;
-    for (int vec : {8, 4, 1})
-        for (int r : {8, 4}) {
-            if (g->channels % vec || g->channels / vec > kGnormThreads) continue;
-            const long l = kGnormThreads / (g->channels / vec), n = images * ((pixels + l * r - 1) / (l * r));
-            most = n > most ? n : most;
-        }
-    const long small = 8 * kFewTasks + images, any = kGnormTarget + images;       // of one pixel a thread; of any tensor
-    return std::max({most, small, any});
-}
+// Pieces that any call of up to `images` images has at most, all images together.
+static long pieces_of(long images) { return kGnormTarget + images; }
 
-// Workspace: the images' counters, the tasks' sums, sums of many tasks, the groups' means, and mean and rstd where the caller keeps
+// Workspace: the images' counters, the pieces' sums, the groups' means, and mean and rstd where the caller keeps
 // none.
-constexpr int kStretches = 1024;
 struct GnormSpace {
-    size_t group_parts, parts, totals, means, stats, bytes;
+    size_t group_parts, parts, means, stats, bytes;
 };
-static GnormSpace space_of(const Gnorm* g, long images, long tasks) {
+static GnormSpace space_of(const Gnorm* g, long images) {
+    const long pieces = pieces_of(images);
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     GnormSpace s;
     s.group_parts = up(sizeof(unsigned) * images);
-    s.parts = s.group_parts + up(sizeof(float2) * tasks * g->groups);
-    s.totals = s.parts + up(sizeof(float2) * tasks * g->channels);
-    s.means = s.totals + up(sizeof(float2) * kStretches * g->channels);
+    s.parts = s.group_parts + up(sizeof(float2) * pieces * g->groups);
+    s.means = s.parts + up(sizeof(float2) * pieces * g->channels);
     s.stats = s.means + up(sizeof(float2) * images * g->groups);
     s.bytes = s.stats + up(2 * sizeof(float) * images * g->groups);
     return s;
 }
-static int ensure_gnorm(Gnorm* g, long images, long tasks, cudaStream_t s) {
-    if (images <= g->images_held && tasks <= g->tasks_held) return ensure_scratch(g->ws, space_of(g, g->images_held, g->tasks_held).bytes, s, "circ_gnorm_reserve");
-    images = std::max(images, g->images_held);
-    tasks = std::max(tasks, g->tasks_held);
-    const int rc = ensure_scratch(g->ws, space_of(g, images, tasks).bytes, s, "circ_gnorm_reserve");
+static int ensure_gnorm(Gnorm* g, long images, cudaStream_t s) {
+    if (images <= g->images_held) return ensure_scratch(g->ws, space_of(g, g->images_held).bytes, s, "circ_gnorm_reserve");
+    const int rc = ensure_scratch(g->ws, space_of(g, images).bytes, s, "circ_gnorm_reserve");
     if (rc != CIRC_OK) {
-        if (!g->ws.ptr) g->images_held = g->tasks_held = 0;
+        if (!g->ws.ptr) g->images_held = 0;
         return rc;
     }
     g->images_held = images;
-    g->tasks_held = tasks;
-    if (cudaMemsetAsync(g->ws.ptr, 0, space_of(g, images, tasks).group_parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+    if (cudaMemsetAsync(g->ws.ptr, 0, space_of(g, images).group_parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaFree(g->ws.ptr);      // this one alone: graphs may hold earlier ones
         g->ws.ptr = nullptr;
         g->ws.bytes = 0;
-        g->images_held = g->tasks_held = 0;
+        g->images_held = 0;
         set_error(CIRC_ERR_CUDA, "clearing the workspace failed: %s", cudaGetErrorString(cudaGetLastError()));
         return CIRC_ERR_CUDA;
     }
@@ -791,25 +839,37 @@ static cudaError_t run_forward(const GnormPlan& p, const GnormArgs& a, const T* 
     return err;
 }
 template <typename T, typename U>
-static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T* x, const U* grad_y, T* grad_x, cudaStream_t s) {
+static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T* x, const U* grad_y, T* grad_x, float* grad_gain, float* grad_bias,
+                                cudaStream_t s, int* launches) {
     cudaError_t err = cudaSuccess;
+    const int totals = grad_gain || grad_bias ? (a.channels + kTotalWide - 1) / kTotalWide : 0;
+    const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles)), threads(kGnormThreads);
+    bool done = false;
+    *launches = 1;
     if (p.vec == 0) {
-        const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles));
-        if ((err = launch_row(gnorm_any_sums_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, grad_y, a)) == cudaSuccess && grad_x)
-            err = launch_row(gnorm_any_grad_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, grad_y, grad_x, a);
-        return err;
+        if ((err = launch_row(gnorm_any_sums_kernel<T, U>, grid, threads, 0, s, x, grad_y, a)) == cudaSuccess && grad_x) {
+            err = launch_row(gnorm_any_grad_kernel<T, U>, grid, threads, 0, s, x, grad_y, grad_x, a);
+            ++*launches;
+        }
+    } else {
+        with_plan<T, true>(p, [&](auto vec, auto r) {
+            constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
+            if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R>, grid, threads, 0, s, x, grad_y, a)) == cudaSuccess && grad_x) {
+                err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, dim3(grid.x + totals), threads, 0, s, x, grad_y, grad_x, grad_gain, grad_bias, totals, a);
+                done = true;
+                ++*launches;
+            }
+        });
     }
-    with_plan<T, true>(p, [&](auto vec, auto r) {
-        constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
-        const dim3 grid((unsigned)((long)a.images * a.pieces));
-        if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, grad_y, a)) == cudaSuccess && grad_x)
-            err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, grad_y, grad_x, a);
-    });
+    if (err == cudaSuccess && totals && !done) {
+        err = launch_row(gnorm_total_kernel, dim3((unsigned)totals), threads, 0, s, grad_gain, grad_bias, a);
+        ++*launches;
+    }
     return err;
 }
 
 static GnormArgs args_of(const Gnorm* g, const GnormPlan& p, const float* gain, const float* bias, const float* mean, const float* rstd, int N, int pixels) {
-    const GnormSpace space = space_of(g, g->images_held, g->tasks_held);
+    const GnormSpace space = space_of(g, g->images_held);
     char* ws = static_cast<char*>(g->ws.ptr);
     GnormArgs a{};
     a.gain = gain;
@@ -832,7 +892,6 @@ static GnormArgs args_of(const Gnorm* g, const GnormPlan& p, const float* gain, 
     a.arrived = reinterpret_cast<unsigned*>(ws);
     a.group_parts = reinterpret_cast<float2*>(ws + space.group_parts);
     a.parts = reinterpret_cast<float2*>(ws + space.parts);
-    a.totals = reinterpret_cast<float2*>(ws + space.totals);
     a.means = reinterpret_cast<float2*>(ws + space.means);
     return a;
 }
@@ -851,7 +910,7 @@ circ_gnorm_handle circ_gnorm_create(int channels, int groups, float eps) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Gnorm* g = new (std::nothrow) Gnorm{device, channels, groups, eps, CIRC_F32, CIRC_F32, CIRC_ACT_NONE, {}, 0, 0};
+    Gnorm* g = new (std::nothrow) Gnorm{device, channels, groups, eps, CIRC_F32, CIRC_F32, CIRC_ACT_NONE, {}, 0};
     if (!g) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_gnorm_handle>(g);
 }
@@ -887,7 +946,7 @@ int circ_gnorm_set_activation(circ_gnorm_handle h, int activation) {
 int circ_gnorm_reserve(circ_gnorm_handle h, int N, int H, int W) {
     Gnorm* g = reinterpret_cast<Gnorm*>(h);
     const int rc = check_gnorm(g, N, H, W);
-    return rc != CIRC_OK || N == 0 ? rc : ensure_gnorm(g, N, tasks_of(g, N, (long)H * W), 0);
+    return rc != CIRC_OK || N == 0 ? rc : ensure_gnorm(g, N, 0);
 }
 
 int circ_gnorm_forward(circ_gnorm_handle h, const void* x, const float* gain, const float* bias, void* y, float* mean, float* rstd, int N, int H,
@@ -906,7 +965,7 @@ int circ_gnorm_forward(circ_gnorm_handle h, const void* x, const float* gain, co
         return CIRC_ERR_ARG;
     }
     const GnormPlan p = plan_of(g, N, H * W, false, address(x) | address(y));
-    if ((rc = ensure_gnorm(g, N, (long)N * p.pieces, s)) != CIRC_OK) return rc;
+    if ((rc = ensure_gnorm(g, N, s)) != CIRC_OK) return rc;
     const GnormArgs a = args_of(g, p, gain, bias, mean, rstd, N, H * W);
     cudaError_t err = cudaSuccess;
     with_dtype(g->x_dtype, [&](auto* t) {
@@ -945,34 +1004,17 @@ int circ_gnorm_backward(circ_gnorm_handle h, const void* x, const float* gain, c
         return CIRC_ERR_ARG;
     }
     const GnormPlan p = plan_of(g, N, H * W, true, address(x) | address(grad_y) | address(grad_x));
-    if ((rc = ensure_gnorm(g, N, (long)N * p.pieces, s)) != CIRC_OK) return rc;
+    if ((rc = ensure_gnorm(g, N, s)) != CIRC_OK) return rc;
     const GnormArgs a = args_of(g, p, gain, bias, mean, rstd, N, H * W);
     cudaError_t err = cudaSuccess;
-    int launches = grad_x ? 2 : 1;
+    int launches = 0;
     with_dtype(g->x_dtype, [&](auto* t) {
         with_dtype(g->y_dtype, [&](auto* u) {
             using T = tag_type<decltype(t)>;
             using U = tag_type<decltype(u)>;
-            err = run_backward(p, a, static_cast<const T*>(x), static_cast<const U*>(grad_y), static_cast<T*>(grad_x), s);
+            err = run_backward(p, a, static_cast<const T*>(x), static_cast<const U*>(grad_y), static_cast<T*>(grad_x), grad_gain, grad_bias, s, &launches);
         });
     });
-    if (err == cudaSuccess && (grad_gain || grad_bias)) {      // over all tasks; where they are many, over stretches of them first
-        const long tasks = (long)N * p.pieces;
-        const unsigned columns = (unsigned)(g->channels + 31) / 32;
-        const float2* in = a.parts;
-        int rows = (int)tasks;
-        if (tasks > 2048) {
-            const int per = (int)std::max(256L, (tasks + kStretches - 1) / kStretches);
-            rows = (int)((tasks + per - 1) / per);
-            err = launch_row(gnorm_total_kernel<false>, dim3(columns, (unsigned)rows), dim3(kTotalThreads), 0, s, in, a.totals, static_cast<float*>(nullptr),
-                             static_cast<float*>(nullptr), (int)tasks, per, g->channels);
-            in = a.totals;
-            ++launches;
-        }
-        if (err == cudaSuccess)
-            err = launch_row(gnorm_total_kernel<true>, dim3(columns), dim3(kTotalThreads), 0, s, in, a.totals, grad_gain, grad_bias, rows, rows, g->channels);
-        ++launches;
-    }
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
     count_launches(launches);
     return CIRC_OK;
