@@ -170,6 +170,39 @@ __device__ __forceinline__ bool last_of_image(const GnormArgs& a, int image) {
     return last;
 }
 
+// Sums over `entries` entries for every group, by a warp each, or the block for few groups: term(group, entry) -> double2, f(group, sum).
+template <typename TERM, typename F>
+__device__ __forceinline__ void over_groups(const GnormArgs& a, int entries, TERM term, F f) {
+    __shared__ double2 red[kGnormThreads / 32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kGnormThreads / 32;
+    const bool wide = a.groups < warps;
+    for (int g = wide ? 0 : warp; g < a.groups; g += wide ? 1 : warps) {
+        double2 s = make_double2(0.0, 0.0);
+#pragma unroll 4
+        for (int i = wide ? threadIdx.x : lane; i < entries; i += wide ? kGnormThreads : 32) {
+            const double2 v = term(g, i);
+            s.x += v.x;
+            s.y += v.y;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
+            s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
+        }
+        if (wide) {
+            __syncthreads();
+            if (lane == 0) red[warp] = s;
+            __syncthreads();
+            s = red[0];
+            for (int w = 1; w < warps; ++w) {
+                s.x += red[w].x;
+                s.y += red[w].y;
+            }
+        }
+        if (wide ? threadIdx.x == 0 : lane == 0) f(g, s);
+    }
+}
+
 // A thread's sums of a channel run around the thread's first value, which bounds what the difference of the two sums loses; means are kept as
 // differences from the channel's first value in the image, so that a large offset costs no digits, until they are joined in float64.
 template <typename T>
@@ -207,34 +240,20 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_stats_kernel(const T*
         a.parts[((size_t)at.image * a.pieces + at.piece) * a.channels + c] = make_float2(mean, m2);
     }
     if (!last_of_image(a, at.image)) return;
-    // a warp a group
-    const int lane = threadIdx.x % 32, entries = a.pieces * a.depth;
-    const double m = (double)a.pixels * a.depth;
-    for (int g = threadIdx.x / 32; g < a.groups; g += kGnormThreads / 32) {
-        const float2* p = a.parts + (size_t)at.image * a.pieces * a.channels + g * a.depth;
-        const T* first = x + (size_t)at.image * a.pixels * a.channels + g * a.depth;
-        double sum = 0.0, m2 = 0.0;
-        for (int i = lane; i < entries; i += 32) {
-            const int piece = i / a.depth;
-            const float2 v = __ldcg(p + (size_t)piece * a.channels + i % a.depth);
-            sum += ((double)v.x + (double)to_float(first[i % a.depth])) * (min(a.pixels, (piece + 1) * a.per) - piece * a.per);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const double mean = sum / m;
-        for (int i = lane; i < entries; i += 32) {
-            const int piece = i / a.depth;
-            const float2 v = __ldcg(p + (size_t)piece * a.channels + i % a.depth);
-            const double d = (double)v.x + (double)to_float(first[i % a.depth]) - mean;
-            m2 += (double)v.y + d * d * (min(a.pixels, (piece + 1) * a.per) - piece * a.per);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-        if (lane == 0) {
-            a.mean[(size_t)at.image * a.groups + g] = (float)mean;
-            a.rstd[(size_t)at.image * a.groups + g] = (float)(1.0 / sqrt(m2 / m + (double)a.eps));
-        }
-    }
+    const T* first = x + (size_t)at.image * a.pixels * a.channels;
+    over_groups(a, a.pieces * a.depth,
+                [&](int g, int i) {
+                    const int piece = i / a.depth, c0 = g * a.depth, k = c0 + i - piece * a.depth;
+                    const float2 v = __ldcg(a.parts + ((size_t)at.image * a.pieces + piece) * a.channels + k);
+                    const double n = (double)(min(a.pixels, (piece + 1) * a.per) - piece * a.per);
+                    const double d = (double)v.x + ((double)to_float(first[k]) - (double)to_float(first[c0]));
+                    return make_double2(n * d, (double)v.y + n * d * d);
+                },
+                [&](int g, double2 s) {
+                    const double mean = s.x * a.inv_m, var = s.y * a.inv_m - mean * mean;
+                    a.mean[(size_t)at.image * a.groups + g] = (float)(mean + (double)to_float(first[g * a.depth]));
+                    a.rstd[(size_t)at.image * a.groups + g] = 1.f / sqrtf((var < 0.0 ? 0.f : (float)var) + a.eps);
+                });
 }
 template <typename T, typename U>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_any_apply_kernel(const T* x, U* y, GnormArgs a) {
@@ -278,24 +297,14 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_sums_kernel(const T* 
         a.parts[((size_t)at.image * a.pieces + at.piece) * a.channels + c] = s;
     }
     if (!last_of_image(a, at.image)) return;
-    const int lane = threadIdx.x % 32, entries = a.pieces * a.depth;
-    const double m = (double)a.pixels * a.depth;
-    for (int g = threadIdx.x / 32; g < a.groups; g += kGnormThreads / 32) {
-        double s1 = 0.0, s2 = 0.0;
-        for (int i = lane; i < entries; i += 32) {
-            const int k = g * a.depth + i % a.depth;
-            const float2 v = __ldcg(a.parts + ((size_t)at.image * a.pieces + i / a.depth) * a.channels + k);
-            const double gain = a.gain ? (double)a.gain[k] : 1.0;
-            s1 += gain * v.x;
-            s2 += gain * v.y;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-            s2 += __shfl_xor_sync(0xffffffffu, s2, o);
-        }
-        if (lane == 0) a.means[(size_t)at.image * a.groups + g] = make_float2((float)(s1 / m), (float)(s2 / m));
-    }
+    over_groups(a, a.pieces * a.depth,
+                [&](int g, int i) {
+                    const int piece = i / a.depth, k = g * a.depth + i - piece * a.depth;
+                    const float2 v = __ldcg(a.parts + ((size_t)at.image * a.pieces + piece) * a.channels + k);
+                    const double gain = a.gain ? (double)a.gain[k] : 1.0;
+                    return make_double2(gain * v.x, gain * v.y);
+                },
+                [&](int g, double2 s) { a.means[(size_t)at.image * a.groups + g] = make_float2((float)(s.x * a.inv_m), (float)(s.y * a.inv_m)); });
 }
 template <typename T, typename U>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
@@ -314,8 +323,8 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* 
 }
 
 // ---- tensors up to 256 vectors of channels wide ----
-// Two launches: the sums of pieces of the images (the block that is last to finish an image's joins them), and the output, which takes the images in reverse
-// order: the last ones read are still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
+// Two launches: the sums of pieces of the images (the block that is last to finish an image's joins them), and the output, which goes the same way back: what
+// was read last is still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
 // (One launch, whose blocks took sums and outputs from a counter and waited for an image's sums, read every image once, but an image's counting, waiting
 // and joining by small tasks cost more than the second reading: 145 us for 32 x 112 x 112 x 256 bfloat16.)
 // A piece takes every pieces-th round of `per` pixels (R of each thread): the blocks that run at once read neighbouring memory.
@@ -411,23 +420,28 @@ __device__ __forceinline__ void each_channel(const GnormArgs& a, F f) {
         f(column * VEC + e, e, column);
     }
 }
-// Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.
-template <int R, int VEC, typename LOAD, typename TAKE>
+// Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.  BACK: from the last round to the first.
+template <int R, bool BACK, int VEC, typename LOAD, typename TAKE>
 __device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, TAKE take) {
-    size_t at = st.at;
-    for (int n = 0; n < st.size.full; ++n, at += st.jump) {
+    auto rest = [&]() {
+        if (st.last <= 0) return;
+        const size_t at = st.at + st.size.full * st.jump;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < st.last) load(i, at + i * st.step);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < st.last) take(i, at + i * st.step);
+    };
+    if (BACK) rest();
+    for (int n = 0; n < st.size.full; ++n) {
+        const size_t at = st.at + (BACK ? st.size.full - 1 - n : n) * st.jump;
 #pragma unroll
         for (int i = 0; i < R; ++i) load(i, at + i * st.step);
 #pragma unroll
         for (int i = 0; i < R; ++i) take(i, at + i * st.step);
     }
-    if (st.last <= 0) return;
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-        if (i < st.last) load(i, at + i * st.step);
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-        if (i < st.last) take(i, at + i * st.step);
+    if (!BACK) rest();
 }
 
 // A piece's sums: a thread's, around the channel's value at its first pixel (which bounds what the difference of the two sums loses), those of the
@@ -452,7 +466,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, 
             pivot[i] = pair_mul(two(own, i), pair_of(-1.f, -1.f));
             s1[i] = s2[i] = pair_of(0.f, 0.f);
         }
-        walk_pixels<R>(st, [&](int i, size_t o) { raw[i].load(x + o); },
+        walk_pixels<R, false>(st, [&](int i, size_t o) { raw[i].load(x + o); },
                        [&](int i, size_t) {
 #pragma unroll
                            for (int k = 0; k < N; ++k) {
@@ -562,7 +576,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, 
     for (int k = 0; k < Channels<VEC>::N; ++k) ch.rstd[k] = pair_mul(ch.rstd[k], ch.gain[k]);
     with_act_of(a.act, [&](auto act) {
         RawVec<T, VEC> raw[R];
-        walk_pixels<R>(st, [&](int i, size_t o) { raw[i].load(x + o); },
+        walk_pixels<R, true>(st, [&](int i, size_t o) { raw[i].load(x + o); },
                        [&](int i, size_t o) {
                            float v[VEC > 1 ? VEC : 2], out[VEC];
 #pragma unroll
@@ -592,7 +606,7 @@ __global__ void __launch_bounds__(kGnormThreads, 2) gnorm_sums_kernel(const T* x
         with_act_of(a.act, [&](auto act) {
             RawVec<T, VEC> raw[R];
             RawVec<U, VEC> graw[R];
-            walk_pixels<R>(st,
+            walk_pixels<R, false>(st,
                            [&](int i, size_t o) {
                                raw[i].load(x + o);
                                graw[i].load(grad_y + o);
@@ -683,7 +697,7 @@ __global__ void __launch_bounds__(kGnormThreads, 2) gnorm_grad_kernel(const T* x
     with_act_of(a.act, [&](auto act) {
         RawVec<T, VEC> raw[R];
         RawVec<U, VEC> graw[R];
-        walk_pixels<R>(st,
+        walk_pixels<R, true>(st,
                        [&](int i, size_t o) {
                            raw[i].load(x + o);
                            graw[i].load(grad_y + o);
@@ -754,7 +768,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.tiles = (g->channels + p.columns - 1) / p.columns;
         const int lanes = kGnormThreads / p.columns;
         const long want = (kGnormTarget + (long)images * p.tiles - 1) / ((long)images * p.tiles), can = (pixels + 8L * lanes - 1) / (8L * lanes);
-        const long pieces = want < can ? want : can;
+        const long pieces = std::min({want, can, 64L});       // one block joins them
         p.per = (int)((pixels + pieces - 1) / pieces);
         p.pieces = (pixels + p.per - 1) / p.per;
     }
