@@ -448,7 +448,7 @@ __device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, T
 // threads that share a channel, and those of a group's channels, each around their joint mean.  Means are kept as differences from the image's first
 // pixel, so that a large offset costs no digits.
 template <typename T, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_stats_kernel(const T* x, GnormArgs a) {
+__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* x, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
     __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ float firsts[kGnormThreads * VEC];
@@ -566,7 +566,7 @@ __device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<
 }
 
 template <typename T, typename U, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
+__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
     pdl_begin();
     const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x, R);
     if (!st.live) return;
