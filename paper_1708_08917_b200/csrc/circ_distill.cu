@@ -690,7 +690,7 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
     }
     const int vectors = RowSpan<VEC, false>::most(a.side.classes);
     const size_t marks = ((size_t)vectors * VEC + 31) / 32 * 4, bytes = (size_t)vectors * 16;
-    const bool few = vectors > 128 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < 148 * 2;
+    const bool few = vectors > 256 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < 148 * 2;
     if (few || marks > 48 * 1024) {
         in_pieces(std::integral_constant<int, VEC>{});
         return err;
@@ -712,6 +712,7 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
             if (vectors <= 32) warps(std::integral_constant<int, 1>{});
             else if (vectors <= 64) warps(std::integral_constant<int, 2>{});
             else if (vectors <= 128) warps(std::integral_constant<int, 4>{});
+            else if (vectors <= 256) warps(std::integral_constant<int, 8>{});
             // small blocks, whose waits overlap; with a gradient no more of them than L2 holds the rows of
             else if (!GRAD || bytes <= 32 * 1024) rows(std::integral_constant<int, 128>{});
             else if (bytes <= 128 * 1024) rows(std::integral_constant<int, 256>{});

@@ -444,11 +444,72 @@ __device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, T
     if (!BACK) rest();
 }
 
+// VEC channels' values of a vector of one a channel (NULL: `none`), and of one a group.
+template <int VEC>
+__device__ __forceinline__ void of_channels(const float* p, int c, float none, float (&v)[VEC]) {
+    if (VEC >= 4 && p && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+        for (int e = 0; e + 3 < VEC; e += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(p + c + e));
+            v[e] = f.x; v[e + 1] = f.y; v[e + 2] = f.z; v[e + 3] = f.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = p ? __ldg(p + c + e) : none;
+}
+template <int VEC, typename V, typename F>
+__device__ __forceinline__ void of_groups(const GnormArgs& a, const Stretch<VEC>& st, const V* p, F set) {
+    p += (size_t)st.image * a.groups;
+    const int c = st.column * VEC, g = c / a.depth;
+    if (a.depth % VEC == 0) {
+        const V v = p[g];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) set(e, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) set(e, p[(c + e) / a.depth]);
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<VEC>& st, Channels<VEC>& ch) {
+    float gain[VEC], bias[VEC], mean[VEC], rstd[VEC];
+    of_channels<VEC>(a.gain, st.column * VEC, 1.f, gain);
+    of_channels<VEC>(a.bias, st.column * VEC, 0.f, bias);
+    of_groups<VEC>(a, st, a.mean, [&](int e, float v) { mean[e] = v; });
+    of_groups<VEC>(a, st, a.rstd, [&](int e, float v) { rstd[e] = v; });
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) ch.set(e, mean[e], rstd[e], gain[e], bias[e]);
+}
+
+template <typename T, typename U, int VEC, int R>
+__device__ __forceinline__ void apply_stretch(const T* x, U* y, const GnormArgs& a, const Stretch<VEC>& st) {
+    if (!st.live) return;
+    Channels<VEC> ch;
+    load_channels(a, st, ch);
+#pragma unroll
+    for (int k = 0; k < Channels<VEC>::N; ++k) ch.rstd[k] = pair_mul(ch.rstd[k], ch.gain[k]);
+    with_act_of(a.act, [&](auto act) {
+        RawVec<T, VEC> raw[R];
+        walk_pixels<R, true>(st, [&](int i, size_t o) { raw[i].load(x + o); },
+                       [&](int i, size_t o) {
+                           float v[VEC > 1 ? VEC : 2], out[VEC];
+#pragma unroll
+                           for (int k = 0; k < Channels<VEC>::N; ++k)
+                               split(pair_fma(pair_add(two(raw[i], k), ch.mean[k]), ch.rstd[k], ch.bias[k]), v[2 * k], v[2 * k + 1]);
+#pragma unroll
+                           for (int e = 0; e < VEC; ++e) out[e] = activate<decltype(act)::value>(v[e]);
+                           store_vec_once<VEC>(y + o, out);
+                       });
+    });
+}
+
 // A piece's sums: a thread's, around the channel's value at its first pixel (which bounds what the difference of the two sums loses), those of the
 // threads that share a channel, and those of a group's channels, each around their joint mean.  Means are kept as differences from the image's first
 // pixel, so that a large offset costs no digits.
-template <typename T, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* x, GnormArgs a) {
+// WHOLE: a block has a whole image, and writes its output too.
+template <typename T, typename U, int VEC, int R, bool WHOLE>
+__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* x, U* y, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
     __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ float firsts[kGnormThreads * VEC];
@@ -525,73 +586,55 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
                     a.mean[(size_t)st.image * a.groups + g] = (float)(mean + (double)to_float(first[g * a.depth]));
                     a.rstd[(size_t)st.image * a.groups + g] = 1.f / sqrtf((var < 0.0 ? 0.f : (float)var) + a.eps);
                 });
-}
-
-// VEC channels' values of a vector of one a channel (NULL: `none`), and of one a group.
-template <int VEC>
-__device__ __forceinline__ void of_channels(const float* p, int c, float none, float (&v)[VEC]) {
-    if (VEC >= 4 && p && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-#pragma unroll
-        for (int e = 0; e + 3 < VEC; e += 4) {
-            const float4 f = __ldg(reinterpret_cast<const float4*>(p + c + e));
-            v[e] = f.x; v[e + 1] = f.y; v[e + 2] = f.z; v[e + 3] = f.w;
-        }
-        return;
+    if constexpr (WHOLE) {
+        __syncthreads();
+        apply_stretch<T, U, VEC, R>(x, y, a, st);
     }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = p ? __ldg(p + c + e) : none;
-}
-template <int VEC, typename V, typename F>
-__device__ __forceinline__ void of_groups(const GnormArgs& a, const Stretch<VEC>& st, const V* p, F set) {
-    p += (size_t)st.image * a.groups;
-    const int c = st.column * VEC, g = c / a.depth;
-    if (a.depth % VEC == 0) {
-        const V v = p[g];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) set(e, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) set(e, p[(c + e) / a.depth]);
-    }
-}
-template <int VEC>
-__device__ __forceinline__ void load_channels(const GnormArgs& a, const Stretch<VEC>& st, Channels<VEC>& ch) {
-    float gain[VEC], bias[VEC], mean[VEC], rstd[VEC];
-    of_channels<VEC>(a.gain, st.column * VEC, 1.f, gain);
-    of_channels<VEC>(a.bias, st.column * VEC, 0.f, bias);
-    of_groups<VEC>(a, st, a.mean, [&](int e, float v) { mean[e] = v; });
-    of_groups<VEC>(a, st, a.rstd, [&](int e, float v) { rstd[e] = v; });
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) ch.set(e, mean[e], rstd[e], gain[e], bias[e]);
 }
 
 template <typename T, typename U, int VEC, int R>
 __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_apply_kernel(const T* x, U* y, GnormArgs a) {
     pdl_begin();
-    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x, R);
+    apply_stretch<T, U, VEC, R>(x, y, a, Stretch<VEC>(a, gridDim.x - 1 - blockIdx.x, R));
+}
+
+template <typename T, typename U, int VEC, int R>
+__device__ __forceinline__ void grad_stretch(const T* x, const U* grad_y, T* grad_x, const GnormArgs& a, const Stretch<VEC>& st) {
+    constexpr int N = Channels<VEC>::N;
     if (!st.live) return;
     Channels<VEC> ch;
     load_channels(a, st, ch);
-#pragma unroll
-    for (int k = 0; k < Channels<VEC>::N; ++k) ch.rstd[k] = pair_mul(ch.rstd[k], ch.gain[k]);
+    Pair mean_a[N], mean_b[N];       // less than 0
+    of_groups<VEC>(a, st, a.means, [&](int e, float2 m) {
+        Channels<VEC>::put(mean_a[e / 2], e % 2, -m.x);
+        Channels<VEC>::put(mean_b[e / 2], e % 2, -m.y);
+    });
     with_act_of(a.act, [&](auto act) {
         RawVec<T, VEC> raw[R];
-        walk_pixels<R, true>(st, [&](int i, size_t o) { raw[i].load(x + o); },
+        RawVec<U, VEC> graw[R];
+        walk_pixels<R, true>(st,
+                       [&](int i, size_t o) {
+                           raw[i].load(x + o);
+                           graw[i].load(grad_y + o);
+                       },
                        [&](int i, size_t o) {
                            float v[VEC > 1 ? VEC : 2], out[VEC];
 #pragma unroll
-                           for (int k = 0; k < Channels<VEC>::N; ++k)
-                               split(pair_fma(pair_add(two(raw[i], k), ch.mean[k]), ch.rstd[k], ch.bias[k]), v[2 * k], v[2 * k + 1]);
+                           for (int k = 0; k < N; ++k) {
+                               Pair u, g;
+                               ch.template slopes<decltype(act)::value>(k, two(raw[i], k), two(graw[i], k), u, g);
+                               split(pair_mul(ch.rstd[k], pair_fma(u, mean_b[k], pair_fma(g, ch.gain[k], mean_a[k]))), v[2 * k], v[2 * k + 1]);
+                           }
 #pragma unroll
-                           for (int e = 0; e < VEC; ++e) out[e] = activate<decltype(act)::value>(v[e]);
-                           store_vec_once<VEC>(y + o, out);
+                           for (int e = 0; e < VEC; ++e) out[e] = v[e];
+                           store_vec_once<VEC>(grad_x + o, out);
                        });
     });
 }
 
 // Backward: the channels' sums of the pieces go to `parts`; the gain's and the bias's gradients are added up from them.
-template <typename T, typename U, int VEC, int R>
-__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x, const U* grad_y, GnormArgs a) {
+template <typename T, typename U, int VEC, int R, bool WHOLE>
+__global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
     __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ double2 red[kGnormThreads];
@@ -651,6 +694,11 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x
     if (!last_of_image(a, st.image)) return;
     join_groups(a, st.image, red, [&](int, float2 v) { return make_double2((double)v.x, (double)v.y); },
                 [&](int g, double2 s) { a.means[(size_t)st.image * a.groups + g] = make_float2((float)(s.x * a.inv_m), (float)(s.y * a.inv_m)); });
+    if constexpr (WHOLE) {
+        if (!grad_x) return;
+        __syncthreads();
+        grad_stretch<T, U, VEC, R>(x, grad_y, grad_x, a, st);
+    }
 }
 // The gradients of kTotalWide channels of the gain and the bias, by one block, from all pieces' sums.
 constexpr int kTotalWide = 8;
@@ -678,43 +726,13 @@ __device__ __forceinline__ void total_of_channels(const GnormArgs& a, int block,
 // Its first `totals` blocks add up the gradients of the gain and the bias meanwhile.
 template <typename T, typename U, int VEC, int R>
 __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_grad_kernel(const T* x, const U* grad_y, T* grad_x, float* grad_gain, float* grad_bias, int totals, GnormArgs a) {
-    constexpr int N = Channels<VEC>::N;
     __shared__ double2 red[kGnormThreads];
     pdl_begin();
     if ((int)blockIdx.x < totals) {
         total_of_channels(a, blockIdx.x, grad_gain, grad_bias, red);
         return;
     }
-    const Stretch<VEC> st(a, gridDim.x - 1 - blockIdx.x, R);
-    if (!st.live) return;
-    Channels<VEC> ch;
-    load_channels(a, st, ch);
-    Pair mean_a[N], mean_b[N];       // less than 0
-    of_groups<VEC>(a, st, a.means, [&](int e, float2 m) {
-        Channels<VEC>::put(mean_a[e / 2], e % 2, -m.x);
-        Channels<VEC>::put(mean_b[e / 2], e % 2, -m.y);
-    });
-    with_act_of(a.act, [&](auto act) {
-        RawVec<T, VEC> raw[R];
-        RawVec<U, VEC> graw[R];
-        walk_pixels<R, true>(st,
-                       [&](int i, size_t o) {
-                           raw[i].load(x + o);
-                           graw[i].load(grad_y + o);
-                       },
-                       [&](int i, size_t o) {
-                           float v[VEC > 1 ? VEC : 2], out[VEC];
-#pragma unroll
-                           for (int k = 0; k < N; ++k) {
-                               Pair u, g;
-                               ch.template slopes<decltype(act)::value>(k, two(raw[i], k), two(graw[i], k), u, g);
-                               split(pair_mul(ch.rstd[k], pair_fma(u, mean_b[k], pair_fma(g, ch.gain[k], mean_a[k]))), v[2 * k], v[2 * k + 1]);
-                           }
-#pragma unroll
-                           for (int e = 0; e < VEC; ++e) out[e] = v[e];
-                           store_vec_once<VEC>(grad_x + o, out);
-                       });
-    });
+    grad_stretch<T, U, VEC, R>(x, grad_y, grad_x, a, Stretch<VEC>(a, gridDim.x - 1 - blockIdx.x, R));
 }
 
 __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_gain, float* grad_bias, GnormArgs a) {
@@ -725,12 +743,14 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
 constexpr double kEndRounds = 3.0;
+constexpr int kWholeRounds = 4;             // rounds that a block takes for a whole image where the images do not fill the machine
 constexpr int kFewPieces = 222;             // rounds below which they are made shorter
 
 // How a call is run.
 struct GnormPlan {
     int vec, r;             // elements a vector, pixels a thread; vec 0: any tensor
     int columns, tiles, pieces, per;
+    bool whole;             // a block an image, in one launch
 };
 static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, uintptr_t addresses) {
     const size_t xb = dtype_bytes(g->x_dtype), yb = dtype_bytes(g->y_dtype), small = xb < yb ? xb : yb;
@@ -750,8 +770,13 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.r = backward || (p.vec == 8 && xb == 4) ? 4 : 8;
         // a round of loads a piece at least, and no more pieces than fill the machine twice over; with few of them, shorter rounds
         auto rounds = [&](int r) { return (pixels + lanes * r - 1) / (lanes * r); };
-        if ((long)images * rounds(p.r) < kFewPieces) p.r = 1;
+        p.whole = rounds(p.r) <= kWholeRounds || images >= 148 * 3;
+        if (!p.whole && (long)images * rounds(p.r) < kFewPieces) p.r = 1;
         p.per = lanes * p.r;
+        if (p.whole) {
+            p.pieces = 1;
+            return p;
+        }
         // As many pieces an image as take the least time: blocks that run at once (three an SM) take the pieces in turns, and a block's beginning and end
         // take as long as some rounds.
         const long slots = 148 * 3, most = std::min((long)rounds(p.r), (kGnormTarget + images) / (long)images);
@@ -852,7 +877,12 @@ static cudaError_t run_forward(const GnormPlan& p, const GnormArgs& a, const T* 
     with_plan<T, false>(p, [&](auto vec, auto r) {
         constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
         const dim3 grid((unsigned)((long)a.images * a.pieces));
-        if ((err = launch_row(gnorm_stats_kernel<T, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, a)) == cudaSuccess)
+        if constexpr (R > 1)
+            if (p.whole) {
+                err = launch_row(gnorm_stats_kernel<T, U, VEC, R, true>, grid, dim3(kGnormThreads), 0, s, x, y, a);
+                return;
+            }
+        if ((err = launch_row(gnorm_stats_kernel<T, U, VEC, R, false>, grid, dim3(kGnormThreads), 0, s, x, y, a)) == cudaSuccess)
             err = launch_row(gnorm_apply_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, y, a);
     });
     return err;
@@ -873,7 +903,12 @@ static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T*
     } else {
         with_plan<T, true>(p, [&](auto vec, auto r) {
             constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
-            if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R>, grid, threads, 0, s, x, grad_y, a)) == cudaSuccess && grad_x) {
+            if constexpr (R > 1)
+                if (p.whole) {
+                    err = launch_row(gnorm_sums_kernel<T, U, VEC, R, true>, grid, threads, 0, s, x, grad_y, grad_x, a);
+                    return;
+                }
+            if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R, false>, grid, threads, 0, s, x, grad_y, grad_x, a)) == cudaSuccess && grad_x) {
                 err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, dim3(grid.x + totals), threads, 0, s, x, grad_y, grad_x, grad_gain, grad_bias, totals, a);
                 done = true;
                 ++*launches;
@@ -995,7 +1030,7 @@ int circ_gnorm_forward(circ_gnorm_handle h, const void* x, const float* gain, co
         });
     });
     CIRC_CUDA_TRY(err, CIRC_ERR_CUDA);
-    count_launches(2);
+    count_launches(p.whole ? 1 : 2);
     return CIRC_OK;
 }
 
