@@ -633,6 +633,125 @@ __global__ void __launch_bounds__(THREADS, PIECES ? 1 : kRowThreads / THREADS) t
     return;
 }
 
+// ---- many rows of middling length: the same by a warp, without a barrier ----
+// 256 maxima a row: eight a lane, of the four vectors that it takes at a time in even turns and in odd ones.
+constexpr int kWarpKeys = 256;
+template <typename T, typename ID>
+__global__ void __launch_bounds__(128, 10) top_warp_kernel(const T* __restrict__ z, TopArgs a) {
+    constexpr int VEC = 16 / (int)sizeof(T);
+    __shared__ uint64_t keys_of[4][kWarpKeys];
+    __shared__ uint16_t hits_of[4][2 * kKept * 32];
+    __shared__ unsigned lengths[4][2];
+    __shared__ AnySpace<1> any[4];
+    pdl_begin();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * 4 + warp;
+    if (row >= a.rows) return;
+    Team<32, 0> team{nullptr, 0, lane};
+    uint64_t* keys = keys_of[warp];
+    uint16_t* hits = hits_of[warp];
+    unsigned *hit = &lengths[warp][0], *taken = &lengths[warp][1];
+    const RowSpan<VEC, false> span(row, a.classes, a.ld);
+    const int vectors = (a.classes - span.shift + VEC - 1) / VEC, w0 = span.whole(0) ? 0 : 1, w1 = span.whole(vectors - 1) ? vectors : vectors - 1, whole = w1 - w0;
+    const T* src = z + span.at(w0) + (size_t)lane * VEC;
+    float best[2][kKept];
+#pragma unroll
+    for (int u = 0; u < 2 * kKept; ++u) best[u / kKept][u % kKept] = -INFINITY;
+    Running run(a.scale);
+    for (int i = 0; i < whole; i += 2 * kKept * 32)
+#pragma unroll
+        for (int odd = 0; odd < 2; ++odd) {
+            const int at = i + odd * kKept * 32;
+            if (at >= whole) break;
+            RawVec<T, VEC> raw[kKept];
+#pragma unroll
+            for (int u = 0; u < kKept; ++u) {
+                raw[u].fill_lowest();
+                if (at + u * 32 + lane < whole) raw[u].load(src + (size_t)(at + u * 32) * VEC);
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kKept; ++u) {
+                const float one = most_nan(raw[u]);
+                best[odd][u] = max_nan(best[odd][u], one);
+                most = max_nan(most, one);
+            }
+            if (a.lse) {
+                run.rise(most);
+                if (run.ex.plain) run.template add<true>(raw);
+                else run.template add<false>(raw);
+            }
+        }
+    const int rest = lane == 0 && w0 == 1 ? 0 : lane == 1 && w1 < vectors && (w1 > 0 || w0 == 0) ? vectors - 1 : -1;
+    float edge[VEC];
+    if (rest >= 0) {
+        RawVec<T, VEC> raw;
+        span.load(raw, z, rest);
+        scores(span, rest, raw, edge);
+        if (a.lse) run.take(edge);
+    }
+    if (a.lse) {
+        const Softmax all = warp_join(run.done(), a.scale);
+        if (lane == 0) write_lse(a, (size_t)row, all);
+    }
+    if (!a.values && !a.ids) return;
+    uint32_t order[2 * kKept];
+#pragma unroll
+    for (int u = 0; u < 2 * kKept; ++u) order[u] = lane + u * 32 < whole ? order_in<T>(best[u / kKept][u % kKept]) : 0u;
+    unsigned reach;
+    const uint32_t bound = find_bound<T>(team, order, (unsigned)a.count, (unsigned)(a.count + a.count / 4 + 4), reach);
+    if (lane == 0) *hit = *taken = 0;
+    __syncwarp();
+    unsigned mine = 0;
+#pragma unroll
+    for (int u = 0; u < 2 * kKept; ++u) mine += order[u] >= bound;
+    unsigned at = team.append(mine, hit);
+#pragma unroll
+    for (int u = 0; u < 2 * kKept; ++u)
+        if (order[u] >= bound) hits[at++] = (uint16_t)(u * 32 + lane);
+    __syncwarp();
+    const int each = (whole + 2 * kKept * 32 - 1) / (2 * kKept * 32), items = (int)*hit * each;
+    for (int i0 = 0; i0 < items; i0 += 32) {
+        const int i = i0 + lane;
+        float s[VEC];
+        int c0 = 0;
+        unsigned above = 0;
+        if (i < items) {
+            const int v = i % each * (2 * kKept * 32) + hits[i / each];
+            if (v < whole) {
+                RawVec<T, VEC> raw;
+                raw.load(z + span.at(w0 + v));
+                c0 = span.col(w0 + v);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    s[e] = raw.get(e);
+                    above |= (unsigned)(order_in<T>(s[e]) >= bound) << e;
+                }
+            }
+        }
+        unsigned to = team.append(__popc(above), taken);
+        if (above)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (above >> e & 1) {
+                    if (to < kWarpKeys) keys[to] = key_of(order_in<T>(s[e]), c0 + e);
+                    ++to;
+                }
+    }
+    if (rest >= 0)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const int c = span.col(rest) + e;
+            if (c < 0 || c >= a.classes || order_in<T>(edge[e]) < bound) continue;
+            const unsigned to = atomicAdd(taken, 1u);
+            if (to < kWarpKeys) keys[to] = key_of(order_in<T>(edge[e]), c);
+        }
+    __syncwarp();
+    if (*taken <= kWarpKeys)
+        put_in_order(team, keys, (int)*taken, a.count, [&](int place, uint64_t key) { write_one<T, ID>(a, (size_t)row, place, key); });
+    else
+        select_any<T, ID>(a, z + (size_t)row * a.ld, (size_t)row, keys, any[warp], team);
+}
+
 constexpr int kTopPieces = 64;                 // a row, at most
 constexpr int kTopFew = 148;                   // rows below this many are cut into pieces
 
@@ -664,8 +783,12 @@ static cudaError_t dispatch_top(const T* z, TopArgs a, cudaStream_t s) {
     using Threads128 = std::integral_constant<int, 128>;
     using Threads256 = std::integral_constant<int, 256>;
     using Threads512 = std::integral_constant<int, 512>;
-    if (vectors <= 32 * MOST) {
+    // rows that fill the machine by a warp each, where its 256 maxima are four for each score
+    const bool warps = a.count <= 64 && vectors <= 1024 && vectors - 2 >= 3 * a.count && a.rows >= 148 * 4;
+    if (vectors <= 32 * MOST && !(warps && vectors >= 64)) {
         held_by(Threads32{});
+    } else if (warps) {
+        err = launch_row(top_warp_kernel<T, ID>, dim3((unsigned)((a.rows + 3) / 4)), dim3(128), 0, s, z, a);
     } else if (vectors <= 128 * MOST) {
         held_by(Threads128{});
     } else if (vectors - 2 < 3 * a.count) {      // with fewer than three vectors for each score too many scores would reach the vectors' bound
