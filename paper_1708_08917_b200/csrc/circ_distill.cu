@@ -568,32 +568,33 @@ __global__ void __launch_bounds__(kPieceThreads) distill_grad_kernel(const T* z,
     const float factor = plan.factor * shared_factor;
     T* g = grad + (size_t)row * a.grad_ld;
     if (!zero) mark_listed(a, p, ids, (size_t)row, marks);
-    for (int v = p.from + tid; v < p.to; v += kPieceThreads) {
-        float out[VEC], old[VEC];
-        const unsigned m = zero ? 0 : marks_of<VEC>(marks, v - p.from);
-        if (zero) {
+    for (int v0 = p.from + tid; v0 < p.to; v0 += kAhead * kPieceThreads) {
+        RawVec<T, VEC> raw[kAhead];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) out[e] = 0.f;
-        } else {
-            RawVec<T, VEC> raw;
-            float s[VEC];
-            p.span.load(raw, z, v);
-            scores(p.span, v, raw, s);
+        for (int u = 0; u < kAhead; ++u) {
+            raw[u].clear();
+            if (!zero && v0 + u * kPieceThreads < p.to) p.span.load(raw[u], z, v0 + u * kPieceThreads);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int v = v0 + u * kPieceThreads, col = p.span.col(v);
+            if (v >= p.to) break;
+            const unsigned m = zero ? 0 : marks_of<VEC>(marks, v - p.from);
+            float s[VEC], out[VEC];
+            scores(p.span, v, raw[u], s);
             ex.of(s, out);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) out[e] *= factor;
-        }
-        const int col = p.span.col(v);
+            for (int e = 0; e < VEC; ++e) {
+                out[e] = zero ? 0.f : out[e] * factor;
+                if (a.add && !(m >> e & 1) && col + e >= 0 && col + e < a.side.classes) out[e] += to_float(g[col + e]);
+            }
+            if (VEC > 1 && p.span.whole(v) && !m) {
+                store_vec<VEC>(g + col, out);
+            } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) old[e] = a.add && !(m >> e & 1) && col + e >= 0 && col + e < a.side.classes ? to_float(g[col + e]) : 0.f;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) out[e] += old[e];
-        if (VEC > 1 && p.span.whole(v) && !m) {
-            store_vec<VEC>(g + col, out);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (col + e >= 0 && col + e < a.side.classes && !(m >> e & 1)) store_one(g + col + e, out[e]);
+                for (int e = 0; e < VEC; ++e)
+                    if (col + e >= 0 && col + e < a.side.classes && !(m >> e & 1)) store_one(g + col + e, out[e]);
+            }
         }
     }
     if (zero) return;
@@ -607,6 +608,10 @@ __global__ void __launch_bounds__(kPieceThreads) distill_grad_kernel(const T* z,
 }
 
 constexpr long kPieceTarget = 148 * 8;      // blocks that fill the machine
+// Fewer rows, each longer, are cut into pieces: a block's own time for a row is longer than that of pieces and their joining (126 rows of 107244 bfloat16 with
+// gradient: 70 us in pieces, 25 by blocks; 9 of 147566 float32: 22 in pieces).
+constexpr int kFewRows = 48;
+constexpr size_t kFewBytes = 256 * 1024;
 
 // Pieces a row: enough for the marks, and more while the rows do not fill the machine (4 vectors a thread left at least).
 static int pieces_of(long rows, int classes, int vec, int* per) {
@@ -690,7 +695,7 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
     }
     const int vectors = RowSpan<VEC, false>::most(a.side.classes);
     const size_t marks = ((size_t)vectors * VEC + 31) / 32 * 4, bytes = (size_t)vectors * 16;
-    const bool few = vectors > 256 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < 148 * 2;
+    const bool few = vectors > 256 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < kFewRows && bytes > kFewBytes;
     if (few || marks > 48 * 1024) {
         in_pieces(std::integral_constant<int, VEC>{});
         return err;
@@ -714,6 +719,7 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
             else if (vectors <= 128) warps(std::integral_constant<int, 4>{});
             else if (vectors <= 256) warps(std::integral_constant<int, 8>{});
             // small blocks, whose waits overlap; with a gradient no more of them than L2 holds the rows of
+            else if (a.rows < 148 * 2) rows(std::integral_constant<int, 512>{});      // (fewer than the machine holds: a row's own time counts)
             else if (!GRAD || bytes <= 32 * 1024) rows(std::integral_constant<int, 128>{});
             else if (bytes <= 128 * 1024) rows(std::integral_constant<int, 256>{});
             else rows(std::integral_constant<int, 512>{});

@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
 constexpr double kEndRounds = 3.0;
-constexpr int kWholeRounds = 4;             // rounds that a block takes for a whole image where the images do not fill the machine
+constexpr int kWholeRounds = 4;             // rounds that a block takes for a whole image where the images do not fill the machine four times over
 constexpr int kFewPieces = 222;             // rounds below which they are made shorter
 
 // How a call is run.
@@ -770,7 +770,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.r = backward || (p.vec == 8 && xb == 4) ? 4 : 8;
         // a round of loads a piece at least, and no more pieces than fill the machine twice over; with few of them, shorter rounds
         auto rounds = [&](int r) { return (pixels + lanes * r - 1) / (lanes * r); };
-        p.whole = rounds(p.r) <= kWholeRounds || images >= 148 * 3;
+        p.whole = rounds(p.r) <= kWholeRounds || images >= 148 * 12;
         if (!p.whole && (long)images * rounds(p.r) < kFewPieces) p.r = 1;
         p.per = lanes * p.r;
         if (p.whole) {

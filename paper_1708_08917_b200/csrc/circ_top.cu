@@ -753,7 +753,8 @@ __global__ void __launch_bounds__(128, 10) top_warp_kernel(const T* __restrict__
 }
 
 constexpr int kTopPieces = 64;                 // a row, at most
-constexpr int kTopFew = 148;                   // rows below this many are cut into pieces
+constexpr int kTopFew = 48;                    // rows below this many, and longer than kTopFewBytes, are cut into pieces
+constexpr size_t kTopFewBytes = 256 * 1024;
 
 // The kernel for a call, by the rows' length, their number and the alignment.
 template <typename T, typename ID>
@@ -783,8 +784,9 @@ static cudaError_t dispatch_top(const T* z, TopArgs a, cudaStream_t s) {
     using Threads128 = std::integral_constant<int, 128>;
     using Threads256 = std::integral_constant<int, 256>;
     using Threads512 = std::integral_constant<int, 512>;
-    // rows that fill the machine by a warp each, where its 256 maxima are four for each score
-    const bool warps = a.count <= 64 && vectors <= 1024 && vectors - 2 >= 3 * a.count && a.rows >= 148 * 4;
+    // Rows that fill the machine by a warp each, where its 256 maxima are four for each score.  Longer rows are better with a block each (4096 x 8192
+    // bfloat16, 32 of each: 36 us against 26; of 3000 float32, 2000 of them: 13 us by warps, 21 by blocks), and so are few (700: 10 against 9).
+    const bool warps = a.count <= 64 && vectors <= 768 && vectors - 2 >= 3 * a.count && a.rows >= 148 * 10;
     if (vectors <= 32 * MOST && !(warps && vectors >= 64)) {
         held_by(Threads32{});
     } else if (warps) {
@@ -797,7 +799,7 @@ static cudaError_t dispatch_top(const T* z, TopArgs a, cudaStream_t s) {
         // few rows: as many pieces as fill the machine twice over, as keep four vectors a thread and three for each score, and as the joining block holds
         const int most = std::min({kTopPieces, kMergeEach * 512 / a.count, vectors / std::max(1024, 3 * a.count + 2)});
         const int pieces = std::min(most, (2 * 148 + a.rows - 1) / a.rows);
-        if (a.rows < kTopFew && pieces > 1) {
+        if (a.rows < kTopFew && (size_t)vectors * 16 > kTopFewBytes && pieces > 1) {
             a.per = (vectors + pieces - 1) / pieces;
             a.pieces = (vectors + a.per - 1) / a.per;
             if (vectors - (a.pieces - 1) * a.per >= 3 * a.count + 2) {      // the last piece is the shortest
@@ -807,7 +809,8 @@ static cudaError_t dispatch_top(const T* z, TopArgs a, cudaStream_t s) {
         }
         // Small blocks, whose waits overlap, but at least two threads for each score, and four where a maximum stands for many vectors, which are
         // read again (64 of 50001 bfloat16: 262 us with 128 threads, 217 with 256; of 8192: 135 with 128, 161 with 256).
-        if (a.count <= 32 || (a.count <= 64 && vectors <= 4 * kKept * 128)) rows(Threads128{}, std::false_type{}, a.rows);
+        if (a.rows < 148 * 2) rows(Threads512{}, std::false_type{}, a.rows);      // (fewer than the machine holds: a row's own time counts)
+        else if (a.count <= 32 || (a.count <= 64 && vectors <= 4 * kKept * 128)) rows(Threads128{}, std::false_type{}, a.rows);
         else if (a.count <= 64 || (a.count <= 128 && vectors <= 4 * kKept * 256)) rows(Threads256{}, std::false_type{}, a.rows);
         else rows(Threads512{}, std::false_type{}, a.rows);
     }
