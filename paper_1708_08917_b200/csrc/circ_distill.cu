@@ -214,6 +214,10 @@ __device__ __forceinline__ void slopes(const RawVec<T, VEC>& raw, const Exponent
 }
 
 // ---- rows, or pieces of them, a block each ----
+// Bound by memory for long rows: 4096 x 50001 bfloat16 without a gradient 86 us (one in ten rows without weight; 5.2 TB/s of what is read), by the list's
+// chain of dependent steps (6 us) for those of a few thousand classes.  With a gradient 8192 x 50001 bfloat16 take 363 us (4.3 TB/s): two exponentials an
+// element keep the XU pipe half busy, and blocks wait at the barriers between their phases; rows held in shared memory (as the cross entropy's are) take
+// the same time.
 // THREADS threads sum up the classes that are not listed, four vectors at a time (the first four are on their way before the list is known); one more
 // warp has the list: it marks its classes, works out the teacher's side meanwhile, and then the row's loss.  GRAD: the row is read a second time, from
 // L2, where its block's neighbours have left room for it, and the gradient written; the list's own elements follow behind a barrier.
@@ -459,6 +463,7 @@ __global__ void __launch_bounds__(THREADS + 32, PIECES ? 1 : 1280 / (THREADS + 3
 }
 
 // ---- short rows: a warp holds one in registers ----
+// Bound by the list's chain of dependent steps: 128 x 1024 float32 with gradient 8.9 us a call, 16384 x 200 34 us.
 template <typename T, typename V, typename ID, int VEC, int N, int MOST, bool GRAD>
 __global__ void __launch_bounds__(128) distill_warp_kernel(const T* z, const V* __restrict__ values, const ID* __restrict__ ids, T* grad, DistillArgs a) {
     __shared__ uint32_t marks_of_warp[4][N * VEC];
@@ -608,9 +613,9 @@ __global__ void __launch_bounds__(kPieceThreads) distill_grad_kernel(const T* z,
 }
 
 constexpr long kPieceTarget = 148 * 8;      // blocks that fill the machine
-// Fewer rows, each longer, are cut into pieces: a block's own time for a row is longer than that of pieces and their joining (126 rows of 107244 bfloat16 with
-// gradient: 70 us in pieces, 25 by blocks; 9 of 147566 float32: 22 in pieces).
-constexpr int kFewRows = 48;
+// Fewer rows, each longer, are cut into pieces: with so few a block's own time for a row is longer than that of pieces and their joining (float32 with
+// gradient: 9 rows of 147566, 22 us in pieces and 29 by blocks; 24 of 131072, 28 and 24; 126 of 107244 bfloat16, 70 and 24).
+constexpr int kFewRows = 16;
 constexpr size_t kFewBytes = 256 * 1024;
 
 // Pieces a row: enough for the marks, and more while the rows do not fill the machine (4 vectors a thread left at least).
