@@ -186,6 +186,15 @@ def test_gradient_in_place_scaled_and_added(rows, classes, dtype, rest):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes,count", [(2047, 40, 5), (2048, 40, 5), (2300, 517, 64), (2050, 2300, 9), (310, 70003, 20), (15, 140001, 256), (16, 140001, 256),
+                                                (2, 500001, 50)])
+@pytest.mark.parametrize("dtype,offset,rest,weighted", [(F32, 0, False, True), (BF16, 0, True, False), (BF16, 1, False, True), (F32, 3, True, True)])
+def test_many_rows_and_the_longest(rows, classes, count, dtype, offset, rest, weighted):
+    case = draw(rows, classes, count, dtype, F32, rows + classes, rest, weighted, 2.0)
+    check(*case, run(*case, tau=2.0, offset=offset), tau=2.0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("classes", [60, 700, 3001, 40000, 130001])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rest", [False, True])

@@ -181,6 +181,19 @@ def test_backward(n, h, w, c, groups, x_dtype, y_dtype, kind, offset):
         assert torch.equal(alone.view(bits if i == 0 else torch.int32), got[i].view(bits if i == 0 else torch.int32))
 
 
+MANY = [(1800, 3, 3, 8, 2), (1776, 11, 12, 64, 8), (1775, 11, 12, 64, 8), (400, 12, 12, 64, 8), (2, 64, 64, 2048, 32), (2, 17, 19, 1028, 4)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,h,w,c,groups", MANY)
+@pytest.mark.parametrize("dtype,kind", [(F32, SILU), (BF16, RELU), (BF16, SILU)])
+def test_many_images_and_wide_pixels(n, h, w, c, groups, dtype, kind):
+    x, gain, bias = draw(n, h, w, c, dtype, n + c)
+    check(x, gain, bias, groups, kind, forward(x, gain, bias, groups, kind, dtype))
+    args = draw_backward(n, h, w, c, groups, dtype, dtype, kind, n + c)
+    check_backward(args, backward(*args))
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,h,w,c,groups", [(2, 9, 11, 60, 12), (1, 28, 28, 256, 32), (1, 90, 75, 24, 3), (3, 5, 5, 6, 2)])
 @pytest.mark.parametrize("dtype", [F32, BF16])

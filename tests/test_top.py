@@ -98,6 +98,29 @@ def test_rows_in_every_order(classes, dtype, count):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes,count", [(1480, 1000, 1), (1500, 2870, 20), (1501, 5001, 64), (1600, 520, 33), (400, 30000, 8), (300, 30000, 200),
+                                                (1, 700000, 40), (47, 600000, 3), (48, 600000, 3)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["random", "few_values", "rising", "mostly_masked"])
+def test_many_rows_and_the_longest(rows, classes, count, dtype, kind):
+    n = torch.arange(classes)
+    if kind == "rising":
+        z = (n / 7 + torch.arange(rows)[:, None]).float()
+    else:
+        z = 3 * torch.randn(rows, classes, generator=rng(classes))
+    if kind == "few_values":
+        z = torch.round(z)
+    if kind == "mostly_masked":
+        z[::2, n % 97 != 5] = -torch.inf
+        z[1::2, n % 89 != 7] = torch.finfo(dtype).min
+        z[::7] = -torch.inf
+        z[3:4, 11] = float("nan")
+    z = z.to(dtype)
+    got = run(z, count, tau=2.0)
+    check(z, count, got, 2.0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("classes", [30, 2048, 40001, 150000])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_with_nothing_left_and_values_that_are_not_finite(classes, dtype):
