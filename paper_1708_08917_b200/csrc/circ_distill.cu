@@ -648,12 +648,20 @@ static DistillSpace space_of(const Distill* d, long rows) {
     s.bytes = s.parts + up(sizeof(Softmax) * (rows * least + 2 * kPieceTarget));
     return s;
 }
+// Clears what it has just allocated, nothing else: the counters of a workspace in use are 0 between calls, and row counts that need the same bytes have the
+// same layout, since no section shrinks as the rows grow.
 static int ensure_distill(Distill* d, long rows, cudaStream_t s) {
-    if (rows <= d->rows_held) return ensure_scratch(d->ws, space_of(d, d->rows_held).bytes, s, "circ_distill_reserve");
-    const int rc = ensure_scratch(d->ws, space_of(d, rows).bytes, s, "circ_distill_reserve");
-    d->rows_held = rc == CIRC_OK ? rows : d->ws.ptr ? d->rows_held : 0;
-    if (rc != CIRC_OK) return rc;
-    if (cudaMemsetAsync(d->ws.ptr, 0, space_of(d, rows).sums, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+    const long held = rows > d->rows_held ? rows : d->rows_held;
+    const DistillSpace space = space_of(d, held);
+    const bool fresh = d->ws.bytes < space.bytes;
+    const int rc = ensure_scratch(d->ws, space.bytes, s, "circ_distill_reserve");
+    if (rc != CIRC_OK) {
+        if (!d->ws.ptr) d->rows_held = 0;
+        return rc;
+    }
+    d->rows_held = held;
+    if (!fresh) return CIRC_OK;
+    if (cudaMemsetAsync(d->ws.ptr, 0, space.sums, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaFree(d->ws.ptr);      // this one alone: graphs may hold earlier ones
         d->ws.ptr = nullptr;
         d->ws.bytes = 0;

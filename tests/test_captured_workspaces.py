@@ -1,0 +1,59 @@
+"""Workspaces of the distillation handle under stream capture: a captured call whose workspace is already as large as it needs is served, one that
+needs more is refused, and either way the capture and the graphs captured before stay whole."""
+import pytest
+import torch
+
+import paper_1708_08917_b200 as circ
+from row_helpers import rng
+
+CLASSES, COUNT, TAU = 1024, 5, 2.0
+
+
+def distill_inputs(rows):
+    g = rng(rows)
+    z = torch.randn(rows, CLASSES, generator=g)
+    ids = torch.stack([torch.randperm(CLASSES, generator=g)[:COUNT] for _ in range(rows)])
+    values = torch.randn(rows, COUNT, generator=g)
+    p = torch.softmax(values.double() / TAU, 1)
+    log_q = torch.log_softmax(z.double() / TAU, 1)
+    loss = (p * (p.log() - log_q.gather(1, ids))).sum(1)
+    return [t.cuda() for t in (z, values, ids)], loss
+
+
+@pytest.mark.gpu
+def test_captured_distillation_of_more_rows():
+    h = circ.circ_distill_create(CLASSES, COUNT)
+    circ.circ_distill_set_temperature(h, TAU)
+    cases = {rows: (*distill_inputs(rows), torch.zeros(rows, device="cuda")) for rows in (1, 5, 5000)}
+
+    def call(rows):
+        (z, values, ids), _, out = cases[rows]
+        circ.circ_distill_forward(h, z, CLASSES, values, ids, None, None, out, None, None, rows, torch.cuda.current_stream())
+
+    call(1)
+    torch.cuda.synchronize()
+    graphs = {rows: torch.cuda.CUDAGraph() for rows in (1, 5, 5000)}
+    for rows in (1, 5):                 # these need the same number of bytes
+        with torch.cuda.graph(graphs[rows]):
+            call(rows)
+    counter = torch.zeros(1, device="cuda")
+    with torch.cuda.graph(graphs[5000]):
+        counter.add_(1)
+        with pytest.raises(circ.CircError) as e:
+            call(5000)
+        counter.add_(1)
+    assert e.value.code == circ.CIRC_ERR_UNSUPPORTED
+    for _ in range(2):
+        for rows in (1, 5):
+            cases[rows][2].zero_()
+            graphs[rows].replay()
+    graphs[5000].replay()
+    call(5000)                          # a larger workspace beside the one that the graphs hold
+    graphs[1].replay()
+    torch.cuda.synchronize()
+    assert float(counter) == 2
+    for rows, (_, want, out) in cases.items():
+        # exponentials with (s - max) / tau above -5: (2 + 15) u, sums of 1024 by 32 lanes: (32 + 16) u, the result: u; together below 1e-5
+        assert float((out.double().cpu() - want).abs().max()) <= 1e-5 * float(want.abs().max().clamp(min=1))
+    del graphs
+    circ.circ_distill_destroy(h)
