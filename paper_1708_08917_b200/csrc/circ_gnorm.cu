@@ -822,15 +822,20 @@ static GnormSpace space_of(const Gnorm* g, long images) {
     s.bytes = s.stats + up(2 * sizeof(float) * images * g->groups);
     return s;
 }
+// Clears what it has just allocated, nothing else: the counters of a workspace in use are 0 between calls, and numbers of images that need the same bytes
+// have the same layout, since no section shrinks as the images grow.
 static int ensure_gnorm(Gnorm* g, long images, cudaStream_t s) {
-    if (images <= g->images_held) return ensure_scratch(g->ws, space_of(g, g->images_held).bytes, s, "circ_gnorm_reserve");
-    const int rc = ensure_scratch(g->ws, space_of(g, images).bytes, s, "circ_gnorm_reserve");
+    const long held = images > g->images_held ? images : g->images_held;
+    const GnormSpace space = space_of(g, held);
+    const bool fresh = g->ws.bytes < space.bytes;
+    const int rc = ensure_scratch(g->ws, space.bytes, s, "circ_gnorm_reserve");
     if (rc != CIRC_OK) {
         if (!g->ws.ptr) g->images_held = 0;
         return rc;
     }
-    g->images_held = images;
-    if (cudaMemsetAsync(g->ws.ptr, 0, space_of(g, images).group_parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+    g->images_held = held;
+    if (!fresh) return CIRC_OK;
+    if (cudaMemsetAsync(g->ws.ptr, 0, space.group_parts, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaFree(g->ws.ptr);      // this one alone: graphs may hold earlier ones
         g->ws.ptr = nullptr;
         g->ws.bytes = 0;
