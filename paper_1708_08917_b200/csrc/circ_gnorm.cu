@@ -61,6 +61,30 @@ __device__ __forceinline__ void with_act_of(int act, F&& f) {
     else f(std::integral_constant<int, CIRC_ACT_NONE>{});
 }
 
+// Values that a thread adds up in float32 at a time (and up to a round of loads more); the sums of longer walks are joined in float64, so that what rounding
+// costs does not grow with the pixels.  A walk's squares are taken around the mean of its first values (at most kPivot), those of later runs around the mean so
+// far: a value far from the others in the first place is lost in neither.  (Variance of 264 normal values, the first 100 deviations out: relative error 5e-6 at most
+// in 60 draws, 3e-4 around the first one alone; 3e-3 and more without runs from 12800 values on.)
+constexpr int kRun = 256;
+constexpr int kPivot = 8;
+// The mean of some values, less a reference, and the sum of squares around the mean.
+struct Moments {
+    double mean, m2;
+    // Those of n values (`inv`: 1 / n) whose sums around `pivot` (less the reference) are s1 and s2.
+    __device__ __forceinline__ static Moments of(double inv, double pivot, float s1, float s2) {
+        const double d = (double)s1 * inv;
+        return Moments{pivot + d, (double)s2 - (double)s1 * d};
+    }
+    // Both: of n0 values, and of n1 more that are `part` of all.
+    __device__ __forceinline__ static Moments join(double n0, Moments a, double part, Moments b) {
+        const double d = b.mean - a.mean;
+        return Moments{a.mean + d * part, a.m2 + b.m2 + d * d * (n0 * part)};
+    }
+};
+// A float64 value in the place of two float32 ones.
+__device__ __forceinline__ float2 as_float2(double v) { return make_float2(__int_as_float(__double2loint(v)), __int_as_float(__double2hiint(v))); }
+__device__ __forceinline__ double as_double(float2 v) { return __hiloint2double(__float_as_int(v.y), __float_as_int(v.x)); }
+
 // What a channel's values go through: v = (x - mean) (rstd gain) + bias.
 struct Channel {
     float mean, rstd, gain, bias;
@@ -203,26 +227,63 @@ __device__ __forceinline__ void over_groups(const GnormArgs& a, int entries, TER
     }
 }
 
-// A thread's sums of a channel run around the thread's first value, which bounds what the difference of the two sums loses; means are kept as
-// differences from the channel's first value in the image, so that a large offset costs no digits, until they are joined in float64.
-template <typename T>
+// Means are kept as differences from the channel's first value in the image, so that a large offset costs no digits, until they are joined in float64.
+// LONG: some threads have more than kRun pixels.
+template <typename T, bool LONG>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_any_stats_kernel(const T* __restrict__ x, GnormArgs a) {
     __shared__ float2 sums[kGnormThreads];
+    __shared__ Moments totals[LONG ? kGnormThreads : 1];      // of a thread's runs that are done
     pdl_begin();
     const GnormPlace at(a);
     if (at.live) {
-        float pivot = 0.f, s1 = 0.f, s2 = 0.f;
-        int n = 0;
-#pragma unroll 4
-        for (int p = at.from + at.lane; p < at.to; p += at.lanes, ++n) {
-            const float v = to_float(x[at.at(a, p)]);
-            if (n == 0) pivot = v;
+        const float first = to_float(x[at.at(a, 0)]);
+        const int p0 = at.from + at.lane;
+        float pivot = 0.f, s1 = 0.f, s2 = 0.f, head[kPivot];
+        auto take = [&](float v) {
             const float d = v - pivot;
             s1 += d;
             s2 = fmaf(d, d, s2);
+        };
+        int n = 0, before = 0;      // values of the run, and of those before it
+#pragma unroll
+        for (int i = 0; i < kPivot; ++i) {
+            head[i] = p0 + i * at.lanes < at.to ? to_float(x[at.at(a, p0 + i * at.lanes)]) : 0.f;
+            pivot += head[i];
+            n += p0 + i * at.lanes < at.to;
         }
-        const float inv = n ? 1.f / (float)n : 0.f;
-        sums[threadIdx.x] = make_float2(fmaf(s1, inv, pivot - to_float(x[at.at(a, 0)])), s2 - s1 * s1 * inv);
+        pivot *= n ? 1.f / (float)n : 0.f;
+#pragma unroll
+        for (int i = 0; i < kPivot; ++i)
+            if (i < n) take(head[i]);
+        int p = p0 + kPivot * at.lanes;
+        if constexpr (LONG) {
+            auto fold = [&]() {
+                Moments all = Moments::of(1.0 / n, (double)pivot - (double)first, s1, s2);
+                if (before) all = Moments::join(before, totals[threadIdx.x], (double)n / (double)(before + n), all);
+                totals[threadIdx.x] = all;
+                before += n;
+            };
+            while (p < at.to) {
+                const int end = min(at.to, p + (kRun - n) * at.lanes);
+#pragma unroll 4
+                for (; p < end; p += at.lanes, ++n) take(to_float(x[at.at(a, p)]));
+                if (p >= at.to) break;
+                fold();
+                pivot = (float)(totals[threadIdx.x].mean + (double)first);
+                s1 = s2 = 0.f;
+                n = 0;
+            }
+            if (before) fold();
+        } else {
+#pragma unroll 4
+            for (; p < at.to; p += at.lanes, ++n) take(to_float(x[at.at(a, p)]));
+        }
+        if (LONG && before) {
+            sums[threadIdx.x] = make_float2((float)totals[threadIdx.x].mean, (float)totals[threadIdx.x].m2);
+        } else {
+            const float inv = n ? 1.f / (float)n : 0.f;
+            sums[threadIdx.x] = make_float2(fmaf(s1, inv, pivot - first), s2 - s1 * s1 * inv);
+        }
     }
     __syncthreads();
     const int c = at.tile * a.columns + threadIdx.x;
@@ -424,27 +485,48 @@ __device__ __forceinline__ void each_channel(const GnormArgs& a, F f) {
     }
 }
 // Calls load(i, element) for a thread's pixels, R at a time, and take(i, element) for each of them behind.  BACK: from the last round to the first.
-template <int R, bool BACK, int VEC, typename LOAD, typename TAKE>
-__device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, TAKE take) {
+// start(pixels) (STARTS): between the first round's loads and takes, with its number of pixels.  fold(pixels) (FOLDS): between every kRun pixels and more, with
+// the number of those before them.
+template <int R, bool BACK, bool STARTS, bool FOLDS, int VEC, typename LOAD, typename TAKE, typename START, typename FOLD>
+__device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, TAKE take, START start, FOLD fold) {
     auto rest = [&]() {
         if (st.last <= 0) return;
         const size_t at = st.at + st.size.full * st.jump;
 #pragma unroll
         for (int i = 0; i < R; ++i)
             if (i < st.last) load(i, at + i * st.step);
+        if (STARTS && st.size.full == 0) start(st.last);
 #pragma unroll
         for (int i = 0; i < R; ++i)
             if (i < st.last) take(i, at + i * st.step);
     };
-    if (BACK) rest();
-    for (int n = 0; n < st.size.full; ++n) {
+    auto round = [&](int n, bool head) {
         const size_t at = st.at + (BACK ? st.size.full - 1 - n : n) * st.jump;
 #pragma unroll
         for (int i = 0; i < R; ++i) load(i, at + i * st.step);
+        if (head) start(R);
 #pragma unroll
         for (int i = 0; i < R; ++i) take(i, at + i * st.step);
+    };
+    if (BACK) rest();
+    int n = 0;
+    if (STARTS && n < st.size.full) round(n++, true);
+    for (;;) {
+        const int end = FOLDS ? min(st.size.full, (n + kRun / R) / (kRun / R) * (kRun / R)) : st.size.full;
+        for (; n < end; ++n) round(n, false);
+        if (!FOLDS || n >= st.size.full) break;
+        fold(n * R - kRun);
     }
     if (!BACK) rest();
+}
+template <int R, bool BACK, int VEC, typename LOAD, typename TAKE>
+__device__ __forceinline__ void walk_pixels(const Stretch<VEC>& st, LOAD load, TAKE take) {
+    walk_pixels<R, BACK, false, false>(st, load, take, [](int) {}, [](int) {});
+}
+// Pixels of a walk that fold() is called for.
+template <int R, int VEC>
+__device__ __forceinline__ int folded_pixels(const Stretch<VEC>& st) {
+    return st.size.full > 0 ? (st.size.full - 1) / (kRun / R) * kRun : 0;
 }
 
 // VEC channels' values of a vector of one a channel (NULL: `none`), and of one a group.
@@ -507,13 +589,14 @@ __device__ __forceinline__ void apply_stretch(const T* x, U* y, const GnormArgs&
     });
 }
 
-// A piece's sums: a thread's, around the channel's value at its first pixel (which bounds what the difference of the two sums loses), those of the
-// threads that share a channel, and those of a group's channels, each around their joint mean.  Means are kept as differences from the image's first
-// pixel, so that a large offset costs no digits.
-// WHOLE: a block has a whole image, and writes its output too.
-template <typename T, typename U, int VEC, int R, bool WHOLE>
+// A piece's sums: a thread's (see kRun; what came before a run waits in shared memory), those of the threads that share a channel, and those of a group's
+// channels, each around their joint mean.  Means are kept as differences from the image's first pixel, so that a large offset costs no digits.
+// WHOLE: a block has a whole image, and writes its output too.  LONG: some threads have more than kRun pixels (a kernel of its own: its registers cost the
+// others 2 to 9 %).
+template <typename T, typename U, int VEC, int R, bool WHOLE, bool LONG>
 __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* x, U* y, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
+    static_assert(R <= kPivot && kRun % R == 0, "");
     __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
     __shared__ float firsts[kGnormThreads * VEC];
     __shared__ double2 red[kGnormThreads];
@@ -521,16 +604,18 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
     const Stretch<VEC> st(a, blockIdx.x, R);
     const T* first = x + (size_t)st.image * a.pixels * a.channels;
     if (st.live) {
-        RawVec<T, VEC> raw[R], zero, own;
-        zero.load(first + st.column * VEC);
-        own.load(st.mine > 0 ? x + st.at : first + st.column * VEC);
+        RawVec<T, VEC> raw[R], zero;
         Pair pivot[N], s1[N], s2[N];       // pivot: less than 0
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            pivot[i] = pair_mul(two(own, i), pair_of(-1.f, -1.f));
-            s1[i] = s2[i] = pair_of(0.f, 0.f);
-        }
-        walk_pixels<R, false>(st, [&](int i, size_t o) { raw[i].load(x + o); },
+        for (int i = 0; i < N; ++i) pivot[i] = s1[i] = s2[i] = pair_of(0.f, 0.f);
+        // values around `p` joined to those before, of which the thread's shared words have the moments
+        auto joined_run = [&](int before, double inv, double part, float f, float p, float sum, float square, int e) {
+            const Moments run = Moments::of(inv, (double)p - (double)f, sum, square);
+            if (before == 0) return run;
+            const int at = e * kGnormThreads + threadIdx.x;
+            return Moments::join(before, Moments{as_double(sums[at]), as_double(joined[at])}, part, run);
+        };
+        walk_pixels<R, false, true, LONG>(st, [&](int i, size_t o) { raw[i].load(x + o); },
                        [&](int i, size_t) {
 #pragma unroll
                            for (int k = 0; k < N; ++k) {
@@ -538,12 +623,49 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
                                s1[k] = pair_add(s1[k], d);
                                s2[k] = pair_fma(d, d, s2[k]);
                            }
+                       },
+                       [&](int n) {
+                           const float inv = -1.f / (float)n;
+#pragma unroll
+                           for (int i = 0; i < R; ++i)
+                               if (i < n)
+#pragma unroll
+                                   for (int k = 0; k < N; ++k) pivot[k] = pair_add(pivot[k], two(raw[i], k));
+#pragma unroll
+                           for (int k = 0; k < N; ++k) pivot[k] = pair_mul(pivot[k], pair_of(inv, inv));
+                       },
+                       [&](int before) {
+                           zero.load(first + st.column * VEC);
+                           const double part = (double)kRun / (double)(before + kRun);
+#pragma unroll
+                           for (int e = 0; e < VEC; ++e) {
+                               const Moments m = joined_run(before, 1.0 / kRun, part, zero.get(e), -half(pivot[e / 2], e), half(s1[e / 2], e), half(s2[e / 2], e), e);
+                               sums[e * kGnormThreads + threadIdx.x] = as_float2(m.mean);
+                               joined[e * kGnormThreads + threadIdx.x] = as_float2(m.m2);
+                               Channels<VEC>::put(pivot[e / 2], e % 2, -(float)(m.mean + (double)zero.get(e)));
+                           }
+#pragma unroll
+                           for (int i = 0; i < N; ++i) s1[i] = s2[i] = pair_of(0.f, 0.f);
                        });
+        zero.load(first + st.column * VEC);
+        const int before = LONG ? folded_pixels<R>(st) : 0;
         const float inv = st.mine > 0 ? 1.f / (float)st.mine : 0.f;
+        double inv_run = 0.0, part = 0.0;
+        if (before > 0) {
+            inv_run = 1.0 / (double)(st.mine - before);
+            part = (double)(st.mine - before) / (double)st.mine;
+        }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const float f = zero.get(e), sum = half(s1[e / 2], e), square = half(s2[e / 2], e);
-            sums[e * kGnormThreads + threadIdx.x] = make_float2(fmaf(sum, inv, -half(pivot[e / 2], e) - f), square - sum * sum * inv);
+            const float f = zero.get(e), p = -half(pivot[e / 2], e), sum = half(s1[e / 2], e), square = half(s2[e / 2], e);
+            float2 both;
+            if (before > 0) {
+                const Moments m = joined_run(before, inv_run, part, f, p, sum, square, e);
+                both = make_float2((float)m.mean, (float)m.m2);
+            } else {
+                both = make_float2(fmaf(sum, inv, p - f), square - sum * sum * inv);
+            }
+            sums[e * kGnormThreads + threadIdx.x] = both;
             if (st.lane == 0) firsts[st.column * VEC + e] = f;
         }
     }
@@ -754,6 +876,7 @@ struct GnormPlan {
     int vec, r;             // elements a vector, pixels a thread; vec 0: any tensor
     int columns, tiles, pieces, per;
     bool whole;             // a block an image, in one launch
+    bool runs;              // a thread may have more than kRun pixels
 };
 static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, uintptr_t addresses) {
     const size_t xb = dtype_bytes(g->x_dtype), yb = dtype_bytes(g->y_dtype), small = xb < yb ? xb : yb;
@@ -778,6 +901,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.per = lanes * p.r;
         if (p.whole) {
             p.pieces = 1;
+            p.runs = pixels / p.per * p.r > kRun;
             return p;
         }
         // As many pieces an image as take the least time: blocks that run at once (three an SM) take the pieces in turns, and a block's beginning and end
@@ -792,6 +916,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
                 p.pieces = (int)k;
             }
         }
+        p.runs = (pixels / p.per + p.pieces - 1) / p.pieces * p.r > kRun;
     } else {
         p.columns = kGnormThreads < g->channels ? kGnormThreads : g->channels;
         p.tiles = (g->channels + p.columns - 1) / p.columns;
@@ -800,6 +925,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         const long pieces = std::min({want, can, 64L});       // one block joins them
         p.per = (int)((pixels + pieces - 1) / pieces);
         p.pieces = (pixels + p.per - 1) / p.per;
+        p.runs = p.per > kRun * lanes;
     }
     return p;
 }
@@ -878,19 +1004,24 @@ static cudaError_t run_forward(const GnormPlan& p, const GnormArgs& a, const T* 
     cudaError_t err = cudaSuccess;
     if (p.vec == 0) {
         const dim3 grid((unsigned)((long)a.images * a.pieces * a.tiles));
-        if ((err = launch_row(gnorm_any_stats_kernel<T>, grid, dim3(kGnormThreads), 0, s, x, a)) == cudaSuccess)
+        const auto stats = p.runs ? gnorm_any_stats_kernel<T, true> : gnorm_any_stats_kernel<T, false>;
+        if ((err = launch_row(stats, grid, dim3(kGnormThreads), 0, s, x, a)) == cudaSuccess)
             err = launch_row(gnorm_any_apply_kernel<T, U>, grid, dim3(kGnormThreads), 0, s, x, y, a);
         return err;
     }
     with_plan<T, false>(p, [&](auto vec, auto r) {
         constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
         const dim3 grid((unsigned)((long)a.images * a.pieces));
-        if constexpr (R > 1)
+        auto stats = gnorm_stats_kernel<T, U, VEC, R, false, false>;
+        if constexpr (R > 1) {      // (rounds of one pixel a thread: a few of them)
             if (p.whole) {
-                err = launch_row(gnorm_stats_kernel<T, U, VEC, R, true>, grid, dim3(kGnormThreads), 0, s, x, y, a);
+                err = launch_row(p.runs ? gnorm_stats_kernel<T, U, VEC, R, true, true> : gnorm_stats_kernel<T, U, VEC, R, true, false>, grid,
+                                 dim3(kGnormThreads), 0, s, x, y, a);
                 return;
             }
-        if ((err = launch_row(gnorm_stats_kernel<T, U, VEC, R, false>, grid, dim3(kGnormThreads), 0, s, x, y, a)) == cudaSuccess)
+            if (p.runs) stats = gnorm_stats_kernel<T, U, VEC, R, false, true>;
+        }
+        if ((err = launch_row(stats, grid, dim3(kGnormThreads), 0, s, x, y, a)) == cudaSuccess)
             err = launch_row(gnorm_apply_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, y, a);
     });
     return err;
