@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_apply_kernel(const T*
             store_one(y + at.at(a, p), activate<decltype(act)::value>(fmaf(to_float(x[at.at(a, p)]) - c.mean, scale, c.bias)));
     });
 }
-template <typename T, typename U>
+template <typename T, typename U, bool LONG>
 __global__ void __launch_bounds__(kGnormThreads) gnorm_any_sums_kernel(const T* __restrict__ x, const U* __restrict__ grad_y, GnormArgs a) {
     __shared__ float2 sums[kGnormThreads];
     pdl_begin();
@@ -337,15 +337,25 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_sums_kernel(const T* 
     if (at.live) {
         const Channel ch = at.channel(a);
         float s1 = 0.f, s2 = 0.f;
+        double2 all = make_double2(0.0, 0.0);       // of the runs that are done
         with_act_of(a.act, [&](auto act) {
+            int p = at.from + at.lane;
+            for (;;) {
+                const int end = LONG ? min(at.to, p + kRun * at.lanes) : at.to;
 #pragma unroll 4
-            for (int p = at.from + at.lane; p < at.to; p += at.lanes) {
-                const float v = to_float(x[at.at(a, p)]), u = ch.unit(v), g = to_float(grad_y[at.at(a, p)]) * ch.template slope<decltype(act)::value>(v, u);
-                s1 += g;
-                s2 = fmaf(g, u, s2);
+                for (; p < end; p += at.lanes) {
+                    const float v = to_float(x[at.at(a, p)]), u = ch.unit(v), g = to_float(grad_y[at.at(a, p)]) * ch.template slope<decltype(act)::value>(v, u);
+                    s1 += g;
+                    s2 = fmaf(g, u, s2);
+                }
+                if (!LONG) break;
+                all.x += (double)s1;
+                all.y += (double)s2;
+                s1 = s2 = 0.f;
+                if (p >= at.to) break;
             }
         });
-        sums[threadIdx.x] = make_float2(s1, s2);
+        sums[threadIdx.x] = LONG ? make_float2((float)all.x, (float)all.y) : make_float2(s1, s2);
     }
     __syncthreads();
     const int c = at.tile * a.columns + threadIdx.x;
@@ -758,7 +768,8 @@ __device__ __forceinline__ void grad_stretch(const T* x, const U* grad_y, T* gra
 }
 
 // Backward: the channels' sums of the pieces go to `parts`; the gain's and the bias's gradients are added up from them.
-template <typename T, typename U, int VEC, int R, bool WHOLE>
+// LONG: some threads have more than kRun pixels; sums of their runs wait in shared memory.
+template <typename T, typename U, int VEC, int R, bool WHOLE, bool LONG>
 __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x, const U* grad_y, T* grad_x, GnormArgs a) {
     constexpr int N = Channels<VEC>::N;
     __shared__ float2 sums[kGnormThreads * VEC], joined[kGnormThreads * VEC];
@@ -771,10 +782,11 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x
         Pair s1[N], s2[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) s1[i] = s2[i] = pair_of(0.f, 0.f);
+        const int at = threadIdx.x;
         with_act_of(a.act, [&](auto act) {
             RawVec<T, VEC> raw[R];
             RawVec<U, VEC> graw[R];
-            walk_pixels<R, false>(st,
+            walk_pixels<R, false, false, LONG>(st,
                            [&](int i, size_t o) {
                                raw[i].load(x + o);
                                graw[i].load(grad_y + o);
@@ -787,10 +799,26 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x
                                    s1[k] = pair_add(s1[k], g);
                                    s2[k] = pair_fma(g, u, s2[k]);
                                }
+                           },
+                           [](int) {},
+                           [&](int before) {
+#pragma unroll
+                               for (int e = 0; e < VEC; ++e) {
+                                   const double old1 = before ? as_double(sums[e * kGnormThreads + at]) : 0.0, old2 = before ? as_double(joined[e * kGnormThreads + at]) : 0.0;
+                                   sums[e * kGnormThreads + at] = as_float2(old1 + (double)half(s1[e / 2], e));
+                                   joined[e * kGnormThreads + at] = as_float2(old2 + (double)half(s2[e / 2], e));
+                               }
+#pragma unroll
+                               for (int i = 0; i < N; ++i) s1[i] = s2[i] = pair_of(0.f, 0.f);
                            });
         });
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sums[e * kGnormThreads + threadIdx.x] = make_float2(half(s1[e / 2], e), half(s2[e / 2], e));
+        for (int e = 0; e < VEC; ++e) {
+            float2 both = make_float2(half(s1[e / 2], e), half(s2[e / 2], e));
+            if (LONG && folded_pixels<R>(st) > 0)
+                both = make_float2((float)(as_double(sums[e * kGnormThreads + at]) + (double)both.x), (float)(as_double(joined[e * kGnormThreads + at]) + (double)both.y));
+            sums[e * kGnormThreads + at] = both;
+        }
     }
     __syncthreads();
     each_channel<VEC>(a, [&](int c, int e, int column) {
@@ -1035,19 +1063,24 @@ static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T*
     bool done = false;
     *launches = 1;
     if (p.vec == 0) {
-        if ((err = launch_row(gnorm_any_sums_kernel<T, U>, grid, threads, 0, s, x, grad_y, a)) == cudaSuccess && grad_x) {
+        const auto sums = p.runs ? gnorm_any_sums_kernel<T, U, true> : gnorm_any_sums_kernel<T, U, false>;
+        if ((err = launch_row(sums, grid, threads, 0, s, x, grad_y, a)) == cudaSuccess && grad_x) {
             err = launch_row(gnorm_any_grad_kernel<T, U>, grid, threads, 0, s, x, grad_y, grad_x, a);
             ++*launches;
         }
     } else {
         with_plan<T, true>(p, [&](auto vec, auto r) {
             constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
-            if constexpr (R > 1)
+            auto sums = gnorm_sums_kernel<T, U, VEC, R, false, false>;
+            if constexpr (R > 1) {
                 if (p.whole) {
-                    err = launch_row(gnorm_sums_kernel<T, U, VEC, R, true>, grid, threads, 0, s, x, grad_y, grad_x, a);
+                    err = launch_row(p.runs ? gnorm_sums_kernel<T, U, VEC, R, true, true> : gnorm_sums_kernel<T, U, VEC, R, true, false>, grid, threads, 0, s, x,
+                                     grad_y, grad_x, a);
                     return;
                 }
-            if ((err = launch_row(gnorm_sums_kernel<T, U, VEC, R, false>, grid, threads, 0, s, x, grad_y, grad_x, a)) == cudaSuccess && grad_x) {
+                if (p.runs) sums = gnorm_sums_kernel<T, U, VEC, R, false, true>;
+            }
+            if ((err = launch_row(sums, grid, threads, 0, s, x, grad_y, grad_x, a)) == cudaSuccess && grad_x) {
                 err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, dim3(grid.x + totals), threads, 0, s, x, grad_y, grad_x, grad_gain, grad_bias, totals, a);
                 done = true;
                 ++*launches;

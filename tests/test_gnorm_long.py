@@ -61,3 +61,29 @@ def test_deviations_of_many_pixels(n, h, w, c, x_dtype, y_dtype):
         v = d * r
         err = r * mean_err + v.abs() * 858 * U + rounding(y_dtype) * v.abs() * (1 + 2 ** -7)
         assert bool(((y[i].double() - v).abs() <= err).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,h,w,c,x_dtype", [(444, 80, 80, 1024, BF16),      # 6400 pixels a thread, in two launches
+                                             (1776, 80, 80, 255, BF16),      # ... in one
+                                             (1, 1024, 800, 257, F32)])      # any width: 12800
+def test_gradients_of_many_pixels(n, h, w, c, x_dtype):
+    """The same gradient everywhere, one whose float32 sum drifts (6400 of them in one run: 9e-5); u = 1 everywhere.  Runs of at most 264 additions, one thread a
+    channel and piece, joined in float64: 268 u."""
+    value = 0.32391423
+    x = torch.ones(n, h * w, c, dtype=x_dtype, device="cuda")
+    grad_y = torch.full((n, h * w, c), value, device="cuda")
+    mean, rstd = torch.zeros(n, c, device="cuda"), torch.ones(n, c, device="cuda")
+    grad_gain, grad_bias = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    hd = handle(c, c, x_dtype, F32)
+    circ.circ_gnorm_backward(hd, x, None, None, mean, rstd, grad_y, grad_y if x_dtype == F32 else x, grad_gain, grad_bias, n, h, w, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    circ.circ_gnorm_destroy(hd)
+    g = float(torch.tensor(value))
+    want = g * n * h * w
+    for got in (grad_gain, grad_bias):
+        assert float((got.double() - want).abs().max()) <= 268 * U * want
+    # grad_x = g - A - u B, both the mean of what was summed up
+    grad_x = grad_y if x_dtype == F32 else x
+    for i in {0, n // 2, n - 1}:
+        assert float((grad_x[i].double() + g).abs().max()) <= (2 * 268 + 4) * U * g + rounding(x_dtype) * g * (1 + 2 ** -7)
