@@ -106,6 +106,11 @@ struct Channel {
     }
 };
 
+// Whether v is above 0.  A call for single channels: in line, its registers cost the other activations of the same kernels (SiLU gradient of 32 x 56 x 56 x 255
+// bfloat16: 102 us, and 93 with the call; ReLU 112 and 120, and 149 with float64 for every value).
+__device__ __noinline__ bool above_zero(float x, float mean, float rstd, float gain, float bias) {
+    return ((double)x + (double)mean) * ((double)rstd * (double)gain) + (double)bias > 0.0;
+}
 // The same for a vector of channels, arithmetic in pairs.
 template <int VEC>
 struct Channels {
@@ -136,17 +141,25 @@ struct Channels {
             split(t, t0, t1);
             split(bias[i], b0, b1);
             split(g, g0, g1);
+            // near 0 the sides come from float64
+            auto near = [](float v, float t, float b) { return fabsf(v) <= 1e-6f * (fabsf(t) + fabsf(b)); };
             bool on0 = v0 > 0.f, on1 = v1 > 0.f;
-            if (fabsf(v0) <= 1e-6f * (fabsf(t0) + fabsf(b0)) || fabsf(v1) <= 1e-6f * (fabsf(t1) + fabsf(b1))) {
+            if (near(v0, t0, b0) || (VEC > 1 && near(v1, t1, b1))) {
                 float x0, x1, m0, m1, r0, r1, a0, a1;
                 split(x, x0, x1);
                 split(mean[i], m0, m1);
                 split(rstd[i], r0, r1);
                 split(gain[i], a0, a1);
-                on0 = ((double)x0 + (double)m0) * ((double)r0 * (double)a0) + (double)b0 > 0.0;
-                on1 = ((double)x1 + (double)m1) * ((double)r1 * (double)a1) + (double)b1 > 0.0;
+                if constexpr (VEC == 1) {
+                    on0 = above_zero(x0, m0, r0, a0, b0);
+                } else {
+                    on0 = ((double)x0 + (double)m0) * ((double)r0 * (double)a0) + (double)b0 > 0.0;
+                    on1 = ((double)x1 + (double)m1) * ((double)r1 * (double)a1) + (double)b1 > 0.0;
+                }
             }
-            g = pair_of(on0 ? g0 : v0 != v0 ? v0 : 0.f, on1 ? g1 : v1 != v1 ? v1 : 0.f);
+            g0 = on0 ? g0 : v0 != v0 ? v0 : 0.f;
+            if constexpr (VEC > 1) g1 = on1 ? g1 : v1 != v1 ? v1 : 0.f;
+            g = pair_of(g0, VEC > 1 ? g1 : 0.f);
         } else {
             const Pair s = pair_of(sigmoid_of(v0), VEC > 1 ? sigmoid_of(v1) : 0.f), one = pair_of(1.f, 1.f);
             g = pair_mul(g, pair_mul(s, pair_fma(v, pair_fma(s, pair_of(-1.f, -1.f), one), one)));
