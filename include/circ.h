@@ -468,7 +468,7 @@ CIRC_API void circ_clip_destroy(circ_clip_handle h);
  *   circ_top_set_temperature : > 0; of lse alone.
  *   circ_top_forward         : logits [rows] of `stride` elements (>= classes).  Any of the three results may be NULL:
  *       values : [rows][count], descending        ids : [rows][count], their classes; equal scores: the lower class first
- *       lse    : float32 [rows], log sum exp(logits / temperature) over all classes
+ *       lse    : float32 [rows], log sum exp(logits / temperature) over all classes: +inf with a logit of +inf, NaN with a NaN
  *   circ_top_reserve         : workspace for calls of up to max_rows rows.
  * A NaN counts as larger than anything else.  Classes masked with -inf come last, in their order.  Equal zeros of either sign are +0 in
  * values.

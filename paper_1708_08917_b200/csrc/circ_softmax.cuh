@@ -85,9 +85,11 @@ __device__ __forceinline__ float most_of(const RawVec<__nv_bfloat16, VEC> (&raw)
 struct Running {
     float top = -INFINITY, sum = 0.f;      // sum of exp(z - top) 2^shift
     Exponent ex;
-    __device__ __forceinline__ explicit Running(float scale = kLog2e) : ex(-INFINITY, scale) {}
+    float limit;                           // the top goes no higher: with FLT_MAX a score of +inf makes the sum +inf, without a limit NaN
+    __device__ __forceinline__ explicit Running(float scale = kLog2e, float l = INFINITY) : ex(-INFINITY, scale), limit(l) {}
     __device__ __forceinline__ void rise(float most) {
         if (!(most > top)) return;
+        most = most > limit ? limit : most;
         const Exponent to(most, ex.scale);
         sum *= top == -INFINITY ? 0.f : exp2_of((top - most) * ex.scale + (to.shift - ex.shift));
         top = most;

@@ -1,4 +1,6 @@
 // The `count` largest of a row's scores in descending order, equal ones by their class, and log sum exp(z / tau) over the whole row.
+#include <float.h>
+
 #include <algorithm>
 #include <new>
 #include <type_traits>
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(kAnyThreads) top_any_kernel(const T* __restric
     for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* zr = z + (size_t)row * a.ld;
         if (a.lse) {
-            Running run(a.scale);
+            Running run(a.scale, FLT_MAX);
             for (int c0 = tid; c0 < a.classes; c0 += kAnyThreads * 8) {
                 float s[8];
 #pragma unroll
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(THREADS < 128 ? 128 : THREADS) top_held_kernel
     uint32_t order[N * VEC];
     {
         RawVec<T, VEC> raw[N];
-        Running run(a.scale);
+        Running run(a.scale, FLT_MAX);
 #pragma unroll
         for (int i = 0; i < N; ++i) span.load(raw[i], z, i * THREADS + rank);
 #pragma unroll
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, PIECES ? 1 : kRowThreads / THREADS) t
     float best[kKept];
 #pragma unroll
     for (int u = 0; u < kKept; ++u) best[u] = -INFINITY;
-    Running run(a.scale);
+    Running run(a.scale, FLT_MAX);
     for (int i = tid; i < whole; i += kKept * THREADS) {
         const T* from = src + (size_t)(i - tid) * VEC;
         RawVec<T, VEC> raw[kKept];
@@ -658,7 +660,7 @@ __global__ void __launch_bounds__(128, 10) top_warp_kernel(const T* __restrict__
     float best[2][kKept];
 #pragma unroll
     for (int u = 0; u < 2 * kKept; ++u) best[u / kKept][u % kKept] = -INFINITY;
-    Running run(a.scale);
+    Running run(a.scale, FLT_MAX);
     for (int i = 0; i < whole; i += 2 * kKept * 32)
 #pragma unroll
         for (int odd = 0; odd < 2; ++odd) {
