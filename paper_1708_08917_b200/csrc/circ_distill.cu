@@ -15,7 +15,8 @@ struct Distill {
     float temperature;
     bool rest, add;
     Scratch ws;
-    long rows_held;      // rows that the workspace is laid out for
+    long rows_held;      // rows that the workspace is laid out for ...
+    long lists_held;     // ... and rows that it has room for the lists of
 };
 
 // A row's part of the gradient kernel's work.
@@ -617,6 +618,7 @@ constexpr long kPieceTarget = 148 * 8;      // blocks that fill the machine
 // gradient: 9 rows of 147566, 22 us in pieces and 29 by blocks; 24 of 131072, 28 and 24; 126 of 107244 bfloat16, 70 and 24).
 constexpr int kFewRows = 16;
 constexpr size_t kFewBytes = 256 * 1024;
+constexpr size_t kMarksMost = 48 * 1024 * 8;      // classes a row whose marks a block holds
 
 // Pieces a row: enough for the marks, and more while the rows do not fill the machine (4 vectors a thread left at least).
 static int pieces_of(long rows, int classes, int vec, int* per) {
@@ -630,11 +632,22 @@ static int pieces_of(long rows, int classes, int vec, int* per) {
     return (int)((vectors + *per - 1) / *per);
 }
 
-// Workspace: counters (256 bytes), the rows' counters, their sums, plans and lists, and the pieces' sums, for `rows` rows.
+// How a call is run: rows, or pieces of them by vectors or by elements.
+enum class Walk { rows, pieces, elements };
+static Walk walk_of(const Distill* d, const void* z, long ld, const void* grad, long grad_ld, long rows) {
+    const int vec = 16 / (int)dtype_bytes(d->dtype);
+    if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (ld - grad_ld) % vec)) return Walk::elements;
+    const long vectors = ((long)d->classes + 2 * vec - 2) / vec;
+    int per;
+    const bool few = vectors > 256 && pieces_of(rows, d->classes, vec, &per) > 1 && rows < kFewRows && (size_t)vectors * 16 > kFewBytes;
+    return few || (size_t)vectors * vec > kMarksMost ? Walk::pieces : Walk::rows;
+}
+
+// Workspace: counters (256 bytes), the rows' counters, their sums and plans, and the pieces' sums, for `rows` rows; the lists' gradients for `lists` rows.
 struct DistillSpace {
-    size_t arrived, grouped, sums, group_sums, plans, listed, parts, bytes;
+    size_t arrived, grouped, sums, group_sums, plans, parts, listed, bytes;
 };
-static DistillSpace space_of(const Distill* d, long rows) {
+static DistillSpace space_of(const Distill* d, long rows, long lists) {
     DistillSpace s;
     const size_t least = ((size_t)d->classes + kPieceBits / 2 - 1) / (kPieceBits / 2) + 1;      // pieces a row where rows fill the machine
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -643,29 +656,34 @@ static DistillSpace space_of(const Distill* d, long rows) {
     s.sums = s.grouped + up(sizeof(unsigned) * (rows / kMeanGroup + 1));
     s.group_sums = s.sums + up(sizeof(double2) * rows);
     s.plans = s.group_sums + up(sizeof(double2) * (rows / kMeanGroup + 1));
-    s.listed = s.plans + up(sizeof(RowPlan) * rows);
-    s.parts = s.listed + up(sizeof(Listed) * rows * d->count);
-    s.bytes = s.parts + up(sizeof(Softmax) * (rows * least + 2 * kPieceTarget));
+    s.parts = s.plans + up(sizeof(RowPlan) * rows);
+    s.listed = s.parts + up(sizeof(Softmax) * (rows * least + 2 * kPieceTarget));
+    s.bytes = s.listed + up(sizeof(Listed) * lists * d->count);
     return s;
 }
-// Clears what it has just allocated, nothing else: the counters of a workspace in use are 0 between calls, and row counts that need the same bytes have the
-// same layout, since no section shrinks as the rows grow.
-static int ensure_distill(Distill* d, long rows, cudaStream_t s) {
-    const long held = rows > d->rows_held ? rows : d->rows_held;
-    const DistillSpace space = space_of(d, held);
+// Only calls in pieces use the lists' room.  Others hold it up to this size all the same, for a call that follows; a forward call over 2^20 rows with lists of 256
+// would hold 2 GB.
+constexpr size_t kListsAnyway = 64 << 20;
+// Clears what it has just allocated, nothing else: the counters of a workspace in use are 0 between calls, and numbers of rows and lists that need the same bytes
+// have the same layout, since no section shrinks as they grow.
+static int ensure_distill(Distill* d, long rows, bool pieces, cudaStream_t s) {
+    const long held = rows > d->rows_held ? rows : d->rows_held, want = pieces || sizeof(Listed) * rows * d->count <= kListsAnyway ? rows : 0;
+    const long lists = want > d->lists_held ? want : d->lists_held;
+    const DistillSpace space = space_of(d, held, lists);
     const bool fresh = d->ws.bytes < space.bytes;
     const int rc = ensure_scratch(d->ws, space.bytes, s, "circ_distill_reserve");
     if (rc != CIRC_OK) {
-        if (!d->ws.ptr) d->rows_held = 0;
+        if (!d->ws.ptr) d->rows_held = d->lists_held = 0;
         return rc;
     }
     d->rows_held = held;
+    d->lists_held = lists;
     if (!fresh) return CIRC_OK;
     if (cudaMemsetAsync(d->ws.ptr, 0, space.sums, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
         cudaFree(d->ws.ptr);      // this one alone: graphs may hold earlier ones
         d->ws.ptr = nullptr;
         d->ws.bytes = 0;
-        d->rows_held = 0;
+        d->rows_held = d->lists_held = 0;
         set_error(CIRC_ERR_CUDA, "clearing the workspace failed: %s", cudaGetErrorString(cudaGetLastError()));
         return CIRC_ERR_CUDA;
     }
@@ -674,7 +692,7 @@ static int ensure_distill(Distill* d, long rows, cudaStream_t s) {
 
 // The kernel for a call, by the rows' length, their number and the alignment.
 template <typename T, typename V, typename ID>
-static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, T* grad, DistillArgs a, cudaStream_t s, int* launches) {
+static cudaError_t dispatch_distill(Walk walk, const T* z, const V* values, const ID* ids, T* grad, DistillArgs a, cudaStream_t s, int* launches) {
     constexpr int VEC = 16 / (int)sizeof(T);
     cudaError_t err = cudaSuccess;
     auto go = [&](auto kernel, long blocks, int threads, size_t smem, auto... args) {
@@ -702,17 +720,16 @@ static cudaError_t dispatch_distill(const T* z, const V* values, const ID* ids, 
         if (a.rows >= kMeanAlone) go(distill_mean_kernel, 1, 1024, 0);
         if (grad) go(distill_grad_kernel<T, ID, N>, blocks, kPieceThreads, 0, z, ids, grad);
     };
-    if (misaligned(z, 16) || misaligned(grad, 16) || (grad && (a.ld - a.grad_ld) % VEC)) {
+    if (walk == Walk::elements) {
         in_pieces(std::integral_constant<int, 1>{});
+        return err;
+    }
+    if (walk == Walk::pieces) {
+        in_pieces(std::integral_constant<int, VEC>{});
         return err;
     }
     const int vectors = RowSpan<VEC, false>::most(a.side.classes);
     const size_t marks = ((size_t)vectors * VEC + 31) / 32 * 4, bytes = (size_t)vectors * 16;
-    const bool few = vectors > 256 && pieces_of(a.rows, a.side.classes, VEC, &a.per) > 1 && a.rows < kFewRows && bytes > kFewBytes;
-    if (few || marks > 48 * 1024) {
-        in_pieces(std::integral_constant<int, VEC>{});
-        return err;
-    }
     a.pieces = 1;
     a.per = 0;
     auto with_grad = [&](auto gradient) {
@@ -771,9 +788,10 @@ static int run_distill(Distill* d, const void* z, long ld, const void* values, c
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    const int rc = ensure_distill(d, rows, s);
+    const Walk walk = walk_of(d, z, ld, grad, grad_ld, rows);
+    const int rc = ensure_distill(d, rows, walk != Walk::rows, s);
     if (rc != CIRC_OK) return rc;
-    const DistillSpace space = space_of(d, d->rows_held);
+    const DistillSpace space = space_of(d, d->rows_held, d->lists_held);
     char* ws = static_cast<char*>(d->ws.ptr);
     DistillArgs a{};
     a.side = ListSide{lse, 1.0 / (double)d->temperature, (float)(1.4426950408889634 / (double)d->temperature), d->classes, d->count, d->rest};
@@ -804,7 +822,7 @@ static int run_distill(Distill* d, const void* z, long ld, const void* values, c
                 using T = tag_type<decltype(t)>;
                 using V = tag_type<decltype(v)>;
                 using ID = tag_type<decltype(i)>;
-                err = dispatch_distill<T, V, ID>(static_cast<const T*>(z), static_cast<const V*>(values), static_cast<const ID*>(ids),
+                err = dispatch_distill<T, V, ID>(walk, static_cast<const T*>(z), static_cast<const V*>(values), static_cast<const ID*>(ids),
                                                  static_cast<T*>(grad), a, s, &launches);
             });
         });
@@ -827,7 +845,7 @@ circ_distill_handle circ_distill_create(int classes, int count) {
     }
     int device;
     if (!current_device(&device)) return nullptr;
-    Distill* d = new (std::nothrow) Distill{device, classes, count, CIRC_F32, CIRC_F32, CIRC_I64, 1.f, false, false, {}, 0};
+    Distill* d = new (std::nothrow) Distill{device, classes, count, CIRC_F32, CIRC_F32, CIRC_I64, 1.f, false, false, {}, 0, 0};
     if (!d) set_error(CIRC_ERR_ALLOC, "host allocation failed");
     return reinterpret_cast<circ_distill_handle>(d);
 }
@@ -887,7 +905,7 @@ int circ_distill_reserve(circ_distill_handle h, long max_rows) {
         set_error(CIRC_ERR_ARG, "bad handle or max_rows %ld", max_rows);
         return CIRC_ERR_ARG;
     }
-    return ensure_distill(d, max_rows, 0);
+    return ensure_distill(d, max_rows, true, 0);
 }
 
 int circ_distill_forward(circ_distill_handle h, const void* logits, long stride, const void* values, const void* ids, const float* lse,

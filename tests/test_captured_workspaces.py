@@ -1,5 +1,5 @@
-"""Workspaces of the distillation and group norm handles under stream capture: a captured call whose workspace is already as large as it needs is served, one that
-needs more is refused, and either way the capture and the graphs captured before stay whole."""
+"""Workspaces of the operators that train a compressed network: no call holds what it does not use; under stream capture a call whose workspace is already
+as large as it needs is served, one that needs more is refused, and either way the capture and the graphs captured before stay whole."""
 import pytest
 import torch
 
@@ -100,3 +100,41 @@ def test_captured_group_norm_of_more_images():
         assert float((y.double().cpu() - want).abs().max()) <= 5e-5
     del graphs
     circ.circ_gnorm_destroy(h)
+
+
+@pytest.mark.gpu
+def test_a_distillation_of_many_rows_holds_no_lists_that_it_does_not_use():
+    rows, classes, count, some = 1 << 19, 264, 256, 1000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    z = torch.randn(rows, classes, device="cuda", generator=g)
+    values = torch.randn(rows, count, device="cuda", generator=g)
+    ids = torch.arange(count, device="cuda").flip(0).expand(rows, count).contiguous()
+    row_loss, mean = torch.empty(rows, device="cuda"), torch.empty(1, device="cuda")
+    h = circ.circ_distill_create(classes, count)
+
+    def forward():
+        circ.circ_distill_forward(h, z, classes, values, ids, None, None, row_loss, None, mean, rows, torch.cuda.current_stream())
+
+    def backward(offset):        # of the first rows; behind a 16-byte boundary it is done in pieces, which use the lists
+        zz = torch.empty(some * classes + offset, device="cuda")[offset:].view(some, classes)
+        zz.copy_(z[:some])
+        grad = torch.empty_like(z[:some])
+        circ.circ_distill_backward(h, zz, classes, values, ids, None, None, None, None, mean, grad, classes, float(some), some, torch.cuda.current_stream())
+        return grad
+
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    forward()
+    torch.cuda.synchronize()
+    assert free - torch.cuda.mem_get_info()[0] < 256 << 20          # the lists of all rows: 1 GB
+    first = row_loss.clone()
+    in_rows, in_pieces = backward(0), backward(1)
+    forward()
+    torch.cuda.synchronize()
+    circ.circ_distill_destroy(h)
+    assert torch.equal(row_loss, first)
+    p, q = torch.softmax(values[:some].double(), 1), torch.softmax(z[:some].double(), 1)
+    want = q.scatter_add(1, ids[:some], -p)
+    for grad in (in_rows, in_pieces):      # probabilities with (2 + 3 * 12 + 264 / 32 + 16) u each, a few roundings
+        assert float((grad.double() - want).abs().max()) <= 1e-5
