@@ -760,6 +760,10 @@ constexpr int kTopPieces = 64;                 // a row, at most
 // Rows below this many, and longer than kTopFewBytes, are cut into pieces (24 x 131072 float32, top 64: 22 us in pieces, 16 by blocks).
 constexpr int kTopFew = 48;
 constexpr size_t kTopFewBytes = 1024 * 1024;
+static bool may_cut(int classes, long rows, int element) {
+    const int vec = 16 / element;
+    return rows < kTopFew && (size_t)(classes + 2 * vec - 2) / vec * 16 > kTopFewBytes;
+}
 
 // The kernel for a call, by the rows' length, their number and the alignment.
 template <typename T, typename ID>
@@ -804,7 +808,7 @@ static cudaError_t dispatch_top(const T* z, TopArgs a, cudaStream_t s) {
         // few rows: as many pieces as fill the machine twice over, as keep four vectors a thread and three for each score, and as the joining block holds
         const int most = std::min({kTopPieces, kMergeEach * 512 / a.count, vectors / std::max(1024, 3 * a.count + 2)});
         const int pieces = std::min(most, (2 * 148 + a.rows - 1) / a.rows);
-        if (a.rows < kTopFew && (size_t)vectors * 16 > kTopFewBytes && pieces > 1) {
+        if (may_cut(a.classes, a.rows, (int)sizeof(T)) && pieces > 1) {
             a.per = (vectors + pieces - 1) / pieces;
             a.pieces = (vectors + a.per - 1) / a.per;
             if (vectors - (a.pieces - 1) * a.per >= 3 * a.count + 2) {      // the last piece is the shortest
@@ -857,7 +861,8 @@ static int run_top(Top* t, const void* z, long ld, void* values, void* ids, floa
         set_error(CIRC_ERR_ARG, "every pointer must be aligned to its element size");
         return CIRC_ERR_ARG;
     }
-    const int rc = ensure_top(t, s);
+    const bool cut = may_cut(t->classes, rows, (int)zb);      // else no workspace is used
+    const int rc = cut ? ensure_top(t, s) : CIRC_OK;
     if (rc != CIRC_OK) return rc;
     char* ws = static_cast<char*>(t->ws.ptr);
     TopArgs a{};
@@ -870,10 +875,12 @@ static int run_top(Top* t, const void* z, long ld, void* values, void* ids, floa
     a.rows = (int)rows;
     a.classes = t->classes;
     a.count = t->count;
-    a.arrived = reinterpret_cast<unsigned*>(ws);
-    a.overflow = reinterpret_cast<int*>(ws + 1024);
-    a.keys = reinterpret_cast<uint64_t*>(ws + 2048);
-    a.parts = reinterpret_cast<Softmax*>(a.keys + (size_t)kTopFew * kTopPieces * t->count);
+    if (cut) {
+        a.arrived = reinterpret_cast<unsigned*>(ws);
+        a.overflow = reinterpret_cast<int*>(ws + 1024);
+        a.keys = reinterpret_cast<uint64_t*>(ws + 2048);
+        a.parts = reinterpret_cast<Softmax*>(a.keys + (size_t)kTopFew * kTopPieces * t->count);
+    }
     cudaError_t err = cudaSuccess;
     with_dtype(t->dtype, [&](auto* e) {
         with_index_type(t->ids_type, [&](auto* i) {
@@ -939,7 +946,7 @@ int circ_top_reserve(circ_top_handle h, long max_rows) {
         set_error(CIRC_ERR_ARG, "bad handle or max_rows %ld", max_rows);
         return CIRC_ERR_ARG;
     }
-    return ensure_top(t, 0);
+    return max_rows > 0 && may_cut(t->classes, 1, 4) ? ensure_top(t, 0) : CIRC_OK;      // (whatever type the logits get)
 }
 
 int circ_top_forward(circ_top_handle h, const void* logits, long stride, void* values, void* ids, float* lse, long rows, void* stream) {

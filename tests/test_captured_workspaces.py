@@ -138,3 +138,39 @@ def test_a_distillation_of_many_rows_holds_no_lists_that_it_does_not_use():
     want = q.scatter_add(1, ids[:some], -p)
     for grad in (in_rows, in_pieces):      # probabilities with (2 + 3 * 12 + 264 / 32 + 16) u each, a few roundings
         assert float((grad.double() - want).abs().max()) <= 1e-5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(200, 1000), (60, 300000), (3, 200000)])
+def test_top_logits_that_use_no_workspace_allocate_none(rows, classes):
+    z = torch.randn(rows, classes, generator=rng(rows)).cuda()
+    ids = torch.empty(rows, 7, dtype=torch.int64, device="cuda")
+    h = circ.circ_top_create(classes, 7)
+    circ.circ_debug_fail_alloc_after(1)
+    try:
+        circ.circ_top_forward(h, z, classes, None, ids, None, rows, torch.cuda.current_stream())
+    finally:
+        circ.circ_debug_fail_alloc_after(0)
+    torch.cuda.synchronize()
+    assert torch.equal(ids, torch.sort(z, dim=1, descending=True, stable=True).indices[:, :7])
+    circ.circ_top_destroy(h)
+
+
+@pytest.mark.gpu
+def test_top_logits_in_pieces_reserved_for_either_type():
+    rows, classes, count = 2, 280001, 9
+    z = torch.randn(rows, classes, generator=rng(3)).cuda()
+    h = circ.circ_top_create(classes, count)
+    circ.circ_top_set_dtypes(h, circ.CIRC_BF16, circ.CIRC_I64)
+    circ.circ_top_reserve(h, rows)
+    circ.circ_top_set_dtypes(h, circ.CIRC_F32, circ.CIRC_I64)
+    values, ids = torch.zeros(rows, count, device="cuda"), torch.zeros(rows, count, dtype=torch.int64, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        circ.circ_top_forward(h, z, classes, values, ids, None, rows, torch.cuda.current_stream())
+    graph.replay()
+    torch.cuda.synchronize()
+    want = torch.sort(z, dim=1, descending=True, stable=True)
+    assert torch.equal(values, want.values[:, :count]) and torch.equal(ids, want.indices[:, :count])
+    del graph
+    circ.circ_top_destroy(h)
