@@ -81,6 +81,8 @@ struct Moments {
         return Moments{a.mean + d * part, a.m2 + b.m2 + d * d * (n0 * part)};
     }
 };
+// The sum of squares around the mean, in float32; squares beyond its range stay +inf.
+__device__ __forceinline__ float around_mean(float s1, float s2, float inv) { return s2 == INFINITY ? s2 : s2 - s1 * s1 * inv; }
 // A float64 value in the place of two float32 ones.
 __device__ __forceinline__ float2 as_float2(double v) { return make_float2(__int_as_float(__double2loint(v)), __int_as_float(__double2hiint(v))); }
 __device__ __forceinline__ double as_double(float2 v) { return __hiloint2double(__float_as_int(v.y), __float_as_int(v.x)); }
@@ -295,18 +297,17 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_stats_kernel(const T*
             sums[threadIdx.x] = make_float2((float)totals[threadIdx.x].mean, (float)totals[threadIdx.x].m2);
         } else {
             const float inv = n ? 1.f / (float)n : 0.f;
-            sums[threadIdx.x] = make_float2(fmaf(s1, inv, pivot - first), s2 - s1 * s1 * inv);
+            sums[threadIdx.x] = make_float2(fmaf(s1, inv, pivot - first), around_mean(s1, s2, inv));
         }
     }
     __syncthreads();
     const int c = at.tile * a.columns + threadIdx.x;
     if ((int)threadIdx.x < a.columns && c < a.channels) {
-        float count = 0.f, mean = 0.f, m2 = 0.f;
-        for (int l = 0; l < at.lanes; ++l) {
-            const int mine = (at.to - at.from - l + at.lanes - 1) / at.lanes;
-            if (mine <= 0) break;
+        auto pixels = [&](int l) { return (at.to - at.from - l + at.lanes - 1) / at.lanes; };
+        float count = (float)pixels(0), mean = sums[threadIdx.x].x, m2 = sums[threadIdx.x].y;
+        for (int l = 1; l < at.lanes && pixels(l) > 0; ++l) {
             const float2 v = sums[l * a.columns + threadIdx.x];
-            const float all = count + (float)mine, d = v.x - mean, part = (float)mine / all;
+            const float mine = (float)pixels(l), all = count + mine, d = v.x - mean, part = mine / all;
             mean = fmaf(d, part, mean);
             m2 += v.y + d * d * count * part;
             count = all;
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
                 const Moments m = joined_run(before, inv_run, part, f, p, sum, square, e);
                 both = make_float2((float)m.mean, (float)m.m2);
             } else {
-                both = make_float2(fmaf(sum, inv, p - f), square - sum * sum * inv);
+                both = make_float2(fmaf(sum, inv, p - f), around_mean(sum, square, inv));
             }
             sums[e * kGnormThreads + threadIdx.x] = both;
             if (st.lane == 0) firsts[st.column * VEC + e] = f;
