@@ -412,7 +412,8 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* 
 // was read last is still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
 // 32 x 112 x 112 x 256 bfloat16 with SiLU take 119 us: the sums read 206 MB at 4.7 TB/s (44 us), the output reads and writes 411 at 5.5, with the XU pipe
 // 70 % busy (two of its instructions an element).  The gradients of 64 x 56 x 56 x 256 take 111 us, 4 XU instructions an element.  Small calls are two
-// launches (11 us), or one where a block has a whole image.
+// launches (10 us with the call), or one where a block has a whole image.  (Rounds of one pixel a thread for few images, so that more blocks share them, were slower in 86 of 176
+// sizes, up to 65 %, and faster in 7, up to 9 %.)
 // (One launch, whose blocks took sums and outputs from a counter and waited for an image's sums, read every image once, but an image's counting, waiting
 // and joining by small tasks cost more than the second reading: 145 us for 32 x 112 x 112 x 256 bfloat16.)
 // A piece takes every pieces-th round of `per` pixels (R of each thread): the blocks that run at once read neighbouring memory.
@@ -911,7 +912,6 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
 constexpr double kEndRounds = 3.0;
 constexpr int kWholeRounds = 4;             // rounds that a block takes for a whole image where the images do not fill the machine four times over
-constexpr int kFewPieces = 222;             // rounds below which they are made shorter
 
 // How a call is run.
 struct GnormPlan {
@@ -936,11 +936,10 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         p.tiles = 1;
         const int lanes = kGnormThreads / p.columns;
         p.r = backward || (p.vec == 8 && xb == 4) ? 4 : 8;
-        // a round of loads a piece at least, and no more pieces than fill the machine twice over; with few of them, shorter rounds
-        auto rounds = [&](int r) { return (pixels + lanes * r - 1) / (lanes * r); };
-        p.whole = rounds(p.r) <= kWholeRounds || images >= 148 * 12;
-        if (!p.whole && (long)images * rounds(p.r) < kFewPieces) p.r = 1;
+        // a round of loads a piece at least, and no more pieces than fill the machine twice over
         p.per = lanes * p.r;
+        const int rounds = (pixels + p.per - 1) / p.per;
+        p.whole = rounds <= kWholeRounds || images >= 148 * 12;
         if (p.whole) {
             p.pieces = 1;
             p.runs = pixels / p.per * p.r > kRun;
@@ -948,11 +947,11 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         }
         // As many pieces an image as take the least time: blocks that run at once (three an SM) take the pieces in turns, and a block's beginning and end
         // take as long as some rounds.
-        const long slots = 148 * 3, most = std::min((long)rounds(p.r), (kGnormTarget + images) / (long)images);
+        const long slots = 148 * 3, most = std::min((long)rounds, (kGnormTarget + images) / (long)images);
         double best = 0.0;
         p.pieces = 1;
         for (long k = 1; k <= most; ++k) {
-            const double cost = (double)((images * k + slots - 1) / slots) * ((double)((rounds(p.r) + k - 1) / k) + kEndRounds);
+            const double cost = (double)((images * k + slots - 1) / slots) * ((double)((rounds + k - 1) / k) + kEndRounds);
             if (k == 1 || cost < best) {
                 best = cost;
                 p.pieces = (int)k;
@@ -1019,8 +1018,7 @@ template <typename T, bool BACKWARD, typename F>
 static void with_plan(const GnormPlan& p, F&& f) {
     auto with_r = [&](auto vec) {
         constexpr int VEC = decltype(vec)::value, R = BACKWARD || (VEC == 8 && sizeof(T) == 4) ? 4 : 8;
-        if (p.r == 1) f(vec, std::integral_constant<int, 1>{});
-        else f(vec, std::integral_constant<int, R>{});
+        f(vec, std::integral_constant<int, R>{});
     };
     if constexpr (!BACKWARD)
         if (p.vec == 8) {
@@ -1054,15 +1052,12 @@ static cudaError_t run_forward(const GnormPlan& p, const GnormArgs& a, const T* 
     with_plan<T, false>(p, [&](auto vec, auto r) {
         constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
         const dim3 grid((unsigned)((long)a.images * a.pieces));
-        auto stats = gnorm_stats_kernel<T, U, VEC, R, false, false>;
-        if constexpr (R > 1) {      // (rounds of one pixel a thread: a few of them)
-            if (p.whole) {
-                err = launch_row(p.runs ? gnorm_stats_kernel<T, U, VEC, R, true, true> : gnorm_stats_kernel<T, U, VEC, R, true, false>, grid,
-                                 dim3(kGnormThreads), 0, s, x, y, a);
-                return;
-            }
-            if (p.runs) stats = gnorm_stats_kernel<T, U, VEC, R, false, true>;
+        if (p.whole) {
+            err = launch_row(p.runs ? gnorm_stats_kernel<T, U, VEC, R, true, true> : gnorm_stats_kernel<T, U, VEC, R, true, false>, grid, dim3(kGnormThreads), 0,
+                             s, x, y, a);
+            return;
         }
+        const auto stats = p.runs ? gnorm_stats_kernel<T, U, VEC, R, false, true> : gnorm_stats_kernel<T, U, VEC, R, false, false>;
         if ((err = launch_row(stats, grid, dim3(kGnormThreads), 0, s, x, y, a)) == cudaSuccess)
             err = launch_row(gnorm_apply_kernel<T, U, VEC, R>, grid, dim3(kGnormThreads), 0, s, x, y, a);
     });
@@ -1085,15 +1080,12 @@ static cudaError_t run_backward(const GnormPlan& p, const GnormArgs& a, const T*
     } else {
         with_plan<T, true>(p, [&](auto vec, auto r) {
             constexpr int VEC = decltype(vec)::value, R = decltype(r)::value;
-            auto sums = gnorm_sums_kernel<T, U, VEC, R, false, false>;
-            if constexpr (R > 1) {
-                if (p.whole) {
-                    err = launch_row(p.runs ? gnorm_sums_kernel<T, U, VEC, R, true, true> : gnorm_sums_kernel<T, U, VEC, R, true, false>, grid, threads, 0, s, x,
-                                     grad_y, grad_x, a);
-                    return;
-                }
-                if (p.runs) sums = gnorm_sums_kernel<T, U, VEC, R, false, true>;
+            if (p.whole) {
+                err = launch_row(p.runs ? gnorm_sums_kernel<T, U, VEC, R, true, true> : gnorm_sums_kernel<T, U, VEC, R, true, false>, grid, threads, 0, s, x, grad_y,
+                                 grad_x, a);
+                return;
             }
+            const auto sums = p.runs ? gnorm_sums_kernel<T, U, VEC, R, false, true> : gnorm_sums_kernel<T, U, VEC, R, false, false>;
             if ((err = launch_row(sums, grid, threads, 0, s, x, grad_y, grad_x, a)) == cudaSuccess && grad_x) {
                 err = launch_row(gnorm_grad_kernel<T, U, VEC, R>, dim3(grid.x + totals), threads, 0, s, x, grad_y, grad_x, grad_gain, grad_bias, totals, a);
                 done = true;
