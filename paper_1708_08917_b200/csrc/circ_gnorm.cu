@@ -911,7 +911,14 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
 constexpr double kEndRounds = 3.0;
-constexpr int kWholeRounds = 4;             // rounds that a block takes for a whole image where the images do not fill the machine four times over
+// Rounds up to which a block takes a whole image, in one launch.  Forward, 256 channels bfloat16, in pieces and whole: 64 images of 1 round 8.2 and 6.5 us, of 4
+// rounds 13.6 and 10.4, of 6 rounds 13.8 and 12.7; 4 images of 3 rounds 9.6 and 9.0, of 4 rounds 9.6 and 10.0, of 6 rounds 9.6 and 12.3.  Backward, where a block's
+// second reading takes longer: 4 images of 2 rounds 8.2 and 8.4, of 4 rounds 8.5 and 11.2; 16 of 2 rounds 8.4 and 8.4, of 4 rounds 8.7 and 11.5; 64 of 4 rounds 11.0 and 11.7
+// (SiLU 10.6 and 9.8); 148 of 2 rounds 11.0 and 10.0, of 4 rounds 13.6 and 13.2; 300 of 4 rounds 19.1 and 18.4.
+constexpr int kWholeRounds = 4, kWholeRoundsFew = 2, kFewImages = 32;
+// Images from which on a block takes a whole one of any size: what it has read last is still near.  In pieces and whole, bfloat16: forward 1776 of 28 x 28 x 64 113 and 88 us (900
+// of them 65 and 55: fewer would gain as well), backward 1800 of them without an activation 173 and 168, 1776 with ReLU 193 and 199.
+constexpr int kManyImages = 148 * 12;
 
 // How a call is run.
 struct GnormPlan {
@@ -939,7 +946,7 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         // a round of loads a piece at least, and no more pieces than fill the machine twice over
         p.per = lanes * p.r;
         const int rounds = (pixels + p.per - 1) / p.per;
-        p.whole = rounds <= kWholeRounds || images >= 148 * 12;
+        p.whole = rounds <= (backward && images < kFewImages ? kWholeRoundsFew : kWholeRounds) || images >= kManyImages;
         if (p.whole) {
             p.pieces = 1;
             p.runs = pixels / p.per * p.r > kRun;
