@@ -463,13 +463,13 @@ CIRC_API void circ_clip_destroy(circ_clip_handle h);
 
 /*
  * circ_top_* -- the `count` largest of `classes` scores a row.
- *   circ_top_create          : 1 <= count <= 256, count <= classes.  Defaults: float32 logits, 64-bit ids, temperature 1.
+ *   circ_top_create          : 1 <= count <= 256, count <= classes <= 2^28.  Defaults: float32 logits, 64-bit ids, temperature 1.
  *   circ_top_set_dtypes      : logits_dtype: logits and values (CIRC_F32 or CIRC_BF16); ids_type: CIRC_I32 or CIRC_I64.
- *   circ_top_set_temperature : > 0; of lse alone.
- *   circ_top_forward         : logits [rows] of `stride` elements (>= classes).  Any of the three results may be NULL:
+ *   circ_top_set_temperature : 1e-6 to 1e6; of lse alone.
+ *   circ_top_forward         : logits [rows] of `stride` elements (>= classes), at most 2^24 rows.  Any of the three results may be NULL:
  *       values : [rows][count], descending        ids : [rows][count], their classes; equal scores: the lower class first
  *       lse    : float32 [rows], log sum exp(logits / temperature) over all classes: +inf with a logit of +inf, NaN with a NaN
- *   circ_top_reserve         : workspace for calls of up to max_rows rows.
+ *   circ_top_reserve         : workspace for calls of up to max_rows rows (only a few long rows, which are cut into pieces, use any).
  * A NaN counts as larger than anything else.  Classes masked with -inf come last, in their order.  Equal zeros of either sign are +0 in
  * values.
  */
@@ -484,15 +484,16 @@ CIRC_API void circ_top_destroy(circ_top_handle h);
 /*
  * circ_distill_* -- divergence of a network's probabilities q = softmax(logits / temperature) over `classes` classes from a teacher's p, of
  * which a list of `count` classes a row is given (as circ_top_forward writes it), and its gradient.
- *   circ_distill_create          : 1 <= count <= 256.  Defaults: float32 logits and values, 64-bit ids, temperature 1, no rest, no addition.
+ *   circ_distill_create          : 1 <= count <= 256, classes <= 2^28.  Defaults: float32 logits and values, 64-bit ids, temperature 1, no
+ *                                  rest, no addition.
  *   circ_distill_set_dtypes      : logits_dtype: logits and their gradient; values_dtype: the teacher's; CIRC_F32 or CIRC_BF16 each.
- *   circ_distill_set_temperature : > 0.
+ *   circ_distill_set_temperature : 1e-6 to 1e6.
  *   circ_distill_set_rest        : 0: p is the softmax of values / temperature over the list, 0 elsewhere.
  *                                  1: p = exp(values / temperature - lse) on the list; all other classes together are one class more, whose
  *                                  probability is max(0, 1 - sum p).  Its term is left out where the network gives them no probability
  *                                  (their logits are -inf, or there are none).
  *   circ_distill_set_add         : 1: the gradient is added to what grad_logits holds.
- *   circ_distill_forward         : logits [rows] of `stride` elements (>= classes); values, ids [rows][count].
+ *   circ_distill_forward         : logits [rows] of `stride` elements (>= classes), at most 2^24 rows; values, ids [rows][count].
  *       lse      : the teacher's, float32 [rows] (with the rest; NULL without).
  *       weights  : float32 [rows], NULL: ones.  A row whose weight is not above 0 is not read: its results are 0.
  *       row_loss : float32 [rows], sum p (log p - log q)                   (any of the three results may be NULL)
@@ -500,10 +501,13 @@ CIRC_API void circ_top_destroy(circ_top_handle h);
  *       mean     : float32 [1], sum of weights row_loss / sum of weights (0 if no weight is above 0)
  *   circ_distill_backward        : the same, and grad_logits [rows] of `grad_stride` elements = the gradient of grad_mean * mean; what lies
  *       between classes and grad_stride is left alone.  grad_logits may be logits (with the same stride, without addition).
- *   circ_distill_reserve         : workspace for calls of up to max_rows rows.
- * An id outside [0, classes) stands for no entry, and so does one that the row's list has already had.  A row without an entry, or whose
- * values (or lse) are all -inf, has no teacher: its loss and gradient are 0.  A class masked with -inf has probability 0; where the teacher's
- * is not, the loss is +inf.  A row whose logits are all -inf has student_lse -inf, loss +inf and a zero gradient.
+ *   circ_distill_reserve         : workspace for calls of up to max_rows rows, 8 bytes for each of their lists' entries among it: calls whose
+ *       logits or gradients are not on 16-byte boundaries, or whose rows are few and long, use them (others hold them up to 64 MB).
+ * An id outside [0, classes) stands for no entry, and so does one that the row's list has already had.  A row without an entry, whose values
+ * are all -inf (without the rest) or whose lse is -inf (with it), has no teacher: its loss and gradient are 0.  With the rest, values of -inf
+ * have probability 0 like any others that are small beside lse.  A class masked with -inf has probability 0; where the teacher's
+ * is not, the loss is +inf.  A row whose logits are all -inf has student_lse -inf, loss +inf and a zero gradient.  A logit of NaN or +inf
+ * leaves no probabilities: student_lse, and the loss and gradient of a row that has a teacher, are NaN.
  */
 typedef struct circ_distill* circ_distill_handle;
 CIRC_API circ_distill_handle circ_distill_create(int classes, int count);
@@ -525,16 +529,20 @@ enum { CIRC_ACT_NONE = 0, CIRC_ACT_RELU = 1, CIRC_ACT_SILU = 2 };
 /*
  * circ_gnorm_* -- group norm with an activation on the channel-last layout of circ_conv_forward's output: over the pixels of an image and
  * the channels of a group, y = act(gain (x - mean) rstd + bias), rstd = 1 / sqrt(variance + eps), variance = mean((x - mean)^2).
- *   circ_gnorm_create         : `channels` in `groups` groups of neighbouring channels (must divide), eps >= 0.  Defaults: float32 x and y,
- *                               no activation.
+ *   circ_gnorm_create         : `channels` (at most 2^16) in `groups` groups of neighbouring channels (must divide), eps >= 0.
+ *                               Defaults: float32 x and y, no activation.
  *   circ_gnorm_set_dtypes     : x_dtype: x and grad_x; y_dtype: y and grad_y; CIRC_F32 or CIRC_BF16.
  *   circ_gnorm_set_activation : CIRC_ACT_*.
- *   circ_gnorm_forward        : x, y [N][H][W][channels]; y may be x where the types are the same.  gain, bias: float32 [channels], NULL:
- *       ones, zeros.  mean, rstd: float32 [N][groups], for the backward pass; NULL to skip.
+ *   circ_gnorm_forward        : x, y [N][H][W][channels], N at most 2^20, H W at most 2^28; y may be x where the types are the same.
+ *       gain, bias: float32 [channels], NULL: ones, zeros.  mean, rstd: float32 [N][groups], for the backward pass; NULL to skip.
  *   circ_gnorm_backward       : gradients from grad_y = dL/dy.  grad_x: may be grad_y or x where the types are the same, NULL to skip.
  *       grad_gain, grad_bias: float32 [channels], overwritten, NULL to skip.  mean, rstd: of the forward pass.  The slope of max(0, v)
  *       is 1 for v > 0 and 0 elsewhere; the side is found in float64.
  *   circ_gnorm_reserve        : workspace for calls of up to N images of H x W pixels.
+ * Sums are float32 over runs of at most 264 values a thread, at most 256 threads' sums and a group's channels, and float64 over runs and
+ * blocks: what rounding costs does not grow with an image.  Deviations between 1e-15 and 1e15 keep their digits when they are squared; beyond
+ * float32's range rstd is 0.  A variance of 0 with eps 0 gives rstd +inf and v NaN, as the formula does.  SiLU: relative error below
+ * (8 + 2 |v|) 2^-24 of the value.
  */
 typedef struct circ_gnorm* circ_gnorm_handle;
 CIRC_API circ_gnorm_handle circ_gnorm_create(int channels, int groups, float eps);

@@ -215,7 +215,7 @@ __device__ __forceinline__ void slopes(const RawVec<T, VEC>& raw, const Exponent
 }
 
 // ---- rows, or pieces of them, a block each ----
-// Bound by memory for long rows: 4096 x 50001 bfloat16 without a gradient 86 us (one in ten rows without weight; 5.2 TB/s of what is read), by the list's
+// Bound by memory for long rows: 4096 x 50001 bfloat16 without a gradient 86 us (one in ten rows without weight; 4.3 TB/s of what is read), by the list's
 // chain of dependent steps (6 us) for those of a few thousand classes.  With a gradient 8192 x 50001 bfloat16 take 363 us (4.3 TB/s): two exponentials an
 // element keep the XU pipe half busy, and blocks wait at the barriers between their phases; rows held in shared memory (as the cross entropy's are) take
 // the same time.
@@ -614,8 +614,9 @@ __global__ void __launch_bounds__(kPieceThreads) distill_grad_kernel(const T* z,
 }
 
 constexpr long kPieceTarget = 148 * 8;      // blocks that fill the machine
-// Fewer rows, each longer, are cut into pieces: with so few a block's own time for a row is longer than that of pieces and their joining (float32 with
-// gradient: 9 rows of 147566, 22 us in pieces and 29 by blocks; 24 of 131072, 28 and 24; 126 of 107244 bfloat16, 70 and 24).
+// Fewer rows, each longer, are cut into pieces: with so few a block's own time for a row is longer than that of pieces and their joining.  Blocks and pieces, us: 140000
+// classes float32 without gradient, 1 row 14.8 and 11.4, 12 rows 15.4 and 11.4, 24 rows 15.7 and 13.5; with gradient 24.5 and 15.7, 24.4 and 19.4, 25.2 and 24.8; bfloat16 with
+// gradient 18.1 and 16.5, 18.0 and 18.8, 18.1 and 21.6.  8 rows of 50000 float32 (200 KB): 10.6 and 10.9, with gradient 13.0 and 15.9; of 80000: 12.0 and 11.0, 15.8 and 16.3.
 constexpr int kFewRows = 16;
 constexpr size_t kFewBytes = 256 * 1024;
 constexpr size_t kMarksMost = 48 * 1024 * 8;      // classes a row whose marks a block holds

@@ -6,7 +6,8 @@
 //   loss = sum p_k (log p_k - s_k / tau + lse) + p_rest (log p_rest - a + lse)
 //   gradient, times tau: P q_k - p_k on the list, exp(s / tau - a) (P q_rest - p_rest) outside, with P = sum p_k + p_rest.
 // The sum over the outside is taken without the listed classes, not as a difference: q_rest keeps its digits where the list holds nearly all.
-// The teacher's side is float64: what the list leaves over, and the loss of a student that has learnt it, are small differences.
+// The teacher's side is float64: what the list leaves over, and the loss of a student that has learnt it, are small differences.  The student's exponentials
+// and their sums are float32 (a few 2^-24 of its probabilities, no more than a float32 logit's rounding makes of them); logarithms and the loss are float64 again.
 #pragma once
 #include "circ_softmax.cuh"
 
