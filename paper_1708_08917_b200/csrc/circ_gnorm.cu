@@ -26,13 +26,13 @@ struct GnormArgs {
     int channels, groups, depth;      // depth: channels a group
     int images, pixels;
     float eps;
-    double inv_m;             // 1 / (pixels depth)
+    double inv_m, inv_depth;  // 1 / (pixels depth), 1 / depth
     // a block's part: `columns` vectors of channels (all, or a tile of them), and pixels of one image
     int columns, tiles, pieces, per;
     int act;
     // workspace
     unsigned* arrived;        // [N] parts of an image that are summed up (0 before and after a call)
-    float2* group_parts;      // [N][pieces][groups] the tasks' sums of the groups
+    double2* group_parts;     // [N][pieces][groups] the pieces' sums of the groups
     float2* parts;            // [N][pieces][C] forward: mean, less the channel's first value, and sum of squares around it; backward: sum of g, of g u
     float2* means;            // [N][groups] backward: A / m, B / m
 };
@@ -456,7 +456,7 @@ __device__ __forceinline__ void join_groups(const GnormArgs& a, int image, doubl
         const int g = g0 + threadIdx.x % wide;
         double2 s = make_double2(0.0, 0.0);
         if (r < rows && g < a.groups) {
-            const float2* p = a.group_parts + (size_t)image * a.pieces * a.groups + g;
+            const double2* p = a.group_parts + (size_t)image * a.pieces * a.groups + g;
 #pragma unroll 4
             for (int t = r; t < a.pieces; t += rows) {
                 const double2 v = term(t, __ldcg(p + (size_t)t * a.groups));
@@ -487,7 +487,8 @@ __device__ __forceinline__ void each_group(const GnormArgs& a, F f) {
         f(g, threadIdx.x & ((1 << shift) - 1), 1 << shift, g < a.groups);
     }
 }
-__device__ __forceinline__ float lanes_sum(float v, int wide) {
+template <typename T>
+__device__ __forceinline__ T lanes_sum(T v, int wide) {
     for (int o = wide / 2; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
@@ -616,8 +617,8 @@ __device__ __forceinline__ void apply_stretch(const T* x, U* y, const GnormArgs&
 }
 
 // A piece's sums: a thread's (see kRun; what came before a run waits in shared memory), those of the threads that share a channel, and those of a group's
-// channels, each around their joint mean.  Means are kept as differences from the image's first pixel, so that a large offset costs no digits (float32: a mean is off by at
-// most a few 2^-24 of that difference, 1e-7 of a deviation for ordinary values).
+// channels, each around their joint mean.  Means are kept as differences from the image's first pixel, so that a large offset costs no digits, and joined in float64, so
+// that a mean that is small beside that pixel keeps its own: each thread's is off by 2^-24 of the difference, and those errors average out.
 // WHOLE: a block has a whole image, and writes its output too.  LONG: some threads have more than kRun pixels (a kernel of its own: its registers cost the
 // others 2 to 9 %).
 template <typename T, typename U, int VEC, int R, bool WHOLE, bool LONG>
@@ -696,42 +697,47 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
             if (st.lane == 0) firsts[st.column * VEC + e] = f;
         }
     }
-    __syncthreads();
     const int here = st.size.pixels(a), least = st.size.full * R + st.size.rest / st.lanes, more = st.size.rest % st.lanes;      // pixels of lane l: least + (l < more)
-    const float inv_here = 1.f / (float)here;
+    const double inv_here = 1.0 / (double)here;
+    __syncthreads();
+    // A channel's mean goes to its first thread's place, which no other channel reads, in float64.
     each_channel<VEC>(a, [&](int c, int e, int column) {
-        const float2* v = sums + e * kGnormThreads + column;
-        float s = 0.f, q = 0.f;
+        float2* v = sums + e * kGnormThreads + column;
+        double s = 0.0;
         for (int l = 0; l < st.lanes; ++l)
-            if (least > 0 || l < more) s = fmaf((float)(least + (l < more)), v[l * a.columns].x, s);
-        const float mean = s * inv_here;
+            if (least > 0 || l < more) s += (double)(least + (l < more)) * (double)v[l * a.columns].x;
+        const double mean = s * inv_here;
+        const float near = (float)mean;
+        float q = 0.f;
         for (int l = 0; l < st.lanes; ++l)
             if (least > 0 || l < more) {
-                const float d = v[l * a.columns].x - mean;
+                const float d = v[l * a.columns].x - near;
                 q += fmaf(d * d, (float)(least + (l < more)), v[l * a.columns].y);
             }
-        joined[c] = make_float2(mean, q);
+        v[0] = as_float2(mean);
+        joined[c].y = q;
     });
     __syncthreads();
     each_group(a, [&](int g, int l, int wide, bool one) {
         const int c0 = g * a.depth, end = one ? a.depth : 0;
-        const float f = one ? firsts[c0] : 0.f;
-        float s = 0.f, q = 0.f;
-        for (int i = l; i < end; i += wide) s += joined[c0 + i].x + (firsts[c0 + i] - f);
-        const float mean = lanes_sum(s, wide) / (float)a.depth;
+        const double f = one ? (double)firsts[c0] : 0.0;
+        auto mean_of = [&](int c) { return as_double(sums[c % VEC * kGnormThreads + c / VEC]) + ((double)firsts[c] - f); };
+        double s = 0.0;
+        float q = 0.f;
+        for (int i = l; i < end; i += wide) s += mean_of(c0 + i);
+        const double mean = lanes_sum(s, wide) * a.inv_depth;
         for (int i = l; i < end; i += wide) {
-            const float2 v = joined[c0 + i];
-            const float d = v.x + (firsts[c0 + i] - f) - mean;
-            q += fmaf(d * d, (float)here, v.y);
+            const float d = (float)(mean_of(c0 + i) - mean);
+            q += fmaf(d * d, (float)here, joined[c0 + i].y);
         }
         q = lanes_sum(q, wide);
-        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_float2(mean, q);
+        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_double2(mean, (double)q);
     });
     if (!last_of_image(a, st.image)) return;
     join_groups(a, st.image, red,
-                [&](int t, float2 v) {
-                    const double k = (double)PieceSize(a, t).pixels(a) * a.depth, mean = (double)v.x;
-                    return make_double2(k * mean, (double)v.y + k * mean * mean);
+                [&](int t, double2 v) {
+                    const double k = (double)PieceSize(a, t).pixels(a) * a.depth, mean = v.x;
+                    return make_double2(k * mean, v.y + k * mean * mean);
                 },
                 [&](int g, double2 s) {
                     const double mean = s.x * a.inv_m, var = s.y * a.inv_m - mean * mean;
@@ -859,10 +865,10 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_sums_kernel(const T* x
         }
         s = lanes_sum(s, wide);
         q = lanes_sum(q, wide);
-        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_float2(s, q);
+        if (one && l == 0) a.group_parts[((size_t)st.image * a.pieces + st.piece) * a.groups + g] = make_double2((double)s, (double)q);
     });
     if (!last_of_image(a, st.image)) return;
-    join_groups(a, st.image, red, [&](int, float2 v) { return make_double2((double)v.x, (double)v.y); },
+    join_groups(a, st.image, red, [&](int, double2 v) { return v; },
                 [&](int g, double2 s) { a.means[(size_t)st.image * a.groups + g] = make_float2((float)(s.x * a.inv_m), (float)(s.y * a.inv_m)); });
     if constexpr (WHOLE) {
         if (!grad_x) return;
@@ -992,7 +998,7 @@ static GnormSpace space_of(const Gnorm* g, long images) {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     GnormSpace s;
     s.group_parts = up(sizeof(unsigned) * images);
-    s.parts = s.group_parts + up(sizeof(float2) * pieces * g->groups);
+    s.parts = s.group_parts + up(sizeof(double2) * pieces * g->groups);
     s.means = s.parts + up(sizeof(float2) * pieces * g->channels);
     s.stats = s.means + up(sizeof(float2) * images * g->groups);
     s.bytes = s.stats + up(2 * sizeof(float) * images * g->groups);
@@ -1125,13 +1131,14 @@ static GnormArgs args_of(const Gnorm* g, const GnormPlan& p, const float* gain, 
     a.pixels = pixels;
     a.eps = g->eps;
     a.inv_m = 1.0 / ((double)pixels * a.depth);
+    a.inv_depth = 1.0 / (double)a.depth;
     a.columns = p.columns;
     a.tiles = p.tiles;
     a.pieces = p.pieces;
     a.per = p.per;
     a.act = g->act;
     a.arrived = reinterpret_cast<unsigned*>(ws);
-    a.group_parts = reinterpret_cast<float2*>(ws + space.group_parts);
+    a.group_parts = reinterpret_cast<double2*>(ws + space.group_parts);
     a.parts = reinterpret_cast<float2*>(ws + space.parts);
     a.means = reinterpret_cast<float2*>(ws + space.means);
     return a;

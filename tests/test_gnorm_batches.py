@@ -78,3 +78,18 @@ def test_a_pixel_left_out_of_the_sums_would_show(n, h, w, c, groups):
     mean, less = g.mean((1, 3)), kept.sum((1, 3)) / (g[0, :, 0].numel())
     rstd, other = (1 / torch.sqrt((v * v).mean((1, 3)) + EPS) for v in (g, kept))
     assert bool((((mean - less).abs() > 40 * U * 6) | ((rstd - other).abs() > 40 * U * rstd)).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,h,w,c,groups,x_dtype", [(1, 68, 80, 3, 1, F32), (2, 68, 80, 24, 1, BF16), (3, 64, 68, 60, 2, F32), (5, 32, 32, 256, 1, BF16), (70, 16, 16, 64, 4, F32),
+                                                    (1800, 16, 16, 64, 1, BF16)])
+def test_means_that_are_small_beside_the_first_pixel(n, h, w, c, groups, x_dtype):
+    """Threads of 8 to 32 whole numbers: their means are exact, and what they are joined to, in float64, is rounded once (and once more where the first pixel is
+    added)."""
+    x = torch.randint(-3, 4, (n, h, w, c), generator=rng(n + c)).to(x_dtype)
+    x[:, 0, 0] = 200.0
+    x[:, -1, -1] = -200.0
+    mean = forward(x, None, None, groups, NONE, x_dtype)[1]
+    want = grouped(x, groups).mean((1, 3))
+    assert float(want.abs().max()) < 0.2                     # a thousandth of the first pixel
+    within(mean, want, 2 * U * want.abs() + 2.0 ** -45)
