@@ -698,22 +698,28 @@ __global__ void __launch_bounds__(kGnormThreads, 3) gnorm_stats_kernel(const T* 
         }
     }
     const int here = st.size.pixels(a), least = st.size.full * R + st.size.rest / st.lanes, more = st.size.rest % st.lanes;      // pixels of lane l: least + (l < more)
-    const double inv_here = 1.0 / (double)here;
+    const double inv_here = 1.0 / (double)here, some = (double)least;
+    const int lanes = least > 0 ? st.lanes : more;      // that have pixels
     __syncthreads();
     // A channel's mean goes to its first thread's place, which no other channel reads, in float64.
     each_channel<VEC>(a, [&](int c, int e, int column) {
         float2* v = sums + e * kGnormThreads + column;
-        double s = 0.0;
-        for (int l = 0; l < st.lanes; ++l)
-            if (least > 0 || l < more) s += (double)(least + (l < more)) * (double)v[l * a.columns].x;
-        const double mean = s * inv_here;
+        double part[4] = {};      // (chains that do not wait for one another, and loads that go together)
+        auto take = [&](int l, int u) { part[u] = fma(l < more ? some + 1.0 : some, (double)v[l * a.columns].x, part[u]); };
+        int l = 0;
+        for (; l + 4 <= lanes; l += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) take(l + u, u);
+        for (; l < lanes; ++l) take(l, 0);
+        const double mean = ((part[0] + part[1]) + (part[2] + part[3])) * inv_here;
         const float near = (float)mean;
         float q = 0.f;
-        for (int l = 0; l < st.lanes; ++l)
-            if (least > 0 || l < more) {
-                const float d = v[l * a.columns].x - near;
-                q += fmaf(d * d, (float)(least + (l < more)), v[l * a.columns].y);
-            }
+#pragma unroll 4
+        for (int l = 0; l < lanes; ++l) {
+            const float2 one = v[l * a.columns];
+            const float d = one.x - near;
+            q += fmaf(d * d, (float)(least + (l < more)), one.y);
+        }
         v[0] = as_float2(mean);
         joined[c].y = q;
     });
@@ -919,13 +925,13 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_total_kernel(float* grad_
 
 constexpr int kGnormTarget = 148 * 8;       // blocks that fill the machine
 constexpr double kEndRounds = 3.0;
-// Rounds up to which a block takes a whole image, in one launch.  Forward, 256 channels bfloat16, in pieces and whole: 64 images of 1 round 8.2 and 6.5 us, of 4
-// rounds 13.6 and 10.4, of 6 rounds 13.8 and 12.7; 4 images of 3 rounds 9.6 and 9.0, of 4 rounds 9.6 and 10.0, of 6 rounds 9.6 and 12.3.  Backward, where a block's
-// second reading takes longer: 4 images of 2 rounds 8.2 and 8.4, of 4 rounds 8.5 and 11.2; 16 of 2 rounds 8.4 and 8.4, of 4 rounds 8.7 and 11.5; 64 of 4 rounds 11.0 and 11.7
-// (SiLU 10.6 and 9.8); 148 of 2 rounds 11.0 and 10.0, of 4 rounds 13.6 and 13.2; 300 of 4 rounds 19.1 and 18.4.
+// Rounds up to which a block takes a whole image, in one launch.  Forward, 256 channels bfloat16, in pieces and whole: 64 images of 1 round 7.7 and 6.1 us, of 4
+// rounds 13.2 and 9.9, of 6 rounds 13.5 and 12.3; 4 images of 3 rounds 8.9 and 8.4, of 4 rounds 8.9 and 9.6, of 6 rounds 9.0 and 11.8.  Backward with ReLU: 148 images of 2
+// rounds 11.1 and 9.9, of 4 rounds 13.6 and 13.4; 64 of 4 rounds 11.1 and 11.7 (SiLU 10.7 and 9.9).  With few images a round's slopes and the second reading make the whole one
+// slow: 4 of 2 rounds 8.0 and 8.2, of 4 rounds 8.3 and 11.1 (SiLU 8.0 and 9.3; without an activation 7.5 and 7.7; single channels, 8 of 86 x 12 x 2 of 3 rounds, 8.0 and 7.2).
 constexpr int kWholeRounds = 4, kWholeRoundsFew = 2, kFewImages = 32;
-// Images from which on a block takes a whole one of any size: what it has read last is still near.  In pieces and whole, bfloat16: forward 1776 of 28 x 28 x 64 113 and 88 us (900
-// of them 65 and 55: fewer would gain as well), backward 1800 of them without an activation 173 and 168, 1776 with ReLU 193 and 199.
+// Images from which on a block takes a whole one of any size: what it has read last is still near.  In pieces and whole, bfloat16: forward 1776 of 28 x 28 x 64 102 and 78 us (900
+// of them 57 and 47: fewer would gain as well), backward 6000 of 14 x 14 x 256 without an activation 528 and 516, 1776 of 28 x 28 x 64 with ReLU 193 and 199.
 constexpr int kManyImages = 148 * 12;
 
 // How a call is run.
@@ -954,7 +960,8 @@ static GnormPlan plan_of(const Gnorm* g, int images, int pixels, bool backward, 
         // a round of loads a piece at least, and no more pieces than fill the machine twice over
         p.per = lanes * p.r;
         const int rounds = (pixels + p.per - 1) / p.per;
-        p.whole = rounds <= (backward && images < kFewImages ? kWholeRoundsFew : kWholeRounds) || images >= kManyImages;
+        const bool slow_rounds = backward && p.vec > 1 && g->act != CIRC_ACT_NONE;
+        p.whole = rounds <= (slow_rounds && images < kFewImages ? kWholeRoundsFew : kWholeRounds) || images >= kManyImages;
         if (p.whole) {
             p.pieces = 1;
             p.runs = pixels / p.per * p.r > kRun;
