@@ -411,10 +411,10 @@ __global__ void __launch_bounds__(kGnormThreads) gnorm_any_grad_kernel(const T* 
 // ---- tensors up to 256 vectors of channels wide ----
 // Two launches: the sums of pieces of the images (the block that is last to finish an image's joins them), and the output, which goes the same way back: what
 // was read last is still in L2.  A thread has one vector of channels, its constants in registers, and R pixels on their way at a time.
-// 32 x 112 x 112 x 256 bfloat16 with SiLU take 119 us: the sums read 206 MB at 4.7 TB/s (44 us), the output reads and writes 411 at 5.5, with the XU pipe
-// 70 % busy (two of its instructions an element).  The gradients of 64 x 56 x 56 x 256 take 111 us, 4 XU instructions an element.  Small calls are two
-// launches (10 us with the call), or one where a block has a whole image.  (Rounds of one pixel a thread for few images, so that more blocks share them, were slower in 86 of 176
-// sizes, up to 65 %, and faster in 7, up to 9 %.)
+// 32 x 112 x 112 x 256 bfloat16 with SiLU take 118 us: the sums read 206 MB at 5.1 TB/s (40 us), the output reads and writes 411 at 5.4, with the XU pipe
+// 69 % busy (two of its instructions an element).  The gradients of 64 x 56 x 56 x 256 take 110 us, 4 XU instructions an element.  Small calls are two
+// launches (10 us with the call), or one where a block has a whole image.  (Rounds of one pixel a thread for few images, so that more blocks share them, were slower in 86 of
+// 176 sizes, up to 65 %, and faster in 7, up to 9 %.)
 // (One launch, whose blocks took sums and outputs from a counter and waited for an image's sums, read every image once, but an image's counting, waiting
 // and joining by small tasks cost more than the second reading: 145 us for 32 x 112 x 112 x 256 bfloat16.)
 // A piece takes every pieces-th round of `per` pixels (R of each thread): the blocks that run at once read neighbouring memory.

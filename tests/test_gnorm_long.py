@@ -66,6 +66,7 @@ def test_deviations_of_many_pixels(n, h, w, c, x_dtype, y_dtype):
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,h,w,c,x_dtype", [(444, 80, 80, 1024, BF16),      # 6400 pixels a thread, in two launches
                                              (1776, 80, 80, 255, BF16),      # ... in one
+                                             (1776, 20, 20, 1024, BF16),     # 400, four channels a thread, in one
                                              (1, 1024, 800, 257, F32)])      # any width: 12800
 def test_gradients_of_many_pixels(n, h, w, c, x_dtype):
     """The same gradient everywhere, one whose float32 sum drifts (6400 of them in one run: 9e-5); u = 1 everywhere.  Runs of at most 264 additions, one thread a
